@@ -68,7 +68,8 @@ enum {
     SV_DEV_NONFINITE = 8,   /* softmax sum not finite (NaN / +Inf logit): sequence emits -1 */
     SV_DEV_TIMEOUT = 16,    /* a bounded device-side wait expired (also: a kernel found its shared
                                memory misaligned and did nothing) */
-    SV_DEV_BAD_LEN = 32     /* seq_len[b] < gamma[b]+1 or beyond the block table: sequence skipped */
+    SV_DEV_BAD_LEN = 32,    /* seq_len[b] < gamma[b]+1 or beyond the block table: sequence skipped */
+    SV_DEV_NO_PAGES = 64    /* fewer free pages than a sequence asks for: its pages stay as they were */
 };
 
 const char *sv_status_str(sv_status s);
@@ -91,6 +92,62 @@ sv_status spec_kv_pool_register(const void *k_pool_device, const void *v_pool_de
                                 int64_t n_pages, int32_t page_size, int32_t hkv, int32_t head_dim,
                                 const int64_t strides[4], sv_kv_pool_t *out);
 sv_status spec_kv_pool_release(sv_kv_pool_t pool);
+
+/* ---------------------------------------------------------------- block tables and slot maps */
+/*
+ * The controller moves every seq_len[b] on the device (gamma_tune_update), so the
+ * pages behind the sequences have to follow there as well (KV caching, paper
+ * Section 5).  This call brings the block table to the lengths of the coming
+ * step, taking pages from a stack of free ones and giving back those that a
+ * shorter or finished sequence no longer needs, and lists where each row of the
+ * step goes.  With need[b] = ceil(seq_len[b] / 16):
+ *   1. release, in the order of b: columns need[b] .. n_held[b]-1 of row b (if any)
+ *      are pushed on the stack free_list[0 .. n_free) in column order and their
+ *      table entries become -1;
+ *   2. acquire, in the order of b: columns n_held[b] .. need[b]-1 (if any) are
+ *      popped one after the other.  A sequence gets all the pages it asks for or
+ *      none, and the first that goes without stops the acquisition for those
+ *      behind it (SV_DEV_NO_PAGES; they keep what they held);
+ *   3. n_held[b] = need[b] where that succeeded, *n_free the pages left.
+ * seq_len[b] = 0 is a sequence that is not (or no longer) there: it gives back
+ * all its pages.  Pages released by a call serve the acquisitions of the same call.
+ * The outcome does not depend on the launch: ids move in the order stated.
+ * Rows (only with slot_map / positions): row r belongs to the sequence b with
+ * cu_q[b] <= r < cu_q[b+1] as its position i = r - cu_q[b]; for i <= gamma[b]
+ *     positions[r] = seq_len[b] - (gamma[b]+1) + i
+ *     slot_map[r]  = page * 16 + positions[r] % 16
+ * and both are -1 in every other row below n_rows (padding, rows behind the last
+ * sequence, sequences that are absent, skipped or without their pages).
+ * Device-detected: seq_len[b] < 0 or beyond the table row, or n_held[b] outside
+ * [0, block_table_stride] -> SV_DEV_BAD_LEN, sequence left as it is; 0 <
+ * seq_len[b] < gamma[b]+1 -> SV_DEV_BAD_LEN, its rows are -1; gamma[b] out of
+ * range -> SV_DEV_BAD_GAMMA, clamped; *n_free outside [0, n_pages] or more pages
+ * given back than the pool has -> SV_DEV_BAD_PAGE, clamped / dropped; a table
+ * entry under a row outside [0, n_pages) -> SV_DEV_BAD_PAGE, its slot is -1.
+ * block_table, n_held, free_list and n_free are the caller's state; a new pool
+ * starts with n_held = 0, table entries -1, free_list = the page ids in any order
+ * and *n_free their number.  One launch.
+ */
+typedef struct sv_kv_pages_params {
+    const int32_t *seq_len;     /* device [batch]: lengths to provide for (draft block included) */
+    int32_t batch;
+    int32_t *block_table;       /* device in/out [batch, block_table_stride] */
+    int64_t block_table_stride; /* elements between rows; batch * block_table_stride < 2^31 */
+    int32_t *n_held;            /* device in/out [batch]: pages each sequence holds */
+    int32_t *free_list;         /* device in/out [n_pages]: the stack; entries at and above *n_free are scratch */
+    int32_t *n_free;            /* device in/out, one word */
+    int64_t n_pages;            /* pages of the pool, < 2^31 */
+    int32_t page_size;          /* 16 */
+    const int32_t *gamma;       /* device [batch]; gamma and cu_q may be NULL when slot_map and positions are */
+    const int32_t *cu_q;        /* device [batch+1], not decreasing */
+    int32_t gamma_max;          /* upper bound of gamma[b] */
+    int64_t *slot_map;          /* device out [n_rows], or NULL */
+    int32_t *positions;         /* device out [n_rows], or NULL */
+    int64_t n_rows;             /* rows of slot_map / positions, < 2^31 */
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_kv_pages_params;
+
+sv_status spec_kv_pages_update(const sv_kv_pages_params *p, void *stream);
 
 /* ---------------------------------------------------------------- attention */
 /*

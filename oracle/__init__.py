@@ -264,3 +264,21 @@ def draft_step(draft_logits, temperature, tau, u, gamma, cu_d, n_drafted, active
 def cost_model(n_tokens, alpha, gamma, c):
     """Inference cost of Eq. 2-6 in units of T_draft."""
     return float(_load().oracle_cost_model(n_tokens, alpha, gamma, c))
+
+
+# --------------------------------------------------------------------------- block tables and slot maps
+def kv_pages_update(seq_len, block_table, n_held, free_list, n_free, n_rows=0, gamma=None, cu_q=None, gamma_max=0):
+    """One page update by the sequential walk over the batch.  Returns new arrays
+    (block_table, n_held, free_list, n_free, slot_map, positions, conditions); the arguments are left alone."""
+    lib = _load()
+    sl = _c(seq_len, np.int32)
+    bt, held, fl = (np.array(a, np.int32, order="C", copy=True) for a in (block_table, n_held, free_list))
+    nf = np.array([int(n_free)], np.int32)
+    slot, pos = np.full(max(n_rows, 1), -9, np.int64), np.full(max(n_rows, 1), -9, np.int32)
+    g, cq = (_c(a, np.int32) if a is not None else None for a in (gamma, cu_q))
+    rows = n_rows > 0
+    cond = lib.oracle_kv_pages_update(_p(sl), ctypes.c_int(len(sl)), _p(bt), ctypes.c_int64(bt.shape[1]), _p(held), _p(fl), _p(nf),
+                                      ctypes.c_int64(len(fl)), _p(g) if rows else None, _p(cq) if rows else None,
+                                      ctypes.c_int(gamma_max), _p(slot) if rows else None, _p(pos) if rows else None,
+                                      ctypes.c_int64(n_rows))
+    return bt, held, fl, int(nf[0]), slot[:n_rows], pos[:n_rows], int(cond)

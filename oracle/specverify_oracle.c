@@ -508,3 +508,72 @@ double oracle_cost_model(double n_tokens, double alpha, double gamma, double c)
     double calls_draft = gamma * n_steps;                   /* Eq. 5 */
     return c * calls_target + 1.0 * calls_draft;            /* Eq. 2 with T_draft = 1, T_target = c */
 }
+
+/* =========================================================================
+ * 6. Block tables and slot maps from the sequences' lengths (KV caching, paper
+ *    Section 5): the sequential walk over the batch.  Pages given back are
+ *    pushed on the free stack first, then pages asked for are popped, both in
+ *    the order of the batch; the first sequence that does not get all its pages
+ *    gets none and neither does any behind it.  Returns the condition bits
+ *    (1 bad gamma, 2 bad page / count, 32 bad length, 64 out of pages).
+ * ========================================================================= */
+int oracle_kv_pages_update(const int32_t *seq_len, int batch, int32_t *block_table, int64_t stride,
+                           int32_t *n_held, int32_t *free_list, int32_t *n_free, int64_t n_pages,
+                           const int32_t *gamma, const int32_t *cu_q, int gamma_max, int64_t *slot_map,
+                           int32_t *positions, int64_t n_rows)
+{
+    int cond = 0;
+    int64_t top = *n_free;
+    if (top < 0) { top = 0; cond |= 2; }
+    if (top > n_pages) { top = n_pages; cond |= 2; }
+    uint8_t *ok = (uint8_t *)malloc((size_t)batch);
+    uint8_t *has = (uint8_t *)malloc((size_t)batch);
+    for (int b = 0; b < batch; ++b) {
+        int64_t need = ((int64_t)seq_len[b] + 15) / 16;
+        ok[b] = seq_len[b] >= 0 && need <= stride && n_held[b] >= 0 && n_held[b] <= stride;
+        has[b] = ok[b];
+        if (!ok[b]) { cond |= 32; continue; }
+        int64_t held = n_held[b];
+        for (int64_t c = need; c < held; ++c) {
+            int32_t *e = block_table + b * stride + c;
+            if (*e < 0 || *e >= n_pages) cond |= 2;
+            if (top < n_pages) free_list[top++] = *e;
+            else cond |= 2;
+            *e = -1;
+        }
+        if (need < held) n_held[b] = (int32_t)need;
+    }
+    int out = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (!ok[b]) continue;
+        int64_t need = ((int64_t)seq_len[b] + 15) / 16;
+        int64_t want = need - n_held[b];
+        if (want <= 0) continue;
+        if (out || want > top) { out = 1; has[b] = 0; cond |= 64; continue; }
+        while (n_held[b] < need) block_table[b * stride + n_held[b]++] = free_list[--top];
+    }
+    *n_free = (int32_t)top;
+    for (int64_t r = 0; r < n_rows; ++r) {
+        if (slot_map) slot_map[r] = -1;
+        if (positions) positions[r] = -1;
+    }
+    for (int b = 0; b < batch && (slot_map || positions); ++b) {
+        int g = gamma[b];
+        if (g < 0 || g > gamma_max) { cond |= 1; g = g < 0 ? 0 : gamma_max; }
+        if (!ok[b] || seq_len[b] == 0) continue;
+        if (seq_len[b] < g + 1) { cond |= 32; continue; }
+        if (!has[b]) continue;
+        for (int i = 0; i <= g; ++i) {
+            int64_t r = (int64_t)cu_q[b] + i;
+            if (r >= cu_q[b + 1] || r >= n_rows) break;
+            int pos = seq_len[b] - (g + 1) + i;
+            int32_t page = block_table[b * stride + pos / 16];
+            if (page < 0 || page >= n_pages) { cond |= 2; continue; }
+            if (slot_map) slot_map[r] = (int64_t)page * 16 + pos % 16;
+            if (positions) positions[r] = pos;
+        }
+    }
+    free(ok);
+    free(has);
+    return cond;
+}

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libspecverify.so")
 
 SV_OK, SV_EINVAL, SV_EUNSUPPORTED, SV_EALIGN, SV_ECUDA, SV_EWORKSPACE = 0, -1, -2, -3, -4, -5
 SV_DEV_BAD_GAMMA, SV_DEV_BAD_PAGE, SV_DEV_BAD_TOKEN = 1, 2, 4
-SV_DEV_NONFINITE, SV_DEV_TIMEOUT, SV_DEV_BAD_LEN = 8, 16, 32
+SV_DEV_NONFINITE, SV_DEV_TIMEOUT, SV_DEV_BAD_LEN, SV_DEV_NO_PAGES = 8, 16, 32, 64
 SV_GT_FIXED, SV_GT_PROPOSED, SV_GT_LITERAL = 0, 1, 2
 
 EXPORTS = (
@@ -27,6 +27,7 @@ EXPORTS = (
     "spec_accept_sample", "spec_accept_sample_static", "gamma_tune_update", "gamma_tune_init",
     "spec_verify_step_host", "spec_draft_stop_workspace_bytes", "spec_draft_stop", "spec_kv_append",
     "sv_selftest_wait_expiry", "spec_verify_attn_layers", "spec_draft_step_workspace_bytes", "spec_draft_step",
+    "spec_kv_pages_update",
 )
 
 
@@ -56,6 +57,15 @@ class KvAppendParams(C.Structure):
                 ("block_table", C.c_void_p), ("block_table_stride", C.c_int64),
                 ("seq_len", C.c_void_p), ("gamma", C.c_void_p), ("cu_q", C.c_void_p),
                 ("batch", C.c_int32), ("gamma_max", C.c_int32), ("device_status", C.c_void_p)]
+
+
+class KvPagesParams(C.Structure):
+    _fields_ = [("seq_len", C.c_void_p), ("batch", C.c_int32), ("block_table", C.c_void_p),
+                ("block_table_stride", C.c_int64), ("n_held", C.c_void_p), ("free_list", C.c_void_p),
+                ("n_free", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int32),
+                ("gamma", C.c_void_p), ("cu_q", C.c_void_p), ("gamma_max", C.c_int32),
+                ("slot_map", C.c_void_p), ("positions", C.c_void_p), ("n_rows", C.c_int64),
+                ("device_status", C.c_void_p)]
 
 
 class AcceptParams(C.Structure):
@@ -152,6 +162,8 @@ def load():
         lib.spec_draft_stop.argtypes = [C.POINTER(DraftStopParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_draft_step_workspace_bytes.restype = C.c_size_t
         lib.spec_draft_step_workspace_bytes.argtypes = [C.c_int32] * 2
+        lib.spec_kv_pages_update.restype = C.c_int32
+        lib.spec_kv_pages_update.argtypes = [C.POINTER(KvPagesParams), C.c_void_p]
         lib.spec_draft_step.restype = C.c_int32
         lib.spec_draft_step.argtypes = [C.POINTER(DraftStepParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_verify_step_host.restype = C.c_int32
@@ -205,6 +217,18 @@ def _host(t, dtype, name, allow_none=False):
     if t.is_cuda or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous host tensor of {dtype}")
     return t.data_ptr()
+
+
+def _check_device(stream, first, *others):
+    """The tensors are on one device and the launch goes there: the stream's device, or the current one."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
+    at = stream.device.index if stream is not None else torch.cuda.current_device()
+    if dev.index != at or (stream is not None and at != torch.cuda.current_device()):
+        raise ValueError(f"tensors are on {dev}, the launch would go to cuda:{at} "
+                         f"(current device: cuda:{torch.cuda.current_device()})")
 
 
 def _nbytes(t) -> int:
@@ -320,6 +344,47 @@ def spec_kv_append(k_new, v_new, pool, block_table, seq_len, gamma, cu_q, gamma_
     """Write the draft block's keys and values behind each sequence's context (asynchronous)."""
     p = kv_append_params(k_new, v_new, pool, block_table, seq_len, gamma, cu_q, gamma_max, device_status)
     _check("spec_kv_append", load().spec_kv_append(C.byref(p), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- block tables and slot maps
+def kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
+                    slot_map=None, positions=None, device_status=None) -> KvPagesParams:
+    p = KvPagesParams()
+    p.seq_len = _dev(seq_len, torch.int32, "seq_len")
+    p.batch = batch = seq_len.numel()
+    p.block_table = _dev(block_table, torch.int32, "block_table")
+    if block_table.dim() != 2 or block_table.shape[0] != batch or n_held.numel() != batch:
+        raise ValueError("block_table and n_held must have one row per sequence")
+    p.block_table_stride = block_table.shape[1]
+    p.n_held = _dev(n_held, torch.int32, "n_held")
+    p.free_list = _dev(free_list, torch.int32, "free_list")
+    p.n_pages = free_list.numel()
+    p.n_free = _dev(n_free, torch.int32, "n_free")
+    p.page_size = 16
+    p.gamma = _dev(gamma, torch.int32, "gamma", True)
+    p.cu_q = _dev(cu_q, torch.int32, "cu_q", True)
+    if (gamma is not None and gamma.numel() != batch) or (cu_q is not None and cu_q.numel() != batch + 1):
+        raise ValueError("gamma must have one entry per sequence, cu_q one more")
+    p.gamma_max = gamma_max
+    p.slot_map = _dev(slot_map, torch.int64, "slot_map", True)
+    p.positions = _dev(positions, torch.int32, "positions", True)
+    if slot_map is not None and positions is not None and slot_map.numel() != positions.numel():
+        raise ValueError("slot_map and positions must have the same number of rows")
+    rows = slot_map if slot_map is not None else positions
+    p.n_rows = rows.numel() if rows is not None else 0
+    p.device_status = _dev(device_status, torch.int32, "device_status", True)
+    return p
+
+
+def spec_kv_pages_update(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
+                         slot_map=None, positions=None, device_status=None, stream=None):
+    """Block table, held pages and free stack brought to the lengths of the coming step, and the cache slot and
+    position of each of its rows (asynchronous)."""
+    p = kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, gamma_max, slot_map,
+                        positions, device_status)
+    _check_device(stream, seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, slot_map, positions,
+                  device_status)
+    _check("spec_kv_pages_update", load().spec_kv_pages_update(C.byref(p), _stream(stream)))
 
 
 # --------------------------------------------------------------------------- accept / resample
