@@ -130,9 +130,9 @@ sv_status spec_kv_pool_release(sv_kv_pool_t pool);
  */
 typedef struct sv_kv_pages_params {
     const int32_t *seq_len;     /* device [batch]: lengths to provide for (draft block included) */
-    int32_t batch;
+    int32_t batch;              /* at most 8192 */
     int32_t *block_table;       /* device in/out [batch, block_table_stride] */
-    int64_t block_table_stride; /* elements between rows; batch * block_table_stride < 2^31 */
+    int64_t block_table_stride; /* elements between rows; batch * block_table_stride <= 2^30 */
     int32_t *n_held;            /* device in/out [batch]: pages each sequence holds */
     int32_t *free_list;         /* device in/out [n_pages]: the stack; entries at and above *n_free are scratch */
     int32_t *n_free;            /* device in/out, one word */

@@ -219,16 +219,27 @@ def _host(t, dtype, name, allow_none=False):
     return t.data_ptr()
 
 
-def _check_device(stream, first, *others):
-    """The tensors are on one device and the launch goes there: the stream's device, or the current one."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"tensors on different devices: {dev} and {t.device}")
-    at = stream.device.index if stream is not None else torch.cuda.current_device()
-    if dev.index != at or (stream is not None and at != torch.cuda.current_device()):
-        raise ValueError(f"tensors are on {dev}, the launch would go to cuda:{at} "
-                         f"(current device: cuda:{torch.cuda.current_device()})")
+def _launch_at(stream, first, name):
+    """Device index and raw stream of a launch: the current device, where the tensors have to be.  (The raw stream of
+    the current device is asked for by index: building a Stream object costs more than the launch.)"""
+    if not first.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    index = torch.cuda.current_device()
+    if stream is None:
+        return index, torch._C._cuda_getCurrentRawStream(index)
+    if stream.device.index != index:
+        raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{index}")
+    return index, stream.cuda_stream
+
+
+def _on(t, dtype, name, index):
+    """Device pointer of a contiguous tensor of `dtype` on CUDA device `index`; None stays None."""
+    if t is None:
+        return None
+    if t.get_device() != index or t.dtype != dtype or not t.is_contiguous():
+        _dev(t, dtype, name)
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
+    return t.data_ptr()
 
 
 def _nbytes(t) -> int:
@@ -348,43 +359,34 @@ def spec_kv_append(k_new, v_new, pool, block_table, seq_len, gamma, cu_q, gamma_
 
 # --------------------------------------------------------------------------- block tables and slot maps
 def kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
-                    slot_map=None, positions=None, device_status=None) -> KvPagesParams:
-    p = KvPagesParams()
-    p.seq_len = _dev(seq_len, torch.int32, "seq_len")
-    p.batch = batch = seq_len.numel()
-    p.block_table = _dev(block_table, torch.int32, "block_table")
+                    slot_map=None, positions=None, device_status=None, index=None) -> KvPagesParams:
+    index = torch.cuda.current_device() if index is None else index
+    batch, n_rows, i32 = seq_len.numel(), 0, torch.int32
     if block_table.dim() != 2 or block_table.shape[0] != batch or n_held.numel() != batch:
         raise ValueError("block_table and n_held must have one row per sequence")
-    p.block_table_stride = block_table.shape[1]
-    p.n_held = _dev(n_held, torch.int32, "n_held")
-    p.free_list = _dev(free_list, torch.int32, "free_list")
-    p.n_pages = free_list.numel()
-    p.n_free = _dev(n_free, torch.int32, "n_free")
-    p.page_size = 16
-    p.gamma = _dev(gamma, torch.int32, "gamma", True)
-    p.cu_q = _dev(cu_q, torch.int32, "cu_q", True)
     if (gamma is not None and gamma.numel() != batch) or (cu_q is not None and cu_q.numel() != batch + 1):
         raise ValueError("gamma must have one entry per sequence, cu_q one more")
-    p.gamma_max = gamma_max
-    p.slot_map = _dev(slot_map, torch.int64, "slot_map", True)
-    p.positions = _dev(positions, torch.int32, "positions", True)
-    if slot_map is not None and positions is not None and slot_map.numel() != positions.numel():
-        raise ValueError("slot_map and positions must have the same number of rows")
-    rows = slot_map if slot_map is not None else positions
-    p.n_rows = rows.numel() if rows is not None else 0
-    p.device_status = _dev(device_status, torch.int32, "device_status", True)
-    return p
+    if slot_map is not None or positions is not None:
+        n_rows = (slot_map if slot_map is not None else positions).numel()
+        if positions is not None and positions.numel() != n_rows:
+            raise ValueError("slot_map and positions must have the same number of rows")
+    if n_free.numel() != 1:
+        raise ValueError("n_free must be one word")
+    return KvPagesParams(_on(seq_len, i32, "seq_len", index), batch, _on(block_table, i32, "block_table", index),
+                         block_table.shape[1], _on(n_held, i32, "n_held", index), _on(free_list, i32, "free_list", index),
+                         _on(n_free, i32, "n_free", index), free_list.numel(), 16, _on(gamma, i32, "gamma", index),
+                         _on(cu_q, i32, "cu_q", index), gamma_max, _on(slot_map, torch.int64, "slot_map", index),
+                         _on(positions, i32, "positions", index), n_rows, _on(device_status, i32, "device_status", index))
 
 
 def spec_kv_pages_update(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
                          slot_map=None, positions=None, device_status=None, stream=None):
     """Block table, held pages and free stack brought to the lengths of the coming step, and the cache slot and
     position of each of its rows (asynchronous)."""
+    index, raw = _launch_at(stream, seq_len, "seq_len")
     p = kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, gamma_max, slot_map,
-                        positions, device_status)
-    _check_device(stream, seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, slot_map, positions,
-                  device_status)
-    _check("spec_kv_pages_update", load().spec_kv_pages_update(C.byref(p), _stream(stream)))
+                        positions, device_status, index)
+    _check("spec_kv_pages_update", load().spec_kv_pages_update(C.byref(p), raw))
 
 
 # --------------------------------------------------------------------------- accept / resample

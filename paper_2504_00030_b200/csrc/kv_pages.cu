@@ -1,8 +1,11 @@
 // Block tables and slot maps built on the device from the sequences' lengths (KV caching, paper Section 5).
 //
-// Three phases with a barrier between them: pages given back are pushed on the free stack, pages asked for
-// are popped, rows are looked up.  Where a page goes follows from two prefix sums over the batch (released and wanted
-// pages), so the result is that of the sequential walk in the order of the batch, whatever the launch.
+// Where a page goes follows from two prefix sums over the batch (released and wanted pages), so the result is that of
+// the sequential walk in the order of the batch, whatever the launch.  An acquired page is found without waiting for the
+// releases: an index below the old top of the stack is read from the stack, one above it names an entry that is
+// being released and is read from the block table.  Reads therefore see the state before the call throughout, and
+// what would overwrite it (-1 in released entries, held pages, the top of the stack) is written behind the one barrier.
+// Only a call that both releases and acquires many pages has a second one, behind which all are read from the stack.
 //
 // What bounds it is latency: a decoding step moves a few hundred words, an admission a few megabytes.  One
 // thread-block cluster does the whole call in one launch: its barrier is a hardware instruction (a grid-wide one would
@@ -14,223 +17,320 @@ namespace sv {
 
 constexpr int KP_THREADS = 1024;       // one scan step covers this many sequences
 constexpr int KP_PAGE = 16;
+constexpr int KP_MAX_BATCH = 8192;     // prefix sums of the whole batch stay in shared memory (16 bytes a sequence)
+constexpr int KP_UNROLL = 8;           // pages a thread has under way
+constexpr int KP_CLUSTER = 8;          // blocks of the cluster (the portable size)
+// Largest batch that one cluster serves alone; above it the pages are moved by the whole GPU and a second launch closes
+// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.5, 512 8.1 / 8.3, 1024 12.8 / 10.0,
+// 4096 37.8 / 21.3; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 6.0 / 7.9,
+// 256 9.0 / 8.5, 1024 23.1 / 13.6.
+constexpr int KP_ONE_CLUSTER = 512;
+constexpr int KP_UNIT = 32 * KP_UNROLL;    // columns of one sequence that a warp moves at a time
 
 struct KvPagesLaunch {
     sv_kv_pages_params p;
+    int search;                        // first step of a thread's binary search: the largest power of two <= batch
 };
 
-struct KvPagesShared {
-    int32_t rel[KP_THREADS];           // exclusive prefix of released / wanted pages within the chunk
-    int32_t req[KP_THREADS];
-    int32_t col[KP_THREADS];           // first column that changes hands
-    int32_t warp_rel[32], warp_req[32];
-    int32_t first_without;             // first sequence that goes without its pages
-    int32_t served;                    // pages acquired
-};
-
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-// every thread of the cluster arrives; global writes before it are visible behind it (release / acquire)
+// every thread of the cluster arrives; global writes before it are visible behind it
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
 }
 
-// pages of one sequence: what it holds, what it needs, whether its numbers make sense
-struct SeqPages {
-    int held, need;
-    bool ok;
-};
-__device__ __forceinline__ SeqPages seq_pages(const sv_kv_pages_params &p, int b)
-{
-    SeqPages s;
-    const int len = __ldg(p.seq_len + b);
-    s.held = __ldcg(p.n_held + b);
-    s.need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
-    s.ok = len >= 0 && s.need <= p.block_table_stride && s.held >= 0 && s.held <= p.block_table_stride;
-    return s;
-}
-
-// exclusive prefix sums of the chunk's released and wanted pages into shared memory; returns the chunk's totals
-__device__ __forceinline__ int2 scan_chunk(KvPagesShared &sh, int rel, int req, int col)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int a = rel, c = req;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int ua = __shfl_up_sync(0xffffffffu, a, d), uc = __shfl_up_sync(0xffffffffu, c, d);
-        if (lane >= d) {
-            a += ua;
-            c += uc;
-        }
-    }
-    __syncthreads();                   // the previous chunk's arrays are no longer read
-    if (lane == 31) {
-        sh.warp_rel[warp] = a;
-        sh.warp_req[warp] = c;
-    }
-    __syncthreads();
-    int ta = sh.warp_rel[lane], tc = sh.warp_req[lane];       // every warp scans the warp totals
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int ua = __shfl_up_sync(0xffffffffu, ta, d), uc = __shfl_up_sync(0xffffffffu, tc, d);
-        if (lane >= d) {
-            ta += ua;
-            tc += uc;
-        }
-    }
-    const int before_a = warp > 0 ? __shfl_sync(0xffffffffu, ta, warp - 1) : 0;
-    const int before_c = warp > 0 ? __shfl_sync(0xffffffffu, tc, warp - 1) : 0;
-    sh.rel[threadIdx.x] = before_a + a - rel;
-    sh.req[threadIdx.x] = before_c + c - req;
-    sh.col[threadIdx.x] = col;
-    const int2 total = make_int2(__shfl_sync(0xffffffffu, ta, 31), __shfl_sync(0xffffffffu, tc, 31));
-    __syncthreads();
-    return total;
-}
-
-// the sequence of the chunk whose share of the prefix sums holds entry e: the last one that starts at or before it
-__device__ __forceinline__ int owner_of(const int32_t *ex, int e)
+// The last sequence whose exclusive prefix is at most e.  ex[0] = 0 <= e and ex[batch] = the total; for e below the
+// total that sequence is the owner of entry e.
+__device__ __forceinline__ int owner_of(const int32_t *ex, int batch, int search, int e)
 {
     int lo = 0;
-#pragma unroll
-    for (int step = KP_THREADS / 2; step > 0; step >>= 1)
-        if (ex[lo + step] <= e) lo += step;
+    for (int step = search; step > 0; step >>= 1)
+        if (lo + step < batch && ex[lo + step] <= e) lo += step;
     return lo;
 }
 
+// the same for a whole warp, 32 candidates a step
+__device__ __forceinline__ int warp_owner_of(const int32_t *ex, int batch, int e, int lane)
+{
+    int lo = 0;
+    for (int stride = batch > 1024 ? 1024 : batch > 32 ? 32 : 1; stride > 0; stride >>= 5) {
+        const int i = lo + lane * stride;
+        lo += (__popc(__ballot_sync(0xffffffffu, i < batch && ex[i] <= e)) - 1) * stride;
+    }
+    return lo;
+}
+
+// What every block knows about the batch: prefix sums in shared memory and the totals that follow from them.
+struct Pages {
+    const int32_t *rel;                // [batch + 1] exclusive prefix of released pages
+    const int32_t *req;                // [batch + 1] exclusive prefix of wanted pages
+    const int32_t *unit;               // [batch + 1] exclusive prefix of units (KP_UNIT columns that change hands)
+    const int32_t *col;                // [batch] first column that changes hands, -1: sequence left alone
+    int n_free;                        // top of the stack before the call
+    int have;                          // and after the releases
+    int from_stack;                    // acquired pages below this index are read from the stack
+    int batch, search;
+
+    // page that is acquired as number e
+    __device__ __forceinline__ int acquired(const sv_kv_pages_params &p, int e) const
+    {
+        const int at = have - 1 - e;
+        if (at < from_stack) return __ldcg(p.free_list + at);
+        const int s = owner_of(rel, batch, search, at - n_free);
+        return __ldcg(p.block_table + (long long)s * p.block_table_stride + col[s] + (at - n_free - rel[s]));
+    }
+
+    // body(sequence, first of its changed columns that the unit holds) for each unit of this warp
+    template <typename F>
+    __device__ __forceinline__ void for_units(int warp, int warps, int lane, F &&body) const
+    {
+        const int total = unit[batch];
+        for (int u = warp; u < total; u += warps) {
+            const int s = warp_owner_of(unit, batch, u, lane);
+            body(s, (u - unit[s]) * KP_UNIT);
+        }
+    }
+};
+
+// WHOLE: the call in one launch by one cluster.  MOVE: what comes before the barrier, by a grid of any size; CLOSE: what
+// comes behind it, by one cluster in a second launch.
+enum { KP_WHOLE, KP_MOVE, KP_CLOSE };
+
+template <int PART>
 __global__ void __launch_bounds__(KP_THREADS)
 kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
 {
     pdl_enter();
-    __shared__ KvPagesShared sh;
+    extern __shared__ int32_t kp_smem[];
+    __shared__ int32_t warp_rel[32], warp_req[32], warp_unit[32];
     const sv_kv_pages_params &p = a.p;
-    const int tid = threadIdx.x, rank = (int)cluster_rank();
-    const int threads = (int)cluster_size() * KP_THREADS, me = rank * KP_THREADS + tid;
-    const int batch = p.batch;
-    const int n_pages = (int)p.n_pages;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int threads = gridDim.x * KP_THREADS, me = blockIdx.x * KP_THREADS + tid;     // a cluster is a whole grid
+    const int my_warp = me >> 5, warps = threads >> 5;
+    const int batch = p.batch, n_pages = (int)p.n_pages;
+    int32_t *rel = kp_smem, *req = rel + batch + 1, *unit = req + batch + 1, *col = unit + batch + 1;
     uint32_t bad = 0;
 
-    int n_free = __ldcg(p.n_free);
-    if (n_free < 0 || n_free > n_pages) {
+    Pages pg;
+    pg.n_free = __ldcg(p.n_free);
+    if (pg.n_free < 0 || pg.n_free > n_pages) {
         bad |= SV_DEV_BAD_PAGE;
-        n_free = min(max(n_free, 0), n_pages);
+        pg.n_free = min(max(pg.n_free, 0), n_pages);
     }
-    // ---- release
-    long long released = 0;
+    // ---- prefix sums
+    int base_rel = 0, base_req = 0, base_unit = 0;
     for (int b0 = 0; b0 < batch; b0 += KP_THREADS) {
-        int rel = 0, req = 0, col = 0;
-        if (b0 + tid < batch) {
-            const SeqPages s = seq_pages(p, b0 + tid);
-            if (s.ok) {
-                rel = max(s.held - s.need, 0);
-                req = max(s.need - s.held, 0);
-                col = min(s.held, s.need);
+        const int b = b0 + tid;
+        int my_rel = 0, my_req = 0, my_col = -1;
+        if (b < batch) {
+            const int len = __ldg(p.seq_len + b), held = __ldcg(p.n_held + b);
+            const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
+            if (len >= 0 && need <= p.block_table_stride && held >= 0 && held <= p.block_table_stride) {
+                my_rel = max(held - need, 0);
+                my_req = max(need - held, 0);
+                my_col = min(held, need);
             } else {
                 bad |= SV_DEV_BAD_LEN;
             }
         }
-        const int total = scan_chunk(sh, rel, req, col).x;
-        for (int e = me; e < total; e += threads) {
-            const int s = owner_of(sh.rel, e);
-            int32_t *entry = p.block_table + (long long)(b0 + s) * p.block_table_stride + sh.col[s] + (e - sh.rel[s]);
-            const int page = __ldcg(entry);
-            if (page < 0 || page >= n_pages) bad |= SV_DEV_BAD_PAGE;
-            const long long at = n_free + released + e;
-            if (at < n_pages) p.free_list[at] = page;
-            else bad |= SV_DEV_BAD_PAGE;
-            *entry = -1;
-        }
-        released += total;
-    }
-    const int have = (int)min((long long)n_free + released, (long long)n_pages);
-    cluster_sync();
-    // ---- acquire
-    int taken = 0, without = batch;
-    for (int b0 = 0; b0 < batch && without == batch; b0 += KP_THREADS) {
-        int req = 0, col = 0;
-        if (b0 + tid < batch) {
-            const SeqPages s = seq_pages(p, b0 + tid);
-            if (s.ok) {
-                req = max(s.need - s.held, 0);
-                col = min(s.held, s.need);
+        const int my_unit = (my_rel + my_req + KP_UNIT - 1) / KP_UNIT;       // one of the two is zero
+        int sum_rel = my_rel, sum_req = my_req, sum_unit = my_unit;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u0 = __shfl_up_sync(0xffffffffu, sum_rel, d), u1 = __shfl_up_sync(0xffffffffu, sum_req, d),
+                      u2 = __shfl_up_sync(0xffffffffu, sum_unit, d);
+            if (lane >= d) {
+                sum_rel += u0;
+                sum_req += u1;
+                sum_unit += u2;
             }
         }
-        if (tid == 0) sh.first_without = batch;
-        const int total = scan_chunk(sh, 0, req, col).y;
-        if (req > 0 && taken + sh.req[tid] + req > have) atomicMin(&sh.first_without, b0 + tid);
+        if (b0 > 0) __syncthreads();   // the warp totals of the previous step are no longer read
+        if (lane == 31) {
+            warp_rel[warp] = sum_rel;
+            warp_req[warp] = sum_req;
+            warp_unit[warp] = sum_unit;
+        }
         __syncthreads();
-        without = sh.first_without;
-        const int served = without < batch ? sh.req[without - b0] : total;
-        for (int e = me; e < served; e += threads) {
-            const int s = owner_of(sh.req, e);
-            p.block_table[(long long)(b0 + s) * p.block_table_stride + sh.col[s] + (e - sh.req[s])] =
-                __ldcg(p.free_list + have - 1 - taken - e);
-        }
-        taken += served;
-    }
-    if (without < batch) bad |= SV_DEV_NO_PAGES;
-    if (me == 0) *p.n_free = have - taken;
-    cluster_sync();
-    // ---- held pages and rows: a warp per sequence
-    const bool rows = p.slot_map != nullptr || p.positions != nullptr;
-    const int lane = tid & 31;
-    for (int b = me >> 5; b < batch; b += threads >> 5) {
-        SeqPages s = seq_pages(p, b);
-        if (s.ok && (b < without || s.need < s.held)) s.held = s.need;
-        __syncwarp();
-        if (lane == 0 && s.ok) p.n_held[b] = s.held;
-        if (!rows) continue;
-        const int len = __ldg(p.seq_len + b);
-        int g = __ldg(p.gamma + b);
-        if (g < 0 || g > p.gamma_max) {
-            bad |= SV_DEV_BAD_GAMMA;
-            g = min(max(g, 0), p.gamma_max);
-        }
-        bool there = s.ok && len > 0 && s.need <= s.held;
-        if (s.ok && len > 0 && len <= g) {
-            bad |= SV_DEV_BAD_LEN;
-            there = false;
-        }
-        const long long lo = max(__ldg(p.cu_q + b), 0), hi = min((long long)__ldg(p.cu_q + b + 1), (long long)p.n_rows);
-        const int32_t *table = p.block_table + (long long)b * p.block_table_stride;
-        for (long long r = lo + lane; r < hi; r += 32) {
-            int pos = -1;
-            long long slot = -1;
-            if (there && r - lo <= g) {
-                pos = len - g - 1 + (int)(r - lo);
-                const int page = __ldcg(table + pos / KP_PAGE);
-                if (page >= 0 && page < n_pages) slot = (long long)page * KP_PAGE + pos % KP_PAGE;
-                else bad |= SV_DEV_BAD_PAGE;
+        int t_rel = warp_rel[lane], t_req = warp_req[lane], t_unit = warp_unit[lane];     // every warp scans the 32 totals
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int u0 = __shfl_up_sync(0xffffffffu, t_rel, d), u1 = __shfl_up_sync(0xffffffffu, t_req, d),
+                      u2 = __shfl_up_sync(0xffffffffu, t_unit, d);
+            if (lane >= d) {
+                t_rel += u0;
+                t_req += u1;
+                t_unit += u2;
             }
-            if (p.slot_map != nullptr) p.slot_map[r] = slot;
-            if (p.positions != nullptr) p.positions[r] = slot >= 0 ? pos : -1;
         }
+        const int prev = warp > 0 ? warp - 1 : 0;
+        const int before_rel = __shfl_sync(0xffffffffu, t_rel, prev), before_req = __shfl_sync(0xffffffffu, t_req, prev),
+                  before_unit = __shfl_sync(0xffffffffu, t_unit, prev);
+        if (b < batch) {
+            rel[b] = base_rel + (warp > 0 ? before_rel : 0) + sum_rel - my_rel;
+            req[b] = base_req + (warp > 0 ? before_req : 0) + sum_req - my_req;
+            unit[b] = base_unit + (warp > 0 ? before_unit : 0) + sum_unit - my_unit;
+            col[b] = my_col;
+        }
+        base_rel += __shfl_sync(0xffffffffu, t_rel, 31);
+        base_req += __shfl_sync(0xffffffffu, t_req, 31);
+        base_unit += __shfl_sync(0xffffffffu, t_unit, 31);
     }
-    // ---- rows of no sequence
-    if (rows) {
-        const long long first = min((long long)max(__ldg(p.cu_q), 0), (long long)p.n_rows);
-        const long long last = max(__ldg(p.cu_q + batch), 0);
-        for (long long r = me; r < first; r += threads) {
-            if (p.slot_map != nullptr) p.slot_map[r] = -1;
-            if (p.positions != nullptr) p.positions[r] = -1;
-        }
-        for (long long r = last + me; r < p.n_rows; r += threads) {
-            if (p.slot_map != nullptr) p.slot_map[r] = -1;
-            if (p.positions != nullptr) p.positions[r] = -1;
-        }
+    if (tid == 0) {
+        rel[batch] = base_rel;
+        req[batch] = base_req;
+        unit[batch] = base_unit;
     }
-    if (bad != 0) set_status(p.device_status, bad);
+    __syncthreads();
+    pg.rel = rel;
+    pg.req = req;
+    pg.unit = unit;
+    pg.col = col;
+    pg.batch = batch;
+    pg.search = a.search;
+    pg.have = (int)min((long long)pg.n_free + base_rel, (long long)n_pages);
+    pg.from_stack = pg.n_free;
+    if ((long long)pg.n_free + base_rel > n_pages) bad |= SV_DEV_BAD_PAGE;
+    // the first sequence that goes without its pages: the one in whose share the last page has been handed out
+    int without = batch, served = base_req;
+    if (base_req > pg.have) {
+        without = owner_of(req, batch, a.search, pg.have);
+        served = req[without];
+        bad |= SV_DEV_NO_PAGES;
+    }
+    if (PART != KP_CLOSE) {
+        // ---- released pages onto the stack
+        if (base_rel > 0) {
+            pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+                const int n = rel[s + 1] - rel[s], at = pg.n_free + rel[s];
+                const int32_t *from = p.block_table + (long long)s * p.block_table_stride + col[s];
+                int page[KP_UNROLL];
+#pragma unroll
+                for (int u = 0; u < KP_UNROLL; ++u) {
+                    const int j = first + u * 32 + lane;
+                    page[u] = j < n ? __ldcg(from + j) : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < KP_UNROLL; ++u) {
+                    const int j = first + u * 32 + lane;
+                    if (j >= n) continue;
+                    if (page[u] < 0 || page[u] >= n_pages) bad |= SV_DEV_BAD_PAGE;
+                    if (j < n_pages - at) p.free_list[at + j] = page[u];
+                }
+            });
+            // A page that is read as an entry being released costs a binary search; for more than a few a thread, the
+            // barrier (about a microsecond) is cheaper.
+            if (PART == KP_WHOLE && served > threads) {
+                cluster_sync();
+                pg.from_stack = pg.have;
+            }
+        }
+        // ---- acquired pages into the table
+        if (served > 0) {
+            pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+                const int n = s < without ? req[s + 1] - req[s] : 0, e = req[s];
+                int32_t *to = p.block_table + (long long)s * p.block_table_stride + col[s];
+                int page[KP_UNROLL];
+#pragma unroll
+                for (int u = 0; u < KP_UNROLL; ++u) {
+                    const int j = first + u * 32 + lane;
+                    page[u] = j < n ? pg.acquired(p, e + j) : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < KP_UNROLL; ++u) {
+                    const int j = first + u * 32 + lane;
+                    if (j < n) to[j] = page[u];
+                }
+            });
+        }
+        // ---- rows: a warp per sequence
+        if (p.slot_map != nullptr || p.positions != nullptr) {
+            // from the other end of the cluster, whose warps have few pages to move
+            for (int b = warps - 1 - my_warp; b < batch; b += warps) {
+                const int len = __ldg(p.seq_len + b);
+                int g = __ldg(p.gamma + b);
+                const long long lo = max(__ldg(p.cu_q + b), 0), hi = min((long long)__ldg(p.cu_q + b + 1), (long long)p.n_rows);
+                if (g < 0 || g > p.gamma_max) {
+                    bad |= SV_DEV_BAD_GAMMA;
+                    g = min(max(g, 0), p.gamma_max);
+                }
+                const int c0 = col[b], wanted = req[b + 1] - req[b];
+                const int held = c0 + (rel[b + 1] - rel[b]);
+                bool there = c0 >= 0 && len > 0 && (wanted == 0 || b < without);
+                if (c0 >= 0 && len > 0 && len <= g) {
+                    bad |= SV_DEV_BAD_LEN;
+                    there = false;
+                }
+                for (long long r = lo + lane; r < hi; r += 32) {
+                    int pos = -1;
+                    long long slot = -1;
+                    if (there && r - lo <= g) {
+                        pos = len - g - 1 + (int)(r - lo);
+                        const int c = pos / KP_PAGE;
+                        const int page = c < held ? __ldcg(p.block_table + (long long)b * p.block_table_stride + c)
+                                                  : pg.acquired(p, req[b] + c - held);
+                        if (page >= 0 && page < n_pages) slot = (long long)page * KP_PAGE + pos % KP_PAGE;
+                        else bad |= SV_DEV_BAD_PAGE;
+                    }
+                    if (p.slot_map != nullptr) p.slot_map[r] = slot;
+                    if (p.positions != nullptr) p.positions[r] = slot >= 0 ? pos : -1;
+                }
+            }
+            // rows of no sequence
+            const long long first = min((long long)max(__ldg(p.cu_q), 0), (long long)p.n_rows);
+            const long long last = max(__ldg(p.cu_q + batch), 0);
+            for (long long r = me; r < first; r += threads) {
+                if (p.slot_map != nullptr) p.slot_map[r] = -1;
+                if (p.positions != nullptr) p.positions[r] = -1;
+            }
+            for (long long r = last + me; r < p.n_rows; r += threads) {
+                if (p.slot_map != nullptr) p.slot_map[r] = -1;
+                if (p.positions != nullptr) p.positions[r] = -1;
+            }
+        }
+        if (bad != 0) set_status(p.device_status, bad);
+    }
+    if (PART == KP_MOVE) return;
+    // ---- nobody reads the old state any more
+    cluster_sync();
+    if (base_rel > 0) {
+        pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+            const int n = min(rel[s + 1] - rel[s] - first, KP_UNIT);
+            int32_t *entry = p.block_table + (long long)s * p.block_table_stride + col[s] + first;
+            for (int j = lane; j < n; j += 32) entry[j] = -1;
+        });
+    }
+    for (int b = me; b < batch; b += threads) {
+        const int n_req = req[b + 1] - req[b], n_rel = rel[b + 1] - rel[b];
+        if (n_rel > 0) p.n_held[b] = col[b];
+        if (n_req > 0 && b < without) p.n_held[b] = col[b] + n_req;
+    }
+    if (me == 0) *p.n_free = pg.have - served;
+}
+
+template <int PART>
+static sv_status launch_pages(const KvPagesLaunch &a, int blocks, cudaStream_t stream)
+{
+    const size_t smem = (size_t)(4 * a.p.batch + 3) * sizeof(int32_t);
+    if (smem > 40 * 1024 &&
+        cudaFuncSetAttribute(kv_pages_kernel<PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return SV_ECUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = KP_THREADS;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = blocks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PART == KP_MOVE ? 1 : 2;
+    ++g_launches;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_pages_kernel<PART>, a);
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e == cudaSuccess ? SV_OK : SV_ECUDA;
 }
 
 }  // namespace sv
@@ -248,26 +348,15 @@ extern "C" sv_status spec_kv_pages_update(const sv_kv_pages_params *p, void *str
         if (p->gamma == nullptr || p->cu_q == nullptr || p->n_rows == 0) return SV_EINVAL;
     }
     if (p->page_size != KP_PAGE) return SV_EUNSUPPORTED;
-    // page and row counts are summed in 32 bits
-    if (p->n_pages > 0x7fffffffLL || p->n_rows > 0x7fffffffLL || p->block_table_stride > 0x7fffffffLL / p->batch)
+    // pages and rows are counted in 32 bits, with room for a loop's last step
+    if (p->batch > KP_MAX_BATCH) return SV_EUNSUPPORTED;
+    if (p->n_pages > 0x7fffffffLL || p->n_rows > 0x7fffffffLL || p->block_table_stride > (1LL << 30) / p->batch)
         return SV_EUNSUPPORTED;
     KvPagesLaunch a;
     a.p = *p;
-    const int blocks = 8;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = blocks;
-    cfg.blockDim = KP_THREADS;
-    cfg.stream = (cudaStream_t)stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = blocks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    ++g_launches;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kv_pages_kernel, a);
-    if (e != cudaSuccess) (void)cudaGetLastError();
-    return e == cudaSuccess ? SV_OK : SV_ECUDA;
+    a.search = 1;
+    while (2 * a.search <= p->batch) a.search *= 2;
+    if (p->batch <= KP_ONE_CLUSTER) return launch_pages<KP_WHOLE>(a, KP_CLUSTER, (cudaStream_t)stream);
+    const sv_status st = launch_pages<KP_MOVE>(a, sm_count(), (cudaStream_t)stream);
+    return st != SV_OK ? st : launch_pages<KP_CLOSE>(a, KP_CLUSTER, (cudaStream_t)stream);
 }
