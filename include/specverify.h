@@ -93,6 +93,54 @@ sv_status spec_kv_pool_register(const void *k_pool_device, const void *v_pool_de
                                 const int64_t strides[4], sv_kv_pool_t *out);
 sv_status spec_kv_pool_release(sv_kv_pool_t pool);
 
+/* ---------------------------------------------------------------- norm, rotation and append in one pass */
+/*
+ * What a target layer does between its projection and the verify attention
+ * (KV caching, paper Section 5), for every row r with slot_map[r] >= 0:
+ *   y = x * w / sqrt(mean_d(x_d^2) + eps)    each query head with q_weight, each key head with
+ *                                            k_weight; y = x where that pointer is NULL
+ *   for each frequency f < rot_dim / 2, with the pair (a, b) = (f, f + rot_dim/2), or (2f, 2f+1)
+ *   if interleaved, and the angle t = positions[axis of f][r] * inv_freq[f]:
+ *       z_a = scale * (y_a cos t - y_b sin t) ;  z_b = scale * (y_b cos t + y_a sin t)
+ *   z_d = y_d for d >= rot_dim
+ * Queries go to q_out, keys to slot slot_map[r] % 16 of page slot_map[r] / 16 of the pool, values
+ * there unchanged.  Rows with a negative slot (padding, as spec_kv_pages_update marks it) are
+ * neither read nor written.  A row is any position: draft blocks, single tokens, prompts.
+ * bf16 inputs, float32 arithmetic, one rounding to bf16 at the end; the angle is formed and
+ * reduced in float64, so that it keeps its digits at far positions.
+ * Slots of different rows must differ.  q_out may be q itself where q's rows are contiguous; it
+ * must not overlap q otherwise, nor k_new or v_new (SV_EINVAL).
+ * A slot at or beyond n_pages * 16 -> SV_DEV_BAD_PAGE, row skipped.  One launch; n_rows == 0
+ * returns SV_OK without one.
+ */
+typedef struct sv_rope_append_params {
+    const void *q;              /* device bf16, row r at r * q_stride: [hq, head_dim] contiguous */
+    int64_t q_stride;           /* elements between rows (a fused projection's width, for one), a multiple of 8 */
+    const void *k_new;          /* device bf16, rows of [hkv, head_dim] */
+    int64_t k_stride;
+    const void *v_new;          /* device bf16, rows of [hkv, head_dim] */
+    int64_t v_stride;
+    void *q_out;                /* device bf16 [n_rows, hq, head_dim]; all four 16-byte aligned */
+    sv_kv_pool_t pool;          /* head_dim a multiple of 16 */
+    int32_t hq;
+    int64_t n_rows;             /* < 2^31 */
+    const int64_t *slot_map;    /* device [n_rows] */
+    const int32_t *positions;   /* device [n_axes, n_rows] */
+    int32_t n_axes;             /* position axes (1; 3 for time, height, width) */
+    const uint8_t *freq_axis;   /* device [rot_dim/2]: axis of each frequency (one >= n_axes: the last), or NULL: axis 0 */
+    const double *inv_freq;     /* device [rot_dim/2]; NULL if rot_dim is 0 */
+    int32_t rot_dim;            /* rotated dims: a multiple of 16, 0 .. head_dim */
+    int32_t interleaved;        /* 0: pairs (f, f + rot_dim/2); 1: pairs (2f, 2f+1) */
+    float rope_scale;           /* factor of the rotated dims, usually 1 */
+    const void *q_weight;       /* device [head_dim], 16-byte aligned, or NULL: queries are not normalised */
+    const void *k_weight;       /* device [head_dim], 16-byte aligned, or NULL: keys are not normalised */
+    int32_t weights_f32;        /* 0: the weights are bf16, 1: float32 */
+    float eps;                  /* >= 0 */
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_rope_append_params;
+
+sv_status spec_rope_append(const sv_rope_append_params *p, void *stream);
+
 /* ---------------------------------------------------------------- block tables and slot maps */
 /*
  * The controller moves every seq_len[b] on the device (gamma_tune_update), so the

@@ -282,3 +282,21 @@ def kv_pages_update(seq_len, block_table, n_held, free_list, n_free, n_rows=0, g
                                       ctypes.c_int(gamma_max), _p(slot) if rows else None, _p(pos) if rows else None,
                                       ctypes.c_int64(n_rows))
     return bt, held, fl, int(nf[0]), slot[:n_rows], pos[:n_rows], int(cond)
+
+
+# --------------------------------------------------------------------------- norm, rotation and append in one pass
+def norm_rotate(x_bits, positions, inv_freq, weight=None, eps=1e-6, interleaved=False, freq_axis=None, scale=1.0):
+    """Per-head norm and rotation of bf16 heads (uint16 [n, heads, D]) at positions int32 [n] or [axes, n].
+    Returns (z, mag), both float64 [n, heads, D]: the unrounded result, and the size that its errors scale with."""
+    lib = _load()
+    x = _c(x_bits, np.uint16)
+    n, heads, D = x.shape
+    pos, f = _c(positions, np.int32), _c(inv_freq, np.float64)
+    assert pos.size % max(n, 1) == 0 and 2 * len(f) <= min(D, 2048)
+    w = _c(weight, np.float64) if weight is not None else None
+    ax = _c(freq_axis, np.uint8) if freq_axis is not None else None
+    z, mag = np.zeros((n, heads, D)), np.zeros((n, heads, D))
+    lib.oracle_norm_rotate_rows(_p(x), ctypes.c_int64(heads * D), ctypes.c_int(n), ctypes.c_int(heads), ctypes.c_int(D),
+                                _p(w) if w is not None else None, ctypes.c_double(eps), _p(pos), _p(ax) if ax is not None else None,
+                                _p(f), ctypes.c_int(2 * len(f)), ctypes.c_int(int(interleaved)), ctypes.c_double(scale), _p(z), _p(mag))
+    return z, mag

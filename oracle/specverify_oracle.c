@@ -577,3 +577,48 @@ int oracle_kv_pages_update(const int32_t *seq_len, int batch, int32_t *block_tab
     free(has);
     return cond;
 }
+
+/* =========================================================================
+ * 7. Norm, rotation and append of one row's heads (KV caching, paper Section 5).
+ *    One head of D bf16 values: y = x * w / sqrt(mean x^2 + eps) (y = x without
+ *    weights), then each pair (a, b) turned by pos * inv_freq and scaled.
+ *    z: the result in float64 (not rounded); mag: scale * (|y_a| + |y_b|) of the
+ *    element's pair (|y_d| outside the rotated dims), the scale that rounding
+ *    errors of the result are measured against.
+ * ========================================================================= */
+void oracle_norm_rotate(const uint16_t *x, int D, const double *weight, double eps, const double *angle, int rot_dim,
+                        int interleaved, double scale, double *z, double *mag)
+{
+    double ss = 0.0;
+    for (int d = 0; d < D; ++d) {
+        z[d] = bf16_bits_to_f64(x[d]);
+        ss += z[d] * z[d];
+    }
+    if (weight)
+        for (int d = 0; d < D; ++d) z[d] = z[d] * weight[d] / sqrt(ss / D + eps);
+    for (int d = 0; d < D; ++d) mag[d] = fabs(z[d]);
+    for (int f = 0; f < rot_dim / 2; ++f) {
+        int a = interleaved ? 2 * f : f, b = interleaved ? 2 * f + 1 : f + rot_dim / 2;
+        double ya = z[a], yb = z[b], c = cos(angle[f]), s = sin(angle[f]);
+        z[a] = scale * (ya * c - yb * s);
+        z[b] = scale * (yb * c + ya * s);
+        mag[a] = mag[b] = fabs(scale) * (fabs(ya) + fabs(yb));
+    }
+}
+
+/* rows [n, heads, D] (row r starts at r * stride): heads of every row through oracle_norm_rotate */
+void oracle_norm_rotate_rows(const uint16_t *x, int64_t stride, int n, int heads, int D, const double *weight, double eps,
+                             const int32_t *positions, const uint8_t *freq_axis, const double *inv_freq, int rot_dim,
+                             int interleaved, double scale, double *z, double *mag)
+{
+#pragma omp parallel for schedule(static)
+    for (int r = 0; r < n; ++r) {
+        double angle[1024];
+        for (int f = 0; f < rot_dim / 2; ++f)
+            angle[f] = (double)positions[(freq_axis ? (int64_t)freq_axis[f] * n : 0) + r] * inv_freq[f];
+        for (int h = 0; h < heads; ++h) {
+            int64_t o = ((int64_t)r * heads + h) * D;
+            oracle_norm_rotate(x + r * stride + (int64_t)h * D, D, weight, eps, angle, rot_dim, interleaved, scale, z + o, mag + o);
+        }
+    }
+}

@@ -27,7 +27,7 @@ EXPORTS = (
     "spec_accept_sample", "spec_accept_sample_static", "gamma_tune_update", "gamma_tune_init",
     "spec_verify_step_host", "spec_draft_stop_workspace_bytes", "spec_draft_stop", "spec_kv_append",
     "sv_selftest_wait_expiry", "spec_verify_attn_layers", "spec_draft_step_workspace_bytes", "spec_draft_step",
-    "spec_kv_pages_update",
+    "spec_kv_pages_update", "spec_rope_append",
 )
 
 
@@ -65,6 +65,16 @@ class KvPagesParams(C.Structure):
                 ("n_free", C.c_void_p), ("n_pages", C.c_int64), ("page_size", C.c_int32),
                 ("gamma", C.c_void_p), ("cu_q", C.c_void_p), ("gamma_max", C.c_int32),
                 ("slot_map", C.c_void_p), ("positions", C.c_void_p), ("n_rows", C.c_int64),
+                ("device_status", C.c_void_p)]
+
+
+class RopeAppendParams(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("k_new", C.c_void_p), ("k_stride", C.c_int64),
+                ("v_new", C.c_void_p), ("v_stride", C.c_int64), ("q_out", C.c_void_p), ("pool", C.c_void_p),
+                ("hq", C.c_int32), ("n_rows", C.c_int64), ("slot_map", C.c_void_p), ("positions", C.c_void_p),
+                ("n_axes", C.c_int32), ("freq_axis", C.c_void_p), ("inv_freq", C.c_void_p), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("rope_scale", C.c_float), ("q_weight", C.c_void_p),
+                ("k_weight", C.c_void_p), ("weights_f32", C.c_int32), ("eps", C.c_float),
                 ("device_status", C.c_void_p)]
 
 
@@ -164,6 +174,8 @@ def load():
         lib.spec_draft_step_workspace_bytes.argtypes = [C.c_int32] * 2
         lib.spec_kv_pages_update.restype = C.c_int32
         lib.spec_kv_pages_update.argtypes = [C.POINTER(KvPagesParams), C.c_void_p]
+        lib.spec_rope_append.restype = C.c_int32
+        lib.spec_rope_append.argtypes = [C.POINTER(RopeAppendParams), C.c_void_p]
         lib.spec_draft_step.restype = C.c_int32
         lib.spec_draft_step.argtypes = [C.POINTER(DraftStepParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_verify_step_host.restype = C.c_int32
@@ -387,6 +399,62 @@ def spec_kv_pages_update(seq_len, block_table, n_held, free_list, n_free, gamma=
     p = kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, gamma_max, slot_map,
                         positions, device_status, index)
     _check("spec_kv_pages_update", load().spec_kv_pages_update(C.byref(p), raw))
+
+
+# --------------------------------------------------------------------------- norm, rotation and append in one pass
+def _head_rows(t, heads, head_dim, n_rows, name, index):
+    """Device pointer and row stride of [n_rows, heads, head_dim] bf16 heads; the rows may be strided."""
+    if t.get_device() != index or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a bf16 tensor on the current device (cuda:{index})")
+    if t.dim() != 3 or t.shape != (n_rows, heads, head_dim):
+        raise ValueError(f"{name} must be [{n_rows}, {heads}, {head_dim}], got {tuple(t.shape)}")
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (s1 != head_dim and heads > 1):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    return t.data_ptr(), s0 if n_rows > 1 else heads * head_dim
+
+
+def rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight=None, k_weight=None,
+                       eps=1e-6, interleaved=False, freq_axis=None, rope_scale=1.0, device_status=None,
+                       index=None) -> RopeAppendParams:
+    index = torch.cuda.current_device() if index is None else index
+    if q.dim() != 3:
+        raise ValueError("q must be [n_rows, hq, head_dim]")
+    n_rows, hq, head_dim = q.shape
+    if head_dim != pool.head_dim:
+        raise ValueError("q's head_dim is not the pool's")
+    qp, qs = _head_rows(q, hq, head_dim, n_rows, "q", index)
+    kp, ks = _head_rows(k_new, pool.hkv, head_dim, n_rows, "k_new", index)
+    vp, vs = _head_rows(v_new, pool.hkv, head_dim, n_rows, "v_new", index)
+    if q_out.shape != q.shape or slot_map.numel() != n_rows:
+        raise ValueError("q_out must have q's shape, slot_map one entry per row")
+    axes = positions.shape[0] if positions.dim() == 2 else 1
+    if positions.numel() != axes * n_rows:
+        raise ValueError("positions must be [n_rows] or [n_axes, n_rows]")
+    rot = 2 * inv_freq.numel() if inv_freq is not None else 0
+    if freq_axis is not None and 2 * freq_axis.numel() != rot:
+        raise ValueError("freq_axis must have one entry per frequency")
+    w = q_weight if q_weight is not None else k_weight
+    wt = w.dtype if w is not None and w.dtype == torch.float32 else torch.bfloat16      # float32 or bf16 weights
+    for x in (q_weight, k_weight):
+        if x is not None and x.numel() != head_dim:
+            raise ValueError("norm weights must have head_dim entries")
+    return RopeAppendParams(qp, qs, kp, ks, vp, vs, _on(q_out, torch.bfloat16, "q_out", index), pool.handle, hq, n_rows,
+                            _on(slot_map, torch.int64, "slot_map", index), _on(positions, torch.int32, "positions", index),
+                            axes, _on(freq_axis, torch.uint8, "freq_axis", index),
+                            _on(inv_freq, torch.float64, "inv_freq", index), rot, 1 if interleaved else 0, rope_scale,
+                            _on(q_weight, wt, "q_weight", index), _on(k_weight, wt, "k_weight", index),
+                            1 if wt == torch.float32 else 0, eps, _on(device_status, torch.int32, "device_status", index))
+
+
+def spec_rope_append(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight=None, k_weight=None,
+                     eps=1e-6, interleaved=False, freq_axis=None, rope_scale=1.0, device_status=None, stream=None):
+    """Per-head norm of queries and keys, position rotation, and keys and values written into the paged cache by slot
+    (asynchronous).  q, k_new and v_new may be views of one projection's output."""
+    index, raw = _launch_at(stream, q, "q")
+    p = rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight, k_weight, eps,
+                           interleaved, freq_axis, rope_scale, device_status, index)
+    _check("spec_rope_append", load().spec_rope_append(C.byref(p), raw))
 
 
 # --------------------------------------------------------------------------- accept / resample
