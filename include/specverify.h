@@ -123,7 +123,7 @@ typedef struct sv_rope_append_params {
     void *q_out;                /* device bf16 [n_rows, hq, head_dim]; all four 16-byte aligned */
     sv_kv_pool_t pool;          /* head_dim a multiple of 16 */
     int32_t hq;
-    int64_t n_rows;             /* < 2^31 */
+    int64_t n_rows;             /* <= 2^30 */
     const int64_t *slot_map;    /* device [n_rows] */
     const int32_t *positions;   /* device [n_axes, n_rows] */
     int32_t n_axes;             /* position axes (1; 3 for time, height, width) */

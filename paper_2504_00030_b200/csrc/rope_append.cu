@@ -1,19 +1,28 @@
 // Per-head norm of queries and keys, position rotation and cache append in one pass (KV caching, paper Section 5).
 //
 // y = x * w * rsqrt(mean(x^2) + eps), then z = y rotated by the row's angles; queries to the attention's input, keys and
-// values to the row's slot of the paged cache.  Every element is read once and written once, so HBM bounds it: the
-// norm's sum lives in the registers of the lanes that hold the head.
+// values to the row's slot of the paged cache.  Every element is read once and written once, so HBM bounds large
+// calls and the latency of one pass through the chain small ones.
 //
-// A lane holds two 16-byte chunks (16 dims) of a head and D / 16 lanes hold the head.  Which two is chosen so that
-// a rotated pair never leaves its lane: chunks j and j + rot/16 where the pairs are (f, f + rot/2), chunks 2j and 2j + 1
-// where they are (2f, 2f + 1).  Either way the lane's eight pairs have the frequencies 8j .. 8j + 7, and only the norm's
-// sum crosses lanes (two to four shuffles).
+// A lane holds two 16-byte chunks (16 dims) of a head and head_dim / 16 lanes hold the head.  Which two is chosen so
+// that a rotated pair never leaves its lane: the norm's sum alone crosses lanes (two or three shuffles).
+//
+// One warp takes one row, or a part of its heads when there are few rows; its heads arrive through a ring of asynchronous
+// copies in shared memory, RA_STAGES - 1 KB ahead, while the angles are formed and earlier heads are finished.  Measured
+// for 16381 rows of 32 + 8 + 8 heads of 128 dims (402 MB, 62 us at the copy rate): 157 us with a block per row and the
+// angles shared through its barrier, 81 us with loads held in registers two rounds ahead, 66 us (6.1 TB/s) with the ring.  Half
+// of that step is instructions: scalar float32 arithmetic took 64 million warp instructions (72 % of the issue
+// slots), the packed form below 42 million.  Warps that loop over rows and fetch the next row's slot early run in step with
+// one another and reach 5.2 TB/s only.
 #include "attn_common.cuh"
 #include "common.cuh"
 
 namespace sv {
 
 constexpr int RA_THREADS = 256;
+constexpr int RA_BLOCKS_PER_SM = 2;        // the factors take registers: three blocks spill, 97 us instead of 66
+constexpr int RA_WARPS = RA_THREADS / 32;
+constexpr int RA_STAGES = 6;               // rounds of a warp under way, in shared memory (1 KB each)
 constexpr int RA_PAGE = 16;
 constexpr int RA_MAX_FREQ = 64;            // rot_dim <= head_dim <= 128
 
@@ -24,159 +33,284 @@ struct RopeAppendLaunch {
     long long n_slots;
     long long stride_page, stride_head, stride_slot;   // in 16-byte chunks
     int hkv, lanes;                        // lanes that hold a head (head_dim / 16)
+    int q_rounds, k_rounds;                // rounds of a row's queries; of its keys, and of its values
+    int rounds, segments;                  // rounds of a warp; warps that share a row
+    float inv_dim;
 };
 
-__device__ __forceinline__ uint4 ld_chunk(const uint4 *p)
+// 16 bytes from global to shared memory, asynchronously; a group is the copies between two commits of a thread
+__device__ __forceinline__ void cp_chunk(uint32_t dst, const uint4 *src)
 {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Two float32 values in a register pair: one instruction does both (the kernel is bound by instructions issued before it is
+// bound by HBM).
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi)
+{
+    f32x2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
     return v;
 }
-__device__ __forceinline__ void unpack8(const uint4 &v, float *x)
+__device__ __forceinline__ float2 split(f32x2 v)
 {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    float2 x;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.x), "=f"(x.y) : "l"(v));
+    return x;
 }
-__device__ __forceinline__ uint4 pack8(const float *x)
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
 {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);      // the one rounding
-        w[i] = *reinterpret_cast<const uint32_t *>(&h);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
-// eight norm weights of a chunk
-__device__ __forceinline__ void load_weights(const void *w, int f32, int chunk, float *x)
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
 {
-    if (f32) {
-        const float4 *s = static_cast<const float4 *>(w) + 2 * chunk;
-        const float4 a = __ldg(s), b = __ldg(s + 1);
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-        unpack8(__ldg(static_cast<const uint4 *>(w) + chunk), x);
-    }
+    f32x2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ f32x2 unpack2(uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t pack2(f32x2 v)                   // the one rounding
+{
+    const float2 x = split(v);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// GL: lanes given to a head (a power of two >= head_dim / 16)
-template <int GL>
-__global__ void __launch_bounds__(RA_THREADS)
+// Fraction of a turn that one position step adds at a frequency, in units of 2^-64.  pos * step in 64-bit integers then
+// drops whole turns exactly, at any 32-bit position: the angle of a far position keeps its digits, and float64
+// arithmetic is needed once per frequency and warp only.
+__device__ __forceinline__ unsigned long long turn_step(double inv_freq)
+{
+    double t = inv_freq * 0.15915494309189535;                       // turns per position
+    t -= floor(t);
+    return __double2ull_rz(t * 18446744073709551616.0);
+}
+
+struct RopeShared {
+    uint4 ring[RA_WARPS][RA_STAGES][2][32];            // a round's chunks on their way: each lane reads back its own
+    float2 turns[RA_WARPS][RA_MAX_FREQ];               // (cos, sin) of the warp's row
+};
+
+// GL: lanes given to a head (a power of two >= head_dim / 16).  PAIRED: pairs (2f, 2f + 1).  WF32: float32 weights.
+// A round is 32 / GL heads of one kind (queries, keys, values); a warp has `rounds` consecutive rounds of a row.
+template <int GL, bool PAIRED, bool WF32>
+__global__ void __launch_bounds__(RA_THREADS, RA_BLOCKS_PER_SM)
 rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
 {
     pdl_enter();
-    __shared__ float2 turn[RA_MAX_FREQ];               // (cos, sin) of the row's angles
+    constexpr int PER_ROUND = 32 / GL;
+    extern __shared__ __align__(16) uint8_t ra_smem[];
+    RopeShared &sh = *reinterpret_cast<RopeShared *>(ra_smem);
     const sv_rope_append_params &p = a.p;
-    const long long row = blockIdx.x;
-    const long long slot = __ldg(p.slot_map + row);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = lane % GL, slot_h = lane / GL;
+    const long long item = (long long)blockIdx.x * RA_WARPS + warp, row = item / a.segments;
+    if (row >= p.n_rows) return;
+    const int k_first = a.q_rounds, v_first = a.q_rounds + a.k_rounds;         // first rounds of keys and of values
+    const int t_begin = (int)(item - row * a.segments) * a.rounds, t_end = min(t_begin + a.rounds, v_first + a.k_rounds);
+    // Loads that nothing waits for come first: the slot, and what belongs to frequencies lane and lane + 32.
+    const long long slot = p.slot_map[row];
+    const bool turning = t_begin < v_first && p.rot_dim > 0;
+    double freq[2] = {0.0, 0.0};
+    int pos[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int f = lane + 32 * i;
+        if (!turning || f >= p.rot_dim / 2) continue;
+        freq[i] = p.inv_freq[f];
+        const int axis = p.freq_axis != nullptr ? min((int)p.freq_axis[f], p.n_axes - 1) : 0;
+        pos[i] = p.positions[axis * p.n_rows + row];
+    }
     if (slot < 0) return;
     if (slot >= a.n_slots) {
-        if (threadIdx.x == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
+        if (lane == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
         return;
     }
-    const int tid = threadIdx.x, j = tid % GL;
-    const int nf = p.rot_dim / 2, pair_lanes = p.rot_dim / 16;
-    const bool live = j < a.lanes, turned = j < pair_lanes;
-    int c0 = 2 * j, c1 = 2 * j + 1;                    // this lane's chunks
-    if (turned && !p.interleaved) {
-        c0 = j;
-        c1 = j + pair_lanes;
-    }
-    for (int f = tid; f < nf; f += RA_THREADS) {
-        const int axis = p.freq_axis != nullptr ? min((int)__ldg(p.freq_axis + f), p.n_axes - 1) : 0;
-        const int pos = __ldg(p.positions + (long long)axis * p.n_rows + row);
-        // whole turns drop out in float64; what is left is below half a turn
-        double t = (double)pos * (__ldg(p.inv_freq + f) * 0.15915494309189535);
-        t -= rint(t);
-        float s, c;
-        sincospif((float)(2.0 * t), &s, &c);
-        turn[f] = make_float2(c * p.rope_scale, s * p.rope_scale);
-    }
-    __syncthreads();
-    float cs[8], sn[8];
+    // This lane's chunks, neighbouring lanes at neighbouring ones.  Where the pairs are (f, f + rot/2), the first rot/16 lanes
+    // hold the turned dims; pairs (2f, 2f + 1) lie within a chunk.
+    const int pair_lanes = PAIRED ? a.lanes : p.rot_dim / 16;
+    const bool live = j < a.lanes, low = j < pair_lanes;
+    const int c0 = low ? j : pair_lanes + j, c1 = low ? j + pair_lanes : a.lanes + j;
+    const bool turn0 = c0 < p.rot_dim / 8, turn1 = c1 < p.rot_dim / 8;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[warp][0][0][lane]);
+    float2 *turns = sh.turns[warp];
+    // ---- producer: the rounds in order, RA_STAGES - 1 of them under way
+    int p_t = t_begin, p_stage = 0;
+    auto issue = [&]() {
+        if (p_t < t_end) {
+            const bool q = p_t < k_first, v = p_t >= v_first;
+            const int h = (p_t - (q ? 0 : v ? v_first : k_first)) * PER_ROUND + slot_h;
+            if (live && h < (q ? p.hq : a.hkv)) {
+                const uint4 *src = static_cast<const uint4 *>(q ? p.q : v ? p.v_new : p.k_new) +
+                                   row * ((q ? p.q_stride : v ? p.v_stride : p.k_stride) / 8) + h * (2 * a.lanes);
+                cp_chunk(ring + p_stage * 1024, src + c0);
+                cp_chunk(ring + p_stage * 1024 + 512, src + c1);
+            }
+            ++p_t;
+        }
+        p_stage = p_stage + 1 == RA_STAGES ? 0 : p_stage + 1;
+        cp_commit();                                   // an empty group where nothing is left
+    };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float2 v = turned ? turn[8 * j + i] : make_float2(1.f, 0.f);
-        cs[i] = v.x;
-        sn[i] = v.y;
+    for (int s = 0; s < RA_STAGES - 1; ++s) issue();
+    // ---- angles
+    if (turning) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (lane + 32 * i >= p.rot_dim / 2) continue;
+            const int t = (int)(turn_step(freq[i]) * (unsigned long long)(long long)pos[i] >> 32);     // [-1/2, 1/2) turns, in units of 2^-32
+            float s, c;
+            sincospif((float)t * 4.656612873077393e-10f, &s, &c);                                      // 2^-31: half turns
+            turns[lane + 32 * i] = make_float2(c * p.rope_scale, s * p.rope_scale);
+        }
+        __syncwarp();
     }
+    // ---- consumer
+    int stage = 0;
     const long long cache = (slot / RA_PAGE) * a.stride_page + (slot % RA_PAGE) * a.stride_slot;
-    const int heads = p.hq + 2 * a.hkv;
-    const int chunks = 2 * a.lanes;
-    // all lanes of a warp make the same number of rounds (the norm's shuffles)
-    for (int h0 = 0; h0 < heads; h0 += RA_THREADS / GL) {
-        const int h = h0 + tid / GL;
-        const uint4 *src = nullptr;
-        uint4 *dst = nullptr;
-        const void *weight = nullptr;
-        bool rotate = turned;
-        if (live && h < heads) {
-            if (h < p.hq) {
-                src = static_cast<const uint4 *>(p.q) + row * (p.q_stride / 8) + (long long)h * chunks;
-                dst = static_cast<uint4 *>(p.q_out) + (row * p.hq + h) * chunks;
-                weight = p.q_weight;
-            } else if (h < p.hq + a.hkv) {
-                src = static_cast<const uint4 *>(p.k_new) + row * (p.k_stride / 8) + (long long)(h - p.hq) * chunks;
-                dst = a.k_pool + cache + (h - p.hq) * a.stride_head;
-                weight = p.k_weight;
-            } else {
-                src = static_cast<const uint4 *>(p.v_new) + row * (p.v_stride / 8) + (long long)(h - p.hq - a.hkv) * chunks;
-                dst = a.v_pool + cache + (h - p.hq - a.hkv) * a.stride_head;
-                rotate = false;
+    // queries, then keys
+    for (int kind = 0; kind < 2; ++kind) {
+        const int first_t = kind == 0 ? 0 : k_first, t0 = max(t_begin, first_t), t1 = min(t_end, kind == 0 ? k_first : v_first);
+        if (t0 >= t1) continue;
+        const int n_heads = kind == 0 ? p.hq : a.hkv;
+        int h = (t0 - first_t) * PER_ROUND + slot_h;
+        const long long dst_head = kind == 0 ? 2 * a.lanes : a.stride_head;
+        uint4 *dst = (kind == 0 ? static_cast<uint4 *>(p.q_out) + row * p.hq * (2 * a.lanes) : a.k_pool + cache) + h * dst_head;
+        const void *weight = kind == 0 ? p.q_weight : p.k_weight;
+        // Factors of the row, weight and angle in one: with the pairs (a, b) in the two chunks,
+        // z_a = r (x_a (w_a cos) + x_b (-w_b sin)) and z_b = r (x_b (w_b cos) + x_a (w_a sin)); with the pairs in a chunk
+        // the same for its even and odd elements.  direct[] multiplies an element itself, across[] its partner.
+        f32x2 direct0[4], direct1[4], across0[4], across1[4];
+        {
+            uint4 w0 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), w1 = w0;      // ones
+            if (!WF32 && weight != nullptr) {
+                w0 = __ldg(static_cast<const uint4 *>(weight) + (live ? c0 : 0));
+                w1 = __ldg(static_cast<const uint4 *>(weight) + (live ? c1 : 0));
             }
-        }
-        uint4 v0 = make_uint4(0, 0, 0, 0), v1 = v0;
-        if (src != nullptr) {
-            v0 = ld_chunk(src + c0);
-            v1 = ld_chunk(src + c1);
-        }
-        float x[16];
-        unpack8(v0, x);
-        unpack8(v1, x + 8);
-        float ss = 0.f;
+            const uint32_t m0[4] = {w0.x, w0.y, w0.z, w0.w}, m1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
-#pragma unroll
-        for (int m = GL / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-        if (src == nullptr) continue;
-        if (weight != nullptr) {
-            const float r = rsqrtf(ss / (float)(16 * a.lanes) + p.eps);
-            float w[16];
-            load_weights(weight, p.weights_f32, c0, w);
-            load_weights(weight, p.weights_f32, c1, w + 8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
-        }
-        if (rotate) {
-            if (p.interleaved) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float u = x[2 * i], v = x[2 * i + 1];
-                    x[2 * i] = u * cs[i] - v * sn[i];
-                    x[2 * i + 1] = v * cs[i] + u * sn[i];
+            for (int i = 0; i < 4; ++i) {
+                f32x2 wa = unpack2(m0[i]), wb = unpack2(m1[i]);
+                if (WF32 && weight != nullptr && live) {
+                    const float2 fa = __ldg(static_cast<const float2 *>(weight) + 4 * c0 + i), fb = __ldg(static_cast<const float2 *>(weight) + 4 * c1 + i);
+                    wa = pair(fa.x, fa.y);
+                    wb = pair(fb.x, fb.y);
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float u = x[i], v = x[8 + i];
-                    x[i] = u * cs[i] - v * sn[i];
-                    x[8 + i] = v * cs[i] + u * sn[i];
+                direct0[i] = wa;
+                direct1[i] = wb;
+                if (PAIRED) {
+                    const float2 ta = turns[turn0 ? 4 * c0 + i : 0], tb = turns[turn1 ? 4 * c1 + i : 0];
+                    const float2 xa = split(wa), xb = split(wb);
+                    if (turn0) direct0[i] = mul2(wa, pair(ta.x, ta.x));
+                    if (turn1) direct1[i] = mul2(wb, pair(tb.x, tb.x));
+                    across0[i] = mul2(pair(xa.y, xa.x), pair(-ta.y, ta.y));
+                    across1[i] = mul2(pair(xb.y, xb.x), pair(-tb.y, tb.y));
+                } else {
+                    const float4 cs = reinterpret_cast<const float4 *>(turns)[turn0 ? 4 * j + i : 0];
+                    if (turn0) {
+                        direct0[i] = mul2(wa, pair(cs.x, cs.z));
+                        direct1[i] = mul2(wb, pair(cs.x, cs.z));
+                    }
+                    across0[i] = mul2(wb, pair(-cs.y, -cs.w));
+                    across1[i] = mul2(wa, pair(cs.y, cs.w));
                 }
             }
         }
-        if (weight == nullptr && !rotate) {            // values, and what is neither normalised nor turned: the same bits
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t) {
+            cp_wait<RA_STAGES - 2>();
+            const uint4 v0 = sh.ring[warp][stage][0][lane], v1 = sh.ring[warp][stage][1][lane];
+            stage = stage + 1 == RA_STAGES ? 0 : stage + 1;
+            const uint32_t b0[4] = {v0.x, v0.y, v0.z, v0.w}, b1[4] = {v1.x, v1.y, v1.z, v1.w};
+            f32x2 x0[4], x1[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x0[i] = unpack2(b0[i]);
+                x1[i] = unpack2(b1[i]);
+            }
+            issue();
+            const bool here = live && h < n_heads;
+            float r = 1.f;
+            if (weight != nullptr) {
+                f32x2 s0 = mul2(x0[0], x0[0]), s1 = mul2(x1[0], x1[0]);
+#pragma unroll
+                for (int i = 1; i < 4; ++i) {
+                    s0 = fma2(x0[i], x0[i], s0);
+                    s1 = fma2(x1[i], x1[i], s1);
+                }
+                float ss = here ? (split(s0).x + split(s0).y) + (split(s1).x + split(s1).y) : 0.f;
+#pragma unroll
+                for (int m = GL / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+                r = rsqrtf(ss * a.inv_dim + p.eps);
+            }
+            const f32x2 rr = pair(r, r);
+            uint32_t z0[4], z1[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f32x2 y0 = mul2(x0[i], direct0[i]), y1 = mul2(x1[i], direct1[i]);
+                if (PAIRED) {
+                    if (turn0) y0 = fma2(pair(split(x0[i]).y, split(x0[i]).x), across0[i], y0);
+                    if (turn1) y1 = fma2(pair(split(x1[i]).y, split(x1[i]).x), across1[i], y1);
+                } else if (turn0) {                // both chunks or none
+                    y0 = fma2(x1[i], across0[i], y0);
+                    y1 = fma2(x0[i], across1[i], y1);
+                }
+                z0[i] = pack2(mul2(y0, rr));
+                z1[i] = pack2(mul2(y1, rr));
+            }
+            if (here) {
+                dst[c0] = make_uint4(z0[0], z0[1], z0[2], z0[3]);
+                dst[c1] = make_uint4(z1[0], z1[1], z1[2], z1[3]);
+            }
+            h += PER_ROUND;
+            dst += PER_ROUND * dst_head;
+        }
+    }
+    // values
+    for (int t = max(t_begin, v_first); t < t_end; ++t) {
+        cp_wait<RA_STAGES - 2>();
+        const uint4 v0 = sh.ring[warp][stage][0][lane], v1 = sh.ring[warp][stage][1][lane];
+        stage = stage + 1 == RA_STAGES ? 0 : stage + 1;
+        const int h = (t - v_first) * PER_ROUND + slot_h;
+        if (live && h < a.hkv) {
+            uint4 *dst = a.v_pool + cache + h * a.stride_head;
             dst[c0] = v0;
             dst[c1] = v1;
-        } else {
-            dst[c0] = pack8(x);
-            dst[c1] = pack8(x + 8);
         }
+        issue();
     }
+}
+
+template <int GL, bool PAIRED, bool WF32>
+static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
+{
+    constexpr int per_round = 32 / GL;
+    a.q_rounds = (a.p.hq + per_round - 1) / per_round;
+    a.k_rounds = (a.hkv + per_round - 1) / per_round;
+    const int all = a.q_rounds + 2 * a.k_rounds;
+    // How many warps share a row: the fewest waves of resident warps, where a row costs a warp about as much as two rounds
+    // before its first one (angles, factors, the pipeline's start).
+    const long long resident = (long long)sm_count() * RA_BLOCKS_PER_SM * RA_WARPS;
+    long long best = -1;
+    for (int segments = 1; segments <= all; ++segments) {
+        const int rounds = (all + segments - 1) / segments;
+        const long long cost = (a.p.n_rows * segments + resident - 1) / resident * (rounds + 2);
+        if (best >= 0 && cost >= best) continue;
+        best = cost;
+        a.rounds = rounds;
+        a.segments = (all + rounds - 1) / rounds;
+    }
+    const long long warps = a.p.n_rows * a.segments;
+    const unsigned blocks = (unsigned)((warps + RA_WARPS - 1) / RA_WARPS);
+    if (cudaFuncSetAttribute(rope_append_kernel<GL, PAIRED, WF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RopeShared)) !=
+        cudaSuccess)
+        return SV_ECUDA;
+    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, dim3(blocks), RA_THREADS, sizeof(RopeShared), stream, a);
 }
 
 // [a, a + na) and [b, b + nb) share a byte
@@ -195,7 +329,7 @@ extern "C" sv_status spec_rope_append(const sv_rope_append_params *p, void *stre
     const sv_kv_pool &pool = *p->pool;
     if (p->hq <= 0 || p->n_axes <= 0 || p->rot_dim < 0 || p->rot_dim > pool.head_dim || !(p->eps >= 0.f)) return SV_EINVAL;
     if (pool.head_dim % 16 != 0 || p->rot_dim % 16 != 0) return SV_EUNSUPPORTED;
-    if (p->n_rows > 0x7fffffffLL) return SV_EUNSUPPORTED;
+    if (p->n_rows > 1 << 30) return SV_EUNSUPPORTED;       // rows are counted in 32 bits, with room for a step
     const long long q_row = (long long)p->hq * pool.head_dim, kv_row = (long long)pool.hkv * pool.head_dim;
     if (p->q_stride < q_row || p->k_stride < kv_row || p->v_stride < kv_row) return SV_EINVAL;
     if (p->n_rows == 0) return SV_OK;
@@ -224,8 +358,17 @@ extern "C" sv_status spec_rope_append(const sv_rope_append_params *p, void *stre
     a.stride_slot = pool.strides[2] / 8;
     a.hkv = pool.hkv;
     a.lanes = pool.head_dim / 16;
-    const dim3 grid((unsigned)p->n_rows);
+    a.inv_dim = 1.f / (float)pool.head_dim;
     cudaStream_t s = (cudaStream_t)stream;
-    if (a.lanes <= 4) return launch_kernel(true, rope_append_kernel<4>, grid, RA_THREADS, 0, s, a);
-    return launch_kernel(true, rope_append_kernel<8>, grid, RA_THREADS, 0, s, a);
+    const int kind = (a.lanes <= 4 ? 0 : 4) + (p->interleaved != 0 ? 2 : 0) + (p->weights_f32 != 0 ? 1 : 0);
+    switch (kind) {
+        case 0: return launch_rope<4, false, false>(a, s);
+        case 1: return launch_rope<4, false, true>(a, s);
+        case 2: return launch_rope<4, true, false>(a, s);
+        case 3: return launch_rope<4, true, true>(a, s);
+        case 4: return launch_rope<8, false, false>(a, s);
+        case 5: return launch_rope<8, false, true>(a, s);
+        case 6: return launch_rope<8, true, false>(a, s);
+        default: return launch_rope<8, true, true>(a, s);
+    }
 }
