@@ -299,6 +299,100 @@ typedef struct sv_attn_layers_params {
 sv_status spec_verify_attn_layers(const sv_attn_layers_params *p, void *workspace_device,
                                   size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- penalties, biases and grammar masks */
+/*
+ * What a request asks for on top of the model's distribution, applied to the
+ * logits that spec_accept_sample (target rows) or spec_draft_step (draft rows)
+ * then reads (paper Section 3: both sides sample from these rows).  For element
+ * k of a row, with C the times token k stands in the row's history, and S = k is
+ * in the history or in the prompt:
+ *     x1 = S ? (x > 0 ? x / repetition : x * repetition) : x
+ *     x2 = x1 - (frequency * C + (C > 0 ? presence : 0))
+ *     x3 = x2 + bias[k]
+ *     out = mask bit k is clear ? -inf : x3
+ * The history of target row i of a block is what the sequence has generated
+ * (token_counts) and the drafts x_0 .. x_{i-1} in front of the row, so that the
+ * row is what decoding token by token would have seen; that of a draft row is
+ * token_counts and the n_drafted[b] tokens drafted so far.
+ * A masked element is -inf whatever it held (NaN too); a row with nothing
+ * allowed is all -inf, which spec_accept_sample reports (SV_DEV_NONFINITE).
+ * float32 arithmetic, one rounding to the logits' type at the end.
+ * Target rows (n_drafted == NULL): rows cu_q[b] .. cu_q[b] + gamma[b]; rows of
+ * no sequence are left as they are.  Draft rows (n_drafted != NULL): row b.
+ * out may be logits itself (same stride): what does not change is then neither
+ * read nor written where the mask and the counts show it.  Otherwise the two
+ * must not overlap (SV_EINVAL).
+ * A bias list that names a token twice: the later entry counts.
+ * Device-detected: gamma[b] or n_drafted[b] outside [0, gamma_max] ->
+ * SV_DEV_BAD_GAMMA, clamped; a block with rows beyond n_rows -> SV_DEV_BAD_LEN,
+ * left as it is; drafts beyond n_d_rows -> SV_DEV_BAD_LEN, not counted; a draft or bias token outside
+ * [0, vocab) -> SV_DEV_BAD_TOKEN, ignored.  One launch, no workspace.
+ */
+typedef struct sv_logits_adjust_params {
+    const void *logits;         /* device [n_rows, row_stride] float32, or bf16 if logits_bf16 */
+    void *out;                  /* device [n_rows, out_stride], the same type */
+    int64_t row_stride;         /* elements between rows (>= vocab); both strides multiples of 4 (bf16: 8) with 16-byte */
+    int64_t out_stride;         /* aligned bases enable 128-bit access */
+    int64_t n_rows;
+    int32_t vocab;
+    int32_t logits_bf16;
+    int32_t batch;
+    int32_t gamma_max;
+    const int32_t *gamma;       /* device [batch]; target rows only */
+    const int32_t *cu_q;        /* device [batch+1]; target rows only */
+    const int32_t *cu_d;        /* device [batch+1]: first draft token of each sequence; with penalties and gamma_max > 0 */
+    const int32_t *n_drafted;   /* device [batch]: draft rows; NULL: target rows */
+    const int32_t *active;      /* device [batch] or NULL: the rows of sequences with active[b] == 0 are left as they are */
+    const int32_t *draft_tokens;/* device [n_d_rows]; with penalties and gamma_max > 0 */
+    int64_t n_d_rows;
+    const int16_t *token_counts;/* device [batch, count_stride], see spec_token_counts_update; needed by the penalties */
+    int64_t count_stride;       /* a multiple of 8, >= vocab; base 16-byte aligned */
+    const float *repetition;    /* device [batch], > 0 (1: none), or NULL */
+    const float *frequency;     /* device [batch] or NULL */
+    const float *presence;      /* device [batch] or NULL */
+    const int32_t *bias_tokens; /* device [batch, bias_stride], or NULL */
+    const float *bias_values;   /* device [batch, bias_stride] */
+    const int32_t *n_bias;      /* device [batch]: entries of each list, at most bias_stride (more: clamped, SV_DEV_BAD_LEN) */
+    int32_t bias_stride;
+    const uint32_t *mask;       /* device [n_rows, mask_stride]: bit k % 32 of word k / 32 set = token k allowed; or NULL */
+    int64_t mask_stride;        /* words between rows, >= ceil(vocab / 32) */
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_logits_adjust_params;
+
+sv_status spec_logits_adjust(const sv_logits_adjust_params *p, void *stream);
+
+/*
+ * The counts behind the penalties, kept on the device: token_counts[b][k] holds
+ * the times token k was generated in its low 15 bits (saturating at 32767) and in
+ * bit 15 whether it stands in the prompt.  One call, per sequence b:
+ *   reset[b] != 0: the row's vocab entries are cleared first (a request is admitted);
+ *   then each of its tokens is counted (prompt == 0), or marked (prompt != 0).
+ * Tokens of b: row b of tokens [batch, token_stride], max_tokens of them, or, with
+ * cu_tokens, tokens[cu_tokens[b]] .. tokens[cu_tokens[b+1] - 1].  Entries of -1
+ * are skipped, so out_tokens of spec_accept_sample (token_stride = max_tokens =
+ * gamma_max + 1) is counted as it stands, padding and all.
+ * The result does not depend on the order in which tokens are counted.
+ * Device-detected: another token outside [0, vocab) -> SV_DEV_BAD_TOKEN, skipped;
+ * a range of cu_tokens outside [0, n_tokens] or longer than max_tokens ->
+ * SV_DEV_BAD_LEN, none of that sequence's tokens are counted.  One launch.
+ */
+typedef struct sv_token_counts_params {
+    int16_t *token_counts;      /* device in/out [batch, count_stride], 16-byte aligned */
+    int64_t count_stride;       /* elements between rows: a multiple of 8, >= vocab */
+    int32_t vocab;
+    int32_t batch;
+    const int32_t *tokens;      /* device; may be NULL if max_tokens is 0 (reset alone) */
+    int64_t token_stride;       /* elements between rows, >= max_tokens; not used with cu_tokens */
+    const int32_t *cu_tokens;   /* device [batch+1], or NULL */
+    int64_t n_tokens;           /* entries of tokens; used with cu_tokens */
+    int32_t max_tokens;         /* most tokens of a sequence; sizes the grid */
+    const int32_t *reset;       /* device [batch] or NULL: nothing is cleared */
+    int32_t prompt;
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_token_counts_params;
+
+sv_status spec_token_counts_update(const sv_token_counts_params *p, void *stream);
+
 /* ---------------------------------------------------------------- accept / resample */
 /*
  * Speculative sampling (paper Section 3, after Leviathan et al. and Chen et

@@ -300,3 +300,37 @@ def norm_rotate(x_bits, positions, inv_freq, weight=None, eps=1e-6, interleaved=
                                 _p(w) if w is not None else None, ctypes.c_double(eps), _p(pos), _p(ax) if ax is not None else None,
                                 _p(f), ctypes.c_int(2 * len(f)), ctypes.c_int(int(interleaved)), ctypes.c_double(scale), _p(z), _p(mag))
     return z, mag
+
+
+# --------------------------------------------------------------------------- penalties, biases and grammar masks
+def logits_adjust(logits, gamma=None, cu_q=None, cu_d=None, n_drafted=None, draft_tokens=None, counts=None, repetition=None,
+                  frequency=None, presence=None, bias_tokens=None, bias_values=None, n_bias=None, mask=None):
+    """Returns (out, mag), float64 [n_rows, V]: the unrounded result (NaN in rows of no sequence), and the sum of the
+    magnitudes of its terms."""
+    lib = _load()
+    x = _c(logits, np.float32)
+    n_rows, V = x.shape
+    batch = len(n_drafted if n_drafted is not None else gamma)
+    opt = lambda a, dt: None if a is None else _c(a, dt)  # noqa: E731
+    g, cq, cd, nd = (opt(a, np.int32) for a in (gamma, cu_q, cu_d, n_drafted))
+    dt, ct = opt(draft_tokens, np.int32), opt(counts, np.int16)
+    rep, fr, pr = (opt(a, np.float32) for a in (repetition, frequency, presence))
+    bt, bv, nb, mk = opt(bias_tokens, np.int32), opt(bias_values, np.float32), opt(n_bias, np.int32), opt(mask, np.uint32)
+    out, mag = np.full((n_rows, V), np.nan), np.full((n_rows, V), np.nan)
+    ptr = lambda a: None if a is None else _p(a)  # noqa: E731
+    lib.oracle_logits_adjust(_p(x), ctypes.c_int64(V), ctypes.c_int(V), ctypes.c_int(batch), ptr(g), ptr(cq), ptr(cd), ptr(nd), ptr(dt), ptr(ct),
+                             ctypes.c_int64(ct.shape[1] if ct is not None else 0), ptr(rep), ptr(fr), ptr(pr), ptr(bt), ptr(bv), ptr(nb),
+                             ctypes.c_int(bt.shape[1] if bt is not None else 0), ptr(mk),
+                             ctypes.c_int64(mk.shape[1] if mk is not None else 0), _p(out), _p(mag))
+    return out, mag
+
+
+def token_counts_update(counts, vocab, tokens, first, n, reset=None, prompt=False):
+    """New counts (int16 [B, stride]) after the tokens tokens[first[b] : first[b] + n[b]] of every sequence."""
+    lib = _load()
+    c = np.array(counts, np.int16, order="C", copy=True)
+    t, f, m = _c(tokens, np.int32).reshape(-1), _c(first, np.int64), _c(n, np.int32)
+    r = None if reset is None else _c(reset, np.int32)
+    lib.oracle_token_counts_update(_p(c), ctypes.c_int64(c.shape[1]), ctypes.c_int(vocab), ctypes.c_int(c.shape[0]), _p(t), _p(f), _p(m),
+                                   None if r is None else _p(r), ctypes.c_int(int(prompt)))
+    return c

@@ -622,3 +622,80 @@ void oracle_norm_rotate_rows(const uint16_t *x, int64_t stride, int n, int heads
         }
     }
 }
+
+/* =========================================================================
+ * 8. Penalties, biases and grammar masks on logit rows, and the token counts
+ *    behind the penalties: the definition, element by element in float64.
+ *    out: the unrounded result; mag: sum of the magnitudes of its terms (the
+ *    scale of float32 rounding errors).  Rows that belong to no sequence are left.
+ * ========================================================================= */
+static void adjust_row(const float *x, int V, const int16_t *counts, const int32_t *drafts, int n_before, double rep, double freq,
+                       double pres, const int32_t *bias_tokens, const float *bias_values, int n_bias, const uint32_t *mask,
+                       double *out, double *mag)
+{
+    int32_t *c = (int32_t *)calloc((size_t)V, sizeof(int32_t));
+    double *bias = (double *)calloc((size_t)V, sizeof(double));
+    for (int j = 0; j < n_before; ++j)
+        if (drafts[j] >= 0 && drafts[j] < V) c[drafts[j]] += 1;
+    for (int e = 0; e < n_bias; ++e)                     /* the later entry counts */
+        if (bias_tokens[e] >= 0 && bias_tokens[e] < V) bias[bias_tokens[e]] = bias_values[e];
+    for (int k = 0; k < V; ++k) {
+        double v = x[k];
+        uint16_t h = counts ? (uint16_t)counts[k] : 0;
+        int n = c[k] + (h & 0x7fff);
+        if (counts) {
+            if (n > 0 || (h & 0x8000)) v = v > 0 ? v / rep : v * rep;
+            mag[k] = fabs(v) + fabs(freq * n) + (n > 0 ? fabs(pres) : 0.0) + fabs(bias[k]);
+            v -= freq * n + (n > 0 ? pres : 0.0);
+        } else {
+            mag[k] = fabs(v) + fabs(bias[k]);
+        }
+        v += bias[k];
+        if (mask && !((mask[k / 32] >> (k % 32)) & 1u)) {
+            v = -INFINITY;
+            mag[k] = 0.0;
+        }
+        out[k] = v;
+    }
+    free(c);
+    free(bias);
+}
+
+void oracle_logits_adjust(const float *logits, int64_t stride, int V, int batch, const int32_t *gamma, const int32_t *cu_q,
+                          const int32_t *cu_d, const int32_t *n_drafted, const int32_t *draft_tokens, const int16_t *counts,
+                          int64_t count_stride, const float *rep, const float *freq, const float *pres, const int32_t *bias_tokens,
+                          const float *bias_values, const int32_t *n_bias, int bias_stride, const uint32_t *mask,
+                          int64_t mask_stride, double *out, double *mag)
+{
+    int penal = rep || freq || pres;
+#pragma omp parallel for schedule(dynamic)
+    for (int b = 0; b < batch; ++b) {
+        int rows = n_drafted ? 1 : gamma[b] + 1;
+        for (int i = 0; i < rows; ++i) {
+            int64_t r = n_drafted ? b : (int64_t)cu_q[b] + i;
+            adjust_row(logits + r * stride, V, penal ? counts + b * count_stride : NULL, draft_tokens + (cu_d ? cu_d[b] : 0),
+                       penal ? (n_drafted ? n_drafted[b] : i) : 0, rep ? rep[b] : 1.0, freq ? freq[b] : 0.0, pres ? pres[b] : 0.0,
+                       bias_tokens + (int64_t)b * bias_stride, bias_values + (int64_t)b * bias_stride, n_bias ? n_bias[b] : 0,
+                       mask ? mask + r * mask_stride : NULL, out + r * V, mag + r * V);
+        }
+    }
+}
+
+/* tokens of b: tokens[first[b]] .. tokens[first[b] + n[b] - 1]; entries outside [0, V) are skipped */
+void oracle_token_counts_update(int16_t *counts, int64_t stride, int V, int batch, const int32_t *tokens, const int64_t *first,
+                                const int32_t *n, const int32_t *reset, int prompt)
+{
+    for (int b = 0; b < batch; ++b) {
+        int16_t *row = counts + b * stride;
+        if (reset && reset[b])
+            for (int k = 0; k < V; ++k) row[k] = 0;
+        for (int j = 0; j < n[b]; ++j) {
+            int32_t t = tokens[first[b] + j];
+            if (t < 0 || t >= V) continue;
+            uint16_t h = (uint16_t)row[t];
+            if (prompt) h |= 0x8000;
+            else if ((h & 0x7fff) < 0x7fff) h += 1;
+            row[t] = (int16_t)h;
+        }
+    }
+}

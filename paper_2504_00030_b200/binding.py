@@ -27,7 +27,7 @@ EXPORTS = (
     "spec_accept_sample", "spec_accept_sample_static", "gamma_tune_update", "gamma_tune_init",
     "spec_verify_step_host", "spec_draft_stop_workspace_bytes", "spec_draft_stop", "spec_kv_append",
     "sv_selftest_wait_expiry", "spec_verify_attn_layers", "spec_draft_step_workspace_bytes", "spec_draft_step",
-    "spec_kv_pages_update", "spec_rope_append",
+    "spec_kv_pages_update", "spec_rope_append", "spec_logits_adjust", "spec_token_counts_update",
 )
 
 
@@ -76,6 +76,25 @@ class RopeAppendParams(C.Structure):
                 ("interleaved", C.c_int32), ("rope_scale", C.c_float), ("q_weight", C.c_void_p),
                 ("k_weight", C.c_void_p), ("weights_f32", C.c_int32), ("eps", C.c_float),
                 ("device_status", C.c_void_p)]
+
+
+class LogitsAdjustParams(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("out", C.c_void_p), ("row_stride", C.c_int64), ("out_stride", C.c_int64),
+                ("n_rows", C.c_int64), ("vocab", C.c_int32), ("logits_bf16", C.c_int32), ("batch", C.c_int32),
+                ("gamma_max", C.c_int32), ("gamma", C.c_void_p), ("cu_q", C.c_void_p), ("cu_d", C.c_void_p),
+                ("n_drafted", C.c_void_p), ("active", C.c_void_p), ("draft_tokens", C.c_void_p),
+                ("n_d_rows", C.c_int64), ("token_counts", C.c_void_p), ("count_stride", C.c_int64),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p),
+                ("bias_tokens", C.c_void_p), ("bias_values", C.c_void_p), ("n_bias", C.c_void_p),
+                ("bias_stride", C.c_int32), ("mask", C.c_void_p), ("mask_stride", C.c_int64),
+                ("device_status", C.c_void_p)]
+
+
+class TokenCountsParams(C.Structure):
+    _fields_ = [("token_counts", C.c_void_p), ("count_stride", C.c_int64), ("vocab", C.c_int32),
+                ("batch", C.c_int32), ("tokens", C.c_void_p), ("token_stride", C.c_int64),
+                ("cu_tokens", C.c_void_p), ("n_tokens", C.c_int64), ("max_tokens", C.c_int32),
+                ("reset", C.c_void_p), ("prompt", C.c_int32), ("device_status", C.c_void_p)]
 
 
 class AcceptParams(C.Structure):
@@ -176,6 +195,10 @@ def load():
         lib.spec_kv_pages_update.argtypes = [C.POINTER(KvPagesParams), C.c_void_p]
         lib.spec_rope_append.restype = C.c_int32
         lib.spec_rope_append.argtypes = [C.POINTER(RopeAppendParams), C.c_void_p]
+        lib.spec_logits_adjust.restype = C.c_int32
+        lib.spec_logits_adjust.argtypes = [C.POINTER(LogitsAdjustParams), C.c_void_p]
+        lib.spec_token_counts_update.restype = C.c_int32
+        lib.spec_token_counts_update.argtypes = [C.POINTER(TokenCountsParams), C.c_void_p]
         lib.spec_draft_step.restype = C.c_int32
         lib.spec_draft_step.argtypes = [C.POINTER(DraftStepParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_verify_step_host.restype = C.c_int32
@@ -455,6 +478,111 @@ def spec_rope_append(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq
     p = rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight, k_weight, eps,
                            interleaved, freq_axis, rope_scale, device_status, index)
     _check("spec_rope_append", load().spec_rope_append(C.byref(p), raw))
+
+
+# --------------------------------------------------------------------------- penalties, biases and grammar masks
+def _rows_on(t, dtype, name, index):
+    """Device pointer and row stride of a 2-D tensor on the device `index` with contiguous rows."""
+    if t.get_device() != index or t.dtype != dtype or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D tensor of {dtype} with contiguous rows on the current device (cuda:{index})")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _entries(t, n, name):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+
+
+def logits_adjust_params(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=None, token_counts=None, repetition=None,
+                         frequency=None, presence=None, bias_tokens=None, bias_values=None, n_bias=None, mask=None,
+                         n_drafted=None, active=None, device_status=None, index=None) -> LogitsAdjustParams:
+    index = torch.cuda.current_device() if index is None else index
+    i32, f32 = torch.int32, torch.float32
+    ldt = torch.bfloat16 if logits.dtype == torch.bfloat16 else f32               # float32 or bf16 logits
+    lp, ls = _rows_on(logits, ldt, "logits", index)
+    op, os_ = (lp, ls) if out is logits else _rows_on(out, ldt, "out", index)
+    n_rows, vocab = logits.shape
+    if out.shape != logits.shape:
+        raise ValueError("out must have the shape of logits")
+    batch = (n_drafted if n_drafted is not None else gamma).numel()
+    for x, name in ((gamma, "gamma"), (active, "active"), (repetition, "repetition"), (frequency, "frequency"),
+                    (presence, "presence"), (n_bias, "n_bias")):
+        if x is not None and x.numel() != batch:
+            raise ValueError(f"{name} must have one entry per sequence")
+    for x, name in ((cu_q, "cu_q"), (cu_d, "cu_d")):
+        _entries(x, batch + 1, name)
+    if n_drafted is not None and n_rows != batch:
+        raise ValueError("draft rows: one row of logits per sequence")
+    cp, cs = None, 0
+    if token_counts is not None:
+        cp, cs = _rows_on(token_counts, torch.int16, "token_counts", index)
+        if token_counts.shape[0] != batch or token_counts.shape[1] < vocab:
+            raise ValueError("token_counts must have a row of at least vocab entries per sequence")
+    width = 0
+    if bias_tokens is not None:
+        width = bias_tokens.shape[-1]
+        if bias_tokens.shape != (batch, width) or bias_values is None or bias_values.shape != bias_tokens.shape:
+            raise ValueError("bias_tokens and bias_values must be [batch, entries]")
+    mp, ms = None, 0
+    if mask is not None:
+        mp, ms = _rows_on(mask, i32, "mask", index)
+        if mask.shape[0] != n_rows or 32 * mask.shape[1] < vocab:
+            raise ValueError("mask must have a row of at least vocab bits per row of logits")
+    return LogitsAdjustParams(lp, op, ls, os_, n_rows, vocab, 0 if ldt == f32 else 1, batch, gamma_max,
+                              _on(gamma, i32, "gamma", index), _on(cu_q, i32, "cu_q", index), _on(cu_d, i32, "cu_d", index),
+                              _on(n_drafted, i32, "n_drafted", index), _on(active, i32, "active", index),
+                              _on(draft_tokens, i32, "draft_tokens", index),
+                              draft_tokens.numel() if draft_tokens is not None else 0, cp, cs,
+                              _on(repetition, f32, "repetition", index), _on(frequency, f32, "frequency", index),
+                              _on(presence, f32, "presence", index), _on(bias_tokens, i32, "bias_tokens", index),
+                              _on(bias_values, f32, "bias_values", index), _on(n_bias, i32, "n_bias", index), width, mp, ms,
+                              _on(device_status, i32, "device_status", index))
+
+
+def spec_logits_adjust(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=None, token_counts=None, repetition=None,
+                       frequency=None, presence=None, bias_tokens=None, bias_values=None, n_bias=None, mask=None,
+                       n_drafted=None, active=None, device_status=None, stream=None):
+    """Penalties, biases and grammar masks on the target rows of every block, or, with n_drafted, on one draft row per
+    sequence (asynchronous).  out may be logits itself.  mask: int32 [n_rows, words], a set bit allows its token."""
+    index, raw = _launch_at(stream, logits, "logits")
+    p = logits_adjust_params(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens, token_counts, repetition, frequency,
+                             presence, bias_tokens, bias_values, n_bias, mask, n_drafted, active, device_status, index)
+    _check("spec_logits_adjust", load().spec_logits_adjust(C.byref(p), raw))
+
+
+def token_counts_params(token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
+                        device_status=None, index=None) -> TokenCountsParams:
+    index = torch.cuda.current_device() if index is None else index
+    i32 = torch.int32
+    cp, cs = _rows_on(token_counts, torch.int16, "token_counts", index)
+    batch = token_counts.shape[0]
+    if token_counts.shape[1] < vocab:
+        raise ValueError("token_counts must have at least vocab entries per row")
+    tp, ts, n_tokens = None, 0, 0
+    if tokens is not None:
+        if cu_tokens is None:
+            tp, ts = _rows_on(tokens, i32, "tokens", index)
+            if tokens.shape[0] != batch:
+                raise ValueError("tokens must have one row per sequence")
+            max_tokens = tokens.shape[1] if max_tokens is None else max_tokens
+            if max_tokens > tokens.shape[1]:
+                raise ValueError("max_tokens is more than tokens has columns")
+        else:
+            tp, n_tokens = _on(tokens, i32, "tokens", index), tokens.numel()
+            max_tokens = n_tokens if max_tokens is None else max_tokens
+    _entries(cu_tokens, batch + 1, "cu_tokens")
+    _entries(reset, batch, "reset")
+    return TokenCountsParams(cp, cs, vocab, batch, tp, ts, _on(cu_tokens, i32, "cu_tokens", index), n_tokens, max_tokens or 0,
+                             _on(reset, i32, "reset", index), 1 if prompt else 0, _on(device_status, i32, "device_status", index))
+
+
+def spec_token_counts_update(token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
+                             device_status=None, stream=None):
+    """Count generated tokens (or mark prompt tokens) in the int16 state behind the penalties, after clearing the rows
+    of newly admitted sequences (asynchronous).  tokens: [batch, columns] padded with -1, or packed with cu_tokens."""
+    index, raw = _launch_at(stream, token_counts, "token_counts")
+    p = token_counts_params(token_counts, vocab, tokens, cu_tokens, max_tokens, reset, prompt, device_status, index)
+    _check("spec_token_counts_update", load().spec_token_counts_update(C.byref(p), raw))
 
 
 # --------------------------------------------------------------------------- accept / resample
