@@ -11,14 +11,17 @@ namespace sv {
 
 constexpr int LA_THREADS = 256;
 constexpr int LA_UNITS = 2;                // 16-byte units of a row that a thread has
-constexpr int LA_AHEAD = 2;                // rows under way
+constexpr int LA_BLOCKS = 5;               // blocks of an SM, with penalties or biases
+constexpr int LA_BLOCKS_MASK = 8;          // and with masks alone
 constexpr int LA_MAX_GAMMA = 64;
+constexpr int LA_STAGES = 4;
+constexpr int LA_BIASES = 1024;            // entries of the bias list at a time
 
 struct LogitsAdjustLaunch {
     sv_logits_adjust_params p;
     int slices;                            // blocks along the vocabulary
     int rows_per_block, chunks;            // rows of a block, blocks along a sequence's rows
-    int in_place, vec;
+    int in_place, vec, ring;
     int penalties;
 };
 
@@ -30,65 +33,42 @@ __device__ __forceinline__ uint4 ld_once(const void *p)
     return v;
 }
 
-template <bool BF16>
-struct Unit {
+// 16 bytes from global to shared memory, asynchronously; a group is the copies between two commits of a thread
+__device__ __forceinline__ void cp_chunk(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// VEC: units are one 16-byte access
+template <bool BF16, bool VEC>
+struct Layout {
     static constexpr int N = BF16 ? 8 : 4;                      // elements of a unit
     static constexpr int SLICE = LA_THREADS * LA_UNITS * N;     // elements of a block
+    // element e of unit u of a thread: units are contiguous where they are one access, else neighbouring threads have neighbouring
+    // elements
+    static __device__ __forceinline__ int at(int u, int e, int tid)
+    {
+        return VEC ? (u * LA_THREADS + tid) * N + e : (u * N + e) * LA_THREADS + tid;
+    }
+    static __device__ __forceinline__ int owner(int at) { return (VEC ? at / N : at) % LA_THREADS; }
 };
 
-// unit at element k of a row; past the vocabulary -inf.  `vec`: whole units are one access
-template <bool BF16>
-__device__ __forceinline__ void unit_load(const void *row, int k, int V, bool vec, uint4 &raw)
-{
-    if (vec && k + Unit<BF16>::N <= V) {
-        raw = BF16 ? ld_once(static_cast<const unsigned short *>(row) + k) : ld_once(static_cast<const float *>(row) + k);
-        return;
-    }
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (BF16) {
-        const unsigned short *s = static_cast<const unsigned short *>(row);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < V) w[e / 2] |= (uint32_t)s[k + e] << (16 * (e & 1));
-    } else {
-        const uint32_t *s = static_cast<const uint32_t *>(row);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k + e < V) w[e] = s[k + e];
-    }
-    raw = make_uint4(w[0], w[1], w[2], w[3]);
-}
-template <bool BF16>
-__device__ __forceinline__ void unit_store(void *row, int k, int V, bool vec, const uint4 &raw)
-{
-    if (vec && k + Unit<BF16>::N <= V) {
-        if (BF16) *reinterpret_cast<uint4 *>(static_cast<unsigned short *>(row) + k) = raw;
-        else *reinterpret_cast<uint4 *>(static_cast<float *>(row) + k) = raw;
-        return;
-    }
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    if (BF16) {
-        unsigned short *s = static_cast<unsigned short *>(row);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (k + e < V) s[k + e] = (unsigned short)(w[e / 2] >> (16 * (e & 1)));
-    } else {
-        uint32_t *s = static_cast<uint32_t *>(row);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (k + e < V) s[k + e] = w[e];
-    }
-}
 
 // ADD: penalties or biases; MASK: grammar masks
-template <bool BF16, bool ADD, bool MASK>
-__global__ void __launch_bounds__(LA_THREADS)
+template <bool BF16, bool ADD, bool MASK, bool VEC>
+__global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 {
     pdl_enter();
-    constexpr int N = Unit<BF16>::N, SLICE = Unit<BF16>::SLICE;
-    __shared__ int bias_at[ADD ? SLICE : 1];           // entry of the bias list that names the element, plus one
-    __shared__ int tokens[LA_MAX_GAMMA];
+    using L = Layout<BF16, VEC>;
+    constexpr int N = L::N, SLICE = L::SLICE;
+    __shared__ int draft_at[LA_MAX_GAMMA];             // element of the slice that draft j names, or -1
+    __shared__ float draft_add[LA_MAX_GAMMA];          // what is added to it once the draft is in the history
+    __shared__ int bias_head[ADD ? LA_THREADS : 1];  // entries of the bias list that name an element of thread t: a linked list, -1 its end
+    __shared__ short bias_next[ADD ? LA_BIASES : 1];
     const sv_logits_adjust_params &p = a.p;
     const int tid = threadIdx.x, V = p.vocab;
     const int slice = blockIdx.x % a.slices, seq_chunk = blockIdx.x / a.slices;
@@ -96,15 +76,13 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     if (p.active != nullptr && p.active[b] == 0) return;
     uint32_t bad = 0;
     const bool draft = p.n_drafted != nullptr;
-    int g = draft ? p.n_drafted[b] : p.gamma[b];
+    int g = draft ? ADD && a.penalties ? p.n_drafted[b] : 0 : p.gamma[b];
     if (g < 0 || g > p.gamma_max) {
         bad |= SV_DEV_BAD_GAMMA;
         g = min(max(g, 0), p.gamma_max);
     }
-    // rows of this block, and drafts in front of its first row
     const int rows = draft ? 1 : g + 1, i_begin = chunk * a.rows_per_block, i_end = min(rows, i_begin + a.rows_per_block);
-    const int before = draft ? g : i_begin;
-    long long row0 = draft ? b : p.cu_q[b];
+    const long long row0 = draft ? b : p.cu_q[b];
     if (i_begin >= i_end) {
         if (bad != 0 && tid == 0) set_status(p.device_status, bad);
         return;
@@ -114,182 +92,310 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
         return;
     }
     const int base = slice * SLICE;
-    int k0[LA_UNITS];
-#pragma unroll
-    for (int u = 0; u < LA_UNITS; ++u) k0[u] = base + (u * LA_THREADS + tid) * N;
 
+    // ---- loads that nothing waits for come first: the first row, unless the counts and the mask may spare it, and the counts
+    const unsigned char *mask = MASK ? reinterpret_cast<const unsigned char *>(p.mask + (row0 + i_begin) * p.mask_stride) : nullptr;
+    const char *src = static_cast<const char *>(p.logits) + (row0 + i_begin) * p.row_stride * (BF16 ? 2 : 4);
+    char *dst = static_cast<char *>(p.out) + (row0 + i_begin) * p.out_stride * (BF16 ? 2 : 4);
+    uint32_t w[LA_UNITS][4];
+    auto load_row = [&](uint32_t allowed, uint32_t still) {
+#pragma unroll
+        for (int u = 0; u < LA_UNITS; ++u) {
+            w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
+            if (VEC) {
+                const int k = base + L::at(u, 0, tid);
+                const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
+                if (k < V && own != 0 && !((still >> u) & 1u && own == (1u << N) - 1)) {
+                    const uint4 v = ld_once(src + (long long)k * (BF16 ? 2 : 4));
+                    w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int k = base + L::at(u, e, tid);
+                    if (k >= V || !((allowed >> (u * N + e)) & 1u)) continue;
+                    if (BF16) w[u][e / 2] |= (uint32_t)reinterpret_cast<const unsigned short *>(src)[k] << (16 * (e & 1));
+                    else w[u][e] = reinterpret_cast<const uint32_t *>(src)[k];
+                }
+            }
+        }
+    };
+    // Rows come through a ring in shared memory, LA_STAGES - 1 ahead, unless the counts and the mask may spare their loads.
+    extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][LA_UNITS][LA_THREADS]: each thread reads back its own
+    const bool ahead = VEC && a.ring;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(la_ring + tid);
+    int p_row = i_begin, p_stage = 0;
+    auto issue = [&]() {
+        if (p_row < i_end) {
+            const char *row = src + (long long)(p_row - i_begin) * p.row_stride * (BF16 ? 2 : 4);
+#pragma unroll
+            for (int u = 0; u < LA_UNITS; ++u) {
+                const int k = base + L::at(u, 0, tid);
+                if (k < V) cp_chunk(ring + (p_stage * LA_UNITS + u) * LA_THREADS * 16, row + (long long)k * (BF16 ? 2 : 4));
+            }
+            ++p_row;
+        }
+        p_stage = p_stage + 1 == LA_STAGES ? 0 : p_stage + 1;
+        cp_commit();                                   // an empty group where nothing is left
+    };
+    if (ahead) {
+#pragma unroll
+        for (int s = 0; s < LA_STAGES - 1; ++s) issue();
+    }
+    const int16_t *counts = ADD && a.penalties ? p.token_counts + b * p.count_stride + base : nullptr;
+    uint32_t held[LA_UNITS][N / 2];                    // counts of this thread's units
+    if (ADD) {
+#pragma unroll
+        for (int u = 0; u < LA_UNITS; ++u) {
+            const int k = L::at(u, 0, tid);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) held[u][i] = 0;
+            if (counts == nullptr) continue;
+            if (VEC) {
+                if (base + k >= V) continue;
+                if (BF16) {
+                    const uint4 c = *reinterpret_cast<const uint4 *>(counts + k);
+                    held[u][0] = c.x; held[u][1] = c.y; held[u][N / 2 - 2] = c.z; held[u][N / 2 - 1] = c.w;
+                } else {
+                    const uint2 c = *reinterpret_cast<const uint2 *>(counts + k);
+                    held[u][0] = c.x; held[u][1] = c.y;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (base + L::at(u, e, tid) < V) held[u][e / 2] |= (uint32_t)(uint16_t)counts[L::at(u, e, tid)] << (16 * (e & 1));
+            }
+        }
+    }
     // ---- what counts and biases do to this thread's elements
     float add[LA_UNITS][N];
     uint32_t seen = 0;                                 // bit u * N + e: the element is in the history or the prompt
-    float rep = 1.f, rep_inv = 1.f, freq = 0.f, pres = 0.f;
-    const int16_t *counts = nullptr;
-    const float *bias = nullptr;
+    float rep = 1.f, rep_inv = 1.f;
+    const int before = draft ? g : i_begin;            // drafts in front of the block's first row
+    const int n_drafts = ADD && a.penalties ? draft ? g : i_end - 1 : 0;       // drafts that some row of this block has in its history
     if (ADD) {
+        float freq = 0.f, pres = 0.f;
+        auto penalty = [&](int c) { return -(freq * (float)c + (c > 0 ? pres : 0.f)); };
+        int my_at = -1;                                // of thread j: the element that draft j names,
+        float my_add = 0.f, my_bias = 0.f;             // its penalty with drafts 0 .. j in the history, its bias
         if (a.penalties) {
-            counts = p.token_counts + b * p.count_stride;
             if (p.repetition != nullptr) rep = p.repetition[b];
             rep_inv = 1.f / rep;
             if (p.frequency != nullptr) freq = p.frequency[b];
             if (p.presence != nullptr) pres = p.presence[b];
-            const int n = draft ? g : i_end - 1;       // drafts that some row of this block has in its history
-            const long long first = n > 0 ? p.cu_d[b] : 0;
-            for (int j = tid; j < n; j += LA_THREADS) {
-                int t = -1;
-                if (first < 0 || first + j >= p.n_d_rows) {
+            if (tid < n_drafts) {                      // at most LA_MAX_GAMMA
+                const long long first = p.cu_d[b];
+                if (first < 0 || first + tid >= p.n_d_rows) {
                     bad |= SV_DEV_BAD_LEN;
                 } else {
-                    t = p.draft_tokens[first + j];
-                    if (t < 0 || t >= V) {
-                        bad |= SV_DEV_BAD_TOKEN;
-                        t = -1;
-                    }
+                    const int t = p.draft_tokens[first + tid];
+                    if (t < 0 || t >= V) bad |= SV_DEV_BAD_TOKEN;
+                    else if (t >= base && t < base + SLICE) my_at = t - base;
                 }
-                tokens[j] = t;
+                draft_at[tid] = my_at;
+            }
+            if (n_drafts > 0) __syncthreads();
+            if (my_at >= 0) {
+                int c = (counts[my_at] & 0x7fff) + 1;
+                for (int i = 0; i < tid; ++i) c += draft_at[i] == my_at ? 1 : 0;
+                my_add = penalty(c);
             }
         }
+#pragma unroll
+        for (int u = 0; u < LA_UNITS; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint32_t h = (held[u][e / 2] >> (16 * (e & 1))) & 0xffffu;
+                seen |= (h != 0 ? 1u : 0u) << (u * N + e);
+                add[u][e] = penalty(h & 0x7fff);
+            }
         if (p.n_bias != nullptr) {
-            bias = p.bias_values + (long long)b * p.bias_stride;
-            for (int i = tid; i < SLICE; i += LA_THREADS) bias_at[i] = 0;
-            __syncthreads();
             int n = p.n_bias[b];
             if (n < 0 || n > p.bias_stride) {
                 bad |= SV_DEV_BAD_LEN;
                 n = min(max(n, 0), p.bias_stride);
             }
-            for (int i = tid; i < n; i += LA_THREADS) {
-                const int t = p.bias_tokens[(long long)b * p.bias_stride + i];
-                if (t < 0 || t >= V) bad |= SV_DEV_BAD_TOKEN;
-                else if (t >= base && t < base + SLICE) atomicMax(&bias_at[t - base], i + 1);      // the later entry counts
+            const int32_t *bias_tokens = p.bias_tokens + (long long)b * p.bias_stride;
+            const float *bias_values = p.bias_values + (long long)b * p.bias_stride;
+            for (int i0 = 0; i0 < n; i0 += LA_BIASES) {
+                if (i0 > 0) __syncthreads();
+                bias_head[tid] = -1;
+                __syncthreads();
+                for (int i = tid; i < min(n - i0, LA_BIASES); i += LA_THREADS) {
+                    const int t = bias_tokens[i0 + i];
+                    if (t < 0 || t >= V) bad |= SV_DEV_BAD_TOKEN;
+                    else if (t >= base && t < base + SLICE) bias_next[i] = (short)atomicExch(&bias_head[L::owner(t - base)], i);
+                }
+                __syncthreads();
+                // value that element `at` gets from this part of the list, if any: the later entry counts
+                auto look_up = [&](int at, float &value) {
+                    int found = -1;
+                    for (int i = bias_head[L::owner(at)]; i >= 0; i = bias_next[i])
+                        if (bias_tokens[i0 + i] == base + at) found = max(found, i);
+                    if (found >= 0) value = bias_values[i0 + found];
+                    return found >= 0;
+                };
+                for (int i = bias_head[tid]; i >= 0; i = bias_next[i]) {
+                    const int at = bias_tokens[i0 + i] - base;
+                    float v = 0.f;
+                    look_up(at, v);
+                    v += penalty(counts != nullptr ? counts[at] & 0x7fff : 0);
+#pragma unroll
+                    for (int u = 0; u < LA_UNITS; ++u)
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (at == L::at(u, e, tid)) add[u][e] = v;
+                }
+                if (my_at >= 0) look_up(my_at, my_bias);
             }
         }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < LA_UNITS; ++u) {
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (counts != nullptr && k0[u] < V) {      // rows of counts are padded to whole units
-                if (BF16) {
-                    const uint4 c = *reinterpret_cast<const uint4 *>(counts + k0[u]);
-                    w[0] = c.x; w[1] = c.y; w[2] = c.z; w[3] = c.w;
-                } else {
-                    const uint2 c = *reinterpret_cast<const uint2 *>(counts + k0[u]);
-                    w[0] = c.x; w[1] = c.y;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const uint32_t h = (w[e / 2] >> (16 * (e & 1))) & 0xffffu, c = h & 0x7fffu;
-                seen |= (h != 0 ? 1u : 0u) << (u * N + e);
-                add[u][e] = -(freq * (float)c + (c > 0 ? pres : 0.f));
-                if (bias != nullptr) {
-                    const int i = bias_at[k0[u] - base + e];
-                    if (i > 0) add[u][e] += bias[i - 1];
-                }
-            }
+        if (n_drafts > 0) {
+            if (my_at >= 0) draft_add[tid] = my_add + my_bias;
+            __syncthreads();
         }
     }
     // draft j of the sequence joins the history of the rows from here on
     auto take = [&](int j) {
-        const int t = tokens[j];
-        if (t < base || t >= base + SLICE) return;
+        const int at = draft_at[j];
+        const float v = draft_add[j];
+        if (at < 0 || L::owner(at) != tid) return;
 #pragma unroll
-        for (int u = 0; u < LA_UNITS; ++u) {
-            if (t < k0[u] || t >= k0[u] + N) continue;
-            int c = (counts[t] & 0x7fff) + 1;          // times in the counts and among drafts 0 .. j
-            for (int i = 0; i < j; ++i) c += tokens[i] == t ? 1 : 0;
-            float v = -(freq * (float)c + pres);
-            const int i = bias != nullptr ? bias_at[t - base] : 0;
-            if (i > 0) v += bias[i - 1];
+        for (int u = 0; u < LA_UNITS; ++u)
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (t == k0[u] + e) add[u][e] = v;
-            seen |= 1u << (u * N + t - k0[u]);
-        }
+                if (at == L::at(u, e, tid)) {
+                    add[u][e] = v;
+                    seen |= 1u << (u * N + e);
+                }
     };
-    if (ADD && a.penalties)
-        for (int j = 0; j < before; ++j) take(j);
-
-    // ---- rows
-    for (int i0 = i_begin; i0 < i_end; i0 += LA_AHEAD) {
-        uint4 raw[LA_AHEAD][LA_UNITS];
-        uint32_t allowed[LA_AHEAD][LA_UNITS];
+    for (int j = 0; j < min(before, n_drafts); ++j) take(j);
+    // In place, a unit that nothing is added to in any of the rows is left alone where the mask allows all of it.
+    uint32_t still = 0;                                // bit u
+    if (a.in_place) {
 #pragma unroll
-        for (int r = 0; r < LA_AHEAD; ++r) {
-            const long long row = row0 + i0 + r;
+        for (int u = 0; u < LA_UNITS; ++u) {
+            bool moves = false;
+            if (ADD) {
+                moves = ((seen >> (u * N)) & ((1u << N) - 1)) != 0;
 #pragma unroll
-            for (int u = 0; u < LA_UNITS; ++u) {
-                allowed[r][u] = (1u << N) - 1;
-                if (MASK && i0 + r < i_end && k0[u] < V)
-                    allowed[r][u] &= __ldg(reinterpret_cast<const unsigned char *>(p.mask + row * p.mask_stride) + k0[u] / 8) >> (k0[u] & 7);
+                for (int e = 0; e < N; ++e) moves = moves || add[u][e] != 0.f;
             }
+            still |= (moves ? 0u : 1u) << u;
         }
-#pragma unroll
-        for (int r = 0; r < LA_AHEAD; ++r) {
-            const void *src = logit_row<BF16>(p.logits, row0 + i0 + r, p.row_stride);
-#pragma unroll
-            for (int u = 0; u < LA_UNITS; ++u) {
-                raw[r][u] = make_uint4(0, 0, 0, 0);
-                if (i0 + r < i_end && k0[u] < V && (!MASK || allowed[r][u] != 0)) unit_load<BF16>(src, k0[u], V, a.vec != 0, raw[r][u]);
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < LA_AHEAD; ++r) {
-            if (i0 + r >= i_end) break;
-            if (ADD && a.penalties && i0 + r > i_begin) take(i0 + r - 1);
-            void *dst = const_cast<void *>(logit_row<BF16>(p.out, row0 + i0 + r, p.out_stride));
-#pragma unroll
-            for (int u = 0; u < LA_UNITS; ++u) {
-                if (k0[u] >= V) continue;
-                uint32_t w[4] = {raw[r][u].x, raw[r][u].y, raw[r][u].z, raw[r][u].w};
-                float x[N];
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    x[e] = BF16 ? __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16) : __uint_as_float(w[e]);
-                if (ADD) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float f = (seen >> (u * N + e)) & 1u ? (x[e] > 0.f ? rep_inv : rep) : 1.f;
-                        x[e] = x[e] * f + add[u][e];
-                    }
-                }
-                if (MASK) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (!((allowed[r][u] >> e) & 1u)) x[e] = -CUDART_INF_F;
-                }
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if (BF16) {
-                        if (e & 1) {
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(x[e - 1], x[e]);        // the one rounding
-                            w[e / 2] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                    } else {
-                        w[e] = __float_as_uint(x[e]);
-                    }
-                }
-                unit_store<BF16>(dst, k0[u], V, a.vec != 0, make_uint4(w[0], w[1], w[2], w[3]));
-            }
+        for (int j = before; j < n_drafts; ++j) {
+            const int at = draft_at[j];
+            if (at < 0 || L::owner(at) != tid) continue;
+            still &= ~(1u << (at / (LA_THREADS * N)));
         }
     }
+
+    // ---- rows
+    auto mask_row = [&]() {                            // what `mask` points to allows of this thread's elements, bit u * N + e
+        uint32_t allowed = 0;
+#pragma unroll
+        for (int u = 0; u < LA_UNITS; ++u) {
+            if (VEC) {
+                const int k = base + L::at(u, 0, tid);
+                if (k < V) allowed |= ((mask[k / 8] >> (k & 7)) & ((1u << N) - 1)) << (u * N);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int k = base + L::at(u, e, tid);
+                    if (k < V) allowed |= ((mask[k / 8] >> (k & 7)) & 1u) << (u * N + e);
+                }
+            }
+        }
+        return allowed;
+    };
+    int stage = 0;
+    uint32_t next = MASK ? mask_row() : 0xffffffffu;
+    for (int i = i_begin; i < i_end; ++i) {
+        const uint32_t allowed = next;
+        if (MASK && i + 1 < i_end) {                   // a row ahead: it decides what is loaded
+            mask += p.mask_stride * 4;
+            next = mask_row();
+        }
+        if (ahead) {
+            cp_wait<LA_STAGES - 2>();
+#pragma unroll
+            for (int u = 0; u < LA_UNITS; ++u) {
+                const uint4 v = la_ring[(stage * LA_UNITS + u) * LA_THREADS + tid];
+                w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
+            }
+            stage = stage + 1 == LA_STAGES ? 0 : stage + 1;
+            issue();
+        } else {
+            load_row(allowed, still);
+            src += p.row_stride * (BF16 ? 2 : 4);
+        }
+        if (i > i_begin && i <= n_drafts) take(i - 1);
+#pragma unroll
+        for (int u = 0; u < LA_UNITS; ++u) {
+            float x[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                x[e] = BF16 ? __uint_as_float(e & 1 ? w[u][e / 2] & 0xffff0000u : w[u][e / 2] << 16) : __uint_as_float(w[u][e & 3]);
+                if (ADD) x[e] = x[e] * ((seen >> (u * N + e)) & 1u ? (x[e] > 0.f ? rep_inv : rep) : 1.f) + add[u][e];
+                if (MASK && !((allowed >> (u * N + e)) & 1u)) x[e] = -CUDART_INF_F;
+                if (!BF16) w[u][e & 3] = __float_as_uint(x[e]);
+                else if (e & 1) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(x[e - 1], x[e]);                // the one rounding
+                    w[u][e / 2] = *reinterpret_cast<const uint32_t *>(&h);
+                }
+            }
+            if (VEC) {
+                const int k = base + L::at(u, 0, tid);
+                const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
+                if (k < V && !((still >> u) & 1u && own == (1u << N) - 1))
+                    *reinterpret_cast<uint4 *>(dst + (long long)k * (BF16 ? 2 : 4)) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const int k = base + L::at(u, e, tid);
+                    if (k >= V) continue;
+                    if (BF16) reinterpret_cast<unsigned short *>(dst)[k] = (unsigned short)(w[u][e / 2] >> (16 * (e & 1)));
+                    else reinterpret_cast<uint32_t *>(dst)[k] = w[u][e & 3];
+                }
+            }
+        }
+        dst += p.out_stride * (BF16 ? 2 : 4);
+    }
     if (bad != 0) set_status(p.device_status, bad);
+}
+
+template <bool BF16, bool ADD, bool MASK, bool VEC>
+static sv_status launch_one(const LogitsAdjustLaunch &a, dim3 grid, cudaStream_t stream)
+{
+    return launch_kernel(true, logits_adjust_kernel<BF16, ADD, MASK, VEC>, grid, LA_THREADS,
+                         a.ring ? (size_t)LA_STAGES * LA_UNITS * LA_THREADS * 16 : 0, stream, a);
+}
+template <bool BF16, bool VEC>
+static sv_status launch_kinds(const LogitsAdjustLaunch &a, bool add, bool mask, dim3 grid, cudaStream_t stream)
+{
+    if (add && mask) return launch_one<BF16, true, true, VEC>(a, grid, stream);
+    if (add) return launch_one<BF16, true, false, VEC>(a, grid, stream);
+    if (mask) return launch_one<BF16, false, true, VEC>(a, grid, stream);
+    return launch_one<BF16, false, false, VEC>(a, grid, stream);
 }
 
 template <bool BF16>
 static sv_status launch_adjust(LogitsAdjustLaunch &a, cudaStream_t stream)
 {
     const sv_logits_adjust_params &p = a.p;
-    a.slices = (p.vocab + Unit<BF16>::SLICE - 1) / Unit<BF16>::SLICE;
+    constexpr int slice = Layout<BF16, true>::SLICE;
+    a.slices = (p.vocab + slice - 1) / slice;
     const int rows = p.n_drafted != nullptr ? 1 : p.gamma_max + 1;
-    a.rows_per_block = rows;
+    // Few blocks: a sequence's rows are dealt out as well.
+    const long long whole = (long long)p.batch * a.slices, resident = (long long)sm_count() * LA_BLOCKS;
+    const long long split = resident / whole < 1 ? 1 : resident / whole < rows ? resident / whole : rows;
+    a.rows_per_block = (int)((rows + split - 1) / split);
     a.chunks = (rows + a.rows_per_block - 1) / a.rows_per_block;
+    a.ring = a.vec && !a.in_place && true;
     const long long blocks = (long long)p.batch * a.chunks * a.slices;
     if (blocks > 0x7fffffffLL) return SV_EUNSUPPORTED;
     const dim3 grid((unsigned)blocks);
     const bool add = a.penalties || p.n_bias != nullptr, mask = p.mask != nullptr;
-    if (add && mask) return launch_kernel(true, logits_adjust_kernel<BF16, true, true>, grid, LA_THREADS, 0, stream, a);
-    if (add) return launch_kernel(true, logits_adjust_kernel<BF16, true, false>, grid, LA_THREADS, 0, stream, a);
-    if (mask) return launch_kernel(true, logits_adjust_kernel<BF16, false, true>, grid, LA_THREADS, 0, stream, a);
-    return launch_kernel(true, logits_adjust_kernel<BF16, false, false>, grid, LA_THREADS, 0, stream, a);
+    return a.vec ? launch_kinds<BF16, true>(a, add, mask, grid, stream) : launch_kinds<BF16, false>(a, add, mask, grid, stream);
 }
 
 }  // namespace sv
@@ -323,6 +429,7 @@ extern "C" sv_status spec_logits_adjust(const sv_logits_adjust_params *p, void *
     a.p = *p;
     a.in_place = in_place;
     a.penalties = penalties;
-    a.vec = logits_vec_ok(p->logits, p->row_stride, p->logits_bf16 != 0) && logits_vec_ok(p->out, p->out_stride, p->logits_bf16 != 0);
+    // whole units, all of them: the vocabulary ends with a unit
+    a.vec = p->vocab % (p->logits_bf16 != 0 ? 8 : 4) == 0 && logits_vec_ok(p->logits, p->row_stride, p->logits_bf16 != 0) && logits_vec_ok(p->out, p->out_stride, p->logits_bf16 != 0);
     return p->logits_bf16 != 0 ? launch_adjust<true>(a, (cudaStream_t)stream) : launch_adjust<false>(a, (cudaStream_t)stream);
 }
