@@ -15,6 +15,7 @@ constexpr int LA_BLOCKS = 5;               // blocks of an SM, with penalties or
 constexpr int LA_BLOCKS_MASK = 8;          // and with masks alone
 constexpr int LA_MAX_GAMMA = 64;
 constexpr int LA_STAGES = 4;
+constexpr int LA_RING = LA_UNITS * LA_THREADS + LA_THREADS / 32;       // vectors of a row in the ring
 constexpr int LA_BIASES = 1024;            // entries of the bias list at a time
 
 struct LogitsAdjustLaunch {
@@ -38,39 +39,58 @@ __device__ __forceinline__ void cp_chunk(uint32_t dst, const void *src)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+// its first `bytes` bytes, zeros behind them; no more is read
+__device__ __forceinline__ void cp_part(uint32_t dst, const void *src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// VEC: units are one 16-byte access
-template <bool BF16, bool VEC>
+// Elements of a slice: a warp has LA_UNITS * 32 neighbouring units of 16 bytes, a thread unit u * 32 + lane of them.
+template <bool BF16>
 struct Layout {
     static constexpr int N = BF16 ? 8 : 4;                      // elements of a unit
     static constexpr int SLICE = LA_THREADS * LA_UNITS * N;     // elements of a block
-    // element e of unit u of a thread: units are contiguous where they are one access, else neighbouring threads have neighbouring
-    // elements
-    static __device__ __forceinline__ int at(int u, int e, int tid)
-    {
-        return VEC ? (u * LA_THREADS + tid) * N + e : (u * N + e) * LA_THREADS + tid;
-    }
-    static __device__ __forceinline__ int owner(int at) { return (VEC ? at / N : at) % LA_THREADS; }
+    static_assert(SLICE <= 1 << 16, "an element of a slice fits 16 bits");
+    static __device__ __forceinline__ int at(int u, int e, int tid) { return (((tid >> 5) * LA_UNITS + u) * 32 + (tid & 31)) * N + e; }
+    static __device__ __forceinline__ int owner(int at) { return at / (32 * LA_UNITS * N) * 32 + at / N % 32; }
+    static __device__ __forceinline__ int unit(int at) { return at / (32 * N) % LA_UNITS; }
 };
 
+// N elements from element `from` (0 <= from < N) of the 2 N elements lo, hi
+template <bool BF16>
+__device__ __forceinline__ void pick(const uint32_t (&lo)[4], const uint32_t (&hi)[4], int from, uint32_t (&out)[4])
+{
+    const int words = BF16 ? from >> 1 : from;
+    uint32_t w[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    if (words & 2)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+    if (words & 1)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = BF16 && (from & 1) ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+}
 
-// ADD: penalties or biases; MASK: grammar masks
+// ADD: penalties or biases; MASK: grammar masks.  VEC: every unit of every row starts on a 16-byte boundary and ends inside
+// the vocabulary.  Elsewhere (a vocabulary of odd size, say) a row's 16-byte boundaries lie d elements behind the units',
+// d differing from row to row: the accesses keep to the boundaries, and the neighbouring lane's part of a unit comes by shuffle.
 template <bool BF16, bool ADD, bool MASK, bool VEC>
 __global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 {
     pdl_enter();
-    using L = Layout<BF16, VEC>;
-    constexpr int N = L::N, SLICE = L::SLICE;
+    using L = Layout<BF16>;
+    constexpr int N = L::N, SLICE = L::SLICE, ES = 16 / N;
     __shared__ int draft_at[LA_MAX_GAMMA];             // element of the slice that draft j names, or -1
     __shared__ float draft_add[LA_MAX_GAMMA];          // what is added to it once the draft is in the history
-    __shared__ int bias_head[ADD ? LA_THREADS : 1];  // entries of the bias list that name an element of thread t: a linked list, -1 its end
-    __shared__ short bias_next[ADD ? LA_BIASES : 1];
+    __shared__ int bias_head[ADD ? LA_THREADS : 1];    // entries of the bias list that name an element of thread t: a linked list, -1 its end
+    __shared__ int bias_node[ADD ? LA_BIASES : 1];     // per entry: its element of the slice, and the next entry of the thread's list << 16
     const sv_logits_adjust_params &p = a.p;
-    const int tid = threadIdx.x, V = p.vocab;
+    const int tid = threadIdx.x, lane = tid & 31, V = p.vocab;
     const int slice = blockIdx.x % a.slices, seq_chunk = blockIdx.x / a.slices;
     const int b = seq_chunk / a.chunks, chunk = seq_chunk - b * a.chunks;
     if (p.active != nullptr && p.active[b] == 0) return;
@@ -83,6 +103,14 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     }
     const int rows = draft ? 1 : g + 1, i_begin = chunk * a.rows_per_block, i_end = min(rows, i_begin + a.rows_per_block);
     const long long row0 = draft ? b : p.cu_q[b];
+    // of thread j: draft j of the sequence, whether or not this step has so many
+    int my_token = 0;
+    bool my_token_there = false;
+    if (ADD && a.penalties && tid < p.gamma_max) {     // at most LA_MAX_GAMMA
+        const long long at = (long long)p.cu_d[b] + tid;
+        my_token_there = at >= tid && at < p.n_d_rows;
+        if (my_token_there) my_token = p.draft_tokens[at];
+    }
     if (i_begin >= i_end) {
         if (bad != 0 && tid == 0) set_status(p.device_status, bad);
         return;
@@ -95,45 +123,34 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 
     // ---- loads that nothing waits for come first: the first row, unless the counts and the mask may spare it, and the counts
     const unsigned char *mask = MASK ? reinterpret_cast<const unsigned char *>(p.mask + (row0 + i_begin) * p.mask_stride) : nullptr;
-    const char *src = static_cast<const char *>(p.logits) + (row0 + i_begin) * p.row_stride * (BF16 ? 2 : 4);
-    char *dst = static_cast<char *>(p.out) + (row0 + i_begin) * p.out_stride * (BF16 ? 2 : 4);
+    const char *src = static_cast<const char *>(p.logits) + (row0 + i_begin) * p.row_stride * ES;
+    char *dst = static_cast<char *>(p.out) + (row0 + i_begin) * p.out_stride * ES;
     uint32_t w[LA_UNITS][4];
-    auto load_row = [&](uint32_t allowed, uint32_t still) {
-#pragma unroll
-        for (int u = 0; u < LA_UNITS; ++u) {
-            w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
-            if (VEC) {
-                const int k = base + L::at(u, 0, tid);
-                const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
-                if (k < V && own != 0 && !((still >> u) & 1u && own == (1u << N) - 1)) {
-                    const uint4 v = ld_once(src + (long long)k * (BF16 ? 2 : 4));
-                    w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int k = base + L::at(u, e, tid);
-                    if (k >= V || !((allowed >> (u * N + e)) & 1u)) continue;
-                    if (BF16) w[u][e / 2] |= (uint32_t)reinterpret_cast<const unsigned short *>(src)[k] << (16 * (e & 1));
-                    else w[u][e] = reinterpret_cast<const uint32_t *>(src)[k];
-                }
-            }
-        }
-    };
     // Rows come through a ring in shared memory, LA_STAGES - 1 ahead, unless the counts and the mask may spare their loads.
-    extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][LA_UNITS][LA_THREADS]: each thread reads back its own
-    const bool ahead = VEC && a.ring;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(la_ring + tid);
+    // Each thread reads back what it copied; the vector in front of a warp's first unit is its first lane's.
+    extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][LA_RING]
+    const bool ahead = !VEC || a.ring;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(la_ring + tid), ring0 = (uint32_t)__cvta_generic_to_shared(la_ring + LA_UNITS * LA_THREADS + (tid >> 5));
     int p_row = i_begin, p_stage = 0;
+    const char *p_src = src;
+    auto shift_of = [&](const void *row) { return VEC ? 0 : (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / ES; };
     auto issue = [&]() {
         if (p_row < i_end) {
-            const char *row = src + (long long)(p_row - i_begin) * p.row_stride * (BF16 ? 2 : 4);
+            const int d = shift_of(p_src);
 #pragma unroll
             for (int u = 0; u < LA_UNITS; ++u) {
-                const int k = base + L::at(u, 0, tid);
-                if (k < V) cp_chunk(ring + (p_stage * LA_UNITS + u) * LA_THREADS * 16, row + (long long)k * (BF16 ? 2 : 4));
+                const int k = base + L::at(u, 0, tid) + d;
+                const uint32_t to = ring + (p_stage * LA_RING + u * LA_THREADS) * 16;
+                if (VEC) {
+                    if (k < V) cp_chunk(to, p_src + (long long)k * ES);
+                } else {
+                    if (k < V) cp_part(to, p_src + (long long)k * ES, min(V - k, N) * ES);
+                    const char *front = p_src + (long long)(k - N) * ES;
+                    if (u == 0 && lane == 0 && d > 0 && k - N < V && front >= p.logits) cp_part(ring0 + p_stage * LA_RING * 16, front, min(V - k + N, N) * ES);
+                }
             }
             ++p_row;
+            p_src += p.row_stride * ES;
         }
         p_stage = p_stage + 1 == LA_STAGES ? 0 : p_stage + 1;
         cp_commit();                                   // an empty group where nothing is left
@@ -151,20 +168,22 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) held[u][i] = 0;
             if (counts == nullptr) continue;
-            if (VEC) {
-                if (base + k >= V) continue;
-                if (BF16) {
-                    const uint4 c = *reinterpret_cast<const uint4 *>(counts + k);
-                    held[u][0] = c.x; held[u][1] = c.y; held[u][N / 2 - 2] = c.z; held[u][N / 2 - 1] = c.w;
-                } else {
-                    const uint2 c = *reinterpret_cast<const uint2 *>(counts + k);
-                    held[u][0] = c.x; held[u][1] = c.y;
-                }
+            if (base + k >= V) continue;               // rows of counts are padded to whole units
+            if (BF16) {
+                const uint4 c = *reinterpret_cast<const uint4 *>(counts + k);
+                held[u][0] = c.x; held[u][1] = c.y; held[u][N / 2 - 2] = c.z; held[u][N / 2 - 1] = c.w;
             } else {
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (base + L::at(u, e, tid) < V) held[u][e / 2] |= (uint32_t)(uint16_t)counts[L::at(u, e, tid)] << (16 * (e & 1));
+                const uint2 c = *reinterpret_cast<const uint2 *>(counts + k);
+                held[u][0] = c.x; held[u][1] = c.y;
             }
+        }
+    }
+    int bias_token[LA_BIASES / LA_THREADS];            // entries tid, tid + LA_THREADS, .. of the bias list
+    if (ADD && p.n_bias != nullptr) {
+#pragma unroll
+        for (int c = 0; c < LA_BIASES / LA_THREADS; ++c) {
+            const int i = c * LA_THREADS + tid;
+            bias_token[c] = i < p.bias_stride ? p.bias_tokens[(long long)b * p.bias_stride + i] : 0;
         }
     }
     // ---- what counts and biases do to this thread's elements
@@ -183,15 +202,10 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
             rep_inv = 1.f / rep;
             if (p.frequency != nullptr) freq = p.frequency[b];
             if (p.presence != nullptr) pres = p.presence[b];
-            if (tid < n_drafts) {                      // at most LA_MAX_GAMMA
-                const long long first = p.cu_d[b];
-                if (first < 0 || first + tid >= p.n_d_rows) {
-                    bad |= SV_DEV_BAD_LEN;
-                } else {
-                    const int t = p.draft_tokens[first + tid];
-                    if (t < 0 || t >= V) bad |= SV_DEV_BAD_TOKEN;
-                    else if (t >= base && t < base + SLICE) my_at = t - base;
-                }
+            if (tid < n_drafts) {
+                if (!my_token_there) bad |= SV_DEV_BAD_LEN;
+                else if (my_token < 0 || my_token >= V) bad |= SV_DEV_BAD_TOKEN;
+                else if (my_token >= base && my_token < base + SLICE) my_at = my_token - base;
                 draft_at[tid] = my_at;
             }
             if (n_drafts > 0) __syncthreads();
@@ -221,32 +235,36 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                 if (i0 > 0) __syncthreads();
                 bias_head[tid] = -1;
                 __syncthreads();
-                for (int i = tid; i < min(n - i0, LA_BIASES); i += LA_THREADS) {
-                    const int t = bias_tokens[i0 + i];
+#pragma unroll
+                for (int c = 0; c < LA_BIASES / LA_THREADS; ++c) {
+                    const int i = c * LA_THREADS + tid, t = i0 == 0 ? bias_token[c] : i0 + i < n ? bias_tokens[i0 + i] : 0;
+                    if (i0 + i >= n) break;
                     if (t < 0 || t >= V) bad |= SV_DEV_BAD_TOKEN;
-                    else if (t >= base && t < base + SLICE) bias_next[i] = (short)atomicExch(&bias_head[L::owner(t - base)], i);
+                    else if (t >= base && t < base + SLICE)
+                        bias_node[i] = (t - base) | atomicExch(&bias_head[L::owner(t - base)], i) << 16;
                 }
                 __syncthreads();
-                // value that element `at` gets from this part of the list, if any: the later entry counts
-                auto look_up = [&](int at, float &value) {
+                // entry that decides about element `at` in this part of the list, or -1: the last that names it
+                auto look_up = [&](int at) {
                     int found = -1;
-                    for (int i = bias_head[L::owner(at)]; i >= 0; i = bias_next[i])
-                        if (bias_tokens[i0 + i] == base + at) found = max(found, i);
-                    if (found >= 0) value = bias_values[i0 + found];
-                    return found >= 0;
+                    for (int i = bias_head[L::owner(at)]; i >= 0; i = bias_node[i] >> 16)
+                        if ((bias_node[i] & 0xffff) == at) found = max(found, i);
+                    return found;
                 };
-                for (int i = bias_head[tid]; i >= 0; i = bias_next[i]) {
-                    const int at = bias_tokens[i0 + i] - base;
-                    float v = 0.f;
-                    look_up(at, v);
-                    v += penalty(counts != nullptr ? counts[at] & 0x7fff : 0);
+                for (int i = bias_head[tid]; i >= 0; i = bias_node[i] >> 16) {
+                    const int at = bias_node[i] & 0xffff;
+                    if (look_up(at) != i) continue;
+                    const float v = bias_values[i0 + i] + penalty(counts != nullptr ? counts[at] & 0x7fff : 0);
 #pragma unroll
                     for (int u = 0; u < LA_UNITS; ++u)
 #pragma unroll
                         for (int e = 0; e < N; ++e)
                             if (at == L::at(u, e, tid)) add[u][e] = v;
                 }
-                if (my_at >= 0) look_up(my_at, my_bias);
+                if (my_at >= 0) {
+                    const int i = look_up(my_at);
+                    if (i >= 0) my_bias = bias_values[i0 + i];
+                }
             }
         }
         if (n_drafts > 0) {
@@ -271,7 +289,7 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     for (int j = 0; j < min(before, n_drafts); ++j) take(j);
     // In place, a unit that nothing is added to in any of the rows is left alone where the mask allows all of it.
     uint32_t still = 0;                                // bit u
-    if (a.in_place) {
+    if (VEC && a.in_place) {
 #pragma unroll
         for (int u = 0; u < LA_UNITS; ++u) {
             bool moves = false;
@@ -285,7 +303,7 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
         for (int j = before; j < n_drafts; ++j) {
             const int at = draft_at[j];
             if (at < 0 || L::owner(at) != tid) continue;
-            still &= ~(1u << (at / (LA_THREADS * N)));
+            still &= ~(1u << L::unit(at));
         }
     }
 
@@ -294,16 +312,8 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
         uint32_t allowed = 0;
 #pragma unroll
         for (int u = 0; u < LA_UNITS; ++u) {
-            if (VEC) {
-                const int k = base + L::at(u, 0, tid);
-                if (k < V) allowed |= ((mask[k / 8] >> (k & 7)) & ((1u << N) - 1)) << (u * N);
-            } else {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const int k = base + L::at(u, e, tid);
-                    if (k < V) allowed |= ((mask[k / 8] >> (k & 7)) & 1u) << (u * N + e);
-                }
-            }
+            const int k = base + L::at(u, 0, tid);
+            if (k < V) allowed |= ((mask[k / 8] >> (k & 7)) & ((1u << N) - 1)) << (u * N);
         }
         return allowed;
     };
@@ -319,15 +329,54 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
             cp_wait<LA_STAGES - 2>();
 #pragma unroll
             for (int u = 0; u < LA_UNITS; ++u) {
-                const uint4 v = la_ring[(stage * LA_UNITS + u) * LA_THREADS + tid];
+                const uint4 v = la_ring[stage * LA_RING + u * LA_THREADS + tid];
                 w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
+            }
+            const int d = shift_of(src);
+            if (!VEC && d > 0) {                       // the first d elements of a unit are in the vector of the lane before
+                uint32_t last[4];                      // of the 32 units before this one's
+                const uint4 v = la_ring[stage * LA_RING + LA_UNITS * LA_THREADS + (tid >> 5)];
+                last[0] = v.x; last[1] = v.y; last[2] = v.z; last[3] = v.w;
+                if (lane == 0 && base + tid == 0 && src - (N - d) * ES < p.logits) {       // nothing lies before the first row
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const int k = e - (N - d);
+                        if (BF16) {
+                            const uint32_t h = k >= 0 && k < V ? (uint32_t)reinterpret_cast<const unsigned short *>(src)[k] : 0;
+                            last[e / 2] = e & 1 ? last[e / 2] | h << 16 : h;
+                        } else {
+                            last[e & 3] = k >= 0 && k < V ? reinterpret_cast<const uint32_t *>(src)[k] : 0;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < LA_UNITS; ++u) {
+                    uint32_t before_w[4], own[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        own[c] = w[u][c];
+                        const uint32_t up = __shfl_up_sync(0xffffffffu, own[c], 1), end = __shfl_sync(0xffffffffu, own[c], 31);
+                        before_w[c] = lane == 0 ? last[c] : up;
+                        last[c] = end;
+                    }
+                    pick<BF16>(before_w, own, N - d, w[u]);
+                }
             }
             stage = stage + 1 == LA_STAGES ? 0 : stage + 1;
             issue();
         } else {
-            load_row(allowed, still);
-            src += p.row_stride * (BF16 ? 2 : 4);
+#pragma unroll
+            for (int u = 0; u < LA_UNITS; ++u) {
+                w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
+                const int k = base + L::at(u, 0, tid);
+                const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
+                if (k < V && own != 0 && !((still >> u) & 1u && own == (1u << N) - 1)) {
+                    const uint4 v = ld_once(src + (long long)k * ES);
+                    w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
+                }
+            }
         }
+        src += p.row_stride * ES;
         if (i > i_begin && i <= n_drafts) take(i - 1);
 #pragma unroll
         for (int u = 0; u < LA_UNITS; ++u) {
@@ -343,22 +392,42 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                     w[u][e / 2] = *reinterpret_cast<const uint32_t *>(&h);
                 }
             }
+        }
+        const int d = shift_of(dst);
+        uint32_t first_of_next[4] = {0, 0, 0, 0};      // first unit behind the 32 of this u
+#pragma unroll
+        for (int u = LA_UNITS - 1; u >= 0; --u) {
+            const int k = base + L::at(u, 0, tid);
             if (VEC) {
-                const int k = base + L::at(u, 0, tid);
                 const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
                 if (k < V && !((still >> u) & 1u && own == (1u << N) - 1))
-                    *reinterpret_cast<uint4 *>(dst + (long long)k * (BF16 ? 2 : 4)) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
-            } else {
+                    *reinterpret_cast<uint4 *>(dst + (long long)k * ES) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
+                continue;
+            }
+            uint32_t z[4] = {w[u][0], w[u][1], w[u][2], w[u][3]};
+            if (d > 0) {                               // the boundary's vector ends with the first d elements of the next unit
+                uint32_t after[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const uint32_t down = __shfl_down_sync(0xffffffffu, w[u][c], 1), head = __shfl_sync(0xffffffffu, w[u][c], 0);
+                    after[c] = lane == 31 ? first_of_next[c] : down;
+                    first_of_next[c] = head;
+                }
+                pick<BF16>(w[u], after, d, z);
+            }
+            const bool whole = k + d + N <= V && (d == 0 || lane < 31 || u < LA_UNITS - 1);
+            if (whole) *reinterpret_cast<uint4 *>(dst + (long long)(k + d) * ES) = make_uint4(z[0], z[1], z[2], z[3]);
+            const bool head = d > 0 && ((lane == 0 && u == 0) || k + d > V);       // nobody's vector has the first d elements
+            if (!whole || head) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const int k = base + L::at(u, e, tid);
-                    if (k >= V) continue;
-                    if (BF16) reinterpret_cast<unsigned short *>(dst)[k] = (unsigned short)(w[u][e / 2] >> (16 * (e & 1)));
-                    else reinterpret_cast<uint32_t *>(dst)[k] = w[u][e & 3];
+                    if (k + e >= V || (e < d ? !head : whole)) continue;
+                    if (BF16) reinterpret_cast<unsigned short *>(dst)[k + e] = (unsigned short)(w[u][e / 2] >> (16 * (e & 1)));
+                    else reinterpret_cast<uint32_t *>(dst)[k + e] = w[u][e & 3];
                 }
             }
         }
-        dst += p.out_stride * (BF16 ? 2 : 4);
+        dst += p.out_stride * ES;
     }
     if (bad != 0) set_status(p.device_status, bad);
 }
@@ -367,7 +436,7 @@ template <bool BF16, bool ADD, bool MASK, bool VEC>
 static sv_status launch_one(const LogitsAdjustLaunch &a, dim3 grid, cudaStream_t stream)
 {
     return launch_kernel(true, logits_adjust_kernel<BF16, ADD, MASK, VEC>, grid, LA_THREADS,
-                         a.ring ? (size_t)LA_STAGES * LA_UNITS * LA_THREADS * 16 : 0, stream, a);
+                         !VEC || a.ring ? (size_t)LA_STAGES * LA_RING * 16 : 0, stream, a);
 }
 template <bool BF16, bool VEC>
 static sv_status launch_kinds(const LogitsAdjustLaunch &a, bool add, bool mask, dim3 grid, cudaStream_t stream)
@@ -382,7 +451,7 @@ template <bool BF16>
 static sv_status launch_adjust(LogitsAdjustLaunch &a, cudaStream_t stream)
 {
     const sv_logits_adjust_params &p = a.p;
-    constexpr int slice = Layout<BF16, true>::SLICE;
+    constexpr int slice = Layout<BF16>::SLICE;
     a.slices = (p.vocab + slice - 1) / slice;
     const int rows = p.n_drafted != nullptr ? 1 : p.gamma_max + 1;
     // Few blocks: a sequence's rows are dealt out as well.
@@ -390,7 +459,7 @@ static sv_status launch_adjust(LogitsAdjustLaunch &a, cudaStream_t stream)
     const long long split = resident / whole < 1 ? 1 : resident / whole < rows ? resident / whole : rows;
     a.rows_per_block = (int)((rows + split - 1) / split);
     a.chunks = (rows + a.rows_per_block - 1) / a.rows_per_block;
-    a.ring = a.vec && !a.in_place && true;
+    a.ring = !a.in_place;
     const long long blocks = (long long)p.batch * a.chunks * a.slices;
     if (blocks > 0x7fffffffLL) return SV_EUNSUPPORTED;
     const dim3 grid((unsigned)blocks);
