@@ -15,7 +15,8 @@ constexpr int LA_BLOCKS = 5;               // blocks of an SM, with penalties or
 constexpr int LA_BLOCKS_MASK = 8;          // and with masks alone
 constexpr int LA_MAX_GAMMA = 64;
 constexpr int LA_STAGES = 4;
-constexpr int LA_RING = LA_UNITS * LA_THREADS + LA_THREADS / 32;       // vectors of a row in the ring
+constexpr int LA_PART = 1 + LA_UNITS * 32; // vectors of a row's part in the ring that a warp has
+constexpr int LA_RING = LA_THREADS / 32 * LA_PART;
 constexpr int LA_BIASES = 1024;            // entries of the bias list at a time
 
 struct LogitsAdjustLaunch {
@@ -59,25 +60,24 @@ struct Layout {
     static __device__ __forceinline__ int unit(int at) { return at / (32 * N) % LA_UNITS; }
 };
 
-// N elements from element `from` (0 <= from < N) of the 2 N elements lo, hi
+// A unit from byte `at` of a warp's part of the ring; at is a multiple of the element size
 template <bool BF16>
-__device__ __forceinline__ void pick(const uint32_t (&lo)[4], const uint32_t (&hi)[4], int from, uint32_t (&out)[4])
+__device__ __forceinline__ void read_unit(const uint32_t *part, int at, uint32_t (&w)[4])
 {
-    const int words = BF16 ? from >> 1 : from;
-    uint32_t w[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    if (words & 2)
+    const uint32_t *s = part + (at >> 2);
 #pragma unroll
-        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-    if (words & 1)
+    for (int i = 0; i < 4; ++i) w[i] = s[i];
+    if (BF16 && (at & 2)) {
+        const uint32_t last = s[4];
 #pragma unroll
-        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = BF16 && (from & 1) ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], i < 3 ? w[i + 1] : last, 16);
+    }
 }
 
 // ADD: penalties or biases; MASK: grammar masks.  VEC: every unit of every row starts on a 16-byte boundary and ends inside
 // the vocabulary.  Elsewhere (a vocabulary of odd size, say) a row's 16-byte boundaries lie d elements behind the units',
-// d differing from row to row: the accesses keep to the boundaries, and the neighbouring lane's part of a unit comes by shuffle.
+// d differing from row to row: global accesses keep to the boundaries, and a warp moves its units to and from them in shared
+// memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us where this takes UNALIGNED.)
 template <bool BF16, bool ADD, bool MASK, bool VEC>
 __global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
@@ -127,10 +127,11 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     char *dst = static_cast<char *>(p.out) + (row0 + i_begin) * p.out_stride * ES;
     uint32_t w[LA_UNITS][4];
     // Rows come through a ring in shared memory, LA_STAGES - 1 ahead, unless the counts and the mask may spare their loads.
-    // Each thread reads back what it copied; the vector in front of a warp's first unit is its first lane's.
-    extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][LA_RING]
+    // A warp's part of a row: the vector in front of its first unit (used where boundaries and units differ), then its vectors.
+    extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][warps][LA_PART]
+    const uint4 *part = la_ring + (tid >> 5) * LA_PART;
     const bool ahead = !VEC || a.ring;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(la_ring + tid), ring0 = (uint32_t)__cvta_generic_to_shared(la_ring + LA_UNITS * LA_THREADS + (tid >> 5));
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(part);
     int p_row = i_begin, p_stage = 0;
     const char *p_src = src;
     auto shift_of = [&](const void *row) { return VEC ? 0 : (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / ES; };
@@ -140,13 +141,13 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 #pragma unroll
             for (int u = 0; u < LA_UNITS; ++u) {
                 const int k = base + L::at(u, 0, tid) + d;
-                const uint32_t to = ring + (p_stage * LA_RING + u * LA_THREADS) * 16;
+                const uint32_t to = ring + (p_stage * LA_RING + 1 + u * 32 + lane) * 16;
                 if (VEC) {
                     if (k < V) cp_chunk(to, p_src + (long long)k * ES);
                 } else {
                     if (k < V) cp_part(to, p_src + (long long)k * ES, min(V - k, N) * ES);
                     const char *front = p_src + (long long)(k - N) * ES;
-                    if (u == 0 && lane == 0 && d > 0 && k - N < V && front >= p.logits) cp_part(ring0 + p_stage * LA_RING * 16, front, min(V - k + N, N) * ES);
+                    if (u == 0 && lane == 0 && d > 0 && k - N < V && front >= p.logits) cp_part(ring + p_stage * LA_RING * 16, front, min(V - k + N, N) * ES);
                 }
             }
             ++p_row;
@@ -325,42 +326,30 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
             mask += p.mask_stride * 4;
             next = mask_row();
         }
+        uint4 *out_slot = nullptr;                     // where the row's results meet
         if (ahead) {
             cp_wait<LA_STAGES - 2>();
-#pragma unroll
-            for (int u = 0; u < LA_UNITS; ++u) {
-                const uint4 v = la_ring[stage * LA_RING + u * LA_THREADS + tid];
-                w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
-            }
-            const int d = shift_of(src);
-            if (!VEC && d > 0) {                       // the first d elements of a unit are in the vector of the lane before
-                uint32_t last[4];                      // of the 32 units before this one's
-                const uint4 v = la_ring[stage * LA_RING + LA_UNITS * LA_THREADS + (tid >> 5)];
-                last[0] = v.x; last[1] = v.y; last[2] = v.z; last[3] = v.w;
-                if (lane == 0 && base + tid == 0 && src - (N - d) * ES < p.logits) {       // nothing lies before the first row
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const int k = e - (N - d);
-                        if (BF16) {
-                            const uint32_t h = k >= 0 && k < V ? (uint32_t)reinterpret_cast<const unsigned short *>(src)[k] : 0;
-                            last[e / 2] = e & 1 ? last[e / 2] | h << 16 : h;
-                        } else {
-                            last[e & 3] = k >= 0 && k < V ? reinterpret_cast<const uint32_t *>(src)[k] : 0;
-                        }
-                    }
-                }
+            const uint4 *slot = part + stage * LA_RING;
+            if (VEC) {
 #pragma unroll
                 for (int u = 0; u < LA_UNITS; ++u) {
-                    uint32_t before_w[4], own[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        own[c] = w[u][c];
-                        const uint32_t up = __shfl_up_sync(0xffffffffu, own[c], 1), end = __shfl_sync(0xffffffffu, own[c], 31);
-                        before_w[c] = lane == 0 ? last[c] : up;
-                        last[c] = end;
-                    }
-                    pick<BF16>(before_w, own, N - d, w[u]);
+                    const uint4 v = slot[1 + u * 32 + lane];
+                    w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
                 }
+            } else {
+                const int d = shift_of(src);
+                if (d > 0 && base + tid == 0 && src - (N - d) * ES < p.logits) {       // nothing lies before the first row
+                    for (int e = 0; e < min(d, V); ++e) {
+                        char *to = reinterpret_cast<char *>(const_cast<uint4 *>(slot)) + 16 - (d - e) * ES;
+                        if (BF16) *reinterpret_cast<unsigned short *>(to) = reinterpret_cast<const unsigned short *>(src)[e];
+                        else *reinterpret_cast<uint32_t *>(to) = reinterpret_cast<const uint32_t *>(src)[e];
+                    }
+                }
+                __syncwarp();                          // every lane's copies of this row are there
+#pragma unroll
+                for (int u = 0; u < LA_UNITS; ++u) read_unit<BF16>(reinterpret_cast<const uint32_t *>(slot), 16 + (u * 32 + lane) * 16 - d * ES, w[u]);
+                __syncwarp();                          // and are read
+                out_slot = const_cast<uint4 *>(slot) + 1;
             }
             stage = stage + 1 == LA_STAGES ? 0 : stage + 1;
             issue();
@@ -393,38 +382,34 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                 }
             }
         }
-        const int d = shift_of(dst);
-        uint32_t first_of_next[4] = {0, 0, 0, 0};      // first unit behind the 32 of this u
+        if (VEC) {
 #pragma unroll
-        for (int u = LA_UNITS - 1; u >= 0; --u) {
-            const int k = base + L::at(u, 0, tid);
-            if (VEC) {
+            for (int u = 0; u < LA_UNITS; ++u) {
+                const int k = base + L::at(u, 0, tid);
                 const uint32_t own = allowed >> (u * N) & ((1u << N) - 1);
                 if (k < V && !((still >> u) & 1u && own == (1u << N) - 1))
                     *reinterpret_cast<uint4 *>(dst + (long long)k * ES) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
-                continue;
             }
-            uint32_t z[4] = {w[u][0], w[u][1], w[u][2], w[u][3]};
-            if (d > 0) {                               // the boundary's vector ends with the first d elements of the next unit
-                uint32_t after[4];
+        } else {
+            const int d = shift_of(dst);
+            const int first = base + L::at(0, 0, tid & ~31), end = min(first + 32 * LA_UNITS * N, V);      // elements of the warp
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const uint32_t down = __shfl_down_sync(0xffffffffu, w[u][c], 1), head = __shfl_sync(0xffffffffu, w[u][c], 0);
-                    after[c] = lane == 31 ? first_of_next[c] : down;
-                    first_of_next[c] = head;
-                }
-                pick<BF16>(w[u], after, d, z);
+            for (int u = 0; u < LA_UNITS; ++u) out_slot[u * 32 + lane] = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < LA_UNITS; ++u) {
+                const int k = first + d + (u * 32 + lane) * N;
+                if (k + N > end) continue;
+                read_unit<BF16>(reinterpret_cast<const uint32_t *>(out_slot), (k - first) * ES, w[u]);
+                *reinterpret_cast<uint4 *>(dst + (long long)k * ES) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
             }
-            const bool whole = k + d + N <= V && (d == 0 || lane < 31 || u < LA_UNITS - 1);
-            if (whole) *reinterpret_cast<uint4 *>(dst + (long long)(k + d) * ES) = make_uint4(z[0], z[1], z[2], z[3]);
-            const bool head = d > 0 && ((lane == 0 && u == 0) || k + d > V);       // nobody's vector has the first d elements
-            if (!whole || head) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if (k + e >= V || (e < d ? !head : whole)) continue;
-                    if (BF16) reinterpret_cast<unsigned short *>(dst)[k + e] = (unsigned short)(w[u][e / 2] >> (16 * (e & 1)));
-                    else reinterpret_cast<uint32_t *>(dst)[k + e] = w[u][e & 3];
-                }
+            // the elements in front of the first boundary, and behind the last vector: fewer than N each
+            const int behind = end - first <= d ? end : end - (end - first - d) % N;
+            const int k = lane < N ? (first + lane < min(first + d, end) ? first + lane : -1)
+                                   : (lane < 2 * N && behind + lane - N < end ? behind + lane - N : -1);
+            if (k >= 0) {
+                if (BF16) reinterpret_cast<unsigned short *>(dst)[k] = reinterpret_cast<const unsigned short *>(out_slot)[k - first];
+                else reinterpret_cast<uint32_t *>(dst)[k] = reinterpret_cast<const uint32_t *>(out_slot)[k - first];
             }
         }
         dst += p.out_stride * ES;
