@@ -2,8 +2,17 @@
 //
 // A block takes a slice of the vocabulary and the rows of one sequence's block.  What the counts and the bias list do to
 // an element is the same for all of these rows, x * factor + add, except where a draft token falls on it: the counts and the
-// list are read once, the two numbers stay in registers, and row i + 1 only updates the element that draft i names.
-// HBM bounds it: the logits in and out, and 2 bytes of counts per 17 rows.
+// list are read once, the two numbers stay in registers, and row i + 1 only updates the element that draft i names.  Rows and
+// masks stream through a ring in shared memory.  HBM bounds it: the logits in and out, a bit of mask per element, and 2 bytes
+// of counts per block of rows.
+//
+// Measured with ADD and masks: 2176 float32 rows of 128256 with 300 biases each 343 us (2.2 GB; 6.7 TB/s with the sectors
+// that the ring does not spare), bf16 rows of 128256 (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases
+// too (38 and 39 us at the copy rate): instructions bound the latter.  Steps that led here: rows loaded to registers two ahead
+// 651 us; the effect of each draft prepared once per block and rows one at a time at a higher occupancy 379 us; the ring 353 us;
+// masks through the ring 343 us.  A correction of the touched elements alone, in the ring, needs fewer instructions where they
+// are few, but the slices that hold most of a history (frequent tokens have neighbouring ids) then keep the others waiting: 4
+// sequences at a vocabulary of 32000 took 8.5 us instead of 3.8, the bf16 rows 49 us instead of 41.
 #include "common.cuh"
 #include "row_stream.cuh"
 
@@ -11,19 +20,21 @@ namespace sv {
 
 constexpr int LA_THREADS = 256;
 constexpr int LA_UNITS = 2;                // 16-byte units of a row that a thread has
-constexpr int LA_BLOCKS = 5;               // blocks of an SM, with penalties or biases
-constexpr int LA_BLOCKS_MASK = 8;          // and with masks alone
+constexpr int LA_BLOCKS = 4;               // blocks of an SM, with penalties or biases
+constexpr int LA_BLOCKS_MASK = 6;          // and with masks alone
+constexpr int LA_BLOCKS_DIRECT = 8;        // or in place
 constexpr int LA_MAX_GAMMA = 64;
-constexpr int LA_STAGES = 4;
+constexpr int LA_STAGES = 4;               // rows of the ring
 constexpr int LA_PART = 1 + LA_UNITS * 32; // vectors of a row's part in the ring that a warp has
 constexpr int LA_RING = LA_THREADS / 32 * LA_PART;
+enum { LA_RING_PATH, LA_DIRECT, LA_SHIFT };
 constexpr int LA_BIASES = 1024;            // entries of the bias list at a time
 
 struct LogitsAdjustLaunch {
     sv_logits_adjust_params p;
     int slices;                            // blocks along the vocabulary
     int rows_per_block, chunks;            // rows of a block, blocks along a sequence's rows
-    int in_place, vec, ring;
+    int in_place, vec;
     int penalties;
 };
 
@@ -45,6 +56,10 @@ __device__ __forceinline__ void cp_part(uint32_t dst, const void *src, int bytes
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void cp_word(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -53,7 +68,8 @@ __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0
 template <bool BF16>
 struct Layout {
     static constexpr int N = BF16 ? 8 : 4;                      // elements of a unit
-    static constexpr int SLICE = LA_THREADS * LA_UNITS * N;     // elements of a block
+    static constexpr int PART = 32 * LA_UNITS * N;              // elements of a warp
+    static constexpr int SLICE = LA_THREADS / 32 * PART;        // elements of a block
     static_assert(SLICE <= 1 << 16, "an element of a slice fits 16 bits");
     static __device__ __forceinline__ int at(int u, int e, int tid) { return (((tid >> 5) * LA_UNITS + u) * 32 + (tid & 31)) * N + e; }
     static __device__ __forceinline__ int owner(int at) { return at / (32 * LA_UNITS * N) * 32 + at / N % 32; }
@@ -74,21 +90,26 @@ __device__ __forceinline__ void read_unit(const uint32_t *part, int at, uint32_t
     }
 }
 
-// ADD: penalties or biases; MASK: grammar masks.  VEC: every unit of every row starts on a 16-byte boundary and ends inside
-// the vocabulary.  Elsewhere (a vocabulary of odd size, say) a row's 16-byte boundaries lie d elements behind the units',
+// ADD: penalties or biases; MASK: grammar masks.  PATH: LA_RING_PATH where every unit of every row starts on a 16-byte boundary
+// and ends inside the vocabulary; LA_DIRECT where that is so and the call works in place: units that do not change are not
+// loaded, so what the mask and the counts say comes before the loads.  Elsewhere LA_SHIFT (a vocabulary of odd size, say) a row's 16-byte boundaries lie d elements behind the units',
 // d differing from row to row: global accesses keep to the boundaries, and a warp moves its units to and from them in shared
-// memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us where this takes UNALIGNED.)
-template <bool BF16, bool ADD, bool MASK, bool VEC>
-__global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : LA_BLOCKS_MASK)
+// memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us for bf16
+// rows of 50257 where this takes 32; by single elements 66.)
+template <bool BF16, bool ADD, bool MASK, int PATH>
+__global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : PATH == LA_DIRECT ? LA_BLOCKS_DIRECT : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 {
     pdl_enter();
     using L = Layout<BF16>;
+    constexpr bool VEC = PATH != LA_SHIFT, ahead = PATH != LA_DIRECT;
     constexpr int N = L::N, SLICE = L::SLICE, ES = 16 / N;
     __shared__ int draft_at[LA_MAX_GAMMA];             // element of the slice that draft j names, or -1
     __shared__ float draft_add[LA_MAX_GAMMA];          // what is added to it once the draft is in the history
     __shared__ int bias_head[ADD ? LA_THREADS : 1];    // entries of the bias list that name an element of thread t: a linked list, -1 its end
     __shared__ int bias_node[ADD ? LA_BIASES : 1];     // per entry: its element of the slice, and the next entry of the thread's list << 16
+    __shared__ uint32_t mask_ring[MASK && ahead ? LA_STAGES : 1][LA_THREADS / 32][L::PART / 32];      // the rows' masks
+    __shared__ uint2 keep[MASK && BF16 && ahead ? 16 : 1];      // what four allowed bits keep of four bf16 elements
     const sv_logits_adjust_params &p = a.p;
     const int tid = threadIdx.x, lane = tid & 31, V = p.vocab;
     const int slice = blockIdx.x % a.slices, seq_chunk = blockIdx.x / a.slices;
@@ -126,14 +147,18 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     const char *src = static_cast<const char *>(p.logits) + (row0 + i_begin) * p.row_stride * ES;
     char *dst = static_cast<char *>(p.out) + (row0 + i_begin) * p.out_stride * ES;
     uint32_t w[LA_UNITS][4];
-    // Rows come through a ring in shared memory, LA_STAGES - 1 ahead, unless the counts and the mask may spare their loads.
+    // Rows come through a ring in shared memory, LA_STAGES - 1 ahead.
     // A warp's part of a row: the vector in front of its first unit (used where boundaries and units differ), then its vectors.
     extern __shared__ __align__(16) uint4 la_ring[];   // [LA_STAGES][warps][LA_PART]
     const uint4 *part = la_ring + (tid >> 5) * LA_PART;
-    const bool ahead = !VEC || a.ring;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(part);
     int p_row = i_begin, p_stage = 0;
     const char *p_src = src;
+    const unsigned char *p_mask = mask;
+    const uint32_t mask_to = (uint32_t)__cvta_generic_to_shared(&mask_ring[0][MASK ? tid >> 5 : 0][MASK ? lane % (L::PART / 32) : 0]);
+    if (MASK && BF16 && ahead && tid < 16)
+        keep[tid] = make_uint2((tid & 1 ? 0xffffu : 0u) | (tid & 2 ? 0xffff0000u : 0u), (tid & 4 ? 0xffffu : 0u) | (tid & 8 ? 0xffff0000u : 0u));
+    if (MASK && BF16 && ahead) __syncthreads();
     auto shift_of = [&](const void *row) { return VEC ? 0 : (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / ES; };
     auto issue = [&]() {
         if (p_row < i_end) {
@@ -149,6 +174,11 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                     const char *front = p_src + (long long)(k - N) * ES;
                     if (u == 0 && lane == 0 && d > 0 && k - N < V && front >= p.logits) cp_part(ring + p_stage * LA_RING * 16, front, min(V - k + N, N) * ES);
                 }
+            }
+            if (MASK) {
+                const int k = base + (tid >> 5) * L::PART + 32 * lane;
+                if (lane < L::PART / 32 && k < V) cp_word(mask_to + p_stage * sizeof(mask_ring[0]), p_mask + k / 8);
+                p_mask += p.mask_stride * 4;
             }
             ++p_row;
             p_src += p.row_stride * ES;
@@ -290,7 +320,7 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     for (int j = 0; j < min(before, n_drafts); ++j) take(j);
     // In place, a unit that nothing is added to in any of the rows is left alone where the mask allows all of it.
     uint32_t still = 0;                                // bit u
-    if (VEC && a.in_place) {
+    if (!ahead) {
 #pragma unroll
         for (int u = 0; u < LA_UNITS; ++u) {
             bool moves = false;
@@ -319,10 +349,10 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
         return allowed;
     };
     int stage = 0;
-    uint32_t next = MASK ? mask_row() : 0xffffffffu;
+    uint32_t next = MASK && !ahead ? mask_row() : 0xffffffffu;
     for (int i = i_begin; i < i_end; ++i) {
-        const uint32_t allowed = next;
-        if (MASK && i + 1 < i_end) {                   // a row ahead: it decides what is loaded
+        uint32_t allowed = next;
+        if (MASK && !ahead && i + 1 < i_end) {         // a row ahead: it decides what is loaded
             mask += p.mask_stride * 4;
             next = mask_row();
         }
@@ -330,6 +360,16 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
         if (ahead) {
             cp_wait<LA_STAGES - 2>();
             const uint4 *slot = part + stage * LA_RING;
+            if (MASK || !VEC) __syncwarp();            // every lane's copies of this row are there
+            if (MASK) {
+                const unsigned char *bits = reinterpret_cast<const unsigned char *>(mask_ring[stage][tid >> 5]);
+                allowed = 0;
+#pragma unroll
+                for (int u = 0; u < LA_UNITS; ++u) {
+                    const int e = (u * 32 + lane) * N;
+                    allowed |= (bits[e / 8] >> (e & 7) & ((1u << N) - 1)) << (u * N);
+                }
+            }
             if (VEC) {
 #pragma unroll
                 for (int u = 0; u < LA_UNITS; ++u) {
@@ -345,7 +385,6 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                         else *reinterpret_cast<uint32_t *>(to) = reinterpret_cast<const uint32_t *>(src)[e];
                     }
                 }
-                __syncwarp();                          // every lane's copies of this row are there
 #pragma unroll
                 for (int u = 0; u < LA_UNITS; ++u) read_unit<BF16>(reinterpret_cast<const uint32_t *>(slot), 16 + (u * 32 + lane) * 16 - d * ES, w[u]);
                 __syncwarp();                          // and are read
@@ -374,12 +413,28 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
             for (int e = 0; e < N; ++e) {
                 x[e] = BF16 ? __uint_as_float(e & 1 ? w[u][e / 2] & 0xffff0000u : w[u][e / 2] << 16) : __uint_as_float(w[u][e & 3]);
                 if (ADD) x[e] = x[e] * ((seen >> (u * N + e)) & 1u ? (x[e] > 0.f ? rep_inv : rep) : 1.f) + add[u][e];
-                if (MASK && !((allowed >> (u * N + e)) & 1u)) x[e] = -CUDART_INF_F;
+                if (MASK && !BF16 && !((allowed >> (u * N + e)) & 1u)) x[e] = -CUDART_INF_F;
                 if (!BF16) w[u][e & 3] = __float_as_uint(x[e]);
                 else if (e & 1) {
                     const __nv_bfloat162 h = __floats2bfloat162_rn(x[e - 1], x[e]);                // the one rounding
                     w[u][e / 2] = *reinterpret_cast<const uint32_t *>(&h);
                 }
+            }
+        }
+        if (MASK && BF16) {                            // -inf in what is not allowed
+#pragma unroll
+            for (int u = 0; u < LA_UNITS; ++u) {
+                uint32_t stay[4];
+                if (ahead) {
+                    const uint2 lo = keep[allowed >> (u * N) & 15], hi = keep[allowed >> (u * N + 4) & 15];
+                    stay[0] = lo.x; stay[1] = lo.y; stay[2] = hi.x; stay[3] = hi.y;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        stay[c] = (allowed >> (u * N + 2 * c) & 1u ? 0xffffu : 0u) | (allowed >> (u * N + 2 * c + 1) & 1u ? 0xffff0000u : 0u);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[u][c] = (w[u][c] & stay[c]) | (0xff80ff80u & ~stay[c]);
             }
         }
         if (VEC) {
@@ -417,19 +472,18 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     if (bad != 0) set_status(p.device_status, bad);
 }
 
-template <bool BF16, bool ADD, bool MASK, bool VEC>
+template <bool BF16, bool ADD, bool MASK, int PATH>
 static sv_status launch_one(const LogitsAdjustLaunch &a, dim3 grid, cudaStream_t stream)
 {
-    return launch_kernel(true, logits_adjust_kernel<BF16, ADD, MASK, VEC>, grid, LA_THREADS,
-                         !VEC || a.ring ? (size_t)LA_STAGES * LA_RING * 16 : 0, stream, a);
+    return launch_kernel(true, logits_adjust_kernel<BF16, ADD, MASK, PATH>, grid, LA_THREADS, PATH != LA_DIRECT ? (size_t)LA_STAGES * LA_RING * 16 : 0, stream, a);
 }
-template <bool BF16, bool VEC>
+template <bool BF16, int PATH>
 static sv_status launch_kinds(const LogitsAdjustLaunch &a, bool add, bool mask, dim3 grid, cudaStream_t stream)
 {
-    if (add && mask) return launch_one<BF16, true, true, VEC>(a, grid, stream);
-    if (add) return launch_one<BF16, true, false, VEC>(a, grid, stream);
-    if (mask) return launch_one<BF16, false, true, VEC>(a, grid, stream);
-    return launch_one<BF16, false, false, VEC>(a, grid, stream);
+    if (add && mask) return launch_one<BF16, true, true, PATH>(a, grid, stream);
+    if (add) return launch_one<BF16, true, false, PATH>(a, grid, stream);
+    if (mask) return launch_one<BF16, false, true, PATH>(a, grid, stream);
+    return launch_one<BF16, false, false, PATH>(a, grid, stream);
 }
 
 template <bool BF16>
@@ -444,12 +498,12 @@ static sv_status launch_adjust(LogitsAdjustLaunch &a, cudaStream_t stream)
     const long long split = resident / whole < 1 ? 1 : resident / whole < rows ? resident / whole : rows;
     a.rows_per_block = (int)((rows + split - 1) / split);
     a.chunks = (rows + a.rows_per_block - 1) / a.rows_per_block;
-    a.ring = !a.in_place;
     const long long blocks = (long long)p.batch * a.chunks * a.slices;
     if (blocks > 0x7fffffffLL) return SV_EUNSUPPORTED;
     const dim3 grid((unsigned)blocks);
     const bool add = a.penalties || p.n_bias != nullptr, mask = p.mask != nullptr;
-    return a.vec ? launch_kinds<BF16, true>(a, add, mask, grid, stream) : launch_kinds<BF16, false>(a, add, mask, grid, stream);
+    if (!a.vec) return launch_kinds<BF16, LA_SHIFT>(a, add, mask, grid, stream);
+    return a.in_place ? launch_kinds<BF16, LA_DIRECT>(a, add, mask, grid, stream) : launch_kinds<BF16, LA_RING_PATH>(a, add, mask, grid, stream);
 }
 
 }  // namespace sv
@@ -473,6 +527,7 @@ extern "C" sv_status spec_logits_adjust(const sv_logits_adjust_params *p, void *
     if (p->mask != nullptr && p->mask_stride < ((int64_t)p->vocab + 31) / 32) return SV_EINVAL;
     const int size = p->logits_bf16 != 0 ? 2 : 4;
     if (reinterpret_cast<uintptr_t>(p->logits) % size != 0 || reinterpret_cast<uintptr_t>(p->out) % size != 0) return SV_EALIGN;
+    if (reinterpret_cast<uintptr_t>(p->mask) % 4 != 0) return SV_EALIGN;
     const bool in_place = p->out == p->logits && p->out_stride == p->row_stride;
     const uintptr_t x = reinterpret_cast<uintptr_t>(p->logits), y = reinterpret_cast<uintptr_t>(p->out);
     const uintptr_t nx = (uintptr_t)((p->n_rows - 1) * p->row_stride + p->vocab) * size;
