@@ -6,8 +6,7 @@
 // masks stream through a ring in shared memory.  HBM bounds it: the logits in and out, a bit of mask per element, and 2 bytes
 // of counts per block of rows.
 //
-// Measured with ADD and masks: 2176 float32 rows of 128256 with 300 biases each 343 us (2.2 GB; 6.7 TB/s with the sectors
-// that the ring does not spare), bf16 rows of 128256 (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases
+// Measured with ADD and masks: 2176 float32 rows of 128256 with 300 biases each 343 us (2.3 GB, 6.7 TB/s), bf16 rows of 128256 (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases
 // too (38 and 39 us at the copy rate): instructions bound the latter.  Steps that led here: rows loaded to registers two ahead
 // 651 us; the effect of each draft prepared once per block and rows one at a time at a higher occupancy 379 us; the ring 353 us;
 // masks through the ring 343 us.  A correction of the touched elements alone, in the ring, needs fewer instructions where they
@@ -90,12 +89,13 @@ __device__ __forceinline__ void read_unit(const uint32_t *part, int at, uint32_t
     }
 }
 
-// ADD: penalties or biases; MASK: grammar masks.  PATH: LA_RING_PATH where every unit of every row starts on a 16-byte boundary
-// and ends inside the vocabulary; LA_DIRECT where that is so and the call works in place: units that do not change are not
-// loaded, so what the mask and the counts say comes before the loads.  Elsewhere LA_SHIFT (a vocabulary of odd size, say) a row's 16-byte boundaries lie d elements behind the units',
-// d differing from row to row: global accesses keep to the boundaries, and a warp moves its units to and from them in shared
-// memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us for bf16
-// rows of 50257 where this takes 32; by single elements 66.)
+// ADD: penalties or biases; MASK: grammar masks.
+// PATH: LA_RING_PATH where every unit of every row starts on a 16-byte boundary and ends inside the vocabulary; LA_DIRECT where
+// that is so and the call works in place: units that do not change are not loaded, so what the mask and the counts say comes
+// before the loads.  Elsewhere LA_SHIFT: a row's 16-byte boundaries lie d elements behind the units' (a vocabulary of odd size,
+// say), d differing from row to row: global accesses keep to the boundaries, and a warp moves its units to and from them in
+// shared memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us for bf16 rows of
+// 50257 where this takes 32; by single elements 66.)
 template <bool BF16, bool ADD, bool MASK, int PATH>
 __global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : PATH == LA_DIRECT ? LA_BLOCKS_DIRECT : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)

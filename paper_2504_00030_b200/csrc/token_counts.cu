@@ -2,14 +2,18 @@
 // (sequence, vocabulary entry).
 //
 // Counting touches a word per token: a warp joins equal tokens first and adds what is left with compare-and-swap, which
-// saturates, so the sum is the same in any order.  An admission writes whole rows: a block takes a slice of the
-// vocabulary, collects the prompt's marks as bits in shared memory (4 KB for 32768 entries) and writes the slice once,
-// cleared and marked together; HBM's write rate bounds it.
+// saturates, so the sum is the same in any order.  An admission writes whole rows: a block takes a slice of the vocabulary,
+// collects the prompt's marks in shared memory (a byte each: no atomics, whose conflicts on frequent tokens cost more) and
+// writes the slice once, cleared and marked together.  Measured for 128 prompts of 4096 to 8192 tokens at a vocabulary of 128256
+// (36 MB, 5.6 us at the copy rate): 11.3 us, of which about 2 are the launch and 3 the prompts, which every slice's block reads
+// for itself (slices of 16384 entries: 15 us).  Marks as bits 11.7 to 12.7 us; slices cleared first and marked in global memory 18
+// to 23 us (scattered two-byte stores).
 #include "common.cuh"
 
 namespace sv {
 
 constexpr int TC_THREADS = 256;
+constexpr int TC_RESET_THREADS = 512;
 constexpr int TC_SLICE = 32768;            // vocabulary entries of a block that clears
 
 struct TokenCountsLaunch {
@@ -86,11 +90,11 @@ token_counts_kernel(const __grid_constant__ TokenCountsLaunch a)
 }
 
 // rows may be cleared: a block per slice of a sequence's vocabulary
-__global__ void __launch_bounds__(TC_THREADS)
+__global__ void __launch_bounds__(TC_RESET_THREADS)
 token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
 {
     pdl_enter();
-    __shared__ unsigned int marks[TC_SLICE / 32];
+    extern __shared__ __align__(16) uint8_t marks[];   // per entry of the slice: 0x80 if the prompt has it
     const sv_token_counts_params &p = a.p;
     const int b = blockIdx.x / a.parts, lo = (blockIdx.x - b * a.parts) * TC_SLICE, tid = threadIdx.x;
     const int hi = min(p.vocab - lo, TC_SLICE) + lo;
@@ -100,18 +104,18 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
     const int32_t *first = nullptr;
     const int n = tc_range(p, b, first, bad);
     if (marking) {
-        for (int i = tid; i < TC_SLICE / 32; i += TC_THREADS) marks[i] = 0;
+        for (int i = tid; i < TC_SLICE / 16; i += TC_RESET_THREADS) reinterpret_cast<uint4 *>(marks)[i] = make_uint4(0, 0, 0, 0);
     } else if (clear) {
-        for (int k = lo + 8 * tid; k + 8 <= hi; k += 8 * TC_THREADS) *reinterpret_cast<uint4 *>(row + k) = make_uint4(0, 0, 0, 0);
-        for (int k = lo + (hi - lo) / 8 * 8 + tid; k < hi; k += TC_THREADS) row[k] = 0;
+        for (int k = lo + 8 * tid; k + 8 <= hi; k += 8 * TC_RESET_THREADS) *reinterpret_cast<uint4 *>(row + k) = make_uint4(0, 0, 0, 0);
+        for (int k = lo + (hi - lo) / 8 * 8 + tid; k < hi; k += TC_RESET_THREADS) row[k] = 0;
     }
     __syncthreads();
     constexpr int AHEAD = 8;
-    for (int i0 = 0; i0 < n; i0 += AHEAD * TC_THREADS) {
+    for (int i0 = 0; i0 < n; i0 += AHEAD * TC_RESET_THREADS) {
         int token[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int i = i0 + u * TC_THREADS + tid;
+            const int i = i0 + u * TC_RESET_THREADS + tid;
             token[u] = i < n ? first[i] : -1;
         }
 #pragma unroll
@@ -119,7 +123,7 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
             if (token[u] < -1 || token[u] >= p.vocab) bad |= SV_DEV_BAD_TOKEN;
             const bool mine = token[u] >= lo && token[u] < hi;
             if (marking) {
-                if (mine) atomicOr(&marks[(token[u] - lo) >> 5], 1u << ((token[u] - lo) & 31));
+                if (mine) marks[token[u] - lo] = 0x80;      // whoever else marks it stores the same
             } else {
                 tc_add_warp(row, token[u], mine, p.prompt != 0, tid & 31);
             }
@@ -127,15 +131,14 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
     }
     if (marking) {
         __syncthreads();
-        for (int k = lo + 8 * tid; k < hi; k += 8 * TC_THREADS) {
-            const unsigned int bits = marks[(k - lo) >> 5] >> ((k - lo) & 31);
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = ((bits >> (2 * i)) & 1u) << 15 | ((bits >> (2 * i + 1)) & 1u) << 31;
+        for (int k = lo + 8 * tid; k < hi; k += 8 * TC_RESET_THREADS) {
+            const uint2 m = *reinterpret_cast<const uint2 *>(marks + k - lo);
+            // a mark's byte becomes the upper one of its 16-bit entry
+            const uint32_t w[4] = {__byte_perm(m.x, 0, 0x1404), __byte_perm(m.x, 0, 0x3424), __byte_perm(m.y, 0, 0x1404), __byte_perm(m.y, 0, 0x3424)};
             if (k + 8 <= hi) {
                 *reinterpret_cast<uint4 *>(row + k) = make_uint4(w[0], w[1], w[2], w[3]);
             } else {
-                for (int i = 0; k + i < hi; ++i) row[k + i] = (int16_t)((bits >> i) & 1u ? 0x8000u : 0u);
+                for (int i = 0; k + i < hi; ++i) row[k + i] = (int16_t)(marks[k - lo + i] << 8);
             }
         }
     }
@@ -163,6 +166,6 @@ extern "C" sv_status spec_token_counts_update(const sv_token_counts_params *p, v
     const long long items = (long long)p->batch * a.parts;
     const long long blocks = p->reset != nullptr ? items : (items + TC_THREADS / 32 - 1) / (TC_THREADS / 32);
     if (blocks > 0x7fffffffLL) return SV_EUNSUPPORTED;
-    return p->reset != nullptr ? launch_kernel(true, token_counts_reset_kernel, dim3((unsigned)blocks), TC_THREADS, 0, s, a)
+    return p->reset != nullptr ? launch_kernel(true, token_counts_reset_kernel, dim3((unsigned)blocks), TC_RESET_THREADS, p->prompt != 0 ? TC_SLICE : 0, s, a)
                                : launch_kernel(true, token_counts_kernel, dim3((unsigned)blocks), TC_THREADS, 0, s, a);
 }
