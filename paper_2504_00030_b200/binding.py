@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -192,13 +193,13 @@ def load():
         lib.spec_draft_step_workspace_bytes.restype = C.c_size_t
         lib.spec_draft_step_workspace_bytes.argtypes = [C.c_int32] * 2
         lib.spec_kv_pages_update.restype = C.c_int32
-        lib.spec_kv_pages_update.argtypes = [C.POINTER(KvPagesParams), C.c_void_p]
+        lib.spec_kv_pages_update.argtypes = [C.c_void_p, C.c_void_p]      # KvPagesParams, or its bytes
         lib.spec_rope_append.restype = C.c_int32
-        lib.spec_rope_append.argtypes = [C.POINTER(RopeAppendParams), C.c_void_p]
+        lib.spec_rope_append.argtypes = [C.c_void_p, C.c_void_p]      # RopeAppendParams, or its bytes
         lib.spec_logits_adjust.restype = C.c_int32
-        lib.spec_logits_adjust.argtypes = [C.POINTER(LogitsAdjustParams), C.c_void_p]
+        lib.spec_logits_adjust.argtypes = [C.c_void_p, C.c_void_p]      # LogitsAdjustParams, or its bytes
         lib.spec_token_counts_update.restype = C.c_int32
-        lib.spec_token_counts_update.argtypes = [C.POINTER(TokenCountsParams), C.c_void_p]
+        lib.spec_token_counts_update.argtypes = [C.c_void_p, C.c_void_p]      # TokenCountsParams, or its bytes
         lib.spec_draft_step.restype = C.c_int32
         lib.spec_draft_step.argtypes = [C.POINTER(DraftStepParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_verify_step_host.restype = C.c_int32
@@ -267,14 +268,32 @@ def _launch_at(stream, first, name):
     return index, stream.cuda_stream
 
 
-def _on(t, dtype, name, index):
-    """Device pointer of a contiguous tensor of `dtype` on CUDA device `index`; None stays None."""
+def _on(t, dtype, name, index, n=-1):
+    """Device pointer of a contiguous tensor of `dtype` (and `n` entries) on CUDA device `index`; 0 for None."""
     if t is None:
-        return None
-    if t.get_device() != index or t.dtype != dtype or not t.is_contiguous():
-        _dev(t, dtype, name)
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
-    return t.data_ptr()
+        return 0
+    if t.get_device() == index and t.dtype is dtype and t.is_contiguous() and (n < 0 or t.numel() == n):
+        return t.data_ptr()
+    _dev(t, dtype, name)
+    if n >= 0 and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+    raise ValueError(f"{name} is on {t.device}, the current device is cuda:{index}")
+
+
+def _rows_on(t, dtype, name, index):
+    """Device pointer, row stride and shape of a 2-D tensor on the device `index` with contiguous rows."""
+    if t.get_device() == index and t.dtype is dtype and t.dim() == 2:
+        rows, cols = t.shape
+        s0, s1 = t.stride()
+        if s1 == 1 or cols <= 1:
+            return t.data_ptr(), s0 if rows > 1 else max(cols, s0), rows, cols
+    raise ValueError(f"{name} must be a 2-D tensor of {dtype} with contiguous rows on the current device (cuda:{index})")
+
+
+def _packer(cls):
+    """Packs field values as the C struct of a ctypes Structure has them: a third of the time that its constructor takes."""
+    codes = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
+    return struct.Struct("@" + "".join(codes[ty] for _, ty in cls._fields_)).pack
 
 
 def _nbytes(t) -> int:
@@ -393,25 +412,25 @@ def spec_kv_append(k_new, v_new, pool, block_table, seq_len, gamma, cu_q, gamma_
 
 
 # --------------------------------------------------------------------------- block tables and slot maps
-def kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
-                    slot_map=None, positions=None, device_status=None, index=None) -> KvPagesParams:
-    index = torch.cuda.current_device() if index is None else index
-    batch, n_rows, i32 = seq_len.numel(), 0, torch.int32
-    if block_table.dim() != 2 or block_table.shape[0] != batch or n_held.numel() != batch:
-        raise ValueError("block_table and n_held must have one row per sequence")
-    if (gamma is not None and gamma.numel() != batch) or (cu_q is not None and cu_q.numel() != batch + 1):
-        raise ValueError("gamma must have one entry per sequence, cu_q one more")
-    if slot_map is not None or positions is not None:
-        n_rows = (slot_map if slot_map is not None else positions).numel()
-        if positions is not None and positions.numel() != n_rows:
-            raise ValueError("slot_map and positions must have the same number of rows")
-    if n_free.numel() != 1:
-        raise ValueError("n_free must be one word")
-    return KvPagesParams(_on(seq_len, i32, "seq_len", index), batch, _on(block_table, i32, "block_table", index),
-                         block_table.shape[1], _on(n_held, i32, "n_held", index), _on(free_list, i32, "free_list", index),
-                         _on(n_free, i32, "n_free", index), free_list.numel(), 16, _on(gamma, i32, "gamma", index),
-                         _on(cu_q, i32, "cu_q", index), gamma_max, _on(slot_map, torch.int64, "slot_map", index),
-                         _on(positions, i32, "positions", index), n_rows, _on(device_status, i32, "device_status", index))
+def _kv_pages_args(index, seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
+                   slot_map=None, positions=None, device_status=None):
+    i32, batch = torch.int32, seq_len.numel()
+    if block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise ValueError("block_table must have one row per sequence")
+    n_rows = slot_map.numel() if slot_map is not None else positions.numel() if positions is not None else 0
+    return (_on(seq_len, i32, "seq_len", index), batch, _on(block_table, i32, "block_table", index), block_table.shape[1],
+            _on(n_held, i32, "n_held", index, batch), _on(free_list, i32, "free_list", index),
+            _on(n_free, i32, "n_free", index, 1), free_list.numel(), 16, _on(gamma, i32, "gamma", index, batch),
+            _on(cu_q, i32, "cu_q", index, batch + 1), gamma_max, _on(slot_map, torch.int64, "slot_map", index),
+            _on(positions, i32, "positions", index, n_rows), n_rows, _on(device_status, i32, "device_status", index))
+
+
+def kv_pages_params(*args, **kwargs) -> KvPagesParams:
+    """Arguments of spec_kv_pages_update (without stream)."""
+    return KvPagesParams(*_kv_pages_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_kv_pages = _packer(KvPagesParams)
 
 
 def spec_kv_pages_update(seq_len, block_table, n_held, free_list, n_free, gamma=None, cu_q=None, gamma_max=0,
@@ -419,9 +438,9 @@ def spec_kv_pages_update(seq_len, block_table, n_held, free_list, n_free, gamma=
     """Block table, held pages and free stack brought to the lengths of the coming step, and the cache slot and
     position of each of its rows (asynchronous)."""
     index, raw = _launch_at(stream, seq_len, "seq_len")
-    p = kv_pages_params(seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, gamma_max, slot_map,
-                        positions, device_status, index)
-    _check("spec_kv_pages_update", load().spec_kv_pages_update(C.byref(p), raw))
+    p = _pack_kv_pages(*_kv_pages_args(index, seq_len, block_table, n_held, free_list, n_free, gamma, cu_q, gamma_max,
+                                       slot_map, positions, device_status))
+    _check("spec_kv_pages_update", load().spec_kv_pages_update(p, raw))
 
 
 # --------------------------------------------------------------------------- norm, rotation and append in one pass
@@ -429,7 +448,7 @@ def _head_rows(t, heads, head_dim, n_rows, name, index):
     """Device pointer and row stride of [n_rows, heads, head_dim] bf16 heads; the rows may be strided."""
     if t.get_device() != index or t.dtype != torch.bfloat16:
         raise ValueError(f"{name} must be a bf16 tensor on the current device (cuda:{index})")
-    if t.dim() != 3 or t.shape != (n_rows, heads, head_dim):
+    if t.shape != (n_rows, heads, head_dim):
         raise ValueError(f"{name} must be [{n_rows}, {heads}, {head_dim}], got {tuple(t.shape)}")
     s0, s1, s2 = t.stride()
     if s2 != 1 or (s1 != head_dim and heads > 1):
@@ -437,10 +456,8 @@ def _head_rows(t, heads, head_dim, n_rows, name, index):
     return t.data_ptr(), s0 if n_rows > 1 else heads * head_dim
 
 
-def rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight=None, k_weight=None,
-                       eps=1e-6, interleaved=False, freq_axis=None, rope_scale=1.0, device_status=None,
-                       index=None) -> RopeAppendParams:
-    index = torch.cuda.current_device() if index is None else index
+def _rope_append_args(index, q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight=None, k_weight=None,
+                      eps=1e-6, interleaved=False, freq_axis=None, rope_scale=1.0, device_status=None):
     if q.dim() != 3:
         raise ValueError("q must be [n_rows, hq, head_dim]")
     n_rows, hq, head_dim = q.shape
@@ -449,25 +466,26 @@ def rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_fr
     qp, qs = _head_rows(q, hq, head_dim, n_rows, "q", index)
     kp, ks = _head_rows(k_new, pool.hkv, head_dim, n_rows, "k_new", index)
     vp, vs = _head_rows(v_new, pool.hkv, head_dim, n_rows, "v_new", index)
-    if q_out.shape != q.shape or slot_map.numel() != n_rows:
-        raise ValueError("q_out must have q's shape, slot_map one entry per row")
+    if q_out.shape != q.shape:
+        raise ValueError("q_out must have q's shape")
     axes = positions.shape[0] if positions.dim() == 2 else 1
-    if positions.numel() != axes * n_rows:
-        raise ValueError("positions must be [n_rows] or [n_axes, n_rows]")
-    rot = 2 * inv_freq.numel() if inv_freq is not None else 0
-    if freq_axis is not None and 2 * freq_axis.numel() != rot:
-        raise ValueError("freq_axis must have one entry per frequency")
+    nf = inv_freq.numel() if inv_freq is not None else 0
     w = q_weight if q_weight is not None else k_weight
-    wt = w.dtype if w is not None and w.dtype == torch.float32 else torch.bfloat16      # float32 or bf16 weights
-    for x in (q_weight, k_weight):
-        if x is not None and x.numel() != head_dim:
-            raise ValueError("norm weights must have head_dim entries")
-    return RopeAppendParams(qp, qs, kp, ks, vp, vs, _on(q_out, torch.bfloat16, "q_out", index), pool.handle, hq, n_rows,
-                            _on(slot_map, torch.int64, "slot_map", index), _on(positions, torch.int32, "positions", index),
-                            axes, _on(freq_axis, torch.uint8, "freq_axis", index),
-                            _on(inv_freq, torch.float64, "inv_freq", index), rot, 1 if interleaved else 0, rope_scale,
-                            _on(q_weight, wt, "q_weight", index), _on(k_weight, wt, "k_weight", index),
-                            1 if wt == torch.float32 else 0, eps, _on(device_status, torch.int32, "device_status", index))
+    wt = torch.float32 if w is not None and w.dtype == torch.float32 else torch.bfloat16      # float32 or bf16 weights
+    return (qp, qs, kp, ks, vp, vs, _on(q_out, torch.bfloat16, "q_out", index), pool.handle.value, hq, n_rows,
+            _on(slot_map, torch.int64, "slot_map", index, n_rows), _on(positions, torch.int32, "positions", index, axes * n_rows),
+            axes, _on(freq_axis, torch.uint8, "freq_axis", index, nf), _on(inv_freq, torch.float64, "inv_freq", index), 2 * nf,
+            1 if interleaved else 0, rope_scale, _on(q_weight, wt, "q_weight", index, head_dim),
+            _on(k_weight, wt, "k_weight", index, head_dim), 1 if wt == torch.float32 else 0, eps,
+            _on(device_status, torch.int32, "device_status", index))
+
+
+def rope_append_params(*args, **kwargs) -> RopeAppendParams:
+    """Arguments of spec_rope_append (without stream)."""
+    return RopeAppendParams(*_rope_append_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_rope_append = _packer(RopeAppendParams)
 
 
 def spec_rope_append(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight=None, k_weight=None,
@@ -475,68 +493,58 @@ def spec_rope_append(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq
     """Per-head norm of queries and keys, position rotation, and keys and values written into the paged cache by slot
     (asynchronous).  q, k_new and v_new may be views of one projection's output."""
     index, raw = _launch_at(stream, q, "q")
-    p = rope_append_params(q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight, k_weight, eps,
-                           interleaved, freq_axis, rope_scale, device_status, index)
-    _check("spec_rope_append", load().spec_rope_append(C.byref(p), raw))
+    p = _pack_rope_append(*_rope_append_args(index, q, k_new, v_new, q_out, pool, positions, slot_map, inv_freq, q_weight,
+                                             k_weight, eps, interleaved, freq_axis, rope_scale, device_status))
+    _check("spec_rope_append", load().spec_rope_append(p, raw))
 
 
 # --------------------------------------------------------------------------- penalties, biases and grammar masks
-def _rows_on(t, dtype, name, index):
-    """Device pointer and row stride of a 2-D tensor on the device `index` with contiguous rows."""
-    if t.get_device() != index or t.dtype != dtype or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"{name} must be a 2-D tensor of {dtype} with contiguous rows on the current device (cuda:{index})")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-
-
-def _entries(t, n, name):
-    if t is not None and t.numel() != n:
-        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
-
-
-def logits_adjust_params(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=None, token_counts=None, repetition=None,
-                         frequency=None, presence=None, bias_tokens=None, bias_values=None, n_bias=None, mask=None,
-                         n_drafted=None, active=None, device_status=None, index=None) -> LogitsAdjustParams:
-    index = torch.cuda.current_device() if index is None else index
+def _logits_adjust_args(index, logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=None, token_counts=None, repetition=None,
+                        frequency=None, presence=None, bias_tokens=None, bias_values=None, n_bias=None, mask=None,
+                        n_drafted=None, active=None, device_status=None):
     i32, f32 = torch.int32, torch.float32
-    ldt = torch.bfloat16 if logits.dtype == torch.bfloat16 else f32               # float32 or bf16 logits
-    lp, ls = _rows_on(logits, ldt, "logits", index)
-    op, os_ = (lp, ls) if out is logits else _rows_on(out, ldt, "out", index)
-    n_rows, vocab = logits.shape
-    if out.shape != logits.shape:
-        raise ValueError("out must have the shape of logits")
+    bf16 = logits.dtype == torch.bfloat16                                         # float32 or bf16 logits
+    ldt = torch.bfloat16 if bf16 else f32
+    lp, ls, n_rows, vocab = _rows_on(logits, ldt, "logits", index)
+    op, os_ = lp, ls
+    if out is not logits:
+        op, os_, o_rows, o_cols = _rows_on(out, ldt, "out", index)
+        if o_rows != n_rows or o_cols != vocab:
+            raise ValueError("out must have the shape of logits")
     batch = (n_drafted if n_drafted is not None else gamma).numel()
-    for x, name in ((gamma, "gamma"), (active, "active"), (repetition, "repetition"), (frequency, "frequency"),
-                    (presence, "presence"), (n_bias, "n_bias")):
-        if x is not None and x.numel() != batch:
-            raise ValueError(f"{name} must have one entry per sequence")
-    for x, name in ((cu_q, "cu_q"), (cu_d, "cu_d")):
-        _entries(x, batch + 1, name)
     if n_drafted is not None and n_rows != batch:
         raise ValueError("draft rows: one row of logits per sequence")
-    cp, cs = None, 0
+    cp = cs = mp = ms = width = n_d_rows = 0
     if token_counts is not None:
-        cp, cs = _rows_on(token_counts, torch.int16, "token_counts", index)
-        if token_counts.shape[0] != batch or token_counts.shape[1] < vocab:
+        cp, cs, c_rows, c_cols = _rows_on(token_counts, torch.int16, "token_counts", index)
+        if c_rows != batch or c_cols < vocab:
             raise ValueError("token_counts must have a row of at least vocab entries per sequence")
-    width = 0
     if bias_tokens is not None:
         width = bias_tokens.shape[-1]
-        if bias_tokens.shape != (batch, width) or bias_values is None or bias_values.shape != bias_tokens.shape:
+        if bias_tokens.dim() != 2 or bias_values is None or bias_values.shape != bias_tokens.shape:
             raise ValueError("bias_tokens and bias_values must be [batch, entries]")
-    mp, ms = None, 0
     if mask is not None:
-        mp, ms = _rows_on(mask, i32, "mask", index)
-        if mask.shape[0] != n_rows or 32 * mask.shape[1] < vocab:
+        mp, ms, m_rows, m_cols = _rows_on(mask, i32, "mask", index)
+        if m_rows != n_rows or 32 * m_cols < vocab:
             raise ValueError("mask must have a row of at least vocab bits per row of logits")
-    return LogitsAdjustParams(lp, op, ls, os_, n_rows, vocab, 0 if ldt == f32 else 1, batch, gamma_max,
-                              _on(gamma, i32, "gamma", index), _on(cu_q, i32, "cu_q", index), _on(cu_d, i32, "cu_d", index),
-                              _on(n_drafted, i32, "n_drafted", index), _on(active, i32, "active", index),
-                              _on(draft_tokens, i32, "draft_tokens", index),
-                              draft_tokens.numel() if draft_tokens is not None else 0, cp, cs,
-                              _on(repetition, f32, "repetition", index), _on(frequency, f32, "frequency", index),
-                              _on(presence, f32, "presence", index), _on(bias_tokens, i32, "bias_tokens", index),
-                              _on(bias_values, f32, "bias_values", index), _on(n_bias, i32, "n_bias", index), width, mp, ms,
-                              _on(device_status, i32, "device_status", index))
+    if draft_tokens is not None:
+        n_d_rows = draft_tokens.numel()
+    return (lp, op, ls, os_, n_rows, vocab, 1 if bf16 else 0, batch, gamma_max, _on(gamma, i32, "gamma", index, batch),
+            _on(cu_q, i32, "cu_q", index, batch + 1), _on(cu_d, i32, "cu_d", index, batch + 1),
+            _on(n_drafted, i32, "n_drafted", index), _on(active, i32, "active", index, batch),
+            _on(draft_tokens, i32, "draft_tokens", index), n_d_rows, cp, cs, _on(repetition, f32, "repetition", index, batch),
+            _on(frequency, f32, "frequency", index, batch), _on(presence, f32, "presence", index, batch),
+            _on(bias_tokens, i32, "bias_tokens", index, batch * width),
+            _on(bias_values, f32, "bias_values", index), _on(n_bias, i32, "n_bias", index, batch), width, mp, ms,
+            _on(device_status, i32, "device_status", index))
+
+
+def logits_adjust_params(*args, **kwargs) -> LogitsAdjustParams:
+    """Arguments of spec_logits_adjust (without stream)."""
+    return LogitsAdjustParams(*_logits_adjust_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_logits_adjust = _packer(LogitsAdjustParams)
 
 
 def spec_logits_adjust(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=None, token_counts=None, repetition=None,
@@ -545,35 +553,38 @@ def spec_logits_adjust(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens=N
     """Penalties, biases and grammar masks on the target rows of every block, or, with n_drafted, on one draft row per
     sequence (asynchronous).  out may be logits itself.  mask: int32 [n_rows, words], a set bit allows its token."""
     index, raw = _launch_at(stream, logits, "logits")
-    p = logits_adjust_params(logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens, token_counts, repetition, frequency,
-                             presence, bias_tokens, bias_values, n_bias, mask, n_drafted, active, device_status, index)
-    _check("spec_logits_adjust", load().spec_logits_adjust(C.byref(p), raw))
+    p = _pack_logits_adjust(*_logits_adjust_args(index, logits, out, gamma, cu_q, cu_d, gamma_max, draft_tokens, token_counts,
+                                                 repetition, frequency, presence, bias_tokens, bias_values, n_bias, mask,
+                                                 n_drafted, active, device_status))
+    _check("spec_logits_adjust", load().spec_logits_adjust(p, raw))
 
 
-def token_counts_params(token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
-                        device_status=None, index=None) -> TokenCountsParams:
-    index = torch.cuda.current_device() if index is None else index
+def _token_counts_args(index, token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
+                       device_status=None):
     i32 = torch.int32
-    cp, cs = _rows_on(token_counts, torch.int16, "token_counts", index)
-    batch = token_counts.shape[0]
-    if token_counts.shape[1] < vocab:
+    cp, cs, batch, cols = _rows_on(token_counts, torch.int16, "token_counts", index)
+    if cols < vocab:
         raise ValueError("token_counts must have at least vocab entries per row")
-    tp, ts, n_tokens = None, 0, 0
+    tp = ts = n_tokens = 0
     if tokens is not None:
         if cu_tokens is None:
-            tp, ts = _rows_on(tokens, i32, "tokens", index)
-            if tokens.shape[0] != batch:
-                raise ValueError("tokens must have one row per sequence")
-            max_tokens = tokens.shape[1] if max_tokens is None else max_tokens
-            if max_tokens > tokens.shape[1]:
-                raise ValueError("max_tokens is more than tokens has columns")
+            tp, ts, t_rows, t_cols = _rows_on(tokens, i32, "tokens", index)
+            max_tokens = t_cols if max_tokens is None else max_tokens
+            if t_rows != batch or max_tokens > t_cols:
+                raise ValueError("tokens must have one row per sequence, of at least max_tokens columns")
         else:
             tp, n_tokens = _on(tokens, i32, "tokens", index), tokens.numel()
             max_tokens = n_tokens if max_tokens is None else max_tokens
-    _entries(cu_tokens, batch + 1, "cu_tokens")
-    _entries(reset, batch, "reset")
-    return TokenCountsParams(cp, cs, vocab, batch, tp, ts, _on(cu_tokens, i32, "cu_tokens", index), n_tokens, max_tokens or 0,
-                             _on(reset, i32, "reset", index), 1 if prompt else 0, _on(device_status, i32, "device_status", index))
+    return (cp, cs, vocab, batch, tp, ts, _on(cu_tokens, i32, "cu_tokens", index, batch + 1), n_tokens, max_tokens or 0,
+            _on(reset, i32, "reset", index, batch), 1 if prompt else 0, _on(device_status, i32, "device_status", index))
+
+
+def token_counts_params(*args, **kwargs) -> TokenCountsParams:
+    """Arguments of spec_token_counts_update (without stream)."""
+    return TokenCountsParams(*_token_counts_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_token_counts = _packer(TokenCountsParams)
 
 
 def spec_token_counts_update(token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
@@ -581,8 +592,9 @@ def spec_token_counts_update(token_counts, vocab, tokens=None, cu_tokens=None, m
     """Count generated tokens (or mark prompt tokens) in the int16 state behind the penalties, after clearing the rows
     of newly admitted sequences (asynchronous).  tokens: [batch, columns] padded with -1, or packed with cu_tokens."""
     index, raw = _launch_at(stream, token_counts, "token_counts")
-    p = token_counts_params(token_counts, vocab, tokens, cu_tokens, max_tokens, reset, prompt, device_status, index)
-    _check("spec_token_counts_update", load().spec_token_counts_update(C.byref(p), raw))
+    p = _pack_token_counts(*_token_counts_args(index, token_counts, vocab, tokens, cu_tokens, max_tokens, reset, prompt,
+                                               device_status))
+    _check("spec_token_counts_update", load().spec_token_counts_update(p, raw))
 
 
 # --------------------------------------------------------------------------- accept / resample
