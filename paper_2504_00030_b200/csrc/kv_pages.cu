@@ -122,7 +122,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         const int b = b0 + tid;
         int my_rel = 0, my_req = 0, my_col = -1;
         if (b < batch) {
-            const int len = __ldg(p.seq_len + b), held = __ldcg(p.n_held + b);
+            const int len = __ldcg(p.seq_len + b), held = __ldcg(p.n_held + b);
             const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
             if (len >= 0 && need <= p.block_table_stride && held >= 0 && held <= p.block_table_stride) {
                 my_rel = max(held - need, 0);
@@ -246,9 +246,9 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         if (p.slot_map != nullptr || p.positions != nullptr) {
             // from the other end of the cluster, whose warps have few pages to move
             for (int b = warps - 1 - my_warp; b < batch; b += warps) {
-                const int len = __ldg(p.seq_len + b);
-                int g = __ldg(p.gamma + b);
-                const long long lo = max(__ldg(p.cu_q + b), 0), hi = min((long long)__ldg(p.cu_q + b + 1), (long long)p.n_rows);
+                const int len = __ldcg(p.seq_len + b);
+                int g = __ldcg(p.gamma + b);
+                const long long lo = max(__ldcg(p.cu_q + b), 0), hi = min((long long)__ldcg(p.cu_q + b + 1), (long long)p.n_rows);
                 if (g < 0 || g > p.gamma_max) {
                     bad |= SV_DEV_BAD_GAMMA;
                     g = min(max(g, 0), p.gamma_max);
@@ -276,8 +276,8 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
                 }
             }
             // rows of no sequence
-            const long long first = min((long long)max(__ldg(p.cu_q), 0), (long long)p.n_rows);
-            const long long last = max(__ldg(p.cu_q + batch), 0);
+            const long long first = min((long long)max(__ldcg(p.cu_q), 0), (long long)p.n_rows);
+            const long long last = max(__ldcg(p.cu_q + batch), 0);
             for (long long r = me; r < first; r += threads) {
                 if (p.slot_map != nullptr) p.slot_map[r] = -1;
                 if (p.positions != nullptr) p.positions[r] = -1;

@@ -189,15 +189,15 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
         {
             uint4 w0 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), w1 = w0;      // ones
             if (!WF32 && weight != nullptr) {
-                w0 = __ldg(static_cast<const uint4 *>(weight) + (live ? c0 : 0));
-                w1 = __ldg(static_cast<const uint4 *>(weight) + (live ? c1 : 0));
+                w0 = static_cast<const uint4 *>(weight)[live ? c0 : 0];
+                w1 = static_cast<const uint4 *>(weight)[live ? c1 : 0];
             }
             const uint32_t m0[4] = {w0.x, w0.y, w0.z, w0.w}, m1[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 f32x2 wa = unpack2(m0[i]), wb = unpack2(m1[i]);
                 if (WF32 && weight != nullptr && live) {
-                    const float2 fa = __ldg(static_cast<const float2 *>(weight) + 4 * c0 + i), fb = __ldg(static_cast<const float2 *>(weight) + 4 * c1 + i);
+                    const float2 fa = static_cast<const float2 *>(weight)[4 * c0 + i], fb = static_cast<const float2 *>(weight)[4 * c1 + i];
                     wa = pair(fa.x, fa.y);
                     wb = pair(fb.x, fb.y);
                 }

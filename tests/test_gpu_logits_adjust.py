@@ -397,3 +397,37 @@ def test_on_another_stream_and_replayed_from_a_graph():
         counts = oracle.token_counts_update(counts, c["V"], t, [0, 5, 10], [5] * 3)
         np.testing.assert_array_equal(kw["token_counts"].cpu().numpy(), counts)
         check({**c, "kw": {**c["kw"], "counts": counts}}, out.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("V", [1, 3, 9, 1000, 2053, 9001])
+def test_logits_and_out_that_lie_differently(V, bf16):
+    """Every pair of offsets from a 16-byte boundary: bases and strides of their own for logits and out."""
+    c = make_case(2, V, 4, 12, bf16=bf16, bias=5, mask=True, gamma=[4, 3])
+    n, dt = c["n_rows"], torch.bfloat16 if bf16 else torch.float32
+    args, kw = gpu_args(c)
+    for off_in, off_out, gap_in, gap_out in ((1, 0, 0, 0), (0, 3, 1, 7), (5, 2, 3, 0), (7, 7, 2, 2), (2, 5, 0, 9)):
+        si, so = V + gap_in, V + gap_out
+        x = torch.full((off_in + n * si + 16,), FILL, device=DEV, dtype=dt)[off_in:off_in + n * si].unflatten(0, (n, si))[:, :V]
+        whole = torch.full((off_out + n * so + 16,), FILL, device=DEV, dtype=dt)
+        out = whole[off_out:off_out + n * so].unflatten(0, (n, so))[:, :V]
+        x.copy_(dev(c["x"]))
+        sv.spec_logits_adjust(x, out, *args, **kw)
+        torch.cuda.synchronize()
+        check({**c, "stride": V}, out.float().cpu().numpy().astype(np.float64))
+        out.fill_(FILL)
+        assert bool((whole == FILL).all())              # nothing in front of, between or behind the rows
+        sv.spec_logits_adjust(x, x, *args, **kw)
+        torch.cuda.synchronize()
+        check({**c, "stride": V}, x.float().cpu().numpy().astype(np.float64), True)
+
+
+@pytest.mark.gpu
+def test_a_bias_list_longer_than_a_block_takes_at_a_time():
+    c = make_case(2, 6000, 2, 13, bias=2500)
+    c["kw"]["n_bias"][:] = [2500, 1100]
+    c["kw"]["bias_tokens"][:, 2000:2040] = c["kw"]["bias_tokens"][:, :40]      # named again by a later part
+    got, status = run(c)
+    assert status == 0
+    check(c, got)

@@ -263,3 +263,13 @@ def test_on_another_stream_and_replayed_from_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert check(c, (q_out, kp, vp, 0)) == 0
+
+
+@pytest.mark.gpu
+def test_no_rows_is_nothing():
+    c = make_case(16, 4, 2, 64, 64, 11)
+    pool = sv.spec_kv_pool_register(dev_bf16(c["pool_k"]), dev_bf16(c["pool_v"]))
+    q, k, v = views(dev_bf16(c["qkv"]), c)
+    before = sv.sv_launch_count()
+    sv.spec_rope_append(q[:0], k[:0], v[:0], torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=DEV), pool, dev(c["pos"])[:0], dev(c["slots"])[:0], dev(c["inv"]))
+    assert sv.sv_launch_count() == before
