@@ -21,9 +21,9 @@ constexpr int KP_MAX_BATCH = 8192;     // prefix sums of the whole batch stay in
 constexpr int KP_UNROLL = 8;           // pages a thread has under way
 constexpr int KP_CLUSTER = 8;          // blocks of the cluster (the portable size)
 // Largest batch that one cluster serves alone; above it the pages are moved by the whole GPU and a second launch closes
-// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.5, 512 8.1 / 8.3, 1024 12.8 / 10.0,
-// 4096 37.8 / 21.3; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 6.0 / 7.9,
-// 256 9.0 / 8.5, 1024 23.1 / 13.6.
+// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.5, 512 8.1 / 8.3, 1024 12.8 / 10.7,
+// 4096 37.8 / 22.1; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 6.1 / 7.9,
+// 256 9.1 / 8.5, 1024 23.1 / 12.5.
 constexpr int KP_ONE_CLUSTER = 512;
 constexpr int KP_UNIT = 32 * KP_UNROLL;    // columns of one sequence that a warp moves at a time
 
@@ -79,12 +79,12 @@ struct Pages {
         return __ldcg(p.block_table + (long long)s * p.block_table_stride + col[s] + (at - n_free - rel[s]));
     }
 
-    // body(sequence, first of its changed columns that the unit holds) for each unit of this warp
+    // body(sequence, first of its changed columns that the unit holds) for each unit of this warp, from unit `begin` on
     template <typename F>
-    __device__ __forceinline__ void for_units(int warp, int warps, int lane, F &&body) const
+    __device__ __forceinline__ void for_units(int begin, int warp, int warps, int lane, F &&body) const
     {
         const int total = unit[batch];
-        for (int u = warp; u < total; u += warps) {
+        for (int u = begin + warp; u < total; u += warps) {
             const int s = warp_owner_of(unit, batch, u, lane);
             body(s, (u - unit[s]) * KP_UNIT);
         }
@@ -122,7 +122,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         const int b = b0 + tid;
         int my_rel = 0, my_req = 0, my_col = -1;
         if (b < batch) {
-            const int len = __ldcg(p.seq_len + b), held = __ldcg(p.n_held + b);
+            const int len = p.seq_len[b], held = __ldcg(p.n_held + b);
             const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
             if (len >= 0 && need <= p.block_table_stride && held >= 0 && held <= p.block_table_stride) {
                 my_rel = max(held - need, 0);
@@ -197,12 +197,15 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         served = req[without];
         bad |= SV_DEV_NO_PAGES;
     }
+    // Released entries that land below this index of the stack are not handed out again, so nobody reads them and they become -1
+    // at once.  (One cluster alone leaves all of them for the end, which measured 0.7 us faster for 128 sequences.)
+    const int untouched = PART == KP_WHOLE ? 0 : pg.have - served;
     if (PART != KP_CLOSE) {
         // ---- released pages onto the stack
         if (base_rel > 0) {
-            pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+            pg.for_units(0, my_warp, warps, lane, [&](int s, int first) {
                 const int n = rel[s + 1] - rel[s], at = pg.n_free + rel[s];
-                const int32_t *from = p.block_table + (long long)s * p.block_table_stride + col[s];
+                int32_t *from = p.block_table + (long long)s * p.block_table_stride + col[s];
                 int page[KP_UNROLL];
 #pragma unroll
                 for (int u = 0; u < KP_UNROLL; ++u) {
@@ -215,6 +218,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
                     if (j >= n) continue;
                     if (page[u] < 0 || page[u] >= n_pages) bad |= SV_DEV_BAD_PAGE;
                     if (j < n_pages - at) p.free_list[at + j] = page[u];
+                    if (PART != KP_WHOLE && j < untouched - at) from[j] = -1;
                 }
             });
             // A page that is read as an entry being released costs a binary search; for more than a few a thread, the
@@ -226,7 +230,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         }
         // ---- acquired pages into the table
         if (served > 0) {
-            pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+            pg.for_units(0, my_warp, warps, lane, [&](int s, int first) {
                 const int n = s < without ? req[s + 1] - req[s] : 0, e = req[s];
                 int32_t *to = p.block_table + (long long)s * p.block_table_stride + col[s];
                 int page[KP_UNROLL];
@@ -246,9 +250,9 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         if (p.slot_map != nullptr || p.positions != nullptr) {
             // from the other end of the cluster, whose warps have few pages to move
             for (int b = warps - 1 - my_warp; b < batch; b += warps) {
-                const int len = __ldcg(p.seq_len + b);
-                int g = __ldcg(p.gamma + b);
-                const long long lo = max(__ldcg(p.cu_q + b), 0), hi = min((long long)__ldcg(p.cu_q + b + 1), (long long)p.n_rows);
+                const int len = p.seq_len[b];
+                int g = p.gamma[b];
+                const long long lo = max(p.cu_q[b], 0), hi = min((long long)p.cu_q[b + 1], (long long)p.n_rows);
                 if (g < 0 || g > p.gamma_max) {
                     bad |= SV_DEV_BAD_GAMMA;
                     g = min(max(g, 0), p.gamma_max);
@@ -276,8 +280,8 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
                 }
             }
             // rows of no sequence
-            const long long first = min((long long)max(__ldcg(p.cu_q), 0), (long long)p.n_rows);
-            const long long last = max(__ldcg(p.cu_q + batch), 0);
+            const long long first = min((long long)max(p.cu_q[0], 0), (long long)p.n_rows);
+            const long long last = max(p.cu_q[batch], 0);
             for (long long r = me; r < first; r += threads) {
                 if (p.slot_map != nullptr) p.slot_map[r] = -1;
                 if (p.positions != nullptr) p.positions[r] = -1;
@@ -292,11 +296,13 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
     if (PART == KP_MOVE) return;
     // ---- nobody reads the old state any more
     cluster_sync();
-    if (base_rel > 0) {
-        pg.for_units(my_warp, warps, lane, [&](int s, int first) {
+    if (untouched - pg.n_free < base_rel) {            // released entries that acquisitions may have read
+        const int from = max(untouched - pg.n_free, 0);
+        pg.for_units(PART == KP_WHOLE ? 0 : unit[owner_of(rel, batch, a.search, from)], my_warp, warps, lane, [&](int s, int first) {
             const int n = min(rel[s + 1] - rel[s] - first, KP_UNIT);
             int32_t *entry = p.block_table + (long long)s * p.block_table_stride + col[s] + first;
-            for (int j = lane; j < n; j += 32) entry[j] = -1;
+            for (int j = lane; j < n; j += 32)
+                if (rel[s] + first + j >= from) entry[j] = -1;
         });
     }
     for (int b = me; b < batch; b += threads) {
