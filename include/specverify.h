@@ -104,8 +104,8 @@ sv_status spec_kv_pool_release(sv_kv_pool_t pool);
  *       z_a = scale * (y_a cos t - y_b sin t) ;  z_b = scale * (y_b cos t + y_a sin t)
  *   z_d = y_d for d >= rot_dim
  * Queries go to q_out, keys to slot slot_map[r] % 16 of page slot_map[r] / 16 of the pool, values
- * there unchanged.  Rows with a negative slot (padding, as spec_kv_pages_update marks it) are
- * neither read nor written.  A row is any position: draft blocks, single tokens, prompts.
+ * there unchanged.  Rows with a negative slot (padding, as spec_kv_pages_update marks it) write
+ * nothing: their part of q_out stays as it is.  A row is any position: draft blocks, single tokens, prompts.
  * bf16 inputs, float32 arithmetic, one rounding to bf16 at the end; the angle is formed and
  * reduced in float64, so that it keeps its digits at far positions.
  * Slots of different rows must differ.  q_out may be q itself where q's rows are contiguous; it

@@ -8,12 +8,13 @@
 // that a rotated pair never leaves its lane: the norm's sum alone crosses lanes (two or three shuffles).
 //
 // One warp takes one row, or a part of its heads when there are few rows; its heads arrive through a ring of asynchronous
-// copies in shared memory, RA_STAGES - 1 KB ahead, while the angles are formed and earlier heads are finished.  Measured
+// copies in shared memory, up to RA_STAGES - 1 KB ahead, while the angles are formed and earlier heads are finished.  Measured
 // for 16381 rows of 32 + 8 + 8 heads of 128 dims (402 MB, 62 us at the copy rate): 157 us with a block per row and the
-// angles shared through its barrier, 81 us with loads held in registers two rounds ahead, 66 us (6.1 TB/s) with the ring.  Half
-// of that step is instructions: scalar float32 arithmetic took 64 million warp instructions (72 % of the issue
-// slots), the packed form below 42 million.  Warps that loop over rows and fetch the next row's slot early run in step with
-// one another and reach 5.2 TB/s only.
+// angles shared through its barrier, 81 us with loads held in registers two rounds ahead, 66 us with the ring, 64.5 us (6.2 TB/s)
+// with the first copies under way before the row's slot is known.  Half of that way is instructions: scalar float32 arithmetic
+// took 64 million warp instructions (72 % of the issue slots), the packed form below 42 million.  Warps that loop over rows
+// and fetch the next row's slot early run in step with one another and reach 5.2 TB/s only.  Rows of few heads are bound by what
+// a row costs before its first head (angles, factors): 16381 rows of 8 + 1 + 1 heads 28 us (13 at the copy rate).
 #include "attn_common.cuh"
 #include "common.cuh"
 
@@ -31,7 +32,9 @@ struct RopeAppendLaunch {
     uint4 *k_pool;
     uint4 *v_pool;
     long long n_slots;
-    long long stride_page, stride_head, stride_slot;   // in 16-byte chunks
+    long long stride_page, stride_head, stride_slot;   // in 16-byte chunks, as the rows' strides
+    long long q_stride, k_stride, v_stride;
+    int q_chunks;                          // of a row of q_out
     int hkv, lanes;                        // lanes that hold a head (head_dim / 16)
     int q_rounds, k_rounds;                // rounds of a row's queries; of its keys, and of its values
     int rounds, segments;                  // rounds of a warp; warps that share a row
@@ -83,13 +86,15 @@ __device__ __forceinline__ uint32_t pack2(f32x2 v)                   // the one 
 }
 
 // Fraction of a turn that one position step adds at a frequency, in units of 2^-64.  pos * step in 64-bit integers then
-// drops whole turns exactly, at any 32-bit position: the angle of a far position keeps its digits, and float64
-// arithmetic is needed once per frequency and warp only.
+// drops whole turns exactly, at any 32-bit position: the angle of a far position keeps its digits, and one product is
+// all that is left to float64 arithmetic.
 __device__ __forceinline__ unsigned long long turn_step(double inv_freq)
 {
-    double t = inv_freq * 0.15915494309189535;                       // turns per position
-    t -= floor(t);
-    return __double2ull_rz(t * 18446744073709551616.0);
+    const long long bits = __double_as_longlong(inv_freq * 0.15915494309189535);        // turns per position
+    const int e = (int)(bits >> 52 & 0x7ff), s = e - 1011;                              // m * 2^(e - 1075) turns
+    const unsigned long long m = (bits & 0xfffffffffffffLL) | (e != 0 ? 1LL << 52 : 0);
+    const unsigned long long x = s >= 64 || s <= -64 ? 0 : s >= 0 ? m << s : m >> -s;
+    return bits < 0 ? 0 - x : x;
 }
 
 struct RopeShared {
@@ -109,10 +114,10 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     RopeShared &sh = *reinterpret_cast<RopeShared *>(ra_smem);
     const sv_rope_append_params &p = a.p;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = lane % GL, slot_h = lane / GL;
-    const long long item = (long long)blockIdx.x * RA_WARPS + warp, row = item / a.segments;
-    if (row >= p.n_rows) return;
+    const unsigned row = blockIdx.x * RA_WARPS + warp;
+    if (row >= (unsigned)p.n_rows) return;
     const int k_first = a.q_rounds, v_first = a.q_rounds + a.k_rounds;         // first rounds of keys and of values
-    const int t_begin = (int)(item - row * a.segments) * a.rounds, t_end = min(t_begin + a.rounds, v_first + a.k_rounds);
+    const int t_begin = blockIdx.y * a.rounds, t_end = min(t_begin + a.rounds, v_first + a.k_rounds);
     // Loads that nothing waits for come first: the slot, and what belongs to frequencies lane and lane + 32.
     const long long slot = p.slot_map[row];
     const bool turning = t_begin < v_first && p.rot_dim > 0;
@@ -126,11 +131,6 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
         const int axis = p.freq_axis != nullptr ? min((int)p.freq_axis[f], p.n_axes - 1) : 0;
         pos[i] = p.positions[axis * p.n_rows + row];
     }
-    if (slot < 0) return;
-    if (slot >= a.n_slots) {
-        if (lane == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
-        return;
-    }
     // This lane's chunks, neighbouring lanes at neighbouring ones.  Where the pairs are (f, f + rot/2), the first rot/16 lanes
     // hold the turned dims; pairs (2f, 2f + 1) lie within a chunk.
     const int pair_lanes = PAIRED ? a.lanes : p.rot_dim / 16;
@@ -139,7 +139,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     const bool turn0 = c0 < p.rot_dim / 8, turn1 = c1 < p.rot_dim / 8;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[warp][0][0][lane]);
     float2 *turns = sh.turns[warp];
-    // ---- producer: the rounds in order, RA_STAGES - 1 of them under way
+    // ---- producer: the rounds in order, RA_STAGES - 1 of them under way (from before the row's slot is known)
     int p_t = t_begin, p_stage = 0;
     auto issue = [&]() {
         if (p_t < t_end) {
@@ -147,7 +147,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
             const int h = (p_t - (q ? 0 : v ? v_first : k_first)) * PER_ROUND + slot_h;
             if (live && h < (q ? p.hq : a.hkv)) {
                 const uint4 *src = static_cast<const uint4 *>(q ? p.q : v ? p.v_new : p.k_new) +
-                                   row * ((q ? p.q_stride : v ? p.v_stride : p.k_stride) / 8) + h * (2 * a.lanes);
+                                   (long long)row * (q ? a.q_stride : v ? a.v_stride : a.k_stride) + h * (2 * a.lanes);
                 cp_chunk(ring + p_stage * 1024, src + c0);
                 cp_chunk(ring + p_stage * 1024 + 512, src + c1);
             }
@@ -158,6 +158,11 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     };
 #pragma unroll
     for (int s = 0; s < RA_STAGES - 1; ++s) issue();
+    if (slot < 0 || slot >= a.n_slots) {
+        if (slot >= 0 && lane == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
+        cp_wait<0>();
+        return;
+    }
     // ---- angles
     if (turning) {
 #pragma unroll
@@ -172,7 +177,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     }
     // ---- consumer
     int stage = 0;
-    const long long cache = (slot / RA_PAGE) * a.stride_page + (slot % RA_PAGE) * a.stride_slot;
+    const long long cache = (long long)((unsigned long long)slot / RA_PAGE) * a.stride_page + (int)(slot & (RA_PAGE - 1)) * a.stride_slot;
     // queries, then keys
     for (int kind = 0; kind < 2; ++kind) {
         const int first_t = kind == 0 ? 0 : k_first, t0 = max(t_begin, first_t), t1 = min(t_end, kind == 0 ? k_first : v_first);
@@ -180,7 +185,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
         const int n_heads = kind == 0 ? p.hq : a.hkv;
         int h = (t0 - first_t) * PER_ROUND + slot_h;
         const long long dst_head = kind == 0 ? 2 * a.lanes : a.stride_head;
-        uint4 *dst = (kind == 0 ? static_cast<uint4 *>(p.q_out) + row * p.hq * (2 * a.lanes) : a.k_pool + cache) + h * dst_head;
+        uint4 *dst = (kind == 0 ? static_cast<uint4 *>(p.q_out) + (long long)row * a.q_chunks : a.k_pool + cache) + h * dst_head;
         const void *weight = kind == 0 ? p.q_weight : p.k_weight;
         // Factors of the row, weight and angle in one: with the pairs (a, b) in the two chunks,
         // z_a = r (x_a (w_a cos) + x_b (-w_b sin)) and z_b = r (x_b (w_b cos) + x_a (w_a sin)); with the pairs in a chunk
@@ -305,12 +310,11 @@ static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
         a.rounds = rounds;
         a.segments = (all + rounds - 1) / rounds;
     }
-    const long long warps = a.p.n_rows * a.segments;
-    const unsigned blocks = (unsigned)((warps + RA_WARPS - 1) / RA_WARPS);
+    const dim3 grid((unsigned)((a.p.n_rows + RA_WARPS - 1) / RA_WARPS), (unsigned)a.segments);
     if (cudaFuncSetAttribute(rope_append_kernel<GL, PAIRED, WF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RopeShared)) !=
         cudaSuccess)
         return SV_ECUDA;
-    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, dim3(blocks), RA_THREADS, sizeof(RopeShared), stream, a);
+    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, grid, RA_THREADS, sizeof(RopeShared), stream, a);
 }
 
 // [a, a + na) and [b, b + nb) share a byte
@@ -357,6 +361,10 @@ extern "C" sv_status spec_rope_append(const sv_rope_append_params *p, void *stre
     a.stride_head = pool.strides[1] / 8;
     a.stride_slot = pool.strides[2] / 8;
     a.hkv = pool.hkv;
+    a.q_stride = p->q_stride / 8;
+    a.k_stride = p->k_stride / 8;
+    a.v_stride = p->v_stride / 8;
+    a.q_chunks = p->hq * (pool.head_dim / 8);
     a.lanes = pool.head_dim / 16;
     a.inv_dim = 1.f / (float)pool.head_dim;
     cudaStream_t s = (cudaStream_t)stream;
