@@ -174,7 +174,7 @@ sv_status spec_rope_append(const sv_rope_append_params *p, void *stream);
  * entry under a row outside [0, n_pages) -> SV_DEV_BAD_PAGE, its slot is -1.
  * block_table, n_held, free_list and n_free are the caller's state; a new pool
  * starts with n_held = 0, table entries -1, free_list = the page ids in any order
- * and *n_free their number.  One launch.
+ * and *n_free their number.  One launch up to 512 sequences, two above; no workspace.
  */
 typedef struct sv_kv_pages_params {
     const int32_t *seq_len;     /* device [batch]: lengths to provide for (draft block included) */
@@ -184,7 +184,7 @@ typedef struct sv_kv_pages_params {
     int32_t *n_held;            /* device in/out [batch]: pages each sequence holds */
     int32_t *free_list;         /* device in/out [n_pages]: the stack; entries at and above *n_free are scratch */
     int32_t *n_free;            /* device in/out, one word */
-    int64_t n_pages;            /* pages of the pool, < 2^31 */
+    int64_t n_pages;            /* pages of the pool, < 2^30 */
     int32_t page_size;          /* 16 */
     const int32_t *gamma;       /* device [batch]; gamma and cu_q may be NULL when slot_map and positions are */
     const int32_t *cu_q;        /* device [batch+1], not decreasing */
@@ -323,8 +323,8 @@ sv_status spec_verify_attn_layers(const sv_attn_layers_params *p, void *workspac
  * read nor written where the mask and the counts show it.  Otherwise the two
  * must not overlap (SV_EINVAL).
  * A bias list that names a token twice: the later entry counts.
- * Device-detected: gamma[b] or n_drafted[b] outside [0, gamma_max] ->
- * SV_DEV_BAD_GAMMA, clamped; a block with rows beyond n_rows -> SV_DEV_BAD_LEN,
+ * Device-detected: gamma[b], or with penalties n_drafted[b], outside [0, gamma_max]
+ * -> SV_DEV_BAD_GAMMA, clamped; a block with rows beyond n_rows -> SV_DEV_BAD_LEN,
  * left as it is; drafts beyond n_d_rows -> SV_DEV_BAD_LEN, not counted; a draft or bias token outside
  * [0, vocab) -> SV_DEV_BAD_TOKEN, ignored.  One launch, no workspace.
  */
@@ -353,8 +353,8 @@ typedef struct sv_logits_adjust_params {
     const int32_t *bias_tokens; /* device [batch, bias_stride], or NULL */
     const float *bias_values;   /* device [batch, bias_stride] */
     const int32_t *n_bias;      /* device [batch]: entries of each list, at most bias_stride (more: clamped, SV_DEV_BAD_LEN) */
-    int32_t bias_stride;
-    const uint32_t *mask;       /* device [n_rows, mask_stride]: bit k % 32 of word k / 32 set = token k allowed; or NULL */
+    int32_t bias_stride;        /* at most 2^30 */
+    const uint32_t *mask;       /* device [n_rows, mask_stride]: bit k % 32 of word k / 32 set = token k allowed; 4-byte aligned, or NULL */
     int64_t mask_stride;        /* words between rows, >= ceil(vocab / 32) */
     uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
 } sv_logits_adjust_params;

@@ -8,9 +8,9 @@
 // Only a call that both releases and acquires many pages has a second one, behind which all are read from the stack.
 //
 // What bounds it is latency: a decoding step moves a few hundred words, an admission a few megabytes.  One
-// thread-block cluster does the whole call in one launch: its barrier is a hardware instruction (a grid-wide one would
-// need a second launch or a spin), every block computes the same prefix sums for itself (a batch's lengths are a
-// few kilobytes in L2), and the pages and rows are dealt out over the cluster's threads.
+// thread-block cluster does the whole call in one launch, up to KP_ONE_CLUSTER sequences: its barrier is a hardware
+// instruction (a grid-wide one would need a second launch or a spin), every block computes the same prefix sums for itself
+// (a batch's lengths are a few kilobytes in L2), and the pages and rows are dealt out over the cluster's threads.
 #include "common.cuh"
 
 namespace sv {
@@ -354,9 +354,10 @@ extern "C" sv_status spec_kv_pages_update(const sv_kv_pages_params *p, void *str
         if (p->gamma == nullptr || p->cu_q == nullptr || p->n_rows == 0) return SV_EINVAL;
     }
     if (p->page_size != KP_PAGE) return SV_EUNSUPPORTED;
-    // pages and rows are counted in 32 bits, with room for a loop's last step
+    // pages and rows are counted in 32 bits, with room for a loop's last step; the top of the stack and what is given back, added
+    // up, as well
     if (p->batch > KP_MAX_BATCH) return SV_EUNSUPPORTED;
-    if (p->n_pages > 0x7fffffffLL || p->n_rows > 0x7fffffffLL || p->block_table_stride > (1LL << 30) / p->batch)
+    if (p->n_pages >= 1LL << 30 || p->n_rows > 0x7fffffffLL || p->block_table_stride > (1LL << 30) / p->batch)
         return SV_EUNSUPPORTED;
     KvPagesLaunch a;
     a.p = *p;

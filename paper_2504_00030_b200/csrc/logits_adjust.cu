@@ -6,8 +6,9 @@
 // masks stream through a ring in shared memory.  HBM bounds it: the logits in and out, a bit of mask per element, and 2 bytes
 // of counts per block of rows.
 //
-// Measured with ADD and masks: 2176 float32 rows of 128256 with 300 biases each 343 us (2.3 GB, 6.7 TB/s), bf16 rows of 128256 (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases
-// too (38 and 39 us at the copy rate): instructions bound the latter.  Steps that led here: rows loaded to registers two ahead
+// Measured: 2176 float32 rows of 128256 with penalties, masks and 300 biases each 343 us (2.3 GB, 6.7 TB/s); bf16 rows of 128256
+// (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases too (38 and 39 us at the copy rate):
+// instructions bound the latter.  Steps that led here: rows loaded to registers two ahead
 // 651 us; the effect of each draft prepared once per block and rows one at a time at a higher occupancy 379 us; the ring 353 us;
 // masks through the ring 343 us.  A correction of the touched elements alone, in the ring, needs fewer instructions where they
 // are few, but the slices that hold most of a history (frequent tokens have neighbouring ids) then keep the others waiting: 4
@@ -514,7 +515,7 @@ extern "C" sv_status spec_logits_adjust(const sv_logits_adjust_params *p, void *
     if (p == nullptr || p->logits == nullptr || p->out == nullptr) return SV_EINVAL;
     if (p->batch <= 0 || p->vocab <= 0 || p->n_rows <= 0 || p->gamma_max < 0) return SV_EINVAL;
     if (p->row_stride < p->vocab || p->out_stride < p->vocab) return SV_EINVAL;
-    if (p->gamma_max > LA_MAX_GAMMA || p->vocab > 1 << 30) return SV_EUNSUPPORTED;
+    if (p->gamma_max > LA_MAX_GAMMA || p->vocab > 1 << 30 || p->bias_stride > 1 << 30) return SV_EUNSUPPORTED;
     if (p->n_drafted == nullptr ? p->gamma == nullptr || p->cu_q == nullptr : p->n_rows < p->batch) return SV_EINVAL;
     const bool penalties = p->repetition != nullptr || p->frequency != nullptr || p->presence != nullptr;
     if (penalties) {

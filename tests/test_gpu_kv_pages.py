@@ -52,7 +52,7 @@ def good_params():
     ("seq_len", None, sv.SV_EINVAL), ("block_table", None, sv.SV_EINVAL), ("n_held", None, sv.SV_EINVAL), ("free_list", None, sv.SV_EINVAL),
     ("n_free", None, sv.SV_EINVAL), ("batch", 0, sv.SV_EINVAL), ("block_table_stride", 0, sv.SV_EINVAL), ("n_pages", 0, sv.SV_EINVAL),
     ("gamma_max", -1, sv.SV_EINVAL), ("n_rows", -1, sv.SV_EINVAL), ("n_rows", 0, sv.SV_EINVAL), ("gamma", None, sv.SV_EINVAL), ("cu_q", None, sv.SV_EINVAL),
-    ("page_size", 32, sv.SV_EUNSUPPORTED), ("n_pages", 1 << 31, sv.SV_EUNSUPPORTED), ("n_rows", 1 << 31, sv.SV_EUNSUPPORTED),
+    ("page_size", 32, sv.SV_EUNSUPPORTED), ("n_pages", 1 << 30, sv.SV_EUNSUPPORTED), ("n_rows", 1 << 31, sv.SV_EUNSUPPORTED),
     ("block_table_stride", 1 << 30, sv.SV_EUNSUPPORTED)])
 def test_refused_before_any_launch(field, value, status):
     p = good_params()

@@ -122,7 +122,7 @@ def good_params():
     ("gamma_max", -1, sv.SV_EINVAL), ("row_stride", 999, sv.SV_EINVAL), ("out_stride", 999, sv.SV_EINVAL), ("gamma", None, sv.SV_EINVAL), ("cu_q", None, sv.SV_EINVAL),
     ("cu_d", None, sv.SV_EINVAL), ("draft_tokens", None, sv.SV_EINVAL), ("token_counts", None, sv.SV_EINVAL), ("count_stride", 992, sv.SV_EINVAL),
     ("n_d_rows", -1, sv.SV_EINVAL), ("bias_tokens", None, sv.SV_EINVAL), ("bias_values", None, sv.SV_EINVAL), ("n_bias", None, sv.SV_EINVAL), ("bias_stride", 0, sv.SV_EINVAL),
-    ("mask_stride", 31, sv.SV_EINVAL), ("gamma_max", 65, sv.SV_EUNSUPPORTED), ("vocab", (1 << 30) + 1, sv.SV_EINVAL), ("token_counts", 4100, sv.SV_EALIGN),
+    ("mask_stride", 31, sv.SV_EINVAL), ("gamma_max", 65, sv.SV_EUNSUPPORTED), ("bias_stride", (1 << 30) + 1, sv.SV_EUNSUPPORTED), ("vocab", (1 << 30) + 1, sv.SV_EINVAL), ("token_counts", 4100, sv.SV_EALIGN),
     ("count_stride", 1004, sv.SV_EALIGN), ("logits", (1 << 20) + 2, sv.SV_EALIGN), ("out", (1 << 20) + 16, sv.SV_EINVAL), ("out", (1 << 20) - 16, sv.SV_EINVAL),
     ("out", (1 << 20) + 4000 * 3 + 3999 // 4 * 4, sv.SV_EINVAL)])
 def test_refused_before_any_launch(field, value, status):
