@@ -5,9 +5,9 @@
 // saturates, so the sum is the same in any order.  An admission writes whole rows: a block takes a slice of the vocabulary,
 // collects the prompt's marks in shared memory (a byte each: no atomics, whose conflicts on frequent tokens cost more) and
 // writes the slice once, cleared and marked together.  Measured for 128 prompts of 4096 to 8192 tokens at a vocabulary of 128256
-// (36 MB, 5.6 us at the copy rate): 11.3 us, of which about 2 are the launch and 3 the prompts, which every slice's block reads
-// for itself (slices of 16384 entries: 15 us).  Marks as bits 11.7 to 12.7 us; slices cleared first and marked in global memory 18
-// to 23 us (scattered two-byte stores).
+// (36 MB, 5.6 us at the copy rate): 9.6 us, of which about 2 are the launch and 2 the prompts, which every slice's block reads
+// for itself (slices of 16384 entries: 11 us; blocks of 256 or 1024 threads: 13 and 12 us; tokens one by one: 9.9 us).  Marks as
+// bits 11.7 to 12.7 us; slices cleared first and marked in global memory 18 to 23 us (scattered two-byte stores).
 #include "common.cuh"
 
 namespace sv {
@@ -90,7 +90,7 @@ token_counts_kernel(const __grid_constant__ TokenCountsLaunch a)
 }
 
 // rows may be cleared: a block per slice of a sequence's vocabulary
-__global__ void __launch_bounds__(TC_RESET_THREADS)
+__global__ void __launch_bounds__(TC_RESET_THREADS, 2048 / TC_RESET_THREADS)      // as many as an SM takes: with more registers 13 us
 token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
 {
     pdl_enter();
@@ -110,23 +110,35 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
         for (int k = lo + (hi - lo) / 8 * 8 + tid; k < hi; k += TC_RESET_THREADS) row[k] = 0;
     }
     __syncthreads();
-    constexpr int AHEAD = 8;
-    for (int i0 = 0; i0 < n; i0 += AHEAD * TC_RESET_THREADS) {
-        int token[AHEAD];
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int i = i0 + u * TC_RESET_THREADS + tid;
-            token[u] = i < n ? first[i] : -1;
+    // of a token: its entry of the slice; at least hi - lo if it is none of them
+    auto entry_of = [&](int token) {
+        const unsigned int at = (unsigned int)token - lo;
+        if (at >= (unsigned int)(hi - lo) && (unsigned int)token + 1 > (unsigned int)p.vocab) bad = SV_DEV_BAD_TOKEN;
+        return at;
+    };
+    if (marking) {
+        // four tokens a load: up to three in front of the first 16-byte boundary and behind the last go one by one
+        auto mark = [&](int token) {
+            const unsigned int at = entry_of(token);
+            if (at < (unsigned int)(hi - lo)) marks[at] = 0x80;        // whoever else marks it stores the same
+        };
+        const int head = min(n, (int)(-(reinterpret_cast<uintptr_t>(first) >> 2) & 3)), vectors = (n - head) / 4;
+        const int4 *four = reinterpret_cast<const int4 *>(first + head);
+#pragma unroll 1                                       // unrolled further it takes registers and time (9.8 to 11 us)
+        for (int i = tid; i < vectors; i += TC_RESET_THREADS) {
+            const int4 t = four[i];
+            mark(t.x);
+            mark(t.y);
+            mark(t.z);
+            mark(t.w);
         }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            if (token[u] < -1 || token[u] >= p.vocab) bad |= SV_DEV_BAD_TOKEN;
-            const bool mine = token[u] >= lo && token[u] < hi;
-            if (marking) {
-                if (mine) marks[token[u] - lo] = 0x80;      // whoever else marks it stores the same
-            } else {
-                tc_add_warp(row, token[u], mine, p.prompt != 0, tid & 31);
-            }
+        const int behind = head + 4 * vectors;
+        if (tid < head) mark(first[tid]);
+        else if (tid - head < n - behind) mark(first[behind + tid - head]);
+    } else {
+        for (int i0 = 0; i0 < n; i0 += TC_RESET_THREADS) {
+            const int token = i0 + tid < n ? first[i0 + tid] : -1;
+            tc_add_warp(row, token, entry_of(token) < (unsigned int)(hi - lo), p.prompt != 0, tid & 31);
         }
     }
     if (marking) {

@@ -357,6 +357,29 @@ def test_counts_saturate_and_neighbours_share_a_word():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prompt", [False, True])
+def test_counts_prompts_of_every_alignment(prompt):
+    """Short prompts from every boundary, with tokens outside the vocabulary at every place of a group of four."""
+    V, top = 40000, 2 ** 31 - 1
+    n = np.asarray([k for k in range(14) for _ in range(3)])
+    cu = np.concatenate([[0], np.cumsum(n)])
+    rng = np.random.default_rng(3)
+    for odd in (0, 1):                                  # without and with what is to be reported
+        flat = rng.integers(0, V, int(cu[-1])).astype(np.int32)
+        flat[rng.random(flat.size) < 0.3] = V - 1
+        flat[rng.random(flat.size) < 0.2] = -1
+        if odd:
+            flat[::5] = rng.choice([-2, V, V + 1, top, -top - 1, 32768 - 65536], flat[::5].size)
+        counts = rng.integers(-32768, 32768, (n.size, V)).astype(np.int16)
+        reset = (np.arange(n.size) % 4 != 0).astype(np.int32)
+        for shift in range(4):
+            d_tokens = torch.zeros(flat.size + 4, dtype=torch.int32, device=DEV)[shift:shift + flat.size]
+            d_tokens.copy_(dev(flat))
+            _, status = counts_both(counts, V, flat, cu[:-1], n, d_tokens, reset=reset, prompt=prompt, cu=cu, most=13)
+            assert status == (4 if odd else 0)
+
+
+@pytest.mark.gpu
 def test_counts_conditions_and_reset_alone():
     V = 100
     counts = np.arange(4 * 104, dtype=np.int16).reshape(4, 104)
