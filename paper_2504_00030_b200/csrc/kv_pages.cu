@@ -15,16 +15,17 @@
 
 namespace sv {
 
-constexpr int KP_THREADS = 1024;       // one scan step covers this many sequences
+constexpr int KP_THREADS = 1024;
 constexpr int KP_PAGE = 16;
 constexpr int KP_MAX_BATCH = 8192;     // prefix sums of the whole batch stay in shared memory (16 bytes a sequence)
 constexpr int KP_UNROLL = 8;           // pages a thread has under way
 constexpr int KP_CLUSTER = 8;          // blocks of the cluster (the portable size)
 // Largest batch that one cluster serves alone; above it the pages are moved by the whole GPU and a second launch closes
-// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.5, 512 8.1 / 8.3, 1024 12.8 / 10.7,
-// 4096 37.8 / 22.1; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 6.1 / 7.9,
-// 256 9.1 / 8.5, 1024 23.1 / 12.5.
+// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.3, 512 8.1 / 8.0, 1024 12.9 / 9.3,
+// 4096 36.6 / 16.7; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 5.9 / 7.5,
+// 256 9.3 / 8.0, 1024 23.5 / 11.1.
 constexpr int KP_ONE_CLUSTER = 512;
+static_assert(KP_ONE_CLUSTER <= KP_THREADS, "one sequence a thread");
 constexpr int KP_UNIT = 32 * KP_UNROLL;    // columns of one sequence that a warp moves at a time
 
 struct KvPagesLaunch {
@@ -99,7 +100,9 @@ template <int PART>
 __global__ void __launch_bounds__(KP_THREADS)
 kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
 {
-    pdl_enter();
+    // The closing launch makes its prefix sums while the first one still moves pages: what they read is not written by it, and
+    // every block of it has waited for the kernels in front of the call before this launch may start.
+    if (PART != KP_CLOSE) pdl_enter();
     extern __shared__ int32_t kp_smem[];
     __shared__ int32_t warp_rel[32], warp_req[32], warp_unit[32];
     const sv_kv_pages_params &p = a.p;
@@ -116,64 +119,79 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         bad |= SV_DEV_BAD_PAGE;
         pg.n_free = min(max(pg.n_free, 0), n_pages);
     }
-    // ---- prefix sums
-    int base_rel = 0, base_req = 0, base_unit = 0;
-    for (int b0 = 0; b0 < batch; b0 += KP_THREADS) {
-        const int b = b0 + tid;
-        int my_rel = 0, my_req = 0, my_col = -1;
-        if (b < batch) {
-            const int len = p.seq_len[b], held = __ldcg(p.n_held + b);
-            const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
-            if (len >= 0 && need <= p.block_table_stride && held >= 0 && held <= p.block_table_stride) {
-                my_rel = max(held - need, 0);
-                my_req = max(need - held, 0);
-                my_col = min(held, need);
-            } else {
-                bad |= SV_DEV_BAD_LEN;
-            }
+    // ---- prefix sums: a thread has `items` neighbouring sequences
+    const int items = PART == KP_WHOLE ? 1 : (batch + KP_THREADS - 1) / KP_THREADS;
+    int my_rel = 0, my_req = 0, my_unit = 0, my_col = -1;
+#pragma unroll 4
+    for (int i = 0; i < items; ++i) {
+        const int b = tid * items + i;
+        if (b >= batch) break;
+        const int len = p.seq_len[b], held = __ldcg(p.n_held + b);
+        const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
+        int n_rel = 0, n_req = 0;
+        my_col = -1;
+        if (len >= 0 && need <= p.block_table_stride && held >= 0 && held <= p.block_table_stride) {
+            n_rel = max(held - need, 0);
+            n_req = max(need - held, 0);
+            my_col = min(held, need);
+        } else {
+            bad |= SV_DEV_BAD_LEN;
         }
-        const int my_unit = (my_rel + my_req + KP_UNIT - 1) / KP_UNIT;       // one of the two is zero
-        int sum_rel = my_rel, sum_req = my_req, sum_unit = my_unit;
+        col[b] = my_col;
+        if (items > 1) {
+            rel[b] = n_rel;
+            req[b] = n_req;
+        }
+        my_rel += n_rel;
+        my_req += n_req;
+        my_unit += (n_rel + n_req + KP_UNIT - 1) / KP_UNIT;     // one of the two is zero
+    }
+    int sum_rel = my_rel, sum_req = my_req, sum_unit = my_unit;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int u0 = __shfl_up_sync(0xffffffffu, sum_rel, d), u1 = __shfl_up_sync(0xffffffffu, sum_req, d),
-                      u2 = __shfl_up_sync(0xffffffffu, sum_unit, d);
-            if (lane >= d) {
-                sum_rel += u0;
-                sum_req += u1;
-                sum_unit += u2;
-            }
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u0 = __shfl_up_sync(0xffffffffu, sum_rel, d), u1 = __shfl_up_sync(0xffffffffu, sum_req, d),
+                  u2 = __shfl_up_sync(0xffffffffu, sum_unit, d);
+        if (lane >= d) {
+            sum_rel += u0;
+            sum_req += u1;
+            sum_unit += u2;
         }
-        if (b0 > 0) __syncthreads();   // the warp totals of the previous step are no longer read
-        if (lane == 31) {
-            warp_rel[warp] = sum_rel;
-            warp_req[warp] = sum_req;
-            warp_unit[warp] = sum_unit;
-        }
-        __syncthreads();
-        int t_rel = warp_rel[lane], t_req = warp_req[lane], t_unit = warp_unit[lane];     // every warp scans the 32 totals
+    }
+    if (lane == 31) {
+        warp_rel[warp] = sum_rel;
+        warp_req[warp] = sum_req;
+        warp_unit[warp] = sum_unit;
+    }
+    __syncthreads();
+    int t_rel = warp_rel[lane], t_req = warp_req[lane], t_unit = warp_unit[lane];     // every warp scans the 32 totals
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int u0 = __shfl_up_sync(0xffffffffu, t_rel, d), u1 = __shfl_up_sync(0xffffffffu, t_req, d),
-                      u2 = __shfl_up_sync(0xffffffffu, t_unit, d);
-            if (lane >= d) {
-                t_rel += u0;
-                t_req += u1;
-                t_unit += u2;
-            }
+    for (int d = 1; d < 32; d <<= 1) {
+        const int u0 = __shfl_up_sync(0xffffffffu, t_rel, d), u1 = __shfl_up_sync(0xffffffffu, t_req, d),
+                  u2 = __shfl_up_sync(0xffffffffu, t_unit, d);
+        if (lane >= d) {
+            t_rel += u0;
+            t_req += u1;
+            t_unit += u2;
         }
-        const int prev = warp > 0 ? warp - 1 : 0;
-        const int before_rel = __shfl_sync(0xffffffffu, t_rel, prev), before_req = __shfl_sync(0xffffffffu, t_req, prev),
-                  before_unit = __shfl_sync(0xffffffffu, t_unit, prev);
-        if (b < batch) {
-            rel[b] = base_rel + (warp > 0 ? before_rel : 0) + sum_rel - my_rel;
-            req[b] = base_req + (warp > 0 ? before_req : 0) + sum_req - my_req;
-            unit[b] = base_unit + (warp > 0 ? before_unit : 0) + sum_unit - my_unit;
-            col[b] = my_col;
-        }
-        base_rel += __shfl_sync(0xffffffffu, t_rel, 31);
-        base_req += __shfl_sync(0xffffffffu, t_req, 31);
-        base_unit += __shfl_sync(0xffffffffu, t_unit, 31);
+    }
+    const int prev = warp > 0 ? warp - 1 : 0;
+    const int before_rel = __shfl_sync(0xffffffffu, t_rel, prev), before_req = __shfl_sync(0xffffffffu, t_req, prev),
+              before_unit = __shfl_sync(0xffffffffu, t_unit, prev);
+    const int base_rel = __shfl_sync(0xffffffffu, t_rel, 31), base_req = __shfl_sync(0xffffffffu, t_req, 31),
+              base_unit = __shfl_sync(0xffffffffu, t_unit, 31);                       // totals of the batch
+    int at_rel = (warp > 0 ? before_rel : 0) + sum_rel - my_rel, at_req = (warp > 0 ? before_req : 0) + sum_req - my_req,
+        at_unit = (warp > 0 ? before_unit : 0) + sum_unit - my_unit;
+#pragma unroll 4
+    for (int i = 0; i < items; ++i) {
+        const int b = tid * items + i;
+        if (b >= batch) break;
+        const int n_rel = items > 1 ? rel[b] : my_rel, n_req = items > 1 ? req[b] : my_req;
+        rel[b] = at_rel;
+        req[b] = at_req;
+        unit[b] = at_unit;
+        at_rel += n_rel;
+        at_req += n_req;
+        at_unit += (n_rel + n_req + KP_UNIT - 1) / KP_UNIT;
     }
     if (tid == 0) {
         rel[batch] = base_rel;
@@ -181,6 +199,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         unit[batch] = base_unit;
     }
     __syncthreads();
+    if (PART == KP_CLOSE) pdl_enter();
     pg.rel = rel;
     pg.req = req;
     pg.unit = unit;
