@@ -23,7 +23,7 @@ namespace sv {
 constexpr int RA_THREADS = 256;
 constexpr int RA_BLOCKS_PER_SM = 2;        // the factors take registers: three blocks spill, 97 us instead of 66
 constexpr int RA_WARPS = RA_THREADS / 32;
-constexpr int RA_STAGES = 6;               // rounds of a warp under way, in shared memory (1 KB each)
+constexpr int RA_STAGES = 5;               // rounds of a warp under way, in shared memory (1 KB each); six measure the same
 constexpr int RA_PAGE = 16;
 constexpr int RA_MAX_FREQ = 64;            // rot_dim <= head_dim <= 128
 
@@ -110,8 +110,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
 {
     pdl_enter();
     constexpr int PER_ROUND = 32 / GL;
-    extern __shared__ __align__(16) uint8_t ra_smem[];
-    RopeShared &sh = *reinterpret_cast<RopeShared *>(ra_smem);
+    __shared__ RopeShared sh;
     const sv_rope_append_params &p = a.p;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = lane % GL, slot_h = lane / GL;
     const unsigned row = blockIdx.x * RA_WARPS + warp;
@@ -311,10 +310,7 @@ static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
         a.segments = (all + rounds - 1) / rounds;
     }
     const dim3 grid((unsigned)((a.p.n_rows + RA_WARPS - 1) / RA_WARPS), (unsigned)a.segments);
-    if (cudaFuncSetAttribute(rope_append_kernel<GL, PAIRED, WF32>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(RopeShared)) !=
-        cudaSuccess)
-        return SV_ECUDA;
-    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, grid, RA_THREADS, sizeof(RopeShared), stream, a);
+    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, grid, RA_THREADS, 0, stream, a);
 }
 
 // [a, a + na) and [b, b + nb) share a byte
