@@ -7,12 +7,14 @@
 // of counts per block of rows.
 //
 // Measured: 2176 float32 rows of 128256 with penalties, masks and 300 biases each 343 us (2.3 GB, 6.7 TB/s); bf16 rows of 128256
-// (64 sequences of 5 to 9) 41 us with penalties, 51 us with masks and 300 biases too (38 and 39 us at the copy rate):
+// (64 sequences of 5 to 9) 41 us with penalties, 50 us with masks and 300 biases too (38 and 39 us at the copy rate):
 // instructions bound the latter.  Steps that led here: rows loaded to registers two ahead
 // 651 us; the effect of each draft prepared once per block and rows one at a time at a higher occupancy 379 us; the ring 353 us;
 // masks through the ring 343 us.  A correction of the touched elements alone, in the ring, needs fewer instructions where they
 // are few, but the slices that hold most of a history (frequent tokens have neighbouring ids) then keep the others waiting: 4
 // sequences at a vocabulary of 32000 took 8.5 us instead of 3.8, the bf16 rows 49 us instead of 41.
+#include <type_traits>
+
 #include "common.cuh"
 #include "row_stream.cuh"
 
@@ -76,17 +78,36 @@ struct Layout {
     static __device__ __forceinline__ int unit(int at) { return at / (32 * N) % LA_UNITS; }
 };
 
-// A unit from byte `at` of a warp's part of the ring; at is a multiple of the element size
+// A thread's units of a row that lies across vectors of shared memory: unit u starts at element s (the same for all lanes) of
+// vector v[32 * u].  Vectors at and behind v_end are not read.  Two 16-byte reads a unit and words picked by a branch: single
+// words, 16 bytes apart from lane to lane, meet in every fourth bank.
 template <bool BF16>
-__device__ __forceinline__ void read_unit(const uint32_t *part, int at, uint32_t (&w)[4])
+__device__ __forceinline__ void read_units(const uint4 *v, const uint4 *v_end, int s, uint32_t (&w)[LA_UNITS][4])
 {
-    const uint32_t *s = part + (at >> 2);
+    uint32_t x[LA_UNITS][8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = s[i];
-    if (BF16 && (at & 2)) {
-        const uint32_t last = s[4];
+    for (int u = 0; u < LA_UNITS; ++u) {
+        const uint4 a = v[32 * u];
+        x[u][0] = a.x; x[u][1] = a.y; x[u][2] = a.z; x[u][3] = a.w;
+        x[u][4] = x[u][5] = x[u][6] = x[u][7] = 0;
+        if (s > 0 && v + 32 * u + 1 < v_end) {
+            const uint4 b = v[32 * u + 1];
+            x[u][4] = b.x; x[u][5] = b.y; x[u][6] = b.z; x[u][7] = b.w;
+        }
+    }
+    auto take = [&](auto first) {                      // words first .. first + 3, half a word further on for odd elements
+        constexpr int F = decltype(first)::value;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], i < 3 ? w[i + 1] : last, 16);
+        for (int u = 0; u < LA_UNITS; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[u][i] = BF16 ? __funnelshift_r(x[u][F + i], x[u][F + i + 1 < 8 ? F + i + 1 : 7], 16 * (s & 1)) : x[u][F + i];
+    };
+    switch (BF16 ? s >> 1 : s) {
+        case 0: return take(std::integral_constant<int, 0>());
+        case 1: return take(std::integral_constant<int, 1>());
+        case 2: return take(std::integral_constant<int, 2>());
+        default: return take(std::integral_constant<int, 3>());
     }
 }
 
@@ -96,7 +117,8 @@ __device__ __forceinline__ void read_unit(const uint32_t *part, int at, uint32_t
 // before the loads.  Elsewhere LA_SHIFT: a row's 16-byte boundaries lie d elements behind the units' (a vocabulary of odd size,
 // say), d differing from row to row: global accesses keep to the boundaries, and a warp moves its units to and from them in
 // shared memory.  (By shuffles and selects instead this took 340 warp instructions per 32 units, and 44 us for bf16 rows of
-// 50257 where this takes 32; by single elements 66.)
+// 50257 where this takes 30.6; by single elements 66; with vectors on the boundaries and what is added to their elements
+// looked up in shared memory 32.7.)
 template <bool BF16, bool ADD, bool MASK, int PATH>
 __global__ void __launch_bounds__(LA_THREADS, ADD ? LA_BLOCKS : PATH == LA_DIRECT ? LA_BLOCKS_DIRECT : LA_BLOCKS_MASK)
 logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
@@ -115,21 +137,24 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
     const int tid = threadIdx.x, lane = tid & 31, V = p.vocab;
     const int slice = blockIdx.x % a.slices, seq_chunk = blockIdx.x / a.slices;
     const int b = seq_chunk / a.chunks, chunk = seq_chunk - b * a.chunks;
-    if (p.active != nullptr && p.active[b] == 0) return;
     uint32_t bad = 0;
     const bool draft = p.n_drafted != nullptr;
+    // what the sequence says, loaded together
+    const int active = p.active != nullptr ? p.active[b] : 1;
+    const long long row0 = draft ? b : p.cu_q[b];
+    const long long first_draft = ADD && a.penalties && p.gamma_max > 0 ? p.cu_d[b] : 0;
     int g = draft ? ADD && a.penalties ? p.n_drafted[b] : 0 : p.gamma[b];
+    if (active == 0) return;
     if (g < 0 || g > p.gamma_max) {
         bad |= SV_DEV_BAD_GAMMA;
         g = min(max(g, 0), p.gamma_max);
     }
     const int rows = draft ? 1 : g + 1, i_begin = chunk * a.rows_per_block, i_end = min(rows, i_begin + a.rows_per_block);
-    const long long row0 = draft ? b : p.cu_q[b];
     // of thread j: draft j of the sequence, whether or not this step has so many
     int my_token = 0;
     bool my_token_there = false;
     if (ADD && a.penalties && tid < p.gamma_max) {     // at most LA_MAX_GAMMA
-        const long long at = (long long)p.cu_d[b] + tid;
+        const long long at = first_draft + tid;
         my_token_there = at >= tid && at < p.n_d_rows;
         if (my_token_there) my_token = p.draft_tokens[at];
     }
@@ -386,8 +411,7 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
                         else *reinterpret_cast<uint32_t *>(to) = reinterpret_cast<const uint32_t *>(src)[e];
                     }
                 }
-#pragma unroll
-                for (int u = 0; u < LA_UNITS; ++u) read_unit<BF16>(reinterpret_cast<const uint32_t *>(slot), 16 + (u * 32 + lane) * 16 - d * ES, w[u]);
+                read_units<BF16>(slot + (d > 0 ? 0 : 1) + lane, slot + LA_PART, d > 0 ? N - d : 0, w);
                 __syncwarp();                          // and are read
                 out_slot = const_cast<uint4 *>(slot) + 1;
             }
@@ -452,12 +476,11 @@ logits_adjust_kernel(const __grid_constant__ LogitsAdjustLaunch a)
 #pragma unroll
             for (int u = 0; u < LA_UNITS; ++u) out_slot[u * 32 + lane] = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
             __syncwarp();
+            read_units<BF16>(out_slot + lane, out_slot + LA_UNITS * 32, d, w);
 #pragma unroll
             for (int u = 0; u < LA_UNITS; ++u) {
                 const int k = first + d + (u * 32 + lane) * N;
-                if (k + N > end) continue;
-                read_unit<BF16>(reinterpret_cast<const uint32_t *>(out_slot), (k - first) * ES, w[u]);
-                *reinterpret_cast<uint4 *>(dst + (long long)k * ES) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
+                if (k + N <= end) *reinterpret_cast<uint4 *>(dst + (long long)k * ES) = make_uint4(w[u][0], w[u][1], w[u][2], w[u][3]);
             }
             // the elements in front of the first boundary, and behind the last vector: fewer than N each
             const int behind = end - first <= d ? end : end - (end - first - d) % N;
