@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(KP_THREADS)
 kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
 {
     // The closing launch makes its prefix sums while the first one still moves pages: what they read is not written by it, and
-    // every block of it has waited for the kernels in front of the call before this launch may start.
+    // every block of it has waited for the kernels in front of the call before this launch may start (whose results are
+    // read from L2: this launch has not waited itself).
     if (PART != KP_CLOSE) pdl_enter();
     extern __shared__ int32_t kp_smem[];
     __shared__ int32_t warp_rel[32], warp_req[32], warp_unit[32];
@@ -126,7 +127,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
     for (int i = 0; i < items; ++i) {
         const int b = tid * items + i;
         if (b >= batch) break;
-        const int len = p.seq_len[b], held = __ldcg(p.n_held + b);
+        const int len = PART == KP_CLOSE ? __ldcg(p.seq_len + b) : p.seq_len[b], held = __ldcg(p.n_held + b);
         const int need = len > 0 ? (len - 1) / KP_PAGE + 1 : 0;
         int n_rel = 0, n_req = 0;
         my_col = -1;

@@ -190,3 +190,50 @@ def test_on_another_stream_and_replayed_from_a_graph():
         np.testing.assert_array_equal(slot.cpu().numpy(), r_slot)
         np.testing.assert_array_equal(pos.cpu().numpy(), r_pos)
         assert int(status.item()) == cond == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("B", [300, 700, 5000])
+def test_behind_the_controller_step_after_step(B, graph):
+    """Lengths that the controller writes directly in front of each call, one step after the other with nothing in between."""
+    rng = np.random.default_rng(B)
+    gmax, steps, stride = 4, 12, 12
+    cfg = sv.GammaConfig(0.5, 2.0, 1, gmax, sv.SV_GT_PROPOSED)
+    g0 = rng.integers(1, gmax + 1, B).astype(np.int32)
+    first = (rng.integers(1, 60, B) + g0 + 1).astype(np.int32)
+    accepted = [rng.integers(0, 2, B).astype(np.int32) for _ in range(steps)]
+    n_pages = B * stride
+    state = new_state(B, stride, n_pages, B)
+    d_state = upload(state)
+    cq, cd = np.concatenate([[0], np.cumsum(g0 + 1)]).astype(np.int32), np.concatenate([[0], np.cumsum(g0)]).astype(np.int32)
+    g, sl, d_cq, d_cd, gbar = dev(g0), dev(first), dev(cq), dev(cd), dev(g0.astype(np.float64))
+    d_acc = [dev(a) for a in accepted]
+    n_rows = B * (gmax + 1)
+    slot, pos = torch.zeros(n_rows, dtype=torch.int64, device=DEV), torch.zeros(n_rows, dtype=torch.int32, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def loop():
+        for a in d_acc:
+            sv.gamma_tune_update(a, gbar, g, sl, d_cq, d_cd, cfg, device_status=status)
+            sv.spec_kv_pages_update(sl, *d_state, g, d_cq, gmax, slot, pos, status)
+
+    torch.cuda.synchronize()
+    if graph:
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured):
+            loop()
+        captured.replay()
+    else:
+        loop()
+    torch.cuda.synchronize()
+    o_g, o_sl, o_gbar = g0, first, g0.astype(np.float64)
+    for a in accepted:
+        o_gbar, o_g, o_sl, o_cq, o_cd = oracle.gamma_tune_update(a, o_gbar, o_g, o_sl, 0.5, 2.0, 1, gmax)
+        *state, r_slot, r_pos, cond = oracle.kv_pages_update(o_sl, *state, n_rows, o_g, o_cq, gmax)
+        assert cond == 0
+    for d, r in zip(d_state, state):
+        np.testing.assert_array_equal(d.cpu().numpy().reshape(-1), np.asarray(r).reshape(-1))
+    np.testing.assert_array_equal(slot.cpu().numpy(), r_slot)
+    np.testing.assert_array_equal(pos.cpu().numpy(), r_pos)
+    assert int(status.item()) == 0
