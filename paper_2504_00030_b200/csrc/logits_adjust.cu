@@ -506,8 +506,8 @@ static sv_status launch_kinds(const LogitsAdjustLaunch &a, bool add, bool mask, 
 {
     if (add && mask) return launch_one<BF16, true, true, PATH>(a, grid, stream);
     if (add) return launch_one<BF16, true, false, PATH>(a, grid, stream);
-    if (mask) return launch_one<BF16, false, true, PATH>(a, grid, stream);
-    return launch_one<BF16, false, false, PATH>(a, grid, stream);
+    if (mask || PATH == LA_DIRECT) return launch_one<BF16, false, true, PATH>(a, grid, stream);
+    return launch_one<BF16, false, PATH == LA_DIRECT, PATH>(a, grid, stream);      // a copy; in place it has returned already
 }
 
 template <bool BF16>
