@@ -260,7 +260,7 @@ def _launch_at(stream, first, name):
     the current device is asked for by index: building a Stream object costs more than the launch.)"""
     if not first.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    index = torch.cuda.current_device()
+    index = torch._C._cuda_getDevice()                         # there is a CUDA tensor, so CUDA has been initialised
     if stream is None:
         return index, torch._C._cuda_getCurrentRawStream(index)
     if stream.device.index != index:
