@@ -174,7 +174,7 @@ sv_status spec_rope_append(const sv_rope_append_params *p, void *stream);
  * entry under a row outside [0, n_pages) -> SV_DEV_BAD_PAGE, its slot is -1.
  * block_table, n_held, free_list and n_free are the caller's state; a new pool
  * starts with n_held = 0, table entries -1, free_list = the page ids in any order
- * and *n_free their number.  One launch up to 512 sequences, two above; no workspace.
+ * and *n_free their number.  One launch up to 384 sequences, two above; no workspace.
  */
 typedef struct sv_kv_pages_params {
     const int32_t *seq_len;     /* device [batch]: lengths to provide for (draft block included) */

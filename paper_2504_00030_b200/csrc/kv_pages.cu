@@ -18,15 +18,13 @@ namespace sv {
 constexpr int KP_THREADS = 1024;
 constexpr int KP_PAGE = 16;
 constexpr int KP_MAX_BATCH = 8192;     // prefix sums of the whole batch stay in shared memory (16 bytes a sequence)
-constexpr int KP_UNROLL = 8;           // pages a thread has under way
 constexpr int KP_CLUSTER = 8;          // blocks of the cluster (the portable size)
 // Largest batch that one cluster serves alone; above it the pages are moved by the whole GPU and a second launch closes
-// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.6 / 7.3, 512 8.1 / 8.0, 1024 12.9 / 9.3,
-// 4096 36.6 / 16.7; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 5.9 / 7.5,
-// 256 9.3 / 8.0, 1024 23.5 / 11.1.
-constexpr int KP_ONE_CLUSTER = 512;
+// the books.  Measured, us a call, one launch / two: 128 sequences that decode 5.2 / 7.1, 384 6.8 / 7.6, 512 7.8 / 7.9,
+// 1024 11.8 / 9.1; half of the batch replaced by other prompts at 8192 tokens on average: 64 sequences 5.3 / 7.2,
+// 256 9.7 / 7.9, 384 11.8 / 8.2, 512 14.8 / 8.8, 1024 31 / 10.8.  Decoding is what most calls do.
+constexpr int KP_ONE_CLUSTER = 384;
 static_assert(KP_ONE_CLUSTER <= KP_THREADS, "one sequence a thread");
-constexpr int KP_UNIT = 32 * KP_UNROLL;    // columns of one sequence that a warp moves at a time
 
 struct KvPagesLaunch {
     sv_kv_pages_params p;
@@ -34,10 +32,8 @@ struct KvPagesLaunch {
 };
 
 // every thread of the cluster arrives; global writes before it are visible behind it
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release;\n barrier.cluster.wait.acquire;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // The last sequence whose exclusive prefix is at most e.  ex[0] = 0 <= e and ex[batch] = the total; for e below the
 // total that sequence is the owner of entry e.
@@ -61,10 +57,12 @@ __device__ __forceinline__ int warp_owner_of(const int32_t *ex, int batch, int e
 }
 
 // What every block knows about the batch: prefix sums in shared memory and the totals that follow from them.
+// UNIT: columns of one sequence that a warp moves at a time.
+template <int UNIT>
 struct Pages {
     const int32_t *rel;                // [batch + 1] exclusive prefix of released pages
     const int32_t *req;                // [batch + 1] exclusive prefix of wanted pages
-    const int32_t *unit;               // [batch + 1] exclusive prefix of units (KP_UNIT columns that change hands)
+    const int32_t *unit;               // [batch + 1] exclusive prefix of units (UNIT columns that change hands)
     const int32_t *col;                // [batch] first column that changes hands, -1: sequence left alone
     int n_free;                        // top of the stack before the call
     int have;                          // and after the releases
@@ -87,7 +85,7 @@ struct Pages {
         const int total = unit[batch];
         for (int u = begin + warp; u < total; u += warps) {
             const int s = warp_owner_of(unit, batch, u, lane);
-            body(s, (u - unit[s]) * KP_UNIT);
+            body(s, (u - unit[s]) * UNIT);
         }
     }
 };
@@ -95,6 +93,10 @@ struct Pages {
 // WHOLE: the call in one launch by one cluster.  MOVE: what comes before the barrier, by a grid of any size; CLOSE: what
 // comes behind it, by one cluster in a second launch.
 enum { KP_WHOLE, KP_MOVE, KP_CLOSE };
+
+// Pages that a thread has under way.  One cluster has more sequences than it has warps for their parts: 128 that decode take 5.5 us
+// with 8 pages a thread, 5.2 with 4; half of 64 replaced 5.9 and 5.4, of 256 9.3 and 9.7.  The whole GPU: half of 1024 10.8 and 13.3.
+constexpr int kp_unroll(int part) { return part == KP_WHOLE ? 4 : 8; }
 
 template <int PART>
 __global__ void __launch_bounds__(KP_THREADS)
@@ -110,11 +112,12 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int threads = gridDim.x * KP_THREADS, me = blockIdx.x * KP_THREADS + tid;     // a cluster is a whole grid
     const int my_warp = me >> 5, warps = threads >> 5;
+    constexpr int UNROLL = kp_unroll(PART), UNIT = 32 * UNROLL;
     const int batch = p.batch, n_pages = (int)p.n_pages;
     int32_t *rel = kp_smem, *req = rel + batch + 1, *unit = req + batch + 1, *col = unit + batch + 1;
     uint32_t bad = 0;
 
-    Pages pg;
+    Pages<UNIT> pg;
     pg.n_free = __ldcg(p.n_free);
     if (pg.n_free < 0 || pg.n_free > n_pages) {
         bad |= SV_DEV_BAD_PAGE;
@@ -145,7 +148,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         }
         my_rel += n_rel;
         my_req += n_req;
-        my_unit += (n_rel + n_req + KP_UNIT - 1) / KP_UNIT;     // one of the two is zero
+        my_unit += (n_rel + n_req + UNIT - 1) / UNIT;     // one of the two is zero
     }
     int sum_rel = my_rel, sum_req = my_req, sum_unit = my_unit;
 #pragma unroll
@@ -192,7 +195,7 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         unit[b] = at_unit;
         at_rel += n_rel;
         at_req += n_req;
-        at_unit += (n_rel + n_req + KP_UNIT - 1) / KP_UNIT;
+        at_unit += (n_rel + n_req + UNIT - 1) / UNIT;
     }
     if (tid == 0) {
         rel[batch] = base_rel;
@@ -200,7 +203,10 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
         unit[batch] = base_unit;
     }
     __syncthreads();
-    if (PART == KP_CLOSE) pdl_enter();
+    if (PART == KP_CLOSE) {
+        cluster_arrive();              // this block has read what the last lines write
+        pdl_enter();
+    }
     pg.rel = rel;
     pg.req = req;
     pg.unit = unit;
@@ -226,14 +232,14 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
             pg.for_units(0, my_warp, warps, lane, [&](int s, int first) {
                 const int n = rel[s + 1] - rel[s], at = pg.n_free + rel[s];
                 int32_t *from = p.block_table + (long long)s * p.block_table_stride + col[s];
-                int page[KP_UNROLL];
+                int page[UNROLL];
 #pragma unroll
-                for (int u = 0; u < KP_UNROLL; ++u) {
+                for (int u = 0; u < UNROLL; ++u) {
                     const int j = first + u * 32 + lane;
                     page[u] = j < n ? __ldcg(from + j) : 0;
                 }
 #pragma unroll
-                for (int u = 0; u < KP_UNROLL; ++u) {
+                for (int u = 0; u < UNROLL; ++u) {
                     const int j = first + u * 32 + lane;
                     if (j >= n) continue;
                     if (page[u] < 0 || page[u] >= n_pages) bad |= SV_DEV_BAD_PAGE;
@@ -244,7 +250,8 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
             // A page that is read as an entry being released costs a binary search; for more than a few a thread, the
             // barrier (about a microsecond) is cheaper.
             if (PART == KP_WHOLE && served > threads) {
-                cluster_sync();
+                cluster_arrive();
+                cluster_wait();
                 pg.from_stack = pg.have;
             }
         }
@@ -253,14 +260,14 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
             pg.for_units(0, my_warp, warps, lane, [&](int s, int first) {
                 const int n = s < without ? req[s + 1] - req[s] : 0, e = req[s];
                 int32_t *to = p.block_table + (long long)s * p.block_table_stride + col[s];
-                int page[KP_UNROLL];
+                int page[UNROLL];
 #pragma unroll
-                for (int u = 0; u < KP_UNROLL; ++u) {
+                for (int u = 0; u < UNROLL; ++u) {
                     const int j = first + u * 32 + lane;
                     page[u] = j < n ? pg.acquired(p, e + j) : 0;
                 }
 #pragma unroll
-                for (int u = 0; u < KP_UNROLL; ++u) {
+                for (int u = 0; u < UNROLL; ++u) {
                     const int j = first + u * 32 + lane;
                     if (j < n) to[j] = page[u];
                 }
@@ -315,11 +322,12 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
     }
     if (PART == KP_MOVE) return;
     // ---- nobody reads the old state any more
-    cluster_sync();
+    if (PART == KP_WHOLE) cluster_arrive();
+    cluster_wait();
     if (untouched - pg.n_free < base_rel) {            // released entries that acquisitions may have read
         const int from = max(untouched - pg.n_free, 0);
         pg.for_units(PART == KP_WHOLE ? 0 : unit[owner_of(rel, batch, a.search, from)], my_warp, warps, lane, [&](int s, int first) {
-            const int n = min(rel[s + 1] - rel[s] - first, KP_UNIT);
+            const int n = min(rel[s + 1] - rel[s] - first, UNIT);
             int32_t *entry = p.block_table + (long long)s * p.block_table_stride + col[s] + first;
             for (int j = lane; j < n; j += 32)
                 if (rel[s] + first + j >= from) entry[j] = -1;

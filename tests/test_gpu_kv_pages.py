@@ -86,7 +86,7 @@ def test_binding_refuses_mismatched_shapes():
 
 # ------------------------------------------------------------------------------------------------ against the oracle
 @pytest.mark.gpu
-@pytest.mark.parametrize("B,stride,gamma_max", [(1, 1, 0), (1, 300, 8), (2, 3, 64), (31, 9, 4), (128, 40, 16), (512, 300, 4), (513, 300, 4), (1024, 5, 2),
+@pytest.mark.parametrize("B,stride,gamma_max", [(1, 1, 0), (1, 300, 8), (2, 3, 64), (31, 9, 4), (128, 40, 16), (384, 30, 4), (385, 30, 4), (512, 300, 4), (513, 300, 4), (1024, 5, 2),
                                                 (1025, 6, 2), (3000, 4, 1)])
 def test_random_walk(B, stride, gamma_max):
     rng = np.random.default_rng([B, stride])
