@@ -6,7 +6,8 @@
 // collects the prompt's marks in shared memory (a byte each: no atomics, whose conflicts on frequent tokens cost more) and
 // writes the slice once, cleared and marked together.  Measured for 128 prompts of 4096 to 8192 tokens at a vocabulary of 128256
 // (36 MB, 5.6 us at the copy rate): 9.6 us, of which about 2 are the launch and 2 the prompts, which every slice's block reads
-// for itself (slices of 16384 entries: 11 us; blocks of 256 or 1024 threads: 13 and 12 us; tokens one by one: 9.9 us).  Marks as
+// for itself (slices of 16384 entries: 11 us; blocks of 256 or 1024 threads: 13 and 12 us; tokens one by one: 9.9 us;
+// the slices as a cluster that shares the prompt and marks in one another's shared memory: 16.5 us).  Marks as
 // bits 11.7 to 12.7 us; slices cleared first and marked in global memory 18 to 23 us (scattered two-byte stores).
 #include "common.cuh"
 
