@@ -5,7 +5,7 @@
 // saturates, so the sum is the same in any order.  An admission writes whole rows: a block takes a slice of the vocabulary,
 // collects the prompt's marks in shared memory (a byte each: no atomics, whose conflicts on frequent tokens cost more) and
 // writes the slice once, cleared and marked together.  Measured for 128 prompts of 4096 to 8192 tokens at a vocabulary of 128256
-// (36 MB, 5.6 us at the copy rate): 9.6 us, of which about 2 are the launch and 2 the prompts, which every slice's block reads
+// (36 MB, 5.6 us at the copy rate): 9.5 us, of which about 2 are the launch and 2 the prompts, which every slice's block reads
 // for itself (slices of 16384 entries: 11 us; blocks of 256 or 1024 threads: 13 and 12 us; tokens one by one: 9.9 us;
 // the slices as a cluster that shares the prompt and marks in one another's shared memory: 16.5 us).  Marks as
 // bits 11.7 to 12.7 us; slices cleared first and marked in global memory 18 to 23 us (scattered two-byte stores).
@@ -104,13 +104,6 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
     uint32_t bad = 0;
     const int32_t *first = nullptr;
     const int n = tc_range(p, b, first, bad);
-    if (marking) {
-        for (int i = tid; i < TC_SLICE / 16; i += TC_RESET_THREADS) reinterpret_cast<uint4 *>(marks)[i] = make_uint4(0, 0, 0, 0);
-    } else if (clear) {
-        for (int k = lo + 8 * tid; k + 8 <= hi; k += 8 * TC_RESET_THREADS) *reinterpret_cast<uint4 *>(row + k) = make_uint4(0, 0, 0, 0);
-        for (int k = lo + (hi - lo) / 8 * 8 + tid; k < hi; k += TC_RESET_THREADS) row[k] = 0;
-    }
-    __syncthreads();
     // of a token: its entry of the slice; at least hi - lo if it is none of them
     auto entry_of = [&](int token) {
         const unsigned int at = (unsigned int)token - lo;
@@ -118,25 +111,33 @@ token_counts_reset_kernel(const __grid_constant__ TokenCountsLaunch a)
         return at;
     };
     if (marking) {
-        // four tokens a load: up to three in front of the first 16-byte boundary and behind the last go one by one
         auto mark = [&](int token) {
             const unsigned int at = entry_of(token);
             if (at < (unsigned int)(hi - lo)) marks[at] = 0x80;        // whoever else marks it stores the same
         };
-        const int head = min(n, (int)(-(reinterpret_cast<uintptr_t>(first) >> 2) & 3)), vectors = (n - head) / 4;
+        // four tokens a load, the next on its way: up to three in front of the first 16-byte boundary and behind the last go one by one
+        const int head = min(n, (int)(-(reinterpret_cast<uintptr_t>(first) >> 2) & 3)), vectors = (n - head) / 4, behind = head + 4 * vectors;
         const int4 *four = reinterpret_cast<const int4 *>(first + head);
-#pragma unroll 1                                       // unrolled further it takes registers and time (9.8 to 11 us)
+        int4 next = tid < vectors ? four[tid] : make_int4(-1, -1, -1, -1);
+        const int single = tid < head ? first[tid] : tid - head < n - behind ? first[behind + tid - head] : -1;
+        for (int i = tid; i < TC_SLICE / 16; i += TC_RESET_THREADS) reinterpret_cast<uint4 *>(marks)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+#pragma unroll 1                                       // unrolled it takes registers and time
         for (int i = tid; i < vectors; i += TC_RESET_THREADS) {
-            const int4 t = four[i];
+            const int4 t = next;
+            if (i + TC_RESET_THREADS < vectors) next = four[i + TC_RESET_THREADS];
             mark(t.x);
             mark(t.y);
             mark(t.z);
             mark(t.w);
         }
-        const int behind = head + 4 * vectors;
-        if (tid < head) mark(first[tid]);
-        else if (tid - head < n - behind) mark(first[behind + tid - head]);
+        mark(single);
     } else {
+        if (clear) {
+            for (int k = lo + 8 * tid; k + 8 <= hi; k += 8 * TC_RESET_THREADS) *reinterpret_cast<uint4 *>(row + k) = make_uint4(0, 0, 0, 0);
+            for (int k = lo + (hi - lo) / 8 * 8 + tid; k < hi; k += TC_RESET_THREADS) row[k] = 0;
+        }
+        __syncthreads();
         for (int i0 = 0; i0 < n; i0 += TC_RESET_THREADS) {
             const int token = i0 + tid < n ? first[i0 + tid] : -1;
             tc_add_warp(row, token, entry_of(token) < (unsigned int)(hi - lo), p.prompt != 0, tid & 31);
