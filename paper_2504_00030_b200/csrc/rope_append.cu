@@ -14,7 +14,10 @@
 // with the first copies under way before the row's slot is known.  Half of that way is instructions: scalar float32 arithmetic
 // took 64 million warp instructions (72 % of the issue slots), the packed form below 42 million.  Warps that loop over rows
 // and fetch the next row's slot early run in step with one another and reach 5.2 TB/s only.  Rows of few heads are bound by what
-// a row costs before its first head (angles, factors): 16381 rows of 8 + 1 + 1 heads 28 us (13 at the copy rate).
+// a row costs before its first head (angles, factors), and their rounds of keys and values leave lanes idle.  Where there are many
+// such rows, a warp takes several, a head of each in a round, and forms the factors' weights once: one row a warp / several, by
+// launch_rope's estimate: 16381 rows of 8 + 1 + 1 heads of 128 27.5 / 23.9 us (13 at the copy rate), of 4 + 1 + 1 heads of 64
+// 21.0 / 10.6 (4), of 1 + 1 + 1 heads of 128 24.0 / 16.4; of 32 + 8 + 8 64.3 / 69.5, 4096 rows of 8 + 1 + 1 8.6 / 9.7.
 #include "attn_common.cuh"
 #include "common.cuh"
 
@@ -23,8 +26,11 @@ namespace sv {
 constexpr int RA_THREADS = 256;
 constexpr int RA_BLOCKS_PER_SM = 2;        // the factors take registers: three blocks spill, 97 us instead of 66
 constexpr int RA_WARPS = RA_THREADS / 32;
-constexpr int RA_STAGES = 5;               // rounds of a warp under way, in shared memory (1 KB each); six measure the same
+constexpr int ra_stages(bool rows) { return rows ? 4 : 5; }      // rounds of a warp under way, in shared memory (1 KB each)
 constexpr int RA_PAGE = 16;
+// What a warp does before its first round (angles, factors, the pipeline's start), in rounds: with one row, and with several
+// (each row's angles, the factors once).
+constexpr int RA_BEFORE = 2, RA_BEFORE_ROWS = 10;
 constexpr int RA_MAX_FREQ = 64;            // rot_dim <= head_dim <= 128
 
 struct RopeAppendLaunch {
@@ -97,34 +103,41 @@ __device__ __forceinline__ unsigned long long turn_step(double inv_freq)
     return bits < 0 ? 0 - x : x;
 }
 
+template <bool ROWS>
 struct RopeShared {
-    uint4 ring[RA_WARPS][RA_STAGES][2][32];            // a round's chunks on their way: each lane reads back its own
-    float2 turns[RA_WARPS][RA_MAX_FREQ];               // (cos, sin) of the warp's row
+    uint4 ring[RA_WARPS][ra_stages(ROWS)][2][32];      // a round's chunks on their way: each lane reads back its own
+    float2 turns[RA_WARPS][(ROWS ? 4 : 1) * RA_MAX_FREQ];      // (cos, sin) of the warp's row or rows
 };
 
 // GL: lanes given to a head (a power of two >= head_dim / 16).  PAIRED: pairs (2f, 2f + 1).  WF32: float32 weights.
-// A round is 32 / GL heads of one kind (queries, keys, values); a warp has `rounds` consecutive rounds of a row.
-template <int GL, bool PAIRED, bool WF32>
+// A round is 32 / GL heads of one kind (queries, keys, values); a warp has `rounds` consecutive rounds of a row.  ROWS: a warp
+// takes 32 / GL rows, a round is one head of each.
+template <int GL, bool PAIRED, bool WF32, bool ROWS>
 __global__ void __launch_bounds__(RA_THREADS, RA_BLOCKS_PER_SM)
 rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
 {
     pdl_enter();
-    constexpr int PER_ROUND = 32 / GL;
-    __shared__ RopeShared sh;
+    constexpr int HEADS = ROWS ? 1 : 32 / GL, ROWS_WARP = ROWS ? 32 / GL : 1, TEAM = ROWS ? GL : 32;      // TEAM lanes share a row
+    constexpr int RA_STAGES = ra_stages(ROWS);
+    __shared__ RopeShared<ROWS> sh;
     const sv_rope_append_params &p = a.p;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = lane % GL, slot_h = lane / GL;
-    const unsigned row = blockIdx.x * RA_WARPS + warp;
-    if (row >= (unsigned)p.n_rows) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = lane % GL, group = lane / GL, slot_h = ROWS ? 0 : group;
+    const unsigned first_row = (blockIdx.x * RA_WARPS + warp) * ROWS_WARP;
+    if (first_row >= (unsigned)p.n_rows) return;
+    const unsigned row = ROWS ? min(first_row + group, (unsigned)p.n_rows - 1) : first_row;      // the last row again where there is none
     const int k_first = a.q_rounds, v_first = a.q_rounds + a.k_rounds;         // first rounds of keys and of values
     const int t_begin = blockIdx.y * a.rounds, t_end = min(t_begin + a.rounds, v_first + a.k_rounds);
-    // Loads that nothing waits for come first: the slot, and what belongs to frequencies lane and lane + 32.
+    // Loads that nothing waits for come first: the slot, and what belongs to this lane's frequencies.
     const long long slot = p.slot_map[row];
     const bool turning = t_begin < v_first && p.rot_dim > 0;
-    double freq[2] = {0.0, 0.0};
-    int pos[2] = {0, 0};
+    constexpr int FREQS = (ROWS ? 8 * GL : RA_MAX_FREQ) / TEAM;         // of a lane
+    double freq[FREQS];
+    int pos[FREQS];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int f = lane + 32 * i;
+    for (int i = 0; i < FREQS; ++i) {
+        const int f = lane % TEAM + TEAM * i;
+        freq[i] = 0.0;
+        pos[i] = 0;
         if (!turning || f >= p.rot_dim / 2) continue;
         freq[i] = p.inv_freq[f];
         const int axis = p.freq_axis != nullptr ? min((int)p.freq_axis[f], p.n_axes - 1) : 0;
@@ -133,17 +146,18 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     // This lane's chunks, neighbouring lanes at neighbouring ones.  Where the pairs are (f, f + rot/2), the first rot/16 lanes
     // hold the turned dims; pairs (2f, 2f + 1) lie within a chunk.
     const int pair_lanes = PAIRED ? a.lanes : p.rot_dim / 16;
-    const bool live = j < a.lanes, low = j < pair_lanes;
+    bool live = j < a.lanes && first_row + (ROWS ? group : 0) < (unsigned)p.n_rows;
+    const bool low = j < pair_lanes;
     const int c0 = low ? j : pair_lanes + j, c1 = low ? j + pair_lanes : a.lanes + j;
     const bool turn0 = c0 < p.rot_dim / 8, turn1 = c1 < p.rot_dim / 8;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[warp][0][0][lane]);
-    float2 *turns = sh.turns[warp];
+    float2 *turns = sh.turns[warp] + (ROWS ? group * 8 * GL : 0);
     // ---- producer: the rounds in order, RA_STAGES - 1 of them under way (from before the row's slot is known)
     int p_t = t_begin, p_stage = 0;
     auto issue = [&]() {
         if (p_t < t_end) {
             const bool q = p_t < k_first, v = p_t >= v_first;
-            const int h = (p_t - (q ? 0 : v ? v_first : k_first)) * PER_ROUND + slot_h;
+            const int h = (p_t - (q ? 0 : v ? v_first : k_first)) * HEADS + slot_h;
             if (live && h < (q ? p.hq : a.hkv)) {
                 const uint4 *src = static_cast<const uint4 *>(q ? p.q : v ? p.v_new : p.k_new) +
                                    (long long)row * (q ? a.q_stride : v ? a.v_stride : a.k_stride) + h * (2 * a.lanes);
@@ -157,20 +171,23 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     };
 #pragma unroll
     for (int s = 0; s < RA_STAGES - 1; ++s) issue();
-    if (slot < 0 || slot >= a.n_slots) {
-        if (slot >= 0 && lane == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
+    const bool placed = slot >= 0 && slot < a.n_slots;
+    if (slot >= a.n_slots && lane % TEAM == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
+    live = live && placed;
+    if (!__any_sync(0xffffffffu, placed)) {
         cp_wait<0>();
         return;
     }
     // ---- angles
     if (turning) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (lane + 32 * i >= p.rot_dim / 2) continue;
+        for (int i = 0; i < FREQS; ++i) {
+            const int f = lane % TEAM + TEAM * i;
+            if (f >= p.rot_dim / 2) continue;
             const int t = (int)(turn_step(freq[i]) * (unsigned long long)(long long)pos[i] >> 32);     // [-1/2, 1/2) turns, in units of 2^-32
             float s, c;
             sincospif((float)t * 4.656612873077393e-10f, &s, &c);                                      // 2^-31: half turns
-            turns[lane + 32 * i] = make_float2(c * p.rope_scale, s * p.rope_scale);
+            turns[f] = make_float2(c * p.rope_scale, s * p.rope_scale);
         }
         __syncwarp();
     }
@@ -182,7 +199,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
         const int first_t = kind == 0 ? 0 : k_first, t0 = max(t_begin, first_t), t1 = min(t_end, kind == 0 ? k_first : v_first);
         if (t0 >= t1) continue;
         const int n_heads = kind == 0 ? p.hq : a.hkv;
-        int h = (t0 - first_t) * PER_ROUND + slot_h;
+        int h = (t0 - first_t) * HEADS + slot_h;
         const long long dst_head = kind == 0 ? 2 * a.lanes : a.stride_head;
         uint4 *dst = (kind == 0 ? static_cast<uint4 *>(p.q_out) + (long long)row * a.q_chunks : a.k_pool + cache) + h * dst_head;
         const void *weight = kind == 0 ? p.q_weight : p.k_weight;
@@ -271,8 +288,8 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
                 dst[c0] = make_uint4(z0[0], z0[1], z0[2], z0[3]);
                 dst[c1] = make_uint4(z1[0], z1[1], z1[2], z1[3]);
             }
-            h += PER_ROUND;
-            dst += PER_ROUND * dst_head;
+            h += HEADS;
+            dst += HEADS * dst_head;
         }
     }
     // values
@@ -280,7 +297,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
         cp_wait<RA_STAGES - 2>();
         const uint4 v0 = sh.ring[warp][stage][0][lane], v1 = sh.ring[warp][stage][1][lane];
         stage = stage + 1 == RA_STAGES ? 0 : stage + 1;
-        const int h = (t - v_first) * PER_ROUND + slot_h;
+        const int h = (t - v_first) * HEADS + slot_h;
         if (live && h < a.hkv) {
             uint4 *dst = a.v_pool + cache + h * a.stride_head;
             dst[c0] = v0;
@@ -290,27 +307,40 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     }
 }
 
-template <int GL, bool PAIRED, bool WF32>
-static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
+// How many warps share a row's rounds (or several rows'): the fewest waves of resident warps, each as long as a warp's rounds and
+// the `before` rounds' worth of what precedes them.  warps: without sharing; heads: of a row in a round.
+static long long best_split(RopeAppendLaunch &a, long long warps, int heads, int before)
 {
-    constexpr int per_round = 32 / GL;
-    a.q_rounds = (a.p.hq + per_round - 1) / per_round;
-    a.k_rounds = (a.hkv + per_round - 1) / per_round;
+    a.q_rounds = (a.p.hq + heads - 1) / heads;
+    a.k_rounds = (a.hkv + heads - 1) / heads;
     const int all = a.q_rounds + 2 * a.k_rounds;
-    // How many warps share a row: the fewest waves of resident warps, where a row costs a warp about as much as two rounds
-    // before its first one (angles, factors, the pipeline's start).
     const long long resident = (long long)sm_count() * RA_BLOCKS_PER_SM * RA_WARPS;
     long long best = -1;
     for (int segments = 1; segments <= all; ++segments) {
         const int rounds = (all + segments - 1) / segments;
-        const long long cost = (a.p.n_rows * segments + resident - 1) / resident * (rounds + 2);
+        const long long cost = (warps * segments + resident - 1) / resident * (rounds + before);
         if (best >= 0 && cost >= best) continue;
         best = cost;
         a.rounds = rounds;
         a.segments = (all + rounds - 1) / rounds;
     }
+    return best;
+}
+
+template <int GL, bool PAIRED, bool WF32>
+static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
+{
+    constexpr int share = 32 / GL;
+    const long long sets = (a.p.n_rows + share - 1) / share;
+    RopeAppendLaunch rows = a;
+    const long long one = best_split(a, a.p.n_rows, share, RA_BEFORE);
+    // rows that do not fill the GPU by themselves are not put together
+    if (a.p.n_rows > (long long)sm_count() * RA_BLOCKS_PER_SM * RA_WARPS && best_split(rows, sets, 1, RA_BEFORE_ROWS) < one) {
+        const dim3 grid((unsigned)((sets + RA_WARPS - 1) / RA_WARPS), (unsigned)rows.segments);
+        return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32, true>, grid, RA_THREADS, 0, stream, rows);
+    }
     const dim3 grid((unsigned)((a.p.n_rows + RA_WARPS - 1) / RA_WARPS), (unsigned)a.segments);
-    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32>, grid, RA_THREADS, 0, stream, a);
+    return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32, false>, grid, RA_THREADS, 0, stream, a);
 }
 
 // [a, a + na) and [b, b + nb) share a byte

@@ -157,6 +157,20 @@ def test_shapes(n, hq, hkv, D, rot):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,hq,hkv,D,rot", [(4800, 1, 1, 128, 128), (4801, 1, 1, 112, 64), (5002, 4, 1, 64, 64), (5007, 2, 1, 48, 16), (16381, 8, 1, 128, 128),
+                                            (9001, 1, 2, 16, 16), (16380, 16, 4, 64, 48), (7003, 3, 1, 80, 0)])
+def test_many_rows_of_few_heads(n, hq, hkv, D, rot):
+    """Enough rows to fill the GPU several times over, so that a warp takes more than one; whole groups of them are padding."""
+    for k in range(4):
+        c = make_case(n, hq, hkv, D, rot, 5 + k, norm=("both", "none", "q", "k")[k], w32=k == 3, interleaved=k % 2 == 1, axes=1 + k, far=70000,
+                      pad=(0.0, 0.9, 0.3, 0.02)[k], scale=1.0 - 0.1 * k)
+        c["slots"][n // 2:n // 2 + 40] = -1
+        if k == 2:
+            c["slots"][n - 1] = c["n_pages"] * 16
+        assert check(c, call(c)) == (sv.SV_DEV_BAD_PAGE if k == 2 else 0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("norm", ["none", "q", "k", "both"])
 @pytest.mark.parametrize("w32", [False, True])
