@@ -16,8 +16,9 @@
 // and fetch the next row's slot early run in step with one another and reach 5.2 TB/s only.  Rows of few heads are bound by what
 // a row costs before its first head (angles, factors), and their rounds of keys and values leave lanes idle.  Where there are many
 // such rows, a warp takes several, a head of each in a round, and forms the factors' weights once: one row a warp / several, by
-// launch_rope's estimate: 16381 rows of 8 + 1 + 1 heads of 128 27.5 / 23.9 us (13 at the copy rate), of 4 + 1 + 1 heads of 64
-// 21.0 / 10.6 (4), of 1 + 1 + 1 heads of 128 24.0 / 16.4; of 32 + 8 + 8 64.3 / 69.5, 4096 rows of 8 + 1 + 1 8.6 / 9.7.
+// launch_rope's estimate: 16381 rows of 8 + 1 + 1 heads of 128 26.5 / 18.9 us (13 at the copy rate), of 4 + 1 + 1 heads of 64
+// 21.5 / 7.6 (4), of 1 + 1 + 1 heads of 128 22.7 / 10.8; of 12 + 4 + 4 (10000 rows) 21.0 / 24.4, of 32 + 8 + 8 63.6 / 69.0.
+// The turns' places in shared memory without bank conflicts are 5 us of the first.
 #include "attn_common.cuh"
 #include "common.cuh"
 
@@ -30,7 +31,11 @@ constexpr int ra_stages(bool rows) { return rows ? 4 : 5; }      // rounds of a 
 constexpr int RA_PAGE = 16;
 // What a warp does before its first round (angles, factors, the pipeline's start), in rounds: with one row, and with several
 // (each row's angles, the factors once).
-constexpr int RA_BEFORE = 2, RA_BEFORE_ROWS = 10;
+constexpr int RA_BEFORE = 2, RA_BEFORE_ROWS = 5;
+// Rows of more rounds than this are not taken several at a time: HBM bounds them, and is read better in whole rows.  One / several,
+// us: 3000 rows of 32 + 32 + 32 heads of 128 25.3 / 27.9, 16381 of 48 + 12 + 12 of 64 51.8 / 58.5 (24 and 10 rounds); 3000 of
+// 16 + 2 + 2 of 128 10.6 / 8.2, 8192 of 12 + 12 + 12 of 64 18.7 / 15.7 (6 rounds).
+constexpr int RA_FEW_ROUNDS = 8;
 constexpr int RA_MAX_FREQ = 64;            // rot_dim <= head_dim <= 128
 
 struct RopeAppendLaunch {
@@ -152,6 +157,8 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     const bool turn0 = c0 < p.rot_dim / 8, turn1 = c1 < p.rot_dim / 8;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&sh.ring[warp][0][0][lane]);
     float2 *turns = sh.turns[warp] + (ROWS ? group * 8 * GL : 0);
+    // where a frequency's turn lies: lanes read every fourth pair of them, which without the exclusive or would be in the same banks
+    auto turn_at = [&](int f) { return f ^ (f >> 4 & 3) << 1 ^ (ROWS ? (group & 1) << 2 : 0); };
     // ---- producer: the rounds in order, RA_STAGES - 1 of them under way (from before the row's slot is known)
     int p_t = t_begin, p_stage = 0;
     auto issue = [&]() {
@@ -187,7 +194,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
             const int t = (int)(turn_step(freq[i]) * (unsigned long long)(long long)pos[i] >> 32);     // [-1/2, 1/2) turns, in units of 2^-32
             float s, c;
             sincospif((float)t * 4.656612873077393e-10f, &s, &c);                                      // 2^-31: half turns
-            turns[f] = make_float2(c * p.rope_scale, s * p.rope_scale);
+            turns[turn_at(f)] = make_float2(c * p.rope_scale, s * p.rope_scale);
         }
         __syncwarp();
     }
@@ -225,14 +232,14 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
                 direct0[i] = wa;
                 direct1[i] = wb;
                 if (PAIRED) {
-                    const float2 ta = turns[turn0 ? 4 * c0 + i : 0], tb = turns[turn1 ? 4 * c1 + i : 0];
+                    const float2 ta = turns[turn0 ? turn_at(4 * c0 + i) : 0], tb = turns[turn1 ? turn_at(4 * c1 + i) : 0];
                     const float2 xa = split(wa), xb = split(wb);
                     if (turn0) direct0[i] = mul2(wa, pair(ta.x, ta.x));
                     if (turn1) direct1[i] = mul2(wb, pair(tb.x, tb.x));
                     across0[i] = mul2(pair(xa.y, xa.x), pair(-ta.y, ta.y));
                     across1[i] = mul2(pair(xb.y, xb.x), pair(-tb.y, tb.y));
                 } else {
-                    const float4 cs = reinterpret_cast<const float4 *>(turns)[turn0 ? 4 * j + i : 0];
+                    const float4 cs = reinterpret_cast<const float4 *>(turns)[turn0 ? turn_at(8 * j + 2 * i) / 2 : 0];
                     if (turn0) {
                         direct0[i] = mul2(wa, pair(cs.x, cs.z));
                         direct1[i] = mul2(wb, pair(cs.x, cs.z));
@@ -334,8 +341,9 @@ static sv_status launch_rope(RopeAppendLaunch &a, cudaStream_t stream)
     const long long sets = (a.p.n_rows + share - 1) / share;
     RopeAppendLaunch rows = a;
     const long long one = best_split(a, a.p.n_rows, share, RA_BEFORE);
-    // rows that do not fill the GPU by themselves are not put together
-    if (a.p.n_rows > (long long)sm_count() * RA_BLOCKS_PER_SM * RA_WARPS && best_split(rows, sets, 1, RA_BEFORE_ROWS) < one) {
+    // rows that do not fill the GPU by themselves are not put together either
+    if (a.q_rounds + 2 * a.k_rounds <= RA_FEW_ROUNDS && a.p.n_rows > (long long)sm_count() * RA_BLOCKS_PER_SM * RA_WARPS &&
+        best_split(rows, sets, 1, RA_BEFORE_ROWS) < one) {
         const dim3 grid((unsigned)((sets + RA_WARPS - 1) / RA_WARPS), (unsigned)rows.segments);
         return launch_kernel(true, rope_append_kernel<GL, PAIRED, WF32, true>, grid, RA_THREADS, 0, stream, rows);
     }
