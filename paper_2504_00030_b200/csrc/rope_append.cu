@@ -151,7 +151,7 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     // This lane's chunks, neighbouring lanes at neighbouring ones.  Where the pairs are (f, f + rot/2), the first rot/16 lanes
     // hold the turned dims; pairs (2f, 2f + 1) lie within a chunk.
     const int pair_lanes = PAIRED ? a.lanes : p.rot_dim / 16;
-    bool live = j < a.lanes && first_row + (ROWS ? group : 0) < (unsigned)p.n_rows;
+    bool live = j < a.lanes && (!ROWS || first_row + group < (unsigned)p.n_rows);
     const bool low = j < pair_lanes;
     const int c0 = low ? j : pair_lanes + j, c1 = low ? j + pair_lanes : a.lanes + j;
     const bool turn0 = c0 < p.rot_dim / 8, turn1 = c1 < p.rot_dim / 8;
@@ -180,8 +180,8 @@ rope_append_kernel(const __grid_constant__ RopeAppendLaunch a)
     for (int s = 0; s < RA_STAGES - 1; ++s) issue();
     const bool placed = slot >= 0 && slot < a.n_slots;
     if (slot >= a.n_slots && lane % TEAM == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
-    live = live && placed;
-    if (!__any_sync(0xffffffffu, placed)) {
+    if (ROWS) live = live && placed;
+    if (ROWS ? !__any_sync(0xffffffffu, placed) : !placed) {
         cp_wait<0>();
         return;
     }
