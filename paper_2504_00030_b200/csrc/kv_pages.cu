@@ -25,6 +25,9 @@ constexpr int KP_CLUSTER = 8;          // blocks of the cluster (the portable si
 // 256 9.7 / 7.9, 384 11.8 / 8.2, 512 14.8 / 8.8, 1024 31 / 10.8.  Decoding is what most calls do.
 constexpr int KP_ONE_CLUSTER = 384;
 static_assert(KP_ONE_CLUSTER <= KP_THREADS, "one sequence a thread");
+constexpr size_t kp_bytes(int batch) { return (size_t)(4 * batch + 3) * sizeof(int32_t); }      // prefix sums and first columns
+constexpr size_t KP_SMEM = 40 * 1024;  // what a kernel may have without asking (48 KB, its static arrays among them)
+static_assert(kp_bytes(KP_ONE_CLUSTER) <= KP_SMEM, "one cluster's kernel never asks");
 
 struct KvPagesLaunch {
     sv_kv_pages_params p;
@@ -341,17 +344,23 @@ kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
     if (me == 0) *p.n_free = pg.have - served;
 }
 
+// Lets a kernel of the two-launch form have the prefix sums of any batch in shared memory.  The limit belongs to the kernel, not to
+// the call, and host threads share it: it is the same for every batch, so that none lowers it under another one's launch.
+template <int PART>
+static bool allow_smem()
+{
+    if (cudaFuncSetAttribute(kv_pages_kernel<PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kp_bytes(KP_MAX_BATCH)) == cudaSuccess) return true;
+    (void)cudaGetLastError();
+    return false;
+}
+
 template <int PART>
 static sv_status launch_pages(const KvPagesLaunch &a, int blocks, cudaStream_t stream)
 {
-    const size_t smem = (size_t)(4 * a.p.batch + 3) * sizeof(int32_t);
-    if (smem > 40 * 1024 &&
-        cudaFuncSetAttribute(kv_pages_kernel<PART>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return SV_ECUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = blocks;
     cfg.blockDim = KP_THREADS;
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = kp_bytes(a.p.batch);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -392,6 +401,8 @@ extern "C" sv_status spec_kv_pages_update(const sv_kv_pages_params *p, void *str
     a.search = 1;
     while (2 * a.search <= p->batch) a.search *= 2;
     if (p->batch <= KP_ONE_CLUSTER) return launch_pages<KP_WHOLE>(a, KP_CLUSTER, (cudaStream_t)stream);
+    // before the first launch: a refusal leaves the state as it was
+    if (kp_bytes(p->batch) > KP_SMEM && !(allow_smem<KP_MOVE>() && allow_smem<KP_CLOSE>())) return SV_ECUDA;
     const sv_status st = launch_pages<KP_MOVE>(a, sm_count(), (cudaStream_t)stream);
     return st != SV_OK ? st : launch_pages<KP_CLOSE>(a, KP_CLUSTER, (cudaStream_t)stream);
 }

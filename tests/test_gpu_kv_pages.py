@@ -1,5 +1,6 @@
 """spec_kv_pages_update against the oracle's sequential walk: every array of the state and both row arrays, whole."""
 import ctypes as C
+import threading
 
 import numpy as np
 import pytest
@@ -237,3 +238,42 @@ def test_behind_the_controller_step_after_step(B, graph):
     np.testing.assert_array_equal(slot.cpu().numpy(), r_slot)
     np.testing.assert_array_equal(pos.cpu().numpy(), r_pos)
     assert int(status.item()) == 0
+
+
+@pytest.mark.gpu
+def test_batches_of_different_sizes_from_several_host_threads():
+    """Threads of one process with states of their own, whose prefix sums take more shared memory than a kernel may have by default."""
+    sizes, steps, stride = (8000, 3000, 5500), 600, 3
+    runs, statuses = [], [[] for _ in sizes]
+    for B in sizes:
+        rng = np.random.default_rng(B)
+        lengths = [rng.integers(0, stride * 16 + 1, B).astype(np.int32) for _ in range(2)]
+        state = new_state(B, stride, B * stride, B)
+        d_state, d_len, cond = upload(state), [dev(a) for a in lengths], torch.zeros(1, dtype=torch.int32, device=DEV)
+        runs.append((lengths, state, d_state, d_len, cond, [sv.kv_pages_params(a, *d_state, device_status=cond) for a in d_len], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    lib, start = sv.load(), threading.Barrier(len(sizes))
+
+    def worker(k):
+        torch.cuda.set_device(DEV)
+        params, stream = runs[k][5], runs[k][6]
+        start.wait()
+        for step in range(steps):
+            statuses[k].append(lib.spec_kv_pages_update(C.byref(params[step % 2]), stream.cuda_stream))
+            if statuses[k][-1] != sv.SV_OK:
+                return
+
+    threads = [threading.Thread(target=worker, args=(k,)) for k in range(len(sizes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert [set(s) for s in statuses] == [{sv.SV_OK}] * len(sizes)
+    for lengths, state, d_state, _, cond, _, _ in runs:
+        for step in range(steps):
+            *state, _, _, o_cond = oracle.kv_pages_update(lengths[step % 2], *state)
+            assert o_cond == 0
+        for d, r in zip(d_state, state):
+            np.testing.assert_array_equal(d.cpu().numpy().reshape(-1), np.asarray(r).reshape(-1))
+        assert int(cond.item()) == 0
