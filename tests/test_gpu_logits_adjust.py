@@ -454,3 +454,31 @@ def test_a_bias_list_longer_than_a_block_takes_at_a_time():
     got, status = run(c)
     assert status == 0
     check(c, got)
+
+
+# Shapes that give a block several rows on 148 multiprocessors, by the 592 blocks that the rows are dealt out over: all rows of a
+# sequence (the ring of four stages comes around), and two to five rows with several blocks along a sequence.
+BLOCKS_OF_ROWS = [(600, 1000, 8, 1000), (600, 1001, 8, 1001), (600, 1003, 8, 1008), (100, 1000, 8, 1000), (150, 1002, 8, 1002), (220, 9001, 8, 9001), (220, 9000, 8, 9008),
+                  (700, 104, 64, 104), (700, 101, 64, 101)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("B,V,gmax,stride", BLOCKS_OF_ROWS)
+def test_blocks_of_several_rows(B, V, gmax, stride, inplace, bf16):
+    """Drafts join the history from row to row, some of them twice, and one where nothing else changes an element near it."""
+    for penal, bias, mask in ((True, 12, True), (True, 0, False), (False, 5, False), (False, 0, True)):
+        c = make_case(B, V, gmax, 14, bf16=bf16, penal=penal, bias=bias, mask=mask, pad_rows=3, stride=stride)
+        far = V - 3                                     # in the last unit or next to it, with neighbours that nothing touches
+        for b in range(B):
+            lo, hi = c["cu_d"][b], c["cu_d"][b + 1]
+            if hi - lo >= 2:
+                c["tokens"][hi - 2] = far if b % 2 else c["tokens"][lo]
+        if penal:
+            c["kw"]["counts"][:, V - 16:V] = 0
+        if bias:
+            c["kw"]["bias_tokens"] %= V - 16
+        got, status = run(c, inplace)
+        assert status == 0
+        check(c, got, inplace)
