@@ -287,3 +287,32 @@ def test_no_rows_is_nothing():
     before = sv.sv_launch_count()
     sv.spec_rope_append(q[:0], k[:0], v[:0], torch.zeros((0, 4, 64), dtype=torch.bfloat16, device=DEV), pool, dev(c["pos"])[:0], dev(c["slots"])[:0], dev(c["inv"]))
     assert sv.sv_launch_count() == before
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,hq,hkv,D,rot", [(2300, 32, 8, 128, 128), (2400, 32, 8, 128, 64), (2300, 64, 8, 64, 64), (4700, 33, 5, 96, 96), (3000, 24, 24, 96, 48),
+                                            (2350, 36, 12, 48, 32), (2368, 40, 9, 64, 16), (1200, 64, 8, 128, 128), (4700, 20, 6, 80, 80)])
+def test_many_rows_of_many_heads(n, hq, hkv, D, rot):
+    """Enough rows that a warp takes 6 to 13 rounds of one, from queries on to keys and to values, the last of each kind a part of a
+    round: on 148 multiprocessors the ring of copies comes around more than once."""
+    for k in range(2):
+        c = make_case(n, hq, hkv, D, rot, 9 + k, norm=("both", "k")[k], w32=k == 1, interleaved=k == 1, axes=1 + 2 * k, far=70000, pad=(0.0, 0.2)[k],
+                      scale=1.0 - 0.1 * k)
+        c["slots"][n // 2:n // 2 + 20] = -1
+        assert check(c, call(c)) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,hq,hkv,D,rot", [(2300, 32, 8, 128, 128), (4700, 33, 5, 96, 64), (5002, 4, 1, 64, 64), (16381, 8, 1, 128, 128)])
+def test_in_place_where_copies_run_ahead_of_the_stores(n, hq, hkv, D, rot):
+    """Many rounds a warp, and several rows a warp, with the queries turned where they are: padding rows stay as they were."""
+    c = make_case(n, hq, hkv, D, rot, 12, pad=0.1, interleaved=hq == 33)
+    q, k, v = (x.contiguous() for x in views(dev_bf16(c["qkv"]), c))
+    kp, vp = dev_bf16(c["pool_k"]), dev_bf16(c["pool_v"])
+    w = [dev(c[x]).to(torch.bfloat16) for x in ("qw", "kw")]
+    sv.spec_rope_append(q, k, v, q, sv.spec_kv_pool_register(kp, vp), dev(c["pos"]), dev(c["slots"]), dev(c["inv"]), *w, c["eps"], c["interleaved"])
+    torch.cuda.synchronize()
+    padding = c["slots"] < 0
+    np.testing.assert_array_equal(bits_of(q)[padding], c["qkv"].reshape(n, -1, D)[padding, :hq])
+    q[dev(padding)] = dev_bf16(np.full((1, hq, D), 0x4242, np.uint16))       # what check expects of rows that are left alone
+    assert check(c, (q, kp, vp, 0)) == 0
