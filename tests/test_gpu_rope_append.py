@@ -1,5 +1,6 @@
 """spec_rope_append against the oracle: queries, and the pools whole, so that a write to a wrong place is caught too."""
 import ctypes as C
+import types
 
 import numpy as np
 import pytest
@@ -316,3 +317,17 @@ def test_in_place_where_copies_run_ahead_of_the_stores(n, hq, hkv, D, rot):
     np.testing.assert_array_equal(bits_of(q)[padding], c["qkv"].reshape(n, -1, D)[padding, :hq])
     q[dev(padding)] = dev_bf16(np.full((1, hq, D), 0x4242, np.uint16))       # what check expects of rows that are left alone
     assert check(c, (q, kp, vp, 0)) == 0
+
+
+@pytest.mark.parametrize("k_at,v_at", [(0, 0), (-1, 0), (0, -1)])
+def test_binding_refuses_a_pool_of_another_device(k_at, v_at):
+    """Host tensors (device index -1) stand for those of the current device: the pool's memory lies on another one."""
+    c = make_case(4, 2, 1, 64, 64, 1)
+    q, k, v = views(torch.from_numpy(c["qkv"].view(np.int16)).view(torch.bfloat16), c)
+    at = lambda i: types.SimpleNamespace(get_device=lambda: i)  # noqa: E731
+    pool = types.SimpleNamespace(hkv=1, head_dim=64, handle=C.c_void_p(4096), k_pool=at(-1), v_pool=at(-1))
+    args = (-1, q, k, v, torch.zeros_like(q).contiguous(), pool, torch.from_numpy(c["pos"]), torch.from_numpy(c["slots"]), torch.from_numpy(c["inv"]))
+    assert 4096 in sv._rope_append_args(*args)
+    pool.k_pool, pool.v_pool = at(k_at), at(v_at)
+    with pytest.raises(ValueError, match="pool"):
+        sv._rope_append_args(*args)
