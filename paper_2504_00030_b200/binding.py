@@ -463,6 +463,8 @@ def _rope_append_args(index, q, k_new, v_new, q_out, pool, positions, slot_map, 
     n_rows, hq, head_dim = q.shape
     if head_dim != pool.head_dim:
         raise ValueError("q's head_dim is not the pool's")
+    if pool.handle is None:
+        raise ValueError("the pool has been released")
     if pool.k_pool.get_device() != index or pool.v_pool.get_device() != index:
         raise ValueError(f"the pool's memory is not on the current device (cuda:{index})")
     qp, qs = _head_rows(q, hq, head_dim, n_rows, "q", index)

@@ -331,3 +331,12 @@ def test_binding_refuses_a_pool_of_another_device(k_at, v_at):
     pool.k_pool, pool.v_pool = at(k_at), at(v_at)
     with pytest.raises(ValueError, match="pool"):
         sv._rope_append_args(*args)
+
+
+def test_binding_refuses_a_released_pool():
+    c = make_case(4, 2, 1, 64, 64, 1)
+    q, k, v = views(torch.from_numpy(c["qkv"].view(np.int16)).view(torch.bfloat16), c)
+    here = types.SimpleNamespace(get_device=lambda: -1)
+    pool = types.SimpleNamespace(hkv=1, head_dim=64, handle=None, k_pool=here, v_pool=here)
+    with pytest.raises(ValueError, match="pool"):
+        sv._rope_append_args(-1, q, k, v, torch.zeros_like(q).contiguous(), pool, torch.from_numpy(c["pos"]), torch.from_numpy(c["slots"]), torch.from_numpy(c["inv"]))
