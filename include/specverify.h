@@ -122,7 +122,7 @@ typedef struct sv_rope_append_params {
     int64_t v_stride;
     void *q_out;                /* device bf16 [n_rows, hq, head_dim]; all four 16-byte aligned */
     sv_kv_pool_t pool;          /* head_dim a multiple of 16 */
-    int32_t hq;
+    int32_t hq;                 /* at most 2^20, as the pool's heads */
     int64_t n_rows;             /* <= 2^30 */
     const int64_t *slot_map;    /* device [n_rows] */
     const int32_t *positions;   /* device [n_axes, n_rows] */

@@ -37,6 +37,7 @@ constexpr int RA_BEFORE = 2, RA_BEFORE_ROWS = 5;
 // 16 + 2 + 2 of 128 10.6 / 8.2, 8192 of 12 + 12 + 12 of 64 18.7 / 15.7 (6 rounds).
 constexpr int RA_FEW_ROUNDS = 8;
 constexpr int RA_MAX_FREQ = 64;            // rot_dim <= head_dim <= 128
+constexpr int RA_MAX_HEADS = 1 << 20;      // a head's place in its row, in chunks, stays within 32 bits
 
 struct RopeAppendLaunch {
     sv_rope_append_params p;
@@ -368,6 +369,7 @@ extern "C" sv_status spec_rope_append(const sv_rope_append_params *p, void *stre
     if (p->hq <= 0 || p->n_axes <= 0 || p->rot_dim < 0 || p->rot_dim > pool.head_dim || !(p->eps >= 0.f)) return SV_EINVAL;
     if (pool.head_dim % 16 != 0 || p->rot_dim % 16 != 0) return SV_EUNSUPPORTED;
     if (p->n_rows > 1 << 30) return SV_EUNSUPPORTED;       // rows are counted in 32 bits, with room for a step
+    if (p->hq > RA_MAX_HEADS || pool.hkv > RA_MAX_HEADS) return SV_EUNSUPPORTED;
     const long long q_row = (long long)p->hq * pool.head_dim, kv_row = (long long)pool.hkv * pool.head_dim;
     if (p->q_stride < q_row || p->k_stride < kv_row || p->v_stride < kv_row) return SV_EINVAL;
     if (p->n_rows == 0) return SV_OK;

@@ -340,3 +340,14 @@ def test_binding_refuses_a_released_pool():
     pool = types.SimpleNamespace(hkv=1, head_dim=64, handle=None, k_pool=here, v_pool=here)
     with pytest.raises(ValueError, match="pool"):
         sv._rope_append_args(-1, q, k, v, torch.zeros_like(q).contiguous(), pool, torch.from_numpy(c["pos"]), torch.from_numpy(c["slots"]), torch.from_numpy(c["inv"]))
+
+
+@pytest.mark.parametrize("hq,hkv", [((1 << 20) + 1, 1), (1 << 28, 1), (2, (1 << 20) + 1)])
+def test_more_heads_than_32_bit_offsets_reach_are_refused(hq, hkv):
+    """Offsets of a head within its row are kept in 32 bits.  (Nothing lies behind these addresses, and nothing is launched.)"""
+    pool = host_pool(96, hkv)
+    p = good_params(pool)
+    p.q, p.k_new, p.v_new, p.q_out = ((i + 1) << 50 for i in range(4))
+    p.rot_dim, p.hq, p.q_stride, p.k_stride, p.v_stride = 96, hq, hq * 96, hkv * 96, hkv * 96
+    assert sv.load().spec_rope_append(C.byref(p), None) == sv.SV_EUNSUPPORTED
+    sv.load().spec_kv_pool_release(pool)
