@@ -202,3 +202,24 @@ def test_draft_rows_then_the_step():
         np.testing.assert_array_equal(n_dr.cpu().numpy(), r_n)
         np.testing.assert_array_equal(active.cpu().numpy(), r_active)
     assert r_n.tolist() == gamma.tolist()
+
+
+def test_parameter_structs_hold_what_the_calls_pack():
+    """The structs for callers of the C entry points, and the bytes that the binding's calls hand over in their place."""
+    i32 = lambda *n: torch.ones(n, dtype=torch.int32, device=DEV)  # noqa: E731
+    b16 = lambda *n: torch.ones(n, dtype=torch.bfloat16, device=DEV)  # noqa: E731
+    index, rows = torch.cuda.current_device(), torch.ones(6, dtype=torch.int64, device=DEV)
+    pool = sv.spec_kv_pool_register(b16(4, 2, 16, 64), b16(4, 2, 16, 64))
+    counts, x, f = torch.ones((2, 104), dtype=torch.int16, device=DEV), torch.ones((6, 100), device=DEV), torch.ones(2, device=DEV)
+    freqs = torch.ones(32, dtype=torch.float64, device=DEV)
+    q, k, v = b16(6, 8 * 64).unflatten(1, (8, 64)).split([4, 2, 2], 1)
+    for struct, args, pack, a, kw in (
+            (sv.kv_pages_params, sv._kv_pages_args, sv._pack_kv_pages, (i32(2), i32(2, 5), i32(2), i32(9), i32(1), i32(2), i32(3), 2, rows, i32(6), i32(1)), {}),
+            (sv.rope_append_params, sv._rope_append_args, sv._pack_rope_append, (q, k, v, b16(6, 4, 64), pool, i32(6), rows, freqs, b16(64), b16(64), 1e-5, True),
+             dict(rope_scale=0.5, device_status=i32(1))),
+            (sv.logits_adjust_params, sv._logits_adjust_args, sv._pack_logits_adjust, (x, torch.ones_like(x), i32(2), i32(3), i32(3), 2, i32(4), counts, f, f, f),
+             dict(bias_tokens=i32(2, 3), bias_values=torch.ones((2, 3), device=DEV), n_bias=i32(2), mask=i32(6, 4), active=i32(2))),
+            (sv.token_counts_params, sv._token_counts_args, sv._pack_token_counts, (counts, 100, i32(7), i32(3), 5, i32(2), True, i32(1)), {})):
+        p = struct(*a, **kw)
+        assert bytes(p) == pack(*args(index, *a, **kw))
+    torch.cuda.synchronize()
