@@ -106,8 +106,9 @@ sv_status spec_kv_pool_release(sv_kv_pool_t pool);
  * Queries go to q_out, keys to slot slot_map[r] % 16 of page slot_map[r] / 16 of the pool, values
  * there unchanged.  Rows with a negative slot (padding, as spec_kv_pages_update marks it) write
  * nothing: their part of q_out stays as it is.  A row is any position: draft blocks, single tokens, prompts.
- * bf16 inputs, float32 arithmetic, one rounding to bf16 at the end; the angle is formed and
- * reduced in float64, so that it keeps its digits at far positions.
+ * bf16 inputs, float32 arithmetic, one rounding to bf16 at the end.  The angle keeps its digits at
+ * far positions: a frequency becomes a 64-bit fraction of a turn, and the product with the
+ * position, in 64-bit integers, drops whole turns exactly before the rest goes to float32.
  * Slots of different rows must differ.  q_out may be q itself where q's rows are contiguous; it
  * must not overlap q otherwise, nor k_new or v_new (SV_EINVAL).
  * A slot at or beyond n_pages * 16 -> SV_DEV_BAD_PAGE, row skipped.  One launch; n_rows == 0
@@ -320,8 +321,9 @@ sv_status spec_verify_attn_layers(const sv_attn_layers_params *p, void *workspac
  * Target rows (n_drafted == NULL): rows cu_q[b] .. cu_q[b] + gamma[b]; rows of
  * no sequence are left as they are.  Draft rows (n_drafted != NULL): row b.
  * out may be logits itself (same stride): what does not change is then neither
- * read nor written where the mask and the counts show it.  Otherwise the two
- * must not overlap (SV_EINVAL).
+ * read nor written where the mask and the counts show it and 128-bit access is
+ * enabled, and written as it was elsewhere.  Otherwise the two must not overlap,
+ * from the first element to the last (SV_EINVAL).
  * A bias list that names a token twice: the later entry counts.
  * Device-detected: gamma[b], or with penalties n_drafted[b], outside [0, gamma_max]
  * -> SV_DEV_BAD_GAMMA, clamped; a block with rows beyond n_rows -> SV_DEV_BAD_LEN,
@@ -334,10 +336,10 @@ typedef struct sv_logits_adjust_params {
     int64_t row_stride;         /* elements between rows (>= vocab); both strides multiples of 4 (bf16: 8) with 16-byte */
     int64_t out_stride;         /* aligned bases enable 128-bit access */
     int64_t n_rows;
-    int32_t vocab;
+    int32_t vocab;              /* at most 2^30 (SV_EUNSUPPORTED, as the next limit); 128-bit access needs a multiple of 4 (bf16: 8) */
     int32_t logits_bf16;
     int32_t batch;
-    int32_t gamma_max;
+    int32_t gamma_max;          /* at most 64 */
     const int32_t *gamma;       /* device [batch]; target rows only */
     const int32_t *cu_q;        /* device [batch+1]; target rows only */
     const int32_t *cu_d;        /* device [batch+1]: first draft token of each sequence; with penalties and gamma_max > 0 */
@@ -379,13 +381,13 @@ sv_status spec_logits_adjust(const sv_logits_adjust_params *p, void *stream);
 typedef struct sv_token_counts_params {
     int16_t *token_counts;      /* device in/out [batch, count_stride], 16-byte aligned */
     int64_t count_stride;       /* elements between rows: a multiple of 8, >= vocab */
-    int32_t vocab;
+    int32_t vocab;              /* at most 2^30, as max_tokens */
     int32_t batch;
     const int32_t *tokens;      /* device; may be NULL if max_tokens is 0 (reset alone) */
     int64_t token_stride;       /* elements between rows, >= max_tokens; not used with cu_tokens */
     const int32_t *cu_tokens;   /* device [batch+1], or NULL */
     int64_t n_tokens;           /* entries of tokens; used with cu_tokens */
-    int32_t max_tokens;         /* most tokens of a sequence; sizes the grid */
+    int32_t max_tokens;         /* most tokens of a sequence; sizes the grid (without reset, a warp per 32 of them and sequence) */
     const int32_t *reset;       /* device [batch] or NULL: nothing is cleared */
     int32_t prompt;
     uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */

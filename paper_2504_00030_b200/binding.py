@@ -594,7 +594,9 @@ _pack_token_counts = _packer(TokenCountsParams)
 def spec_token_counts_update(token_counts, vocab, tokens=None, cu_tokens=None, max_tokens=None, reset=None, prompt=False,
                              device_status=None, stream=None):
     """Count generated tokens (or mark prompt tokens) in the int16 state behind the penalties, after clearing the rows
-    of newly admitted sequences (asynchronous).  tokens: [batch, columns] padded with -1, or packed with cu_tokens."""
+    of newly admitted sequences (asynchronous).  tokens: [batch, columns] padded with -1, or packed with cu_tokens.
+    max_tokens: the most that a sequence has; it sizes the grid, and with cu_tokens it should be given: where it is
+    left out it is the number of all tokens, for each sequence (128 prompts of 8192 marked without reset: 404 us, not 9)."""
     index, raw = _launch_at(stream, token_counts, "token_counts")
     p = _pack_token_counts(*_token_counts_args(index, token_counts, vocab, tokens, cu_tokens, max_tokens, reset, prompt,
                                                device_status))

@@ -105,9 +105,10 @@ template <int PART>
 __global__ void __launch_bounds__(KP_THREADS)
 kv_pages_kernel(const __grid_constant__ KvPagesLaunch a)
 {
-    // The closing launch makes its prefix sums while the first one still moves pages: what they read is not written by it, and
-    // every block of it has waited for the kernels in front of the call before this launch may start (whose results are
-    // read from L2: this launch has not waited itself).
+    // The closing launch may start, and make its prefix sums, before the first one has ended: what they read is not written by it,
+    // and every block of it has waited for the kernels in front of the call before this launch may start (whose results are
+    // read from L2: this launch has not waited itself).  A closing block (32 registers a thread) does not fit beside a moving one
+    // (40) in a multiprocessor's 65536, so its sums run beside the last moving blocks only, where others have ended.
     if (PART != KP_CLOSE) pdl_enter();
     extern __shared__ int32_t kp_smem[];
     __shared__ int32_t warp_rel[32], warp_req[32], warp_unit[32];
