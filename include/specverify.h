@@ -270,6 +270,127 @@ typedef struct sv_kv_append_params {
 
 sv_status spec_kv_append(const sv_kv_append_params *p, void *stream);
 
+/* ---------------------------------------------------------------- bounds of every page's keys */
+/*
+ * Long contexts (KV caching, paper Section 5): instead of all of its cache a row may read the pages that matter to it,
+ * found by a cheap score on a summary of every page.  This call keeps the summary, next to the cache append.  For every
+ * page of sequence b that holds a position of [start, seq_len[b]), with start = seq_len[b] - (gamma[b]+1), or first[b]
+ * where first is given (gamma NULL), and for every kv head, over the page's positions below seq_len[b]:
+ *     M_d = max k_d,  m_d = min k_d,  scale = max_d max(|M_d|, |m_d|) * (1/127)
+ *     bounds[page][head][0][d] = round(M_d / scale),  bounds[page][head][1][d] = round(m_d / scale)      (0 if scale is 0)
+ * float32, each operation and the constant 1/127 rounded once, round half to even.  Other pages' entries stay.  seq_len[b] = 0 is an absent
+ * sequence.  A page that two sequences bring up to date is written by both; they have to fill it alike.
+ * Device-detected: gamma[b] outside [0, max_new) -> SV_DEV_BAD_GAMMA, clamped; a start below 0, more than max_new
+ * positions or a length beyond the table row -> SV_DEV_BAD_LEN, sequence skipped; a page id outside the pool ->
+ * SV_DEV_BAD_PAGE, page skipped.  One launch.
+ */
+typedef struct sv_page_bounds_params {
+    sv_kv_pool_t pool;          /* head_dim 64 or 128 */
+    int8_t *bounds;             /* device in/out [n_pages, hkv, 2, head_dim], 16-byte aligned */
+    float *scales;              /* device in/out [n_pages, hkv] */
+    const int32_t *block_table; /* device [batch, block_table_stride] */
+    int64_t block_table_stride;
+    const int32_t *seq_len;     /* device [batch] */
+    const int32_t *gamma;       /* device [batch], or NULL: first */
+    const int32_t *first;       /* device [batch], or NULL: gamma */
+    int32_t batch;
+    int32_t max_new;            /* upper bound of the positions of a sequence (gamma_max + 1 behind a draft block); sizes the grid */
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_page_bounds_params;
+
+sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
+
+/* ---------------------------------------------------------------- pages that a row reads */
+/*
+ * For row i of sequence b's block at position pos = seq_len[b] - (gamma[b]+1) + i (the pages 0 .. pos / 16 are before it)
+ * and kv head g, with the group's query heads h:
+ *     s = max_{h,d} |q_hd| * (1/127),  qi_hd = round(q_hd / s)                (as above; at most 127 in magnitude)
+ *     score(page) = scales[page] * max_h sum_d max(qi_hd bounds[page][g][0][d], qi_hd bounds[page][g][1][d])
+ * The row reads the first n_first pages, the last n_last up to and including its own, and of the others those with the
+ * highest scores, the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole
+ * numbers and the product with the scale is rounded once, so a row of a block reads the pages that the same position would
+ * have read decoded alone: n_last >= 1 keeps pages with keys behind the row out of the comparison.
+ * Output per sequence and kv head: the pages that any row of the block reads, in ascending order (indices into the block
+ * table row), and for each the rows that do (bit i: row i).  Entries at and beyond n_list are left as they are.  A skipped
+ * sequence has n_list 0.
+ * Device-detected: gamma[b] out of range -> SV_DEV_BAD_GAMMA, clamped; seq_len[b] < gamma[b]+1 or > max_seq_len ->
+ * SV_DEV_BAD_LEN, sequence skipped; a page id outside [0, n_pages) -> SV_DEV_BAD_PAGE, that page's score is 0.
+ * Two launches.
+ */
+typedef struct sv_page_select_params {
+    const void *q;              /* device bf16 [n_rows, hq, head_dim], 16-byte aligned: what the attention reads */
+    const int8_t *bounds;       /* device [n_pages, hkv, 2, head_dim], 16-byte aligned */
+    const float *scales;        /* device [n_pages, hkv] */
+    int64_t n_pages;
+    const int32_t *block_table; /* device [batch, block_table_stride] */
+    int64_t block_table_stride; /* elements between rows; >= ceil(max_seq_len / 16) */
+    const int32_t *seq_len;     /* device [batch] */
+    const int32_t *gamma;       /* device [batch] */
+    const int32_t *cu_q;        /* device [batch+1] */
+    int32_t batch;
+    int32_t gamma_max;          /* at most 63 */
+    int32_t hq, hkv, head_dim;  /* head_dim 64 or 128, hq / hkv at most 128 */
+    int32_t max_seq_len;        /* upper bound of seq_len[b]; sizes the grid and the workspace */
+    int32_t n_select;           /* pages of a row, >= n_first + n_last */
+    int32_t n_first;            /* >= 0 */
+    int32_t n_last;             /* >= 1 */
+    int32_t *page_list;         /* device out [batch, hkv, list_stride] */
+    uint64_t *row_mask;         /* device out [batch, hkv, list_stride] */
+    int32_t *n_list;            /* device out [batch, hkv] */
+    int64_t list_stride;        /* >= min(ceil(max_seq_len / 16), (gamma_max+1) * n_select) */
+    uint32_t *device_status;    /* device, one word, OR-ed into; may be NULL */
+} sv_page_select_params;
+
+/* Bytes of device scratch for these bounds (the scores of all rows). */
+size_t spec_page_select_workspace_bytes(int32_t batch, int32_t gamma_max, int32_t hkv, int32_t max_seq_len);
+
+sv_status spec_page_select(const sv_page_select_params *p, void *workspace_device, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------- attention over listed pages */
+/*
+ * spec_verify_attn where row i of sequence b reads, for kv head g, only the keys of those listed pages whose mask has bit
+ * i set (and, as there, none behind its position): j runs over the positions of pages page_list[b][g][e], e <
+ * n_list[b][g], with bit i of row_mask[b][g][e].  A row without any key gives o = 0 and lse = -inf.  The lists are those
+ * of spec_page_select, or any others: pages in any order, each once.
+ * Arguments of attn as in spec_verify_attn; gamma_max at most 63, hq / hkv at most 128.
+ * Device-detected: as spec_verify_attn; a listed page outside the sequence's pages -> SV_DEV_BAD_PAGE, not read; n_list
+ * outside [0, list_stride] -> SV_DEV_BAD_LEN, clamped.  Two launches.
+ */
+typedef struct sv_attn_pages_params {
+    sv_attn_params attn;
+    const int32_t *page_list;   /* device [batch, hkv, list_stride] */
+    const uint64_t *row_mask;   /* device [batch, hkv, list_stride] */
+    const int32_t *n_list;      /* device [batch, hkv] */
+    int64_t list_stride;
+} sv_attn_pages_params;
+
+size_t spec_verify_attn_pages_workspace_bytes(int32_t batch, int32_t gamma_max, int32_t hq, int32_t hkv, int32_t head_dim);
+
+sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void *workspace_device, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------- attention behind shared prefixes */
+/*
+ * spec_verify_attn (the same result up to rounding) of a batch in which groups of sequences share the pages of a long
+ * prefix: the prefix's keys and values are read once per group and meet all of its rows together.
+ * Sequence b belongs to group[b] (0 .. n_groups-1; -1: to none).  The first prefix_len[g] / 16 entries (whole pages; a
+ * rest counts to the sequences) of the members' block table rows must be the same pages.  A member whose block begins
+ * inside these pages (seq_len[b] - (gamma[b]+1) < 16 * pages) is computed by itself; so is the only member of a group.
+ * Device-detected: as spec_verify_attn; group[b] outside [-1, n_groups) or prefix_len[g] negative or beyond the table
+ * row -> SV_DEV_BAD_LEN, the sequence or group is computed without sharing.  Four launches.
+ */
+typedef struct sv_attn_prefix_params {
+    sv_attn_params attn;        /* batch at most 8192, hq / hkv at most 128 */
+    const int32_t *group;       /* device [batch] */
+    const int32_t *prefix_len;  /* device [n_groups], tokens */
+    int32_t n_groups;           /* 1 .. batch */
+} sv_attn_prefix_params;
+
+size_t spec_verify_attn_prefix_workspace_bytes(int32_t batch, int32_t gamma_max, int32_t hq, int32_t hkv, int32_t head_dim,
+                                               int32_t n_groups);
+
+sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, void *workspace_device, size_t workspace_bytes,
+                                  void *stream);
+
 /* ---------------------------------------------------------------- all layers of a step */
 /*
  * A target model keeps one KV cache per layer (KV caching, paper Section 5), all

@@ -334,3 +334,65 @@ def token_counts_update(counts, vocab, tokens, first, n, reset=None, prompt=Fals
     lib.oracle_token_counts_update(_p(c), ctypes.c_int64(c.shape[1]), ctypes.c_int(vocab), ctypes.c_int(c.shape[0]), _p(t), _p(f), _p(m),
                                    None if r is None else _p(r), ctypes.c_int(int(prompt)))
     return c
+
+
+# --------------------------------------------------------------------------- long contexts: bounds, choice and listed pages
+def page_bounds_update(k_pool_bits, kv_strides, block_table, seq_len, first, bounds, scales, page_size=16):
+    """New (bounds int8 [n_pages, hkv, 2, D], scales float32 [n_pages, hkv]) with the pages of positions first[b] ..
+    seq_len[b] - 1 of every sequence brought up to date; the arguments are left alone."""
+    lib = _load()
+    bd, sc = np.array(bounds, np.int8, order="C", copy=True), np.array(scales, np.float32, order="C", copy=True)
+    bt, sl, f, st = _c(block_table, np.int32), _c(seq_len, np.int32), _c(first, np.int32), _c(kv_strides, np.int64)
+    assert k_pool_bits.dtype == np.uint16
+    lib.oracle_page_bounds_update(_p(k_pool_bits), _p(st), _p(bt), ctypes.c_int64(bt.shape[1]), _p(sl), _p(f), ctypes.c_int(len(sl)),
+                                  ctypes.c_int(bd.shape[1]), ctypes.c_int(bd.shape[3]), ctypes.c_int(page_size), _p(bd), _p(sc))
+    return bd, sc
+
+
+def page_choice(q_bits, bounds, scales, head, table_row, n_seen, n_select, n_first, n_last):
+    """One row and kv head: (scores float32 [n_seen], chosen bool [n_seen]); q_bits uint16 [G, D], the group's heads."""
+    lib = _load()
+    q, bd, sc, t = _c(q_bits, np.uint16), _c(bounds, np.int8), _c(scales, np.float32), _c(table_row, np.int32)
+    score, chosen = np.zeros(n_seen, np.float32), np.zeros(n_seen, np.uint8)
+    lib.oracle_page_choice(_p(q), ctypes.c_int(q.shape[0]), ctypes.c_int(q.shape[1]), _p(bd), _p(sc), ctypes.c_int(bd.shape[1]),
+                           ctypes.c_int(head), _p(t), ctypes.c_int(n_seen), ctypes.c_int(n_select), ctypes.c_int(n_first),
+                           ctypes.c_int(n_last), _p(score), _p(chosen))
+    return score, chosen != 0
+
+
+def page_select(q_bits, bounds, scales, block_table, seq_len, gamma, cu_q, n_select, n_first, n_last, page_size=16):
+    """Lists of pages and row masks: [batch][hkv] of (pages ascending, masks), from page_choice row by row."""
+    hkv = bounds.shape[1]
+    G = q_bits.shape[1] // hkv
+    out = []
+    for b in range(len(seq_len)):
+        R, heads = int(gamma[b]) + 1, []
+        for h in range(hkv):
+            mask = {}
+            for i in range(R):
+                n_seen = (int(seq_len[b]) - R + i) // page_size + 1
+                _, chosen = page_choice(q_bits[cu_q[b] + i, h * G:(h + 1) * G], bounds, scales, h, block_table[b], n_seen, n_select,
+                                        n_first, n_last)
+                for p in np.nonzero(chosen)[0]:
+                    mask[int(p)] = mask.get(int(p), 0) | 1 << i
+            heads.append((sorted(mask), [mask[p] for p in sorted(mask)]))
+        out.append(heads)
+    return out
+
+
+def attn_pages(q_bits, k_pool_bits, v_pool_bits, kv_strides, block_table, seq_len, gamma, cu_q, hkv, scale, page_list=None,
+               row_mask=None, n_list=None, page_size=16):
+    """Attention over listed pages (all of a row's positions where the lists are None).  Returns (o, mag, lse), float64:
+    mag is the attention over |v|."""
+    lib = _load()
+    q = _c(q_bits, np.uint16)
+    n_rows, hq, D = q.shape
+    st, bt = _c(kv_strides, np.int64), _c(block_table, np.int32)
+    sl, g, cq = _c(seq_len, np.int32), _c(gamma, np.int32), _c(cu_q, np.int32)
+    pl, rm, nl = (None if a is None else _c(a, t) for a, t in ((page_list, np.int32), (row_mask, np.uint64), (n_list, np.int32)))
+    o, mag, lse = np.zeros((n_rows, hq, D)), np.zeros((n_rows, hq, D)), np.zeros((n_rows, hq))
+    ptr = lambda a: None if a is None else _p(a)  # noqa: E731
+    lib.oracle_attn_pages(_p(q), _p(k_pool_bits), _p(v_pool_bits), _p(st), _p(bt), ctypes.c_int64(bt.shape[1]), _p(sl), _p(g), _p(cq),
+                          ctypes.c_int(len(sl)), ctypes.c_int(hq), ctypes.c_int(hkv), ctypes.c_int(D), ctypes.c_int(page_size), ptr(pl),
+                          ptr(rm), ptr(nl), ctypes.c_int64(0 if pl is None else pl.shape[2]), ctypes.c_double(scale), _p(o), _p(mag), _p(lse))
+    return o, mag, lse

@@ -699,3 +699,153 @@ void oracle_token_counts_update(int16_t *counts, int64_t stride, int V, int batc
         }
     }
 }
+
+/* -------------------------------------------------------------------------
+ * Long contexts (KV caching, paper Section 5): a summary of every page's keys,
+ * the pages that a row reads by a score on it, attention over listed pages.
+ * The summary and the score are defined in float32, every operation rounded
+ * once, so that whole numbers and choices can be compared for equality.
+ * ------------------------------------------------------------------------- */
+static float bf16_bits_to_f32(uint16_t h)
+{
+    union { uint32_t u; float f; } x;
+    x.u = (uint32_t)h << 16;
+    return x.f;
+}
+
+static int whole(float x, float scale)
+{
+    if (!(scale > 0.f)) return 0;
+    float n = rintf(x / scale);                          /* half to even: the default rounding mode */
+    return n > 127.f ? 127 : n < -127.f ? -127 : (int)n;
+}
+
+/* pages first[b] / 16 .. of positions first[b] .. seq_len[b] - 1 of every sequence */
+void oracle_page_bounds_update(const uint16_t *k_pool, const int64_t *kv_strides, const int32_t *block_table, int64_t stride,
+                               const int32_t *seq_len, const int32_t *first, int batch, int hkv, int D, int page_size,
+                               int8_t *bounds, float *scales)
+{
+    for (int b = 0; b < batch; ++b)
+        for (int lp = first[b] / page_size; first[b] < seq_len[b] && lp * page_size < seq_len[b]; ++lp) {
+            int64_t page = block_table[b * stride + lp];
+            int n = seq_len[b] - lp * page_size < page_size ? seq_len[b] - lp * page_size : page_size;
+            for (int h = 0; h < hkv; ++h) {
+                float hi[256], lo[256], big = 0.f;
+                for (int d = 0; d < D; ++d) {
+                    hi[d] = -INFINITY;
+                    lo[d] = INFINITY;
+                    for (int s = 0; s < n; ++s) {
+                        float k = bf16_bits_to_f32(k_pool[page * kv_strides[0] + h * kv_strides[1] + s * kv_strides[2] + d * kv_strides[3]]);
+                        if (k > hi[d]) hi[d] = k;
+                        if (k < lo[d]) lo[d] = k;
+                    }
+                    if (fabsf(hi[d]) > big) big = fabsf(hi[d]);
+                    if (fabsf(lo[d]) > big) big = fabsf(lo[d]);
+                }
+                float scale = big * (1.f / 127.f);
+                int8_t *out = bounds + (page * hkv + h) * 2 * D;
+                for (int d = 0; d < D; ++d) {
+                    out[d] = (int8_t)whole(hi[d], scale);
+                    out[D + d] = (int8_t)whole(lo[d], scale);
+                }
+                scales[page * hkv + h] = scale;
+            }
+        }
+}
+
+/* chosen [n_seen]: 1 for the pages that one row and kv head reads; q: the group's heads [G, D] */
+void oracle_page_choice(const uint16_t *q, int G, int D, const int8_t *bounds, const float *scales, int hkv, int head,
+                        const int32_t *table, int n_seen, int n_select, int n_first, int n_last, float *score, uint8_t *chosen)
+{
+    float big = 0.f;
+    for (int e = 0; e < G * D; ++e)
+        if (fabsf(bf16_bits_to_f32(q[e])) > big) big = fabsf(bf16_bits_to_f32(q[e]));
+    float scale = big * (1.f / 127.f);
+    for (int p = 0; p < n_seen; ++p) {
+        const int8_t *bd = bounds + ((int64_t)table[p] * hkv + head) * 2 * D;
+        int best = 0;
+        for (int g = 0; g < G; ++g) {
+            int sum = 0;
+            for (int d = 0; d < D; ++d) {
+                int x = whole(bf16_bits_to_f32(q[g * D + d]), scale), u = x * bd[d], v = x * bd[D + d];
+                sum += u > v ? u : v;
+            }
+            if (g == 0 || sum > best) best = sum;
+        }
+        score[p] = (float)best * scales[(int64_t)table[p] * hkv + head];
+        chosen[p] = (uint8_t)(p < n_first || p >= n_seen - n_last || n_seen <= n_select);
+    }
+    for (int left = n_select - n_first - n_last; n_seen > n_select && left > 0; --left) {
+        int at = -1;
+        for (int p = 0; p < n_seen; ++p)
+            if (!chosen[p] && (at < 0 || score[p] > score[at])) at = p;      /* the lower page on ties */
+        chosen[at] = 1;
+    }
+}
+
+/* attention of one query row over the given positions; mag[d]: the weighted sum of |v_d|, what rounded weights err by */
+void oracle_attn_positions(const uint16_t *q_row, const uint16_t *k_pool, const uint16_t *v_pool, const int64_t *kv_strides,
+                           const int32_t *table, int page_size, int kv_head, int D, const int32_t *positions, int n, double scale,
+                           double *o, double *mag, double *lse)
+{
+    double *s = (double *)malloc(sizeof(double) * (size_t)(n > 0 ? n : 1)), m = -INFINITY, Z = 0.0;
+    for (int d = 0; d < D; ++d) o[d] = mag[d] = 0.0;
+    for (int j = 0; j < n; ++j) {
+        const uint16_t *k = k_pool + table[positions[j] / page_size] * kv_strides[0] + kv_head * kv_strides[1] +
+                            positions[j] % page_size * kv_strides[2];
+        double dot = 0.0;
+        for (int d = 0; d < D; ++d) dot += bf16_bits_to_f64(q_row[d]) * bf16_bits_to_f64(k[d * kv_strides[3]]);
+        s[j] = dot * scale;
+        if (s[j] > m) m = s[j];
+    }
+    for (int j = 0; j < n; ++j) {
+        const uint16_t *v = v_pool + table[positions[j] / page_size] * kv_strides[0] + kv_head * kv_strides[1] +
+                            positions[j] % page_size * kv_strides[2];
+        double e = exp(s[j] - m);
+        Z += e;
+        for (int d = 0; d < D; ++d) {
+            double x = bf16_bits_to_f64(v[d * kv_strides[3]]);
+            o[d] += e * x;
+            mag[d] += e * fabs(x);
+        }
+    }
+    for (int d = 0; d < D && n > 0; ++d) {
+        o[d] /= Z;
+        mag[d] /= Z;
+    }
+    *lse = n > 0 ? m + log(Z) : -INFINITY;
+    free(s);
+}
+
+/* listed pages with row masks; n_list NULL: every row reads all of its positions */
+void oracle_attn_pages(const uint16_t *q, const uint16_t *k_pool, const uint16_t *v_pool, const int64_t *kv_strides,
+                       const int32_t *block_table, int64_t stride, const int32_t *seq_len, const int32_t *gamma, const int32_t *cu_q,
+                       int batch, int hq, int hkv, int D, int page_size, const int32_t *page_list, const uint64_t *row_mask,
+                       const int32_t *n_list, int64_t list_stride, double scale, double *o, double *mag, double *lse)
+{
+    int G = hq / hkv;
+    for (int b = 0; b < batch; ++b) {
+        int R = gamma[b] + 1;
+#pragma omp parallel for schedule(dynamic)
+        for (int64_t it = 0; it < (int64_t)R * hq; ++it) {
+            int i = (int)(it / hq), h = (int)(it % hq), g = h / G, pos = seq_len[b] - R + i, n = 0;
+            int32_t *at = (int32_t *)malloc(sizeof(int32_t) * (size_t)(pos + 1));
+            if (n_list == NULL) {
+                for (n = 0; n <= pos; ++n) at[n] = n;
+            } else {
+                int64_t base = ((int64_t)b * hkv + g) * list_stride;
+                for (int e = 0; e < n_list[b * hkv + g]; ++e) {
+                    if (!((row_mask[base + e] >> i) & 1u)) continue;
+                    for (int s = 0; s < page_size; ++s) {
+                        int t = page_list[base + e] * page_size + s;
+                        if (t <= pos) at[n++] = t;
+                    }
+                }
+            }
+            int64_t row = ((int64_t)cu_q[b] + i) * hq + h;
+            oracle_attn_positions(q + row * D, k_pool, v_pool, kv_strides, block_table + b * stride, page_size, g, D, at, n, scale,
+                                  o + row * D, mag + row * D, lse + row);
+            free(at);
+        }
+    }
+}

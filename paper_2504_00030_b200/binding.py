@@ -29,6 +29,8 @@ EXPORTS = (
     "spec_verify_step_host", "spec_draft_stop_workspace_bytes", "spec_draft_stop", "spec_kv_append",
     "sv_selftest_wait_expiry", "spec_verify_attn_layers", "spec_draft_step_workspace_bytes", "spec_draft_step",
     "spec_kv_pages_update", "spec_rope_append", "spec_logits_adjust", "spec_token_counts_update",
+    "spec_page_bounds_update", "spec_page_select", "spec_page_select_workspace_bytes", "spec_verify_attn_pages",
+    "spec_verify_attn_pages_workspace_bytes", "spec_verify_attn_prefix", "spec_verify_attn_prefix_workspace_bytes",
 )
 
 
@@ -96,6 +98,31 @@ class TokenCountsParams(C.Structure):
                 ("batch", C.c_int32), ("tokens", C.c_void_p), ("token_stride", C.c_int64),
                 ("cu_tokens", C.c_void_p), ("n_tokens", C.c_int64), ("max_tokens", C.c_int32),
                 ("reset", C.c_void_p), ("prompt", C.c_int32), ("device_status", C.c_void_p)]
+
+
+class PageBoundsParams(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("bounds", C.c_void_p), ("scales", C.c_void_p), ("block_table", C.c_void_p),
+                ("block_table_stride", C.c_int64), ("seq_len", C.c_void_p), ("gamma", C.c_void_p),
+                ("first", C.c_void_p), ("batch", C.c_int32), ("max_new", C.c_int32), ("device_status", C.c_void_p)]
+
+
+class PageSelectParams(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("bounds", C.c_void_p), ("scales", C.c_void_p), ("n_pages", C.c_int64),
+                ("block_table", C.c_void_p), ("block_table_stride", C.c_int64), ("seq_len", C.c_void_p),
+                ("gamma", C.c_void_p), ("cu_q", C.c_void_p), ("batch", C.c_int32), ("gamma_max", C.c_int32),
+                ("hq", C.c_int32), ("hkv", C.c_int32), ("head_dim", C.c_int32), ("max_seq_len", C.c_int32),
+                ("n_select", C.c_int32), ("n_first", C.c_int32), ("n_last", C.c_int32), ("page_list", C.c_void_p),
+                ("row_mask", C.c_void_p), ("n_list", C.c_void_p), ("list_stride", C.c_int64),
+                ("device_status", C.c_void_p)]
+
+
+class AttnPagesParams(C.Structure):
+    _fields_ = [("attn", AttnParams), ("page_list", C.c_void_p), ("row_mask", C.c_void_p), ("n_list", C.c_void_p),
+                ("list_stride", C.c_int64)]
+
+
+class AttnPrefixParams(C.Structure):
+    _fields_ = [("attn", AttnParams), ("group", C.c_void_p), ("prefix_len", C.c_void_p), ("n_groups", C.c_int32)]
 
 
 class AcceptParams(C.Structure):
@@ -200,6 +227,20 @@ def load():
         lib.spec_logits_adjust.argtypes = [C.c_void_p, C.c_void_p]      # LogitsAdjustParams, or its bytes
         lib.spec_token_counts_update.restype = C.c_int32
         lib.spec_token_counts_update.argtypes = [C.c_void_p, C.c_void_p]      # TokenCountsParams, or its bytes
+        lib.spec_page_bounds_update.restype = C.c_int32
+        lib.spec_page_bounds_update.argtypes = [C.c_void_p, C.c_void_p]      # PageBoundsParams, or its bytes
+        lib.spec_page_select_workspace_bytes.restype = C.c_size_t
+        lib.spec_page_select_workspace_bytes.argtypes = [C.c_int32] * 4
+        lib.spec_page_select.restype = C.c_int32
+        lib.spec_page_select.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]      # PageSelectParams, or its bytes
+        lib.spec_verify_attn_pages_workspace_bytes.restype = C.c_size_t
+        lib.spec_verify_attn_pages_workspace_bytes.argtypes = [C.c_int32] * 5
+        lib.spec_verify_attn_pages.restype = C.c_int32
+        lib.spec_verify_attn_pages.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]      # AttnPagesParams, or its bytes
+        lib.spec_verify_attn_prefix_workspace_bytes.restype = C.c_size_t
+        lib.spec_verify_attn_prefix_workspace_bytes.argtypes = [C.c_int32] * 6
+        lib.spec_verify_attn_prefix.restype = C.c_int32
+        lib.spec_verify_attn_prefix.argtypes = [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]      # AttnPrefixParams, or its bytes
         lib.spec_draft_step.restype = C.c_int32
         lib.spec_draft_step.argtypes = [C.POINTER(DraftStepParams), C.c_void_p, C.c_size_t, C.c_void_p]
         lib.spec_verify_step_host.restype = C.c_int32
@@ -293,7 +334,11 @@ def _rows_on(t, dtype, name, index):
 def _packer(cls):
     """Packs field values as the C struct of a ctypes Structure has them: a third of the time that its constructor takes."""
     codes = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
-    return struct.Struct("@" + "".join(codes[ty] for _, ty in cls._fields_)).pack
+
+    def of(c):      # a nested struct's fields in its place: it is aligned as its first field, a pointer, is, and padded to one
+        return "".join(of(ty) + "0q" if issubclass(ty, C.Structure) else codes[ty] for _, ty in c._fields_)
+
+    return struct.Struct("@" + of(cls) + "0q").pack
 
 
 def _nbytes(t) -> int:
@@ -601,6 +646,152 @@ def spec_token_counts_update(token_counts, vocab, tokens=None, cu_tokens=None, m
     p = _pack_token_counts(*_token_counts_args(index, token_counts, vocab, tokens, cu_tokens, max_tokens, reset, prompt,
                                                device_status))
     _check("spec_token_counts_update", load().spec_token_counts_update(p, raw))
+
+
+# --------------------------------------------------------------------------- long contexts: pages that matter, shared prefixes
+def _pool_on(pool, index):
+    """Handle of a registered pool whose memory is on the current device."""
+    if pool.handle is None:
+        raise ValueError("the pool has been released")
+    if pool.k_pool.get_device() != index or pool.v_pool.get_device() != index:
+        raise ValueError(f"the pool's memory is not on the current device (cuda:{index})")
+    return pool.handle.value
+
+
+def _workspace_on(workspace, index):
+    if workspace is None or workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on the current device (cuda:{index})")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _table_on(block_table, batch, index):
+    if block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise ValueError("block_table must have one row per sequence")
+    return _on(block_table, torch.int32, "block_table", index), block_table.shape[1]
+
+
+def _bounds_on(bounds, scales, shape, index):
+    if tuple(bounds.shape) != shape:
+        raise ValueError(f"bounds must be {list(shape)}, got {list(bounds.shape)}")
+    return _on(bounds, torch.int8, "bounds", index), _on(scales, torch.float32, "scales", index, shape[0] * shape[1])
+
+
+def _page_bounds_args(index, pool, bounds, scales, block_table, seq_len, gamma=None, first=None, max_new=1, device_status=None):
+    i32, batch = torch.int32, seq_len.numel()
+    bp, sp = _bounds_on(bounds, scales, (pool.n_pages, pool.hkv, 2, pool.head_dim), index)
+    tp, ts = _table_on(block_table, batch, index)
+    return (_pool_on(pool, index), bp, sp, tp, ts, _on(seq_len, i32, "seq_len", index), _on(gamma, i32, "gamma", index, batch),
+            _on(first, i32, "first", index, batch), batch, max_new, _on(device_status, i32, "device_status", index))
+
+
+def page_bounds_params(*args, **kwargs) -> PageBoundsParams:
+    """Arguments of spec_page_bounds_update (without stream)."""
+    return PageBoundsParams(*_page_bounds_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_page_bounds = _packer(PageBoundsParams)
+
+
+def spec_page_bounds_update(pool, bounds, scales, block_table, seq_len, gamma=None, first=None, max_new=1, device_status=None,
+                            stream=None):
+    """Bounds of the keys of every page that holds a new position, in 8 bits with a scale per page and kv head
+    (asynchronous).  New are the gamma+1 positions of the draft block, or those from first on; max_new bounds their number."""
+    index, raw = _launch_at(stream, seq_len, "seq_len")
+    p = _pack_page_bounds(*_page_bounds_args(index, pool, bounds, scales, block_table, seq_len, gamma, first, max_new, device_status))
+    _check("spec_page_bounds_update", load().spec_page_bounds_update(p, raw))
+
+
+def spec_page_select_workspace_bytes(batch, gamma_max, hkv, max_seq_len) -> int:
+    return int(load().spec_page_select_workspace_bytes(batch, gamma_max, hkv, max_seq_len))
+
+
+def _lists_on(page_list, row_mask, n_list, batch, hkv, index):
+    if page_list.dim() != 3 or page_list.shape[0] != batch or page_list.shape[1] != hkv or row_mask.shape != page_list.shape:
+        raise ValueError("page_list and row_mask must be [batch, hkv, entries]")
+    return (_on(page_list, torch.int32, "page_list", index), _on(row_mask, torch.int64, "row_mask", index),
+            _on(n_list, torch.int32, "n_list", index, batch * hkv), page_list.shape[2])
+
+
+def _page_select_args(index, q, bounds, scales, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, n_select, n_first, n_last,
+                      page_list, row_mask, n_list, device_status=None):
+    i32, batch = torch.int32, seq_len.numel()
+    if q.dim() != 3 or bounds.dim() != 4:
+        raise ValueError("q must be [n_rows, hq, head_dim] and bounds [n_pages, hkv, 2, head_dim]")
+    _, hq, head_dim = q.shape
+    n_pages, hkv = bounds.shape[:2]
+    bp, sp = _bounds_on(bounds, scales, (n_pages, hkv, 2, head_dim), index)
+    tp, ts = _table_on(block_table, batch, index)
+    lp, mp, np_, width = _lists_on(page_list, row_mask, n_list, batch, hkv, index)
+    return (_on(q, torch.bfloat16, "q", index), bp, sp, n_pages, tp, ts, _on(seq_len, i32, "seq_len", index),
+            _on(gamma, i32, "gamma", index, batch), _on(cu_q, i32, "cu_q", index, batch + 1), batch, gamma_max, hq, hkv, head_dim,
+            max_seq_len, n_select, n_first, n_last, lp, mp, np_, width, _on(device_status, i32, "device_status", index))
+
+
+def page_select_params(*args, **kwargs) -> PageSelectParams:
+    """Arguments of spec_page_select (without workspace and stream)."""
+    return PageSelectParams(*_page_select_args(torch.cuda.current_device(), *args, **kwargs))
+
+
+_pack_page_select = _packer(PageSelectParams)
+
+
+def spec_page_select(q, bounds, scales, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, n_select, n_first, n_last,
+                     page_list, row_mask, n_list, workspace, device_status=None, stream=None):
+    """The n_select pages that each row of a block reads, by a score on the pages' bounds, as one list per sequence and kv
+    head with a mask of the rows that read each page (asynchronous).  row_mask: int64, bit i for row i."""
+    index, raw = _launch_at(stream, q, "q")
+    p = _pack_page_select(*_page_select_args(index, q, bounds, scales, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len,
+                                             n_select, n_first, n_last, page_list, row_mask, n_list, device_status))
+    _check("spec_page_select", load().spec_page_select(p, *_workspace_on(workspace, index), raw))
+
+
+def _attn_args(index, q, o, pool, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, sm_scale=None, lse=None,
+               device_status=None):
+    i32, batch = torch.int32, seq_len.numel()
+    if q.dim() != 3 or o.shape != q.shape:
+        raise ValueError("q and o must be [n_rows, hq, head_dim]")
+    n_rows, hq, head_dim = q.shape
+    tp, ts = _table_on(block_table, batch, index)
+    return (_on(q, torch.bfloat16, "q", index), _on(o, torch.bfloat16, "o", index), _on(lse, torch.float32, "lse", index, n_rows * hq),
+            _pool_on(pool, index), tp, ts, _on(seq_len, i32, "seq_len", index), _on(gamma, i32, "gamma", index, batch),
+            _on(cu_q, i32, "cu_q", index, batch + 1), batch, gamma_max, hq, pool.hkv, head_dim, max_seq_len,
+            sm_scale if sm_scale is not None else head_dim ** -0.5, _on(device_status, i32, "device_status", index))
+
+
+def spec_verify_attn_pages_workspace_bytes(batch, gamma_max, hq, hkv, head_dim) -> int:
+    return int(load().spec_verify_attn_pages_workspace_bytes(batch, gamma_max, hq, hkv, head_dim))
+
+
+_pack_attn_pages = _packer(AttnPagesParams)
+
+
+def spec_verify_attn_pages(q, o, pool, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, page_list, row_mask, n_list,
+                           workspace, sm_scale=None, lse=None, device_status=None, stream=None):
+    """Attention of the draft block over the listed pages, each row over those whose mask names it (asynchronous)."""
+    index, raw = _launch_at(stream, q, "q")
+    lists = _lists_on(page_list, row_mask, n_list, seq_len.numel(), pool.hkv, index)
+    p = _pack_attn_pages(*_attn_args(index, q, o, pool, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, sm_scale, lse,
+                                     device_status), *lists)
+    _check("spec_verify_attn_pages", load().spec_verify_attn_pages(p, *_workspace_on(workspace, index), raw))
+
+
+def spec_verify_attn_prefix_workspace_bytes(batch, gamma_max, hq, hkv, head_dim, n_groups) -> int:
+    return int(load().spec_verify_attn_prefix_workspace_bytes(batch, gamma_max, hq, hkv, head_dim, n_groups))
+
+
+_pack_attn_prefix = _packer(AttnPrefixParams)
+
+
+def spec_verify_attn_prefix(q, o, pool, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, group, prefix_len, workspace,
+                            sm_scale=None, lse=None, device_status=None, stream=None):
+    """Attention of the draft block against the paged KV cache of a batch in which the sequences of a group share the pages
+    of their first prefix_len[group] tokens: those are read once per group (asynchronous).  group[b] = -1: none."""
+    index, raw = _launch_at(stream, q, "q")
+    p = _pack_attn_prefix(*_attn_args(index, q, o, pool, block_table, seq_len, gamma, cu_q, gamma_max, max_seq_len, sm_scale, lse,
+                                      device_status),
+                          _on(group, torch.int32, "group", index, seq_len.numel()), _on(prefix_len, torch.int32, "prefix_len", index),
+                          prefix_len.numel())
+    _check("spec_verify_attn_prefix", load().spec_verify_attn_prefix(p, *_workspace_on(workspace, index), raw))
 
 
 # --------------------------------------------------------------------------- accept / resample

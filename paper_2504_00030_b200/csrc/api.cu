@@ -138,6 +138,9 @@ static sv_status check_attn(const sv_attn_params *p)
     return SV_OK;
 }
 
+// the same checks for the attention calls of other files
+sv_status sv::check_attn_params(const sv_attn_params *p) { return check_attn(p); }
+
 extern "C" size_t spec_verify_attn_workspace_bytes(int32_t batch, int32_t gamma_max, int32_t hq,
                                                    int32_t hkv, int32_t head_dim, int32_t max_seq_len)
 {

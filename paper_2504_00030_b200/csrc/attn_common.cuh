@@ -18,6 +18,9 @@ struct sv_kv_pool {
 
 namespace sv {
 
+// Argument checks of the verify attention (api.cu).
+sv_status check_attn_params(const sv_attn_params *p);
+
 // Attention on CUDA cores, one thread block per (query row, head).  Any head_dim <= 128;
 // used for shapes the tensor-core kernel does not cover and as a tiny-problem path.
 sv_status launch_attn_simple(const sv_attn_params &p, cudaStream_t stream);

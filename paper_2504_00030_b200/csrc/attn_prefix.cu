@@ -1,0 +1,208 @@
+// The verify attention of a batch whose sequences share long prefixes (spec_verify_attn_prefix).
+//
+// softmax over the keys of a row splits into parts: with m, l and o of the shared prefix (computed for all rows of a group
+// at once) and of the sequence's own keys, the row is (2^(m1-m) o1 + 2^(m2-m) o2) / (2^(m1-m) l1 + 2^(m2-m) l2).  Launches:
+//   plan      the members of each group and where their rows are;
+//   groups    the prefixes: 256 rows of any members meet each key tile (tensor-core bound; a rows * heads * head_dim fp32
+//             partial per group is written and read once, 520 bytes a row and head);
+//   sequences the rest of every sequence, finished with the group's partials;
+//   combine   pairs that were split over blocks.
+#include "attn_seg.cuh"
+
+namespace sv {
+
+constexpr int PLAN_THREADS = 256;
+constexpr int MAX_PREFIX_BATCH = 8192;
+
+// Block g: group g.  Two passes over the batch: how many members and rows, then where each member's rows go.
+__global__ void __launch_bounds__(PLAN_THREADS)
+prefix_plan_kernel(const __grid_constant__ SegLaunch a, const int32_t *prefix_len, int n_groups)
+{
+    pdl_enter();
+    const sv_attn_params &p = a.p;
+    const PrefixPlan &pl = a.plan;
+    const int g = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    __shared__ int s_sum[3][PLAN_THREADS / 32], s_rep;
+    const int len = prefix_len[g];
+    int pages = len / 16;
+    if (len < 0 || pages > p.block_table_stride) {
+        if (tid == 0) set_status(p.device_status, SV_DEV_BAD_LEN);
+        pages = 0;
+    }
+    if (tid == 0) s_rep = 0x7fffffff;
+    // rows of sequence b (0: skipped), its group
+    auto rows_of = [&](int b, int &gid) {
+        gid = a.seq_group[b];
+        if (gid < -1 || gid >= n_groups) {
+            if (g == 0) set_status(p.device_status, SV_DEV_BAD_LEN);
+            gid = -1;
+        }
+        const int gam = min(max(p.gamma[b], 0), p.gamma_max), L = p.seq_len[b];
+        if (L < gam + 1 || (long long)(L + 15) / 16 > p.block_table_stride || L > p.max_seq_len) return 0;
+        return gam + 1;
+    };
+    int before = 0, rows = 0, members = 0, rep = 0x7fffffff;
+    for (int b = tid; b < p.batch; b += PLAN_THREADS) {
+        int gid;
+        const int R = rows_of(b, gid);
+        if (gid >= 0 && gid < g) before += R;
+        if (gid == g && R > 0 && p.seq_len[b] - R >= 16 * pages) {
+            rows += R;
+            ++members;
+            rep = min(rep, b);
+        }
+        if (g == 0 && gid < 0) pl.seq_pages[b] = 0;
+    }
+    before = __reduce_add_sync(0xffffffffu, before);
+    rows = __reduce_add_sync(0xffffffffu, rows);
+    members = __reduce_add_sync(0xffffffffu, members);
+    rep = __reduce_min_sync(0xffffffffu, rep);
+    __syncthreads();
+    if (lane == 0) {
+        s_sum[0][warp] = before; s_sum[1][warp] = rows; s_sum[2][warp] = members;
+        atomicMin(&s_rep, rep);
+    }
+    __syncthreads();
+    before = rows = members = 0;
+    for (int w = 0; w < PLAN_THREADS / 32; ++w) { before += s_sum[0][w]; rows += s_sum[1][w]; members += s_sum[2][w]; }
+    if (members < 2) pages = 0;                        // nobody to share with
+    if (tid == 0) {
+        pl.grp_pages[g] = pages;
+        pl.grp_rep[g] = members > 0 ? s_rep : 0;
+        pl.grp_n[g] = pages > 0 ? rows : 0;
+        pl.grp_base[g] = before;
+    }
+    int at0 = 0;
+    for (int base = 0; base < p.batch; base += PLAN_THREADS) {
+        const int b = base + tid;
+        int R = 0, gid = -1;
+        if (b < p.batch) R = rows_of(b, gid);
+        const bool mine = b < p.batch && gid == g;
+        const bool member = mine && R > 0 && pages > 0 && p.seq_len[b] - R >= 16 * pages;
+        const int n = member ? R : 0;
+        int v = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += t;
+        }
+        __syncthreads();
+        if (lane == 31) s_sum[0][warp] = v;
+        __syncthreads();
+        int at = at0 + v - n;
+        for (int w = 0; w < PLAN_THREADS / 32; ++w) {
+            if (w < warp) at += s_sum[0][w];
+            at0 += s_sum[0][w];
+        }
+        if (mine) {
+            pl.seq_pages[b] = member ? pages : 0;
+            pl.seq_at[b] = at;
+        }
+        if (member)
+            for (int i = 0; i < R; ++i) pl.row_list[before + at + i] = p.cu_q[b] + i;
+    }
+}
+
+// ---------------------------------------------------------------------------- host side
+// Pairs of the group launch: every group's rows in chunks of 2 * ppl positions, per kv head.
+static long long prefix_max_pairs(int batch, int gamma_max, int group, int hkv, int n_groups)
+{
+    const long long ppp = 2 * (128 / group), rows = (long long)batch * (gamma_max + 1);
+    return (rows / ppp + n_groups) * hkv;
+}
+
+struct PrefixLayout {
+    size_t at[16], bytes;
+};
+
+static PrefixLayout prefix_layout(int batch, int gamma_max, int hq, int hkv, int n_groups)
+{
+    const int group = hq / hkv;
+    const long long pairs = prefix_max_pairs(batch, gamma_max, group, hkv, n_groups);
+    const size_t w = sizeof(int32_t);
+    const size_t sizes[] = {
+        n_groups * w, n_groups * w, n_groups * w, n_groups * w,               // grp_pages, grp_rep, grp_n, grp_base
+        (size_t)batch * (gamma_max + 1) * w, batch * w, batch * w,            // row_list, seq_pages, seq_at
+        n_groups * w, n_groups * w,                                           // grp_tile0, grp_pair0
+        (size_t)pairs * w, (size_t)pairs * w,                                 // pair_first, pair_last
+        (SEG_MAX_GRID + 1) * w, SEG_MAX_GRID * 4 * w,                         // bounds, desc of the group launch
+        seg_table_bytes(),                                                    // bounds and desc of the sequences' launch
+        seg_part_bytes(seg_nl(group * (gamma_max + 1))),                      // partials of the sequences' launch
+        (size_t)(pairs + seg_grid(2)) * seg_slot_floats(256) * sizeof(float), // partials of the group launch
+    };
+    PrefixLayout l;
+    size_t at = 0;
+    for (int i = 0; i < 16; ++i) {
+        l.at[i] = at;
+        at += seg_round(sizes[i]);
+    }
+    l.bytes = at;
+    return l;
+}
+
+template <int NL>
+static sv_status launch_sequences(SegLaunch &a, cudaStream_t s)
+{
+    const int grid = seg_grid(NL);
+    sv_status st = a.p.head_dim == 128 ? launch_seg<SEG_SEQ, NL, 128>(a, grid, true, s) : launch_seg<SEG_SEQ, NL, 64>(a, grid, true, s);
+    if (st != SV_OK) return st;
+    return a.p.head_dim == 128 ? launch_seg_combine<SEG_SEQ, NL, 128>(a, grid, s) : launch_seg_combine<SEG_SEQ, NL, 64>(a, grid, s);
+}
+
+}  // namespace sv
+
+extern "C" size_t spec_verify_attn_prefix_workspace_bytes(int32_t batch, int32_t gamma_max, int32_t hq, int32_t hkv, int32_t head_dim,
+                                                          int32_t n_groups)
+{
+    using namespace sv;
+    if (batch <= 0 || batch > MAX_PREFIX_BATCH || gamma_max < 0 || gamma_max > 4095 || hq <= 0 || hkv <= 0 || hq % hkv != 0 ||
+        hq / hkv > 128 || (head_dim != 64 && head_dim != 128) || n_groups <= 0 || n_groups > batch)
+        return 0;
+    return prefix_layout(batch, gamma_max, hq, hkv, n_groups).bytes;
+}
+
+extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace sv;
+    if (p == nullptr) return SV_EINVAL;
+    const sv_attn_params &at = p->attn;
+    sv_status st = check_attn_params(&at);
+    if (st != SV_OK) return st;
+    if (p->group == nullptr || p->prefix_len == nullptr || p->n_groups <= 0 || p->n_groups > at.batch) return SV_EINVAL;
+    if (at.batch > MAX_PREFIX_BATCH || at.gamma_max > 4095 || at.hq / at.hkv > 128 || !at.pool->has_maps) return SV_EUNSUPPORTED;
+    if (workspace == nullptr ||
+        workspace_bytes < spec_verify_attn_prefix_workspace_bytes(at.batch, at.gamma_max, at.hq, at.hkv, at.head_dim, p->n_groups))
+        return SV_EWORKSPACE;
+    if (!aligned16(workspace)) return SV_EALIGN;
+    if (seg_grid(1) > SEG_MAX_GRID) return SV_EUNSUPPORTED;
+    const PrefixLayout l = prefix_layout(at.batch, at.gamma_max, at.hq, at.hkv, p->n_groups);
+    uint8_t *w = static_cast<uint8_t *>(workspace);
+    auto ints = [&](int i) { return reinterpret_cast<int32_t *>(w + l.at[i]); };
+    SegLaunch a = {};
+    a.p = at;
+    a.n_pool_pages = at.pool->n_pages;
+    a.group = at.hq / at.hkv;
+    a.ppl = 128 / a.group;
+    a.seq_group = p->group;
+    PrefixPlan &pl = a.plan;
+    pl.grp_pages = ints(0); pl.grp_rep = ints(1); pl.grp_n = ints(2); pl.grp_base = ints(3);
+    pl.row_list = ints(4); pl.seq_pages = ints(5); pl.seq_at = ints(6);
+    pl.grp_tile0 = ints(7); pl.grp_pair0 = ints(8);
+    pl.pair_first = ints(9); pl.pair_last = ints(10);
+    pl.bounds = ints(11);
+    pl.part = reinterpret_cast<float *>(w + l.at[15]);
+    cudaStream_t s = (cudaStream_t)stream;
+    st = launch_kernel(true, prefix_plan_kernel, p->n_groups, PLAN_THREADS, 0, s, a, p->prefix_len, p->n_groups);
+    if (st != SV_OK) return st;
+    a.n_owners = p->n_groups;
+    a.bounds = pl.bounds;
+    a.desc = ints(12);
+    a.part = pl.part;
+    st = at.head_dim == 128 ? launch_seg<SEG_GROUP, 2, 128>(a, seg_grid(2), true, s) : launch_seg<SEG_GROUP, 2, 64>(a, seg_grid(2), true, s);
+    if (st != SV_OK) return st;
+    a.n_owners = at.batch;
+    a.bounds = ints(13);
+    a.desc = reinterpret_cast<int32_t *>(w + l.at[13] + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
+    a.part = reinterpret_cast<float *>(w + l.at[14]);
+    return seg_nl(a.group * (at.gamma_max + 1)) == 1 ? launch_sequences<1>(a, s) : launch_sequences<2>(a, s);
+}

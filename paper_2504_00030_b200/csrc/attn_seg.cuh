@@ -1,0 +1,892 @@
+// Attention over parts of the cache (tcgen05, sm_100a): the kernel behind spec_verify_attn_pages and
+// spec_verify_attn_prefix.
+//
+// Work.  An owner is what has keys of its own: a sequence, a (sequence, kv head) with its page list, or a group of
+// sequences with its shared prefix.  An owner's query rows -- positions times the group's query heads -- are cut into
+// tiles of 128 rows, NL tiles to a pair; a pair walks the owner's keys in tiles of TILE tokens.  The key tiles of all
+// pairs form one list that is shared out over the grid by cost (lengths and lists live on the device, so every block
+// finds its share in its prologue); a block's piece of a pair is a segment.  A segment that covers its pair writes the
+// output, one that does not leaves its unnormalised rows (fp32 O, running maximum and sum) in the workspace.
+//
+// NL = 1: one row tile, TILE = 64, 113 KB of shared memory and half of the tensor memory, so that two blocks share a
+//   multiprocessor: the one streams while the other changes pairs.  S is double buffered.  Taken where a pair has at most
+//   128 rows (G (gamma_max+1) <= 128): there the keys are read for few rows and HBM is the limit.
+// NL = 2: two row tiles that share each key tile of 128 tokens, one block a multiprocessor; while the tensor core works for
+//   one of them the softmax warps of the other have the exponentials.  Taken for more rows and for the groups, where the
+//   tensor core and the exponentials are the limit.
+//
+// Warps: 0 = TMA of K, 2 = TMA of V, 1 = MMA issuer and TMEM owner, 3 idle; then four softmax warps per row tile (thread = row
+// = TMEM lane).  All hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
+#pragma once
+
+#include "attn_common.cuh"
+#include "attn_softmax.cuh"
+#include "tc_ptx.cuh"
+
+#include <math_constants.h>
+
+namespace sv {
+
+enum SegKind { SEG_LIST = 0, SEG_SEQ = 1, SEG_GROUP = 2 };
+
+constexpr int SEG_MAX_GRID = 1024;
+constexpr int SEG_PITCH = 128;                 // floats between rows of a partial (both head sizes)
+constexpr int SEG_RING = 8;                    // most ring slots
+
+__host__ __device__ inline size_t seg_slot_floats(int rows) { return (size_t)rows * (SEG_PITCH + 2); }
+
+// What the plan of spec_verify_attn_prefix leaves for its attention launches.
+struct PrefixPlan {
+    int32_t *grp_pages;      // [n_groups] shared pages (0: nothing is shared)
+    int32_t *grp_rep;        // [n_groups] a member: its block table row has the pages
+    int32_t *grp_n;          // [n_groups] positions of all members
+    int32_t *grp_base;       // [n_groups] first of them in row_list
+    int32_t *row_list;       // query row of each position, group by group
+    int32_t *seq_pages;      // [batch] shared pages in front of the sequence (0: none)
+    int32_t *seq_at;         // [batch] first of the sequence's positions among its group's
+    int32_t *grp_tile0;      // [n_groups] first tile and first pair of a group in the group launch
+    int32_t *grp_pair0;      // [n_groups]
+    int32_t *pair_first;     // [pairs of the group launch] block that holds a pair's first tile,
+    int32_t *pair_last;      // and its last one
+    int32_t *bounds;         // [grid + 1] of the group launch
+    float *part;             // partials of the group launch: slot = pair + block
+};
+
+struct SegLaunch {
+    sv_attn_params p;
+    int64_t n_pool_pages;
+    int group;               // query heads per kv head
+    int ppl;                 // positions of a row tile: 128 / group
+    int n_slots;             // K/V ring slots
+    int n_owners;
+    const int32_t *page_list;      // SEG_LIST
+    const uint64_t *row_mask;
+    const int32_t *n_list;
+    int64_t list_stride;
+    const int32_t *seq_group;      // SEG_SEQ, SEG_GROUP
+    PrefixPlan plan;
+    int32_t *bounds;         // [grid + 1]: first tile of every block
+    int32_t *desc;           // [grid * 4]: a block's last segment, if its pair goes on: owner, sub, slot, tiles left
+    float *part;             // partials: block * 2 + (0: the block's first segment, 1: its last)
+};
+
+// The walk over (owner, pair of the owner, tile).
+struct SegCursor {
+    int o, s, t;             // owner, pair of the owner, tile of the pair
+    int n_sub, n_tiles;      // pairs of the owner, tiles of each
+    int pair;                // pairs before this one (SEG_GROUP)
+    int b, h, chunk;         // sequence (SEG_GROUP: group), kv head, row chunk
+    int R, L;                // positions of the owner, length (SEG_GROUP: of the prefix)
+    int n_pages, page0;      // pages to read: entries of the list, or of the table from page0 on
+};
+
+// Pairs and tiles of owner c.o (0 tiles: nothing to do); fills the owner's part of the cursor.
+template <int KIND, int NL, int TILE>
+__device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool report)
+{
+    constexpr int PPT = TILE / 16;
+    const sv_attn_params &p = a.p;
+    const int ppp = NL * a.ppl;
+    c.n_sub = c.n_tiles = 0;
+    c.page0 = 0;
+    if (KIND == SEG_GROUP) {
+        c.b = c.o;
+        c.R = a.plan.grp_n[c.o];
+        c.n_pages = a.plan.grp_pages[c.o];
+        c.L = c.n_pages * 16;
+        if (c.R <= 0 || c.n_pages <= 0) return;
+        c.n_sub = p.hkv * ((c.R + ppp - 1) / ppp);
+        c.n_tiles = (c.n_pages + PPT - 1) / PPT;
+        return;
+    }
+    c.b = KIND == SEG_LIST ? c.o / p.hkv : c.o;
+    int g = p.gamma[c.b];
+    c.L = p.seq_len[c.b];
+    int n = KIND == SEG_LIST ? a.n_list[c.o] : a.plan.seq_pages[c.b];
+    if (g < 0 || g > p.gamma_max) {
+        if (report) set_status(p.device_status, SV_DEV_BAD_GAMMA);
+        g = min(max(g, 0), p.gamma_max);
+    }
+    c.R = g + 1;
+    if (c.L < c.R || (long long)(c.L + 15) / 16 > p.block_table_stride || c.L > p.max_seq_len) {
+        if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
+        return;
+    }
+    const int chunks = (c.R + ppp - 1) / ppp;
+    if (KIND == SEG_LIST) {
+        if (n < 0 || n > a.list_stride) {
+            if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
+            n = (int)min((long long)max(n, 0), (long long)a.list_stride);
+        }
+        c.n_pages = n;
+        c.n_sub = chunks;
+        c.n_tiles = max(1, (n + PPT - 1) / PPT);       // an empty list still has outputs
+    } else {
+        c.page0 = n;
+        c.n_pages = (c.L + 15) / 16 - n;
+        c.n_sub = p.hkv * chunks;
+        c.n_tiles = (c.n_pages + PPT - 1) / PPT;
+    }
+}
+
+template <int KIND, int NL>
+__device__ __forceinline__ void seg_pair(const SegLaunch &a, SegCursor &c)
+{
+    const int ppp = NL * a.ppl;
+    if (KIND == SEG_LIST) {
+        c.h = c.o - c.b * a.p.hkv;
+        c.chunk = c.s;
+    } else {
+        const int chunks = (c.R + ppp - 1) / ppp;
+        c.h = c.s / chunks;
+        c.chunk = c.s - c.h * chunks;
+    }
+}
+
+template <int KIND, int NL, int TILE>
+__device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
+{
+    c.t = 0;
+    ++c.pair;
+    if (++c.s >= c.n_sub) {
+        c.s = 0;
+        c.n_tiles = 0;
+        while (c.n_tiles == 0 && ++c.o < a.n_owners) seg_owner<KIND, NL, TILE>(a, c, false);
+        if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; c.b = c.h = c.chunk = 0; return; }     // past the end: never used
+    }
+    seg_pair<KIND, NL>(a, c);
+}
+
+struct SegShare {
+    long long t_begin, t_end;    // this block's tiles
+    int o, s, t, pair;           // where t_begin is
+};
+
+// The calling block's share, by the whole block (NT threads).  A pair costs its tiles and SEG_COST more; block 0 publishes
+// where each group begins, every block its first tile.
+template <int KIND, int NL, int TILE, int NT>
+__device__ __forceinline__ void seg_plan(const SegLaunch &a, int seg_cost, SegShare *sh, long long (*red)[NT / 32])
+{
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    SegCursor c;
+    long long cost = 0, tiles = 0;
+    for (int o = tid; o < a.n_owners; o += NT) {
+        c.o = o;
+        seg_owner<KIND, NL, TILE>(a, c, blockIdx.x == 0);
+        tiles += (long long)c.n_sub * c.n_tiles;
+        cost += c.n_tiles > 0 ? (long long)c.n_sub * (c.n_tiles + seg_cost) : 0;
+    }
+    auto warp_sum = [](long long v) {
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        return v;
+    };
+    cost = warp_sum(cost);
+    tiles = warp_sum(tiles);
+    if (lane == 0) { red[0][warp] = cost; red[1][warp] = tiles; }
+    __syncthreads();
+    long long cost_all = 0, tiles_all = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) { cost_all += red[0][w]; tiles_all += red[1][w]; }
+    const long long xb = blockIdx.x * cost_all / gridDim.x, xe = (blockIdx.x + 1LL) * cost_all / gridDim.x;
+    if (tid == 0) {
+        sh->t_begin = sh->t_end = tiles_all;
+        sh->o = a.n_owners; sh->s = sh->t = sh->pair = 0;
+    }
+    __syncthreads();
+    long long cost0 = 0, tiles0 = 0, pairs0 = 0;
+    for (int base = 0; base < a.n_owners; base += NT) {
+        c.o = base + tid;
+        c.n_sub = c.n_tiles = 0;
+        if (c.o < a.n_owners) seg_owner<KIND, NL, TILE>(a, c, false);
+        const long long w_cost = c.n_tiles > 0 ? (long long)c.n_sub * (c.n_tiles + seg_cost) : 0;
+        const long long w_tiles = (long long)c.n_sub * c.n_tiles, w_pairs = c.n_tiles > 0 ? c.n_sub : 0;
+        long long vc = w_cost, vt = w_tiles, vp = w_pairs;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long x = __shfl_up_sync(0xffffffffu, vc, d), y = __shfl_up_sync(0xffffffffu, vt, d),
+                            z = __shfl_up_sync(0xffffffffu, vp, d);
+            if (lane >= d) { vc += x; vt += y; vp += z; }
+        }
+        if (lane == 31) { red[0][warp] = vc; red[1][warp] = vt; red[2][warp] = vp; }
+        __syncthreads();
+        long long bc = cost0, bt = tiles0, bp = pairs0;
+#pragma unroll
+        for (int w = 0; w < NT / 32; ++w) {
+            if (w < warp) { bc += red[0][w]; bt += red[1][w]; bp += red[2][w]; }
+            cost0 += red[0][w]; tiles0 += red[1][w]; pairs0 += red[2][w];
+        }
+        const long long lo = bc + vc - w_cost, hi = bc + vc;
+        const long long tile_lo = bt + vt - w_tiles, pair_lo = bp + vp - w_pairs;
+        if (w_cost > 0) {
+            if (KIND == SEG_GROUP && blockIdx.x == 0) {
+                a.plan.grp_tile0[c.o] = (int)tile_lo;
+                a.plan.grp_pair0[c.o] = (int)pair_lo;
+            }
+            const int per = c.n_tiles + seg_cost;
+            if (lo <= xb && xb < hi) {
+                const long long j = (xb - lo) / per, off = min(xb - lo - j * per, (long long)c.n_tiles);
+                sh->t_begin = tile_lo + j * c.n_tiles + off;
+                sh->o = c.o; sh->s = (int)j; sh->t = (int)off; sh->pair = (int)(pair_lo + j);
+            }
+            if (lo <= xe && xe < hi) {
+                const long long j = (xe - lo) / per, off = min(xe - lo - j * per, (long long)c.n_tiles);
+                sh->t_end = tile_lo + j * c.n_tiles + off;
+            }
+        }
+        __syncthreads();
+    }
+    if (tid == 0) {
+        a.bounds[blockIdx.x] = (int)sh->t_begin;
+        if (blockIdx.x + 1 == gridDim.x) a.bounds[gridDim.x] = (int)tiles_all;
+        a.desc[blockIdx.x * 4] = -1;
+    }
+}
+
+template <int KIND, int NL, int TILE>
+__device__ __forceinline__ void seg_start(const SegLaunch &a, const SegShare &sh, SegCursor &c)
+{
+    c.o = sh.o; c.s = sh.s; c.t = sh.t; c.pair = sh.pair;
+    c.b = c.h = c.chunk = 0;
+    if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; return; }
+    seg_owner<KIND, NL, TILE>(a, c, false);
+    seg_pair<KIND, NL>(a, c);
+    if (c.t >= c.n_tiles) seg_next<KIND, NL, TILE>(a, c);
+}
+
+struct SegShared {
+    uint64_t full[SEG_RING];     // ring slot filled by TMA
+    uint64_t empty[SEG_RING];    // ring slot consumed by the tensor core
+    uint64_t s_full[2];          // S ready           (NL = 1: by tile parity; NL = 2: by row tile)
+    uint64_t p_full[2];          // P written
+    uint64_t o_done[2];          // P V finished
+    uint64_t q_full;             // a segment's query rows are in shared memory
+    uint64_t drained;            // tensor core idle (after an expired wait)
+    uint32_t tmem_base;
+    int abort_flag;
+    SegShare share;
+};
+
+// bounded_wait whose outcome a warp agrees on, so that it stays together when a wait is given up
+__device__ __forceinline__ bool seg_wait(uint32_t bar, uint32_t parity, int *abort_flag, uint32_t *status)
+{
+    return __all_sync(0xffffffffu, bounded_wait(bar, parity, abort_flag, status));
+}
+
+// The online softmax of one row's TILE scores, as softmax_tile, with the keys that the row may see given per page:
+// lim[j] is the last visible slot of the tile's page j (below 0: none; 15 or more: all).
+template <int TILE, int O_CHUNKS, typename WaitPV>
+__device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, const int (&lim)[TILE / 16], float c_scale,
+                                            bool first_tile, float &m_ref, float &l_sum, WaitPV &&wait_prev_pv)
+{
+    uint32_t s[TILE];
+#pragma unroll
+    for (int ch = 0; ch < TILE / 32; ++ch) tc_ld32_nowait(s_addr + ch * 32, s + ch * 32);
+    tc_wait_ld();
+    bool partial = false, none = false;
+#pragma unroll
+    for (int j = 0; j < TILE / 16; ++j) {
+        partial |= lim[j] >= 0 && lim[j] < 15;
+        none |= lim[j] < 0;
+    }
+    if (partial) {
+#pragma unroll
+        for (int c = 0; c < TILE; ++c)
+            if ((c & 15) > lim[c >> 4]) s[c] = 0xff800000u;     // -inf
+    } else if (none) {
+#pragma unroll
+        for (int c = 0; c < TILE; ++c)
+            if (lim[c >> 4] < 0) s[c] = 0xff800000u;
+    }
+    float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, m2 = -CUDART_INF_F, m3 = -CUDART_INF_F;
+#pragma unroll
+    for (int c = 0; c < TILE; c += 4) {
+        m0 = fmaxf(m0, __uint_as_float(s[c]));
+        m1 = fmaxf(m1, __uint_as_float(s[c + 1]));
+        m2 = fmaxf(m2, __uint_as_float(s[c + 2]));
+        m3 = fmaxf(m3, __uint_as_float(s[c + 3]));
+    }
+    const float m_tile = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * c_scale;
+    float factor = 1.f;
+    bool rescale = false;
+    if ((m_tile > m_ref + RESCALE_THRESHOLD || m_ref == -CUDART_INF_F) && m_tile > -CUDART_INF_F) {
+        rescale = m_ref > -CUDART_INF_F;
+        factor = rescale ? ex2_approx(m_ref - m_tile) : 1.f;
+        m_ref = m_tile;
+    }
+    const float m_use = (m_ref == -CUDART_INF_F) ? 0.f : m_ref;
+    if (rescale) l_sum *= factor;
+    // tensor-memory accesses are warp-wide: if any row of the warp has to rescale, the whole warp goes through (factor 1)
+    if (__any_sync(0xffffffffu, rescale && !first_tile)) {
+        if (!wait_prev_pv()) return false;
+        tc_fence_after();
+        const float f = (rescale && !first_tile) ? factor : 1.f;
+#pragma unroll
+        for (int ch = 0; ch < O_CHUNKS; ++ch) {
+            uint32_t o[32];
+            tc_ld32(o_addr + ch * 32, o);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+            tc_st32(o_addr + ch * 32, o);
+        }
+    }
+    // P = 2^(s*c - m_ref) as bf16 pairs over S: the tensor core multiplies bf16; the sums stay fp32 and unrounded, so P's
+    // rounding (2^-9 relative, independent from key to key) averages out below the output's own
+    float tile_sum = 0.f;
+#pragma unroll
+    for (int ch = 0; ch < TILE / 32; ++ch) {
+        float sum0 = 0.f, sum1 = 0.f;
+        uint32_t pk[16];
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+            const float e0 = ex2_approx(fmaf(__uint_as_float(s[ch * 32 + c]), c_scale, -m_use));
+            const float e1 = ex2_approx(fmaf(__uint_as_float(s[ch * 32 + c + 1]), c_scale, -m_use));
+            sum0 += e0;
+            sum1 += e1;
+            pk[c >> 1] = pack_bf16(e0, e1);
+        }
+        tile_sum += sum0 + sum1;
+        asm volatile(
+            "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+            "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(s_addr + ch * 16),
+            "r"(pk[0]), "r"(pk[1]), "r"(pk[2]), "r"(pk[3]), "r"(pk[4]), "r"(pk[5]), "r"(pk[6]), "r"(pk[7]), "r"(pk[8]),
+            "r"(pk[9]), "r"(pk[10]), "r"(pk[11]), "r"(pk[12]), "r"(pk[13]), "r"(pk[14]), "r"(pk[15])
+            : "memory");
+    }
+    l_sum += tile_sum;
+    return true;
+}
+
+// Partials of a sequence row's shared prefix: blocks first .. last of the group launch hold slots pair + block, the row is
+// row `row` of each.
+struct PrefixParts {
+    int pair, first, last, row;
+};
+
+__device__ __forceinline__ PrefixParts prefix_parts(const SegLaunch &a, int b, int h, int i, int hh)
+{
+    PrefixParts x;
+    const PrefixPlan &pl = a.plan;
+    const int g = a.seq_group[b], k = pl.seq_at[b] + i;
+    const int ppp = 2 * a.ppl, chunks = (pl.grp_n[g] + ppp - 1) / ppp;       // the group launch has two row tiles a pair
+    const int chunk = k / ppp, in = k - chunk * ppp, tile = in / a.ppl;
+    x.pair = pl.grp_pair0[g] + h * chunks + chunk;
+    x.first = pl.pair_first[x.pair];
+    x.last = pl.pair_last[x.pair];
+    x.row = tile * 128 + (in - tile * a.ppl) * a.group + hh;
+    return x;
+}
+__device__ __forceinline__ bool prefix_part_empty(const SegLaunch &a, int block)
+{
+    return a.plan.bounds[block] == a.plan.bounds[block + 1];
+}
+__device__ __forceinline__ const float *prefix_part_slot(const SegLaunch &a, const PrefixParts &x, int block)
+{
+    return a.plan.part + (size_t)(x.pair + block) * seg_slot_floats(256);
+}
+
+template <int NL> struct SegConfig {
+    static constexpr int TILE = NL == 1 ? 64 : 128;
+    static constexpr int THREADS = 128 + 128 * NL;
+    static constexpr int BLOCKS = NL == 1 ? 2 : 1;             // blocks per multiprocessor
+    static constexpr uint32_t TMEM_COLS = NL == 1 ? 256 : 512;
+    static constexpr int COST = NL == 1 ? 4 : 4;               // a pair's start and end, in key tiles
+};
+
+template <int KIND, int NL, int D>
+__global__ void __launch_bounds__(SegConfig<NL>::THREADS, SegConfig<NL>::BLOCKS)
+attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUtensorMap k_map,
+                const __grid_constant__ CUtensorMap v_map)
+{
+    constexpr int TILE = SegConfig<NL>::TILE, NT = SegConfig<NL>::THREADS;
+    constexpr int PPT = TILE / 16;                             // pages per tile
+    constexpr int HALF = TILE * 128;                           // bytes of a tile's 64 dims
+    constexpr int SLOT_BYTES = TILE * D * 2;
+    constexpr int Q_BYTES = 128 * D * 2;
+    constexpr uint32_t TMEM_COLS = SegConfig<NL>::TMEM_COLS;
+    constexpr int O_COL0 = 2 * TILE;                           // two S buffers, then O of each row tile
+    constexpr int OCH = D / 32;
+    pdl_enter();
+    extern __shared__ __align__(1024) uint8_t seg_smem[];
+    uint8_t *ring = seg_smem;
+    const sv_attn_params &p = a.p;
+    if ((smem_u32(ring) & 1023u) != 0) {                       // never seen; refuse rather than compute garbage
+        if (threadIdx.x == 0) set_status(p.device_status, SV_DEV_TIMEOUT);
+        return;
+    }
+    const int n_slots = a.n_slots;
+    uint8_t *q_smem = ring + (size_t)n_slots * SLOT_BYTES;
+    SegShared *sh = reinterpret_cast<SegShared *>(q_smem + (size_t)NL * Q_BYTES);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = a.group, ppl = a.ppl;
+
+    if (tid == 0) {
+        for (int i = 0; i < n_slots; ++i) {
+            mbar_init(smem_u32(&sh->full[i]), 1);
+            mbar_init(smem_u32(&sh->empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh->s_full[i]), 1);
+            mbar_init(smem_u32(&sh->p_full[i]), 128);
+            mbar_init(smem_u32(&sh->o_done[i]), 1);
+        }
+        mbar_init(smem_u32(&sh->q_full), 128 * NL);
+        mbar_init(smem_u32(&sh->drained), 1);
+        sh->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                     "r"(TMEM_COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // the plan's sums share the ring's memory, which no copy touches before the barrier below
+    seg_plan<KIND, NL, TILE, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(ring));
+    tc_fence_before();
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    tc_fence_after();
+
+    const long long t_begin = sh->share.t_begin, t_end = sh->share.t_end;
+    const uint32_t tmem = sh->tmem_base;
+    int *abort_flag = &sh->abort_flag;
+    uint32_t *status = p.device_status;
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (t_end > t_begin && (warp == 0 || warp == 2)) {
+            // ================================================================ TMA producers: warp 0 K, warp 2 V
+            SegCursor cur;
+            seg_start<KIND, NL, TILE>(a, sh->share, cur);
+            const bool is_v = warp == 2;
+            constexpr int HV = D / 64;                         // 64-dim halves of a page
+            const int page_in_tile = lane / HV, half = lane % HV;
+            uint32_t u = 0;                                    // tiles of this block so far
+            bool ok = true;
+            int ids = 0;                                       // lane l: page of entry ids_base + l
+            for (long long tg = t_begin; tg < t_end && ok;) {
+                const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+                const int32_t *table;
+                {
+                    const int tb = KIND == SEG_GROUP ? a.plan.grp_rep[cur.o] : cur.b;
+                    table = p.block_table + (long long)tb * p.block_table_stride;
+                }
+                const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
+                const int seq_pages = (cur.L + 15) / 16;
+                int ids_base = -1;
+                for (int ti = 0; ti < seg_tiles; ++ti, ++u) {
+                    const int e0 = (cur.t + ti) * PPT;
+                    if (ids_base < 0 || e0 + PPT > ids_base + 32) {          // the next 32 page ids
+                        ids_base = e0;
+                        const int e = e0 + lane;
+                        int phys = (int)a.n_pool_pages;        // out of range: TMA fills zeros, no traffic
+                        if (e < cur.n_pages) {
+                            int lp = cur.page0 + e;
+                            if (KIND == SEG_LIST) lp = list[e];
+                            int id = -1;
+                            if (KIND != SEG_LIST || (lp >= 0 && lp < seq_pages)) id = table[lp];
+                            if (id < 0 || id >= a.n_pool_pages) set_status(status, SV_DEV_BAD_PAGE);
+                            else phys = id;
+                        }
+                        ids = phys;
+                    }
+                    const int phys = __shfl_sync(0xffffffffu, ids, (e0 - ids_base + page_in_tile) & 31);
+                    const uint32_t item = 2 * u + (is_v ? 1 : 0);
+                    const uint32_t slot = item % (uint32_t)n_slots, use = item / (uint32_t)n_slots;
+                    const uint32_t full = smem_u32(&sh->full[slot]);
+                    if (use > 0) ok = seg_wait(smem_u32(&sh->empty[slot]), (use - 1) & 1, abort_flag, status);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(full, SLOT_BYTES);
+                    __syncwarp();
+                    if (lane < PPT * HV) {
+                        const uint32_t dst = smem_u32(ring + slot * SLOT_BYTES + half * HALF + page_in_tile * 2048);
+                        tma_load_4d(dst, is_v ? &v_map : &k_map, half * 64, 0, cur.h, phys, full);
+                    }
+                }
+                tg += seg_tiles;
+                cur.t += seg_tiles;
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+            }
+            if (!ok && lane == 0) {
+                // given up: the copies under way end before the block does (each slot's last use by this warp)
+                for (uint32_t k = 0; k < (uint32_t)n_slots && k < u; ++k) {
+                    const uint32_t item = 2 * (u - 1 - k) + (is_v ? 1 : 0);
+                    if (item + n_slots < 2 * u) break;
+                    const uint32_t bar = smem_u32(&sh->full[item % (uint32_t)n_slots]), par = (item / (uint32_t)n_slots) & 1;
+                    for (int it = 0; it < (1 << 20) && !mbar_try_wait(bar, par); ++it) { }
+                }
+            }
+        } else if (t_end > t_begin && warp == 1) {
+            // ================================================================ MMA issuer
+            const uint32_t idesc_qk = instr_desc(false, TILE), idesc_pv = instr_desc(true, D);
+            SegCursor cur;
+            seg_start<KIND, NL, TILE>(a, sh->share, cur);
+            uint32_t u = 0, seg_no = 0;
+            uint32_t cnt[2] = {0, 0};                          // NL = 2: tiles done per row tile; NL = 1: cnt[0] = u
+            bool ok = true;
+            for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
+                const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+                const int n_pos = cur.R - cur.chunk * NL * ppl;
+                const int lanes = NL == 2 && n_pos > ppl ? 2 : 1;
+                ok = seg_wait(smem_u32(&sh->q_full), seg_no & 1, abort_flag, status);
+                tc_fence_after();
+                auto issue_qk = [&](int l, int ti) {
+                    const uint32_t item = 2 * (u + ti), slot = item % (uint32_t)n_slots;
+                    ok = ok && seg_wait(smem_u32(&sh->full[slot]), (item / (uint32_t)n_slots) & 1, abort_flag, status);
+                    if (!ok) return;
+                    tc_fence_after();
+                    const int buf = NL == 2 ? l : (int)((u + ti) & 1);
+                    const uint64_t qd = smem_desc(smem_u32(q_smem + l * Q_BYTES), 16, 1024);
+                    const uint64_t kd = smem_desc(smem_u32(ring + slot * SLOT_BYTES), 16, 1024);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks)
+                            tc_mma_ss(tmem + buf * TILE, qd + (((ks >> 2) * 16384 + (ks & 3) * 32) >> 4),
+                                      kd + (((ks >> 2) * HALF + (ks & 3) * 32) >> 4), idesc_qk, ks > 0);
+                        tc_commit(smem_u32(&sh->s_full[buf]));
+                        if (l == lanes - 1) tc_commit(smem_u32(&sh->empty[slot]));         // K tile consumed
+                    }
+                    __syncwarp();
+                };
+                issue_qk(0, 0);
+                if (NL == 2) { if (lanes == 2) issue_qk(1, 0); }
+                else if (seg_tiles > 1) issue_qk(0, 1);
+                for (int ti = 0; ti < seg_tiles && ok; ++ti) {
+#pragma unroll
+                    for (int l = 0; l < NL; ++l) {
+                        if (l >= lanes || !ok) break;
+                        const uint32_t g = NL == 2 ? cnt[l] : u + ti;
+                        const int buf = NL == 2 ? l : (int)(g & 1);
+                        const uint32_t phase = NL == 2 ? g & 1 : (g >> 1) & 1;
+                        ok = seg_wait(smem_u32(&sh->p_full[buf]), phase, abort_flag, status);
+                        const uint32_t item = 2 * (u + ti) + 1, slot = item % (uint32_t)n_slots;
+                        if (ok) ok = seg_wait(smem_u32(&sh->full[slot]), (item / (uint32_t)n_slots) & 1, abort_flag, status);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t vd = smem_desc(smem_u32(ring + slot * SLOT_BYTES), HALF, 1024);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < TILE / 16; ++ks)
+                                tc_mma_ts(tmem + O_COL0 + l * 128, tmem + buf * TILE + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)),
+                                          idesc_pv, (ti > 0 || ks > 0) ? 1u : 0u);
+                            tc_commit(smem_u32(&sh->o_done[buf]));
+                            if (l == lanes - 1) tc_commit(smem_u32(&sh->empty[slot]));     // V tile consumed
+                        }
+                        __syncwarp();
+                        if (NL == 2) {
+                            ++cnt[l];
+                            if (ti + 1 < seg_tiles) issue_qk(l, ti + 1);
+                        } else if (ti + 2 < seg_tiles) {
+                            issue_qk(0, ti + 2);
+                        }
+                    }
+                }
+                u += seg_tiles;
+                tg += seg_tiles;
+                cur.t += seg_tiles;
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+            }
+            if (!ok) {                                         // given up: let the issued instructions finish
+                if (elect_one()) tc_commit(smem_u32(&sh->drained));
+                __syncwarp();
+                for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained), 0); ++it) { }
+            }
+        }
+    } else {
+        if (NL == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        if (t_end > t_begin) {
+            // ================================================================ softmax / epilogue, a thread per row
+            const int l = NL == 2 ? (warp - 4) >> 2 : 0;       // row tile
+            const int quarter = warp & 3;
+            const int r = quarter * 32 + lane;                 // row of the tile = TMEM lane
+            const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+            const uint32_t o_addr = tmem + lane_addr + O_COL0 + l * 128;
+            const float c_scale = p.sm_scale * 1.4426950408889634f;          // scores in log2 units
+            const int ri = r / G, hh = r - ri * G;             // position and head of the row within its tile
+            SegCursor cur;
+            seg_start<KIND, NL, TILE>(a, sh->share, cur);
+            uint32_t cnt = 0, seg_no = 0;                      // tiles of this row tile so far
+            bool ok = true;
+            for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
+                const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+                const int pos0 = cur.chunk * NL * ppl + l * ppl;               // first position of the row tile
+                const int n_pos = min(cur.R - pos0, ppl);
+                const bool tile_active = n_pos > 0;
+                const bool warp_active = tile_active && quarter * 32 < n_pos * G;
+                const bool row_ok = ri < n_pos;
+                const int i = pos0 + ri;
+                long long q_row = 0;
+                if (row_ok) {
+                    const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + i] : p.cu_q[cur.b] + i;
+                    q_row = (long long)at * p.hq + (long long)cur.h * G + hh;
+                }
+                // ---- this thread's query row into shared memory.  Every instruction that read the rows before has
+                // completed: this thread has seen the last S that they gave.
+                if (warp_active) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D);
+                    uint8_t *dst = q_smem + l * Q_BYTES + r * 128;
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) {
+                        const uint4 v = row_ok ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4 *>(dst + (c >> 3) * 16384 + (((c & 7) ^ (r & 7)) << 4)) = v;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                mbar_arrive(smem_u32(&sh->q_full));
+                const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
+                PrefixParts parts = {0, 0, -1, 0};
+                if (KIND == SEG_SEQ && whole && row_ok && cur.page0 > 0) parts = prefix_parts(a, cur.b, cur.h, i, hh);
+                const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
+                const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
+                const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
+                const int seq_pages = (cur.L + 15) / 16;
+                float m_ref = -CUDART_INF_F, l_sum = 0.f;
+                if (tile_active) {
+                    for (int ti = 0; ti < seg_tiles && ok; ++ti, ++cnt) {
+                        const int buf = NL == 2 ? l : (int)(cnt & 1);
+                        const uint32_t phase = NL == 2 ? cnt & 1 : (cnt >> 1) & 1;
+                        int lim[PPT];
+                        if (KIND == SEG_LIST) {
+#pragma unroll
+                            for (int j = 0; j < PPT; ++j) {
+                                const int e = (cur.t + ti) * PPT + j;
+                                lim[j] = -1;
+                                if (row_ok && e < cur.n_pages) {
+                                    const int lp = __ldg(list + e);
+                                    const uint64_t mk = __ldg(reinterpret_cast<const unsigned long long *>(masks) + e);
+                                    if (((mk >> i) & 1) && lp >= 0 && lp < seq_pages) lim[j] = max(last - lp * 16, -1);
+                                }
+                            }
+                        } else {
+                            const int tok0 = (cur.page0 + (cur.t + ti) * PPT) * 16;
+#pragma unroll
+                            for (int j = 0; j < PPT; ++j) lim[j] = last - tok0 - j * 16;
+                        }
+                        ok = seg_wait(smem_u32(&sh->s_full[buf]), phase, abort_flag, status);
+                        if (!ok) break;
+                        if (!warp_active) {                    // all 32 rows are padding
+                            mbar_arrive(smem_u32(&sh->p_full[buf]));
+                            continue;
+                        }
+                        tc_fence_after();
+                        ok = seg_softmax<TILE, OCH>(tmem + lane_addr + buf * TILE, o_addr, lim, c_scale, ti == 0, m_ref, l_sum, [&]() {
+                            const uint32_t g = cnt - 1;
+                            return seg_wait(smem_u32(&sh->o_done[NL == 2 ? l : (int)(g & 1)]), NL == 2 ? g & 1 : (g >> 1) & 1,
+                                            abort_flag, status);
+                        });
+                        if (!ok) break;
+                        tc_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(smem_u32(&sh->p_full[buf]));
+                    }
+                    if (!ok) break;
+                    if (warp_active) {
+                        const uint32_t g = cnt - 1;            // the last P V
+                        ok = seg_wait(smem_u32(&sh->o_done[NL == 2 ? l : (int)(g & 1)]), NL == 2 ? g & 1 : (g >> 1) & 1, abort_flag, status);
+                    }
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (!warp_active) {
+                    // nothing to write
+                } else if (KIND != SEG_GROUP && whole) {
+                    float m_all = m_ref, w0 = 1.f;
+                    if (KIND == SEG_SEQ && parts.last >= 0) {
+                        for (int c = parts.first; c <= parts.last; ++c)
+                            if (!prefix_part_empty(a, c))
+                                m_all = fmaxf(m_all, prefix_part_slot(a, parts, c)[256 * SEG_PITCH + parts.row]);
+                        w0 = m_ref == -CUDART_INF_F ? 0.f : exp2f(m_ref - m_all);
+                        l_sum *= w0;
+                        for (int c = parts.first; c <= parts.last; ++c)
+                            if (!prefix_part_empty(a, c)) {
+                                const float *slot = prefix_part_slot(a, parts, c) + 256 * SEG_PITCH + parts.row;
+                                l_sum += exp2f(slot[0] - m_all) * slot[256];
+                            }
+                    }
+                    const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
+                    __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
+#pragma unroll
+                    for (int ch = 0; ch < OCH; ++ch) {
+                        uint32_t o[32];
+                        tc_ld32(o_addr + ch * 32, o);
+                        if (row_ok) {
+                            if (KIND == SEG_SEQ && parts.last >= 0) {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * w0);
+                                for (int bl = parts.first; bl <= parts.last; ++bl) {
+                                    if (prefix_part_empty(a, bl)) continue;
+                                    const float *slot = prefix_part_slot(a, parts, bl);
+                                    const float w = exp2f(slot[256 * SEG_PITCH + parts.row] - m_all);
+                                    const float4 *x = reinterpret_cast<const float4 *>(slot + (size_t)parts.row * SEG_PITCH + ch * 32);
+#pragma unroll
+                                    for (int c = 0; c < 8; ++c) {
+                                        const float4 v = x[c];
+                                        o[4 * c] = __float_as_uint(fmaf(w, v.x, __uint_as_float(o[4 * c])));
+                                        o[4 * c + 1] = __float_as_uint(fmaf(w, v.y, __uint_as_float(o[4 * c + 1])));
+                                        o[4 * c + 2] = __float_as_uint(fmaf(w, v.z, __uint_as_float(o[4 * c + 2])));
+                                        o[4 * c + 3] = __float_as_uint(fmaf(w, v.w, __uint_as_float(o[4 * c + 3])));
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int c = 0; c < 32; c += 8) {
+                                uint4 w;
+                                w.x = pack_bf16(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv);
+                                w.y = pack_bf16(__uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
+                                w.z = pack_bf16(__uint_as_float(o[c + 4]) * inv, __uint_as_float(o[c + 5]) * inv);
+                                w.w = pack_bf16(__uint_as_float(o[c + 6]) * inv, __uint_as_float(o[c + 7]) * inv);
+                                *reinterpret_cast<uint4 *>(dst + ch * 32 + c) = w;
+                            }
+                        }
+                    }
+                    if (row_ok && p.lse != nullptr)
+                        p.lse[q_row] = l_sum > 0.f ? (m_all + log2f(l_sum)) * 0.6931471805599453f : -CUDART_INF_F;
+                } else {
+                    const int slot_rows = NL * 128;
+                    const size_t slot_no = KIND == SEG_GROUP ? (size_t)cur.pair + blockIdx.x : (size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
+                    float *slot = (KIND == SEG_GROUP ? a.plan.part : a.part) + slot_no * seg_slot_floats(slot_rows);
+                    const int row = l * 128 + r;
+#pragma unroll
+                    for (int ch = 0; ch < OCH; ++ch) {
+                        uint32_t o[32];
+                        tc_ld32(o_addr + ch * 32, o);
+                        if (row_ok) {
+#pragma unroll
+                            for (int c = 0; c < 32; c += 4)
+                                *reinterpret_cast<uint4 *>(slot + (size_t)row * SEG_PITCH + ch * 32 + c) =
+                                    make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                        }
+                    }
+                    if (row_ok) {
+                        slot[(size_t)slot_rows * SEG_PITCH + row] = m_ref;
+                        slot[(size_t)slot_rows * SEG_PITCH + slot_rows + row] = l_sum;
+                    }
+                }
+                tc_fence_before();
+                if (l == 0 && r == 0) {
+                    if (KIND == SEG_GROUP) {
+                        if (cur.t == 0) a.plan.pair_first[cur.pair] = blockIdx.x;
+                        if (cur.t + seg_tiles == cur.n_tiles) a.plan.pair_last[cur.pair] = blockIdx.x;
+                    } else if (cur.t == 0 && seg_tiles < cur.n_tiles) {
+                        // the pair goes on in the next blocks: this one's merges its parts
+                        int32_t *d = a.desc + blockIdx.x * 4;
+                        d[1] = cur.s;
+                        d[2] = blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
+                        d[3] = cur.n_tiles - seg_tiles;
+                        d[0] = cur.o;
+                    }
+                }
+                tg += seg_tiles;
+                cur.t += seg_tiles;
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------- pairs that were split over blocks
+constexpr int SEG_COMBINE_WARPS = 8;
+
+// Block c merges the pair that begins in block c of the main kernel and goes on behind it (gridDim.y shares the rows).
+template <int KIND, int NL, int D>
+__global__ void __launch_bounds__(SEG_COMBINE_WARPS * 32)
+attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid)
+{
+    constexpr int TILE = SegConfig<NL>::TILE, SLOT_ROWS = NL * 128;
+    pdl_enter();
+    const int32_t *d = a.desc + blockIdx.x * 4;
+    if (d[0] < 0) return;
+    const sv_attn_params &p = a.p;
+    SegCursor cur;
+    cur.o = d[0]; cur.s = d[1]; cur.t = cur.pair = 0;
+    const int first_slot = d[2], tiles_left = d[3];
+    seg_owner<KIND, NL, TILE>(a, cur, false);
+    seg_pair<KIND, NL>(a, cur);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.group;
+    const int pos0 = cur.chunk * NL * a.ppl, n_pos = min(cur.R - pos0, NL * a.ppl);
+    const bool lane_on = 4 * lane < D;
+    const size_t slot_floats = seg_slot_floats(SLOT_ROWS);
+    for (int k = blockIdx.y * SEG_COMBINE_WARPS + warp; k < n_pos * G; k += gridDim.y * SEG_COMBINE_WARPS) {
+        const int in = k / G, hh = k - in * G, i = pos0 + in;
+        const int tile = in / a.ppl, row = tile * 128 + (in - tile * a.ppl) * G + hh;
+        float m_run = -CUDART_INF_F, l_run = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](const float *slot, int rows, int r) {
+            const float m = slot[(size_t)rows * SEG_PITCH + r], l = slot[(size_t)rows * SEG_PITCH + rows + r];
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (lane_on) v = reinterpret_cast<const float4 *>(slot + (size_t)r * SEG_PITCH)[lane];
+            if (m == -CUDART_INF_F) return;
+            const float m_new = fmaxf(m_run, m), w_old = exp2f(m_run - m_new), w = exp2f(m - m_new);
+            l_run = l_run * w_old + l * w;
+            acc.x = acc.x * w_old + v.x * w;
+            acc.y = acc.y * w_old + v.y * w;
+            acc.z = acc.z * w_old + v.z * w;
+            acc.w = acc.w * w_old + v.w * w;
+            m_run = m_new;
+        };
+        add(a.part + (size_t)first_slot * slot_floats, SLOT_ROWS, row);
+        for (int c = blockIdx.x + 1, left = tiles_left; left > 0 && c < main_grid; ++c) {
+            const int n = a.bounds[c + 1] - a.bounds[c];
+            if (n <= 0) continue;
+            add(a.part + (size_t)c * 2 * slot_floats, SLOT_ROWS, row);
+            left -= n;
+        }
+        if (KIND == SEG_SEQ && cur.page0 > 0) {
+            const PrefixParts x = prefix_parts(a, cur.b, cur.h, i, hh);
+            for (int c = x.first; c <= x.last; ++c)
+                if (!prefix_part_empty(a, c)) add(prefix_part_slot(a, x, c), 256, x.row);
+        }
+        const long long q_row = ((long long)p.cu_q[cur.b] + i) * p.hq + (long long)cur.h * G + hh;
+        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+        if (lane_on) {
+            uint2 w;
+            w.x = pack_bf16(acc.x * inv, acc.y * inv);
+            w.y = pack_bf16(acc.z * inv, acc.w * inv);
+            reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + q_row * D)[lane] = w;
+        }
+        if (lane == 0 && p.lse != nullptr)
+            p.lse[q_row] = l_run > 0.f ? (m_run + log2f(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
+    }
+}
+
+// ---------------------------------------------------------------------------- host side
+inline int seg_nl(int rows) { return rows <= 128 ? 1 : 2; }
+inline int seg_grid(int nl) { return sm_count() * (nl == 1 ? 2 : 1); }
+inline size_t seg_round(size_t n) { return (n + 255) & ~(size_t)255; }
+// bounds, descriptors and partials of one launch
+inline size_t seg_table_bytes() { return seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)) + seg_round(SEG_MAX_GRID * 4 * sizeof(int32_t)); }
+inline size_t seg_part_bytes(int nl) { return (size_t)seg_grid(nl) * 2 * seg_slot_floats(nl * 128) * sizeof(float); }
+
+template <int KIND, int NL, int D>
+sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
+{
+    constexpr int slot_bytes = SegConfig<NL>::TILE * D * 2;
+    // shared memory of a multiprocessor less 1 KB that each block takes by itself
+    const size_t budget = 228 * 1024 / SegConfig<NL>::BLOCKS - 1024;
+    const size_t fixed = (size_t)NL * 128 * D * 2 + ((sizeof(SegShared) + 15) & ~(size_t)15);
+    a.n_slots = (int)((budget - fixed) / slot_bytes);
+    if (a.n_slots > SEG_RING) a.n_slots = SEG_RING;
+    if (a.n_slots < 4) return SV_EUNSUPPORTED;
+    const size_t smem = fixed + (size_t)a.n_slots * slot_bytes;
+    if (cudaFuncSetAttribute(attn_seg_kernel<KIND, NL, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        return SV_ECUDA;
+    return launch_kernel(early, attn_seg_kernel<KIND, NL, D>, grid, SegConfig<NL>::THREADS, smem, stream, a, a.p.pool->k_map,
+                         a.p.pool->v_map);
+}
+
+template <int KIND, int NL, int D>
+sv_status launch_seg_combine(const SegLaunch &a, int grid, cudaStream_t stream)
+{
+    return launch_kernel(true, attn_seg_combine_kernel<KIND, NL, D>, dim3((unsigned)grid, NL), SEG_COMBINE_WARPS * 32, 0, stream, a, grid);
+}
+
+}  // namespace sv
