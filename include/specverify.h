@@ -376,7 +376,7 @@ sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void *workspace_
  * rest counts to the sequences) of the members' block table rows must be the same pages.  A member whose block begins
  * inside these pages (seq_len[b] - (gamma[b]+1) < 16 * pages) is computed by itself; so is the only member of a group.
  * Device-detected: as spec_verify_attn; group[b] outside [-1, n_groups) or prefix_len[g] negative or beyond the table
- * row -> SV_DEV_BAD_LEN, the sequence or group is computed without sharing.  Four launches.
+ * row -> SV_DEV_BAD_LEN, the sequence or group is computed without sharing.  Five launches.
  */
 typedef struct sv_attn_prefix_params {
     sv_attn_params attn;        /* batch at most 8192, hq / hkv at most 128 */

@@ -6,7 +6,7 @@
 //   groups    the prefixes: 256 rows of any members meet each key tile (tensor-core bound; a rows * heads * head_dim fp32
 //             partial per group is written and read once, 520 bytes a row and head);
 //   sequences the rest of every sequence, finished with the group's partials;
-//   combine   pairs that were split over blocks.
+//   combine   behind either of the two: pairs that were split over blocks.
 #include "attn_seg.cuh"
 
 namespace sv {
@@ -111,8 +111,10 @@ static long long prefix_max_pairs(int batch, int gamma_max, int group, int hkv, 
     return (rows / ppp + n_groups) * hkv;
 }
 
+constexpr int PREFIX_PARTS = 13;
+
 struct PrefixLayout {
-    size_t at[16], bytes;
+    size_t at[PREFIX_PARTS], bytes;
 };
 
 static PrefixLayout prefix_layout(int batch, int gamma_max, int hq, int hkv, int n_groups)
@@ -123,21 +125,27 @@ static PrefixLayout prefix_layout(int batch, int gamma_max, int hq, int hkv, int
     const size_t sizes[] = {
         n_groups * w, n_groups * w, n_groups * w, n_groups * w,               // grp_pages, grp_rep, grp_n, grp_base
         (size_t)batch * (gamma_max + 1) * w, batch * w, batch * w,            // row_list, seq_pages, seq_at
-        n_groups * w, n_groups * w,                                           // grp_tile0, grp_pair0
-        (size_t)pairs * w, (size_t)pairs * w,                                 // pair_first, pair_last
-        (SEG_MAX_GRID + 1) * w, SEG_MAX_GRID * 4 * w,                         // bounds, desc of the group launch
+        n_groups * w, (size_t)pairs * w,                                      // grp_pair0, pair_first
+        seg_table_bytes(),                                                    // bounds and desc of the group launch
         seg_table_bytes(),                                                    // bounds and desc of the sequences' launch
         seg_part_bytes(seg_nl(group * (gamma_max + 1))),                      // partials of the sequences' launch
         (size_t)(pairs + seg_grid(2)) * seg_slot_floats(256) * sizeof(float), // partials of the group launch
     };
     PrefixLayout l;
     size_t at = 0;
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < PREFIX_PARTS; ++i) {
         l.at[i] = at;
         at += seg_round(sizes[i]);
     }
     l.bytes = at;
     return l;
+}
+
+template <int D>
+static sv_status launch_groups(SegLaunch &a, cudaStream_t s)
+{
+    const sv_status st = launch_seg<SEG_GROUP, 2, D>(a, seg_grid(2), true, s);
+    return st != SV_OK ? st : launch_seg_combine<SEG_GROUP, 2, D>(a, seg_grid(2), s);
 }
 
 template <int NL>
@@ -187,22 +195,21 @@ extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, voi
     PrefixPlan &pl = a.plan;
     pl.grp_pages = ints(0); pl.grp_rep = ints(1); pl.grp_n = ints(2); pl.grp_base = ints(3);
     pl.row_list = ints(4); pl.seq_pages = ints(5); pl.seq_at = ints(6);
-    pl.grp_tile0 = ints(7); pl.grp_pair0 = ints(8);
-    pl.pair_first = ints(9); pl.pair_last = ints(10);
-    pl.bounds = ints(11);
-    pl.part = reinterpret_cast<float *>(w + l.at[15]);
+    pl.grp_pair0 = ints(7); pl.pair_first = ints(8);
+    pl.part = reinterpret_cast<float *>(w + l.at[12]);
     cudaStream_t s = (cudaStream_t)stream;
     st = launch_kernel(true, prefix_plan_kernel, p->n_groups, PLAN_THREADS, 0, s, a, p->prefix_len, p->n_groups);
     if (st != SV_OK) return st;
+    auto tables = [&](int i) {
+        a.bounds = ints(i);
+        a.desc = reinterpret_cast<int32_t *>(w + l.at[i] + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
+    };
     a.n_owners = p->n_groups;
-    a.bounds = pl.bounds;
-    a.desc = ints(12);
-    a.part = pl.part;
-    st = at.head_dim == 128 ? launch_seg<SEG_GROUP, 2, 128>(a, seg_grid(2), true, s) : launch_seg<SEG_GROUP, 2, 64>(a, seg_grid(2), true, s);
+    tables(9);
+    st = at.head_dim == 128 ? launch_groups<128>(a, s) : launch_groups<64>(a, s);
     if (st != SV_OK) return st;
     a.n_owners = at.batch;
-    a.bounds = ints(13);
-    a.desc = reinterpret_cast<int32_t *>(w + l.at[13] + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
-    a.part = reinterpret_cast<float *>(w + l.at[14]);
+    tables(10);
+    a.part = reinterpret_cast<float *>(w + l.at[11]);
     return seg_nl(a.group * (at.gamma_max + 1)) == 1 ? launch_sequences<1>(a, s) : launch_sequences<2>(a, s);
 }

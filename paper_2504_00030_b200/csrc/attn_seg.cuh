@@ -8,20 +8,24 @@
 // finds its share in its prologue); a block's piece of a pair is a segment.  A segment that covers its pair writes the
 // output, one that does not leaves its unnormalised rows (fp32 O, running maximum and sum) in the workspace.
 //
-// NL = 1: one row tile, TILE = 64, 113 KB of shared memory and half of the tensor memory, so that two blocks share a
-//   multiprocessor: the one streams while the other changes pairs.  S is double buffered.  Taken where a pair has at most
-//   128 rows (G (gamma_max+1) <= 128): there the keys are read for few rows and HBM is the limit.
-// NL = 2: two row tiles that share each key tile of 128 tokens, one block a multiprocessor; while the tensor core works for
-//   one of them the softmax warps of the other have the exponentials.  Taken for more rows and for the groups, where the
-//   tensor core and the exponentials are the limit.
+// NL = 1: one row tile, 113 KB of shared memory and half of the tensor memory, so that two blocks share a multiprocessor:
+//   the one streams while the other changes pairs.  Taken where a pair has at most 128 rows (G (gamma_max+1) <= 128): there
+//   the keys are read for few rows and HBM is the limit.
+// NL = 2: two row tiles that share the key tiles, one block a multiprocessor; while the tensor core works for one of them
+//   the softmax warps of the other have the exponentials.  Taken for more rows and for the groups, where the tensor core and
+//   the exponentials are the limit.
+// A key tile has 64 tokens, so that every row tile has two S buffers in tensor memory (2 * 64 columns beside O's 128): the
+// scores of the next tile are there when the softmax of this one is done.  (128 tokens and one buffer, whose S = Q K^T is a
+// quarter cheaper on the tensor core: 600 us for the groups of 128 sequences behind three prefixes where this takes 520.)
 //
-// Warps: 0 = TMA of K, 2 = TMA of V, 1 = MMA issuer and TMEM owner, 3 idle; then four softmax warps per row tile (thread = row
-// = TMEM lane).  All hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
+// Warps: 0 = TMA of K, 2 = TMA of V, 1 and 3 = MMA issuers of the row tiles (1 owns the tensor memory; with one row tile 3
+// idles); then four softmax warps per row tile (thread = row = TMEM lane).  All hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
 #pragma once
 
 #include "attn_common.cuh"
 #include "attn_softmax.cuh"
 #include "tc_ptx.cuh"
+#include "work_share.cuh"
 
 #include <math_constants.h>
 
@@ -31,7 +35,9 @@ enum SegKind { SEG_LIST = 0, SEG_SEQ = 1, SEG_GROUP = 2 };
 
 constexpr int SEG_MAX_GRID = 1024;
 constexpr int SEG_PITCH = 128;                 // floats between rows of a partial (both head sizes)
-constexpr int SEG_RING = 8;                    // most ring slots
+constexpr int SEG_RING = 12;                   // most ring slots
+constexpr int SEG_TILE = 64;                   // tokens of a key tile
+constexpr int SEG_S_BUFS = 2;                  // S buffers of a row tile
 
 __host__ __device__ inline size_t seg_slot_floats(int rows) { return (size_t)rows * (SEG_PITCH + 2); }
 
@@ -44,11 +50,8 @@ struct PrefixPlan {
     int32_t *row_list;       // query row of each position, group by group
     int32_t *seq_pages;      // [batch] shared pages in front of the sequence (0: none)
     int32_t *seq_at;         // [batch] first of the sequence's positions among its group's
-    int32_t *grp_tile0;      // [n_groups] first tile and first pair of a group in the group launch
-    int32_t *grp_pair0;      // [n_groups]
-    int32_t *pair_first;     // [pairs of the group launch] block that holds a pair's first tile,
-    int32_t *pair_last;      // and its last one
-    int32_t *bounds;         // [grid + 1] of the group launch
+    int32_t *grp_pair0;      // [n_groups] first pair of a group in the group launch
+    int32_t *pair_first;     // [pairs of the group launch] block that holds a pair's first tile
     float *part;             // partials of the group launch: slot = pair + block
 };
 
@@ -66,7 +69,8 @@ struct SegLaunch {
     const int32_t *seq_group;      // SEG_SEQ, SEG_GROUP
     PrefixPlan plan;
     int32_t *bounds;         // [grid + 1]: first tile of every block
-    int32_t *desc;           // [grid * 4]: a block's last segment, if its pair goes on: owner, sub, slot, tiles left
+    int32_t *desc;           // [grid * 4]: a block's last segment, if its pair begins there and goes on: owner (else -1), pair
+                             // of the owner, slot of the partial, the pair's end in the list of tiles
     float *part;             // partials: block * 2 + (0: the block's first segment, 1: its last)
 };
 
@@ -81,10 +85,10 @@ struct SegCursor {
 };
 
 // Pairs and tiles of owner c.o (0 tiles: nothing to do); fills the owner's part of the cursor.
-template <int KIND, int NL, int TILE>
+template <int KIND, int NL>
 __device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool report)
 {
-    constexpr int PPT = TILE / 16;
+    constexpr int PPT = SEG_TILE / 16;
     const sv_attn_params &p = a.p;
     const int ppp = NL * a.ppl;
     c.n_sub = c.n_tiles = 0;
@@ -143,7 +147,7 @@ __device__ __forceinline__ void seg_pair(const SegLaunch &a, SegCursor &c)
     }
 }
 
-template <int KIND, int NL, int TILE>
+template <int KIND, int NL>
 __device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
 {
     c.t = 0;
@@ -151,120 +155,71 @@ __device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
     if (++c.s >= c.n_sub) {
         c.s = 0;
         c.n_tiles = 0;
-        while (c.n_tiles == 0 && ++c.o < a.n_owners) seg_owner<KIND, NL, TILE>(a, c, false);
+        while (c.n_tiles == 0 && ++c.o < a.n_owners) seg_owner<KIND, NL>(a, c, false);
         if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; c.b = c.h = c.chunk = 0; return; }     // past the end: never used
     }
     seg_pair<KIND, NL>(a, c);
 }
 
-struct SegShare {
-    long long t_begin, t_end;    // this block's tiles
-    int o, s, t, pair;           // where t_begin is
-};
-
-// The calling block's share, by the whole block (NT threads).  A pair costs its tiles and SEG_COST more; block 0 publishes
-// where each group begins, every block its first tile.
-template <int KIND, int NL, int TILE, int NT>
-__device__ __forceinline__ void seg_plan(const SegLaunch &a, int seg_cost, SegShare *sh, long long (*red)[NT / 32])
+// The calling block's share, by the whole block (NT threads); block 0 publishes where each group begins, every block its first
+// tile.
+template <int KIND, int NL, int NT>
+__device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, WorkShare *sh, long long (*red)[NT / 32])
 {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    SegCursor c;
-    long long cost = 0, tiles = 0;
-    for (int o = tid; o < a.n_owners; o += NT) {
-        c.o = o;
-        seg_owner<KIND, NL, TILE>(a, c, blockIdx.x == 0);
-        tiles += (long long)c.n_sub * c.n_tiles;
-        cost += c.n_tiles > 0 ? (long long)c.n_sub * (c.n_tiles + seg_cost) : 0;
-    }
-    auto warp_sum = [](long long v) {
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        return v;
-    };
-    cost = warp_sum(cost);
-    tiles = warp_sum(tiles);
-    if (lane == 0) { red[0][warp] = cost; red[1][warp] = tiles; }
-    __syncthreads();
-    long long cost_all = 0, tiles_all = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) { cost_all += red[0][w]; tiles_all += red[1][w]; }
-    const long long xb = blockIdx.x * cost_all / gridDim.x, xe = (blockIdx.x + 1LL) * cost_all / gridDim.x;
-    if (tid == 0) {
-        sh->t_begin = sh->t_end = tiles_all;
-        sh->o = a.n_owners; sh->s = sh->t = sh->pair = 0;
-    }
-    __syncthreads();
-    long long cost0 = 0, tiles0 = 0, pairs0 = 0;
-    for (int base = 0; base < a.n_owners; base += NT) {
-        c.o = base + tid;
-        c.n_sub = c.n_tiles = 0;
-        if (c.o < a.n_owners) seg_owner<KIND, NL, TILE>(a, c, false);
-        const long long w_cost = c.n_tiles > 0 ? (long long)c.n_sub * (c.n_tiles + seg_cost) : 0;
-        const long long w_tiles = (long long)c.n_sub * c.n_tiles, w_pairs = c.n_tiles > 0 ? c.n_sub : 0;
-        long long vc = w_cost, vt = w_tiles, vp = w_pairs;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, vc, d), y = __shfl_up_sync(0xffffffffu, vt, d),
-                            z = __shfl_up_sync(0xffffffffu, vp, d);
-            if (lane >= d) { vc += x; vt += y; vp += z; }
-        }
-        if (lane == 31) { red[0][warp] = vc; red[1][warp] = vt; red[2][warp] = vp; }
-        __syncthreads();
-        long long bc = cost0, bt = tiles0, bp = pairs0;
-#pragma unroll
-        for (int w = 0; w < NT / 32; ++w) {
-            if (w < warp) { bc += red[0][w]; bt += red[1][w]; bp += red[2][w]; }
-            cost0 += red[0][w]; tiles0 += red[1][w]; pairs0 += red[2][w];
-        }
-        const long long lo = bc + vc - w_cost, hi = bc + vc;
-        const long long tile_lo = bt + vt - w_tiles, pair_lo = bp + vp - w_pairs;
-        if (w_cost > 0) {
-            if (KIND == SEG_GROUP && blockIdx.x == 0) {
-                a.plan.grp_tile0[c.o] = (int)tile_lo;
-                a.plan.grp_pair0[c.o] = (int)pair_lo;
-            }
-            const int per = c.n_tiles + seg_cost;
-            if (lo <= xb && xb < hi) {
-                const long long j = (xb - lo) / per, off = min(xb - lo - j * per, (long long)c.n_tiles);
-                sh->t_begin = tile_lo + j * c.n_tiles + off;
-                sh->o = c.o; sh->s = (int)j; sh->t = (int)off; sh->pair = (int)(pair_lo + j);
-            }
-            if (lo <= xe && xe < hi) {
-                const long long j = (xe - lo) / per, off = min(xe - lo - j * per, (long long)c.n_tiles);
-                sh->t_end = tile_lo + j * c.n_tiles + off;
-            }
-        }
-        __syncthreads();
-    }
-    if (tid == 0) {
+    plan_work_share<NT>(
+        a.n_owners, pair_cost,
+        [&](int o, bool first) {
+            SegCursor c;
+            c.o = o;
+            seg_owner<KIND, NL>(a, c, first && blockIdx.x == 0);
+            return OwnerWork{c.n_sub, c.n_tiles};
+        },
+        [&](int o, int pair) {
+            if (KIND == SEG_GROUP && blockIdx.x == 0) a.plan.grp_pair0[o] = pair;
+        },
+        sh, red);
+    if (threadIdx.x == 0) {
         a.bounds[blockIdx.x] = (int)sh->t_begin;
-        if (blockIdx.x + 1 == gridDim.x) a.bounds[gridDim.x] = (int)tiles_all;
+        if (blockIdx.x + 1 == gridDim.x) a.bounds[gridDim.x] = (int)sh->total;
         a.desc[blockIdx.x * 4] = -1;
     }
 }
 
-template <int KIND, int NL, int TILE>
-__device__ __forceinline__ void seg_start(const SegLaunch &a, const SegShare &sh, SegCursor &c)
+template <int KIND, int NL>
+__device__ __forceinline__ void seg_start(const SegLaunch &a, const WorkShare &sh, SegCursor &c)
 {
     c.o = sh.o; c.s = sh.s; c.t = sh.t; c.pair = sh.pair;
     c.b = c.h = c.chunk = 0;
     if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; return; }
-    seg_owner<KIND, NL, TILE>(a, c, false);
+    seg_owner<KIND, NL>(a, c, false);
     seg_pair<KIND, NL>(a, c);
-    if (c.t >= c.n_tiles) seg_next<KIND, NL, TILE>(a, c);
+    if (c.t >= c.n_tiles) seg_next<KIND, NL>(a, c);
 }
 
 struct SegShared {
     uint64_t full[SEG_RING];     // ring slot filled by TMA
     uint64_t empty[SEG_RING];    // ring slot consumed by the tensor core
-    uint64_t s_full[2];          // S ready           (NL = 1: by tile parity; NL = 2: by row tile)
-    uint64_t p_full[2];          // P written
-    uint64_t o_done[2];          // P V finished
+    uint64_t s_full[4];          // S ready (row tile * 2 + parity of the key tile)
+    uint64_t p_full[4];          // P written
+    uint64_t o_done[4];          // P V finished
     uint64_t q_full;             // a segment's query rows are in shared memory
-    uint64_t drained;            // tensor core idle (after an expired wait)
+    uint64_t drained[2];         // a row tile's instructions are through (after an expired wait)
     uint32_t tmem_base;
     int abort_flag;
-    SegShare share;
+    WorkShare share;
+};
+
+// Place in the ring of the tiles' K (first = 0) or V (first = 1): the items K, V of tile 0, K, V of tile 1 ... take the slots in
+// turn.  Advanced by additions: divisions by the slot count cost the MMA warp more cycles than its instructions took.
+struct RingPos {
+    int slot;
+    uint32_t use;            // times the ring has wrapped
+    __device__ __forceinline__ explicit RingPos(int first) : slot(first), use(0) {}
+    __device__ __forceinline__ void next(int n_slots)
+    {
+        slot += 2;
+        if (slot >= n_slots) { slot -= n_slots; ++use; }
+    }
 };
 
 // bounded_wait whose outcome a warp agrees on, so that it stays together when a wait is given up
@@ -357,40 +312,28 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
     return true;
 }
 
-// Partials of a sequence row's shared prefix: blocks first .. last of the group launch hold slots pair + block, the row is
-// row `row` of each.
-struct PrefixParts {
-    int pair, first, last, row;
+// The partial of a sequence row's shared prefix: row `row` of a slot of the group launch (a pair's parts have been merged into
+// the first of them).
+struct PrefixPart {
+    const float *slot;       // NULL: nothing is shared
+    int row;
 };
 
-__device__ __forceinline__ PrefixParts prefix_parts(const SegLaunch &a, int b, int h, int i, int hh)
+__device__ __forceinline__ PrefixPart prefix_part(const SegLaunch &a, int b, int h, int i, int hh)
 {
-    PrefixParts x;
     const PrefixPlan &pl = a.plan;
     const int g = a.seq_group[b], k = pl.seq_at[b] + i;
     const int ppp = 2 * a.ppl, chunks = (pl.grp_n[g] + ppp - 1) / ppp;       // the group launch has two row tiles a pair
     const int chunk = k / ppp, in = k - chunk * ppp, tile = in / a.ppl;
-    x.pair = pl.grp_pair0[g] + h * chunks + chunk;
-    x.first = pl.pair_first[x.pair];
-    x.last = pl.pair_last[x.pair];
-    x.row = tile * 128 + (in - tile * a.ppl) * a.group + hh;
-    return x;
-}
-__device__ __forceinline__ bool prefix_part_empty(const SegLaunch &a, int block)
-{
-    return a.plan.bounds[block] == a.plan.bounds[block + 1];
-}
-__device__ __forceinline__ const float *prefix_part_slot(const SegLaunch &a, const PrefixParts &x, int block)
-{
-    return a.plan.part + (size_t)(x.pair + block) * seg_slot_floats(256);
+    const int pair = pl.grp_pair0[g] + h * chunks + chunk;
+    return {pl.part + (size_t)(pair + pl.pair_first[pair]) * seg_slot_floats(256), tile * 128 + (in - tile * a.ppl) * a.group + hh};
 }
 
 template <int NL> struct SegConfig {
-    static constexpr int TILE = NL == 1 ? 64 : 128;
     static constexpr int THREADS = 128 + 128 * NL;
     static constexpr int BLOCKS = NL == 1 ? 2 : 1;             // blocks per multiprocessor
     static constexpr uint32_t TMEM_COLS = NL == 1 ? 256 : 512;
-    static constexpr int COST = NL == 1 ? 4 : 4;               // a pair's start and end, in key tiles
+    static constexpr int COST = 4;                             // a pair's start and end, in key tiles
 };
 
 template <int KIND, int NL, int D>
@@ -398,13 +341,14 @@ __global__ void __launch_bounds__(SegConfig<NL>::THREADS, SegConfig<NL>::BLOCKS)
 attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUtensorMap k_map,
                 const __grid_constant__ CUtensorMap v_map)
 {
-    constexpr int TILE = SegConfig<NL>::TILE, NT = SegConfig<NL>::THREADS;
+    constexpr int TILE = SEG_TILE, NT = SegConfig<NL>::THREADS;
+    constexpr int NB = SEG_S_BUFS;
     constexpr int PPT = TILE / 16;                             // pages per tile
     constexpr int HALF = TILE * 128;                           // bytes of a tile's 64 dims
     constexpr int SLOT_BYTES = TILE * D * 2;
     constexpr int Q_BYTES = 128 * D * 2;
     constexpr uint32_t TMEM_COLS = SegConfig<NL>::TMEM_COLS;
-    constexpr int O_COL0 = 2 * TILE;                           // two S buffers, then O of each row tile
+    constexpr int O_COL0 = NL * NB * TILE;                     // the row tiles' S buffers, then their O
     constexpr int OCH = D / 32;
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t seg_smem[];
@@ -423,15 +367,15 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
             mbar_init(smem_u32(&sh->full[i]), 1);
-            mbar_init(smem_u32(&sh->empty[i]), 1);
+            mbar_init(smem_u32(&sh->empty[i]), NL);            // every row tile's MMA warp
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < NB * NL; ++i) {
             mbar_init(smem_u32(&sh->s_full[i]), 1);
             mbar_init(smem_u32(&sh->p_full[i]), 128);
             mbar_init(smem_u32(&sh->o_done[i]), 1);
         }
         mbar_init(smem_u32(&sh->q_full), 128 * NL);
-        mbar_init(smem_u32(&sh->drained), 1);
+        for (int i = 0; i < NL; ++i) mbar_init(smem_u32(&sh->drained[i]), 1);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -442,7 +386,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // the plan's sums share the ring's memory, which no copy touches before the barrier below
-    seg_plan<KIND, NL, TILE, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(ring));
+    seg_plan<KIND, NL, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(ring));
     tc_fence_before();
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
@@ -454,15 +398,17 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
     uint32_t *status = p.device_status;
 
     if (warp < 4) {
+        // of the block's registers (128 or 168 a thread at launch): 56 + 200 = 2 * 128, 56 + 2 * 224 = 3 * 168
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (t_end > t_begin && (warp == 0 || warp == 2)) {
             // ================================================================ TMA producers: warp 0 K, warp 2 V
             SegCursor cur;
-            seg_start<KIND, NL, TILE>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, cur);
             const bool is_v = warp == 2;
             constexpr int HV = D / 64;                         // 64-dim halves of a page
             const int page_in_tile = lane / HV, half = lane % HV;
             uint32_t u = 0;                                    // tiles of this block so far
+            RingPos at(is_v ? 1 : 0);
             bool ok = true;
             int ids = 0;                                       // lane l: page of entry ids_base + l
             for (long long tg = t_begin; tg < t_end && ok;) {
@@ -475,7 +421,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
                 const int seq_pages = (cur.L + 15) / 16;
                 int ids_base = -1;
-                for (int ti = 0; ti < seg_tiles; ++ti, ++u) {
+                for (int ti = 0; ti < seg_tiles; ++ti, ++u, at.next(n_slots)) {
                     const int e0 = (cur.t + ti) * PPT;
                     if (ids_base < 0 || e0 + PPT > ids_base + 32) {          // the next 32 page ids
                         ids_base = e0;
@@ -492,21 +438,19 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         ids = phys;
                     }
                     const int phys = __shfl_sync(0xffffffffu, ids, (e0 - ids_base + page_in_tile) & 31);
-                    const uint32_t item = 2 * u + (is_v ? 1 : 0);
-                    const uint32_t slot = item % (uint32_t)n_slots, use = item / (uint32_t)n_slots;
-                    const uint32_t full = smem_u32(&sh->full[slot]);
-                    if (use > 0) ok = seg_wait(smem_u32(&sh->empty[slot]), (use - 1) & 1, abort_flag, status);
+                    const uint32_t full = smem_u32(&sh->full[at.slot]);
+                    if (at.use > 0) ok = seg_wait(smem_u32(&sh->empty[at.slot]), (at.use - 1) & 1, abort_flag, status);
                     if (!ok) break;
                     if (lane == 0) mbar_expect_tx(full, SLOT_BYTES);
                     __syncwarp();
                     if (lane < PPT * HV) {
-                        const uint32_t dst = smem_u32(ring + slot * SLOT_BYTES + half * HALF + page_in_tile * 2048);
+                        const uint32_t dst = smem_u32(ring + at.slot * SLOT_BYTES + half * HALF + page_in_tile * 2048);
                         tma_load_4d(dst, is_v ? &v_map : &k_map, half * 64, 0, cur.h, phys, full);
                     }
                 }
                 tg += seg_tiles;
                 cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
             }
             if (!ok && lane == 0) {
                 // given up: the copies under way end before the block does (each slot's last use by this warp)
@@ -517,80 +461,89 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     for (int it = 0; it < (1 << 20) && !mbar_try_wait(bar, par); ++it) { }
                 }
             }
-        } else if (t_end > t_begin && warp == 1) {
-            // ================================================================ MMA issuer
+        } else if (t_end > t_begin && (warp == 1 || NL == 2)) {
+            // ================================================================ MMA issuers: a warp per row tile
+            // An issuing warp spends about half of its time on waits (130 cycles each, also for what is there already), and
+            // the tensor core's queue is short: with one warp for both row tiles a step of 64 keys took 2570 cycles
+            // where the instructions take 1290.
+            const int l = NL == 2 && warp == 3 ? 1 : 0;
             const uint32_t idesc_qk = instr_desc(false, TILE), idesc_pv = instr_desc(true, D);
             SegCursor cur;
-            seg_start<KIND, NL, TILE>(a, sh->share, cur);
-            uint32_t u = 0, seg_no = 0;
-            uint32_t cnt[2] = {0, 0};                          // NL = 2: tiles done per row tile; NL = 1: cnt[0] = u
+            seg_start<KIND, NL>(a, sh->share, cur);
+            uint32_t seg_no = 0, cnt = 0;                      // cnt: tiles of this row tile so far
+            RingPos k_at(0), v_at(1);                          // of the next Q K^T and the next P V
+            // What steers the loops and makes up the descriptors goes through a warp-wide reduction, whose result the
+            // compiler knows to be the same in all lanes: the operands of the instructions then stay in uniform registers,
+            // where otherwise each instruction waits for its operands to be moved there.
+            const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
+            const uint64_t qd = smem_desc(smem_u32(q_smem + l * Q_BYTES), 16, 1024);
+            int left = __reduce_max_sync(0xffffffffu, (int)(t_end - t_begin));
             bool ok = true;
-            for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
-                const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+            for (; left > 0 && ok; ++seg_no) {
+                const int seg_tiles = __reduce_max_sync(0xffffffffu, min(cur.n_tiles - cur.t, left));
                 const int n_pos = cur.R - cur.chunk * NL * ppl;
-                const int lanes = NL == 2 && n_pos > ppl ? 2 : 1;
+                const bool active = NL == 1 || l == 0 || __reduce_max_sync(0xffffffffu, n_pos > ppl ? 1 : 0) != 0;
                 ok = seg_wait(smem_u32(&sh->q_full), seg_no & 1, abort_flag, status);
                 tc_fence_after();
-                auto issue_qk = [&](int l, int ti) {
-                    const uint32_t item = 2 * (u + ti), slot = item % (uint32_t)n_slots;
-                    ok = ok && seg_wait(smem_u32(&sh->full[slot]), (item / (uint32_t)n_slots) & 1, abort_flag, status);
+                auto issue_qk = [&](int ti) {
+                    ok = ok && seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
                     if (!ok) return;
                     tc_fence_after();
-                    const int buf = NL == 2 ? l : (int)((u + ti) & 1);
-                    const uint64_t qd = smem_desc(smem_u32(q_smem + l * Q_BYTES), 16, 1024);
-                    const uint64_t kd = smem_desc(smem_u32(ring + slot * SLOT_BYTES), 16, 1024);
+                    const int buf = l * NB + (int)((cnt + ti) % NB);
+                    const uint64_t kd = smem_desc(smem_u32(ring + k_at.slot * SLOT_BYTES), 16, 1024);
                     if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            tc_mma_ss(tmem + buf * TILE, qd + (((ks >> 2) * 16384 + (ks & 3) * 32) >> 4),
+                            tc_mma_ss(tm + buf * TILE, qd + (((ks >> 2) * 16384 + (ks & 3) * 32) >> 4),
                                       kd + (((ks >> 2) * HALF + (ks & 3) * 32) >> 4), idesc_qk, ks > 0);
                         tc_commit(smem_u32(&sh->s_full[buf]));
-                        if (l == lanes - 1) tc_commit(smem_u32(&sh->empty[slot]));         // K tile consumed
+                        tc_commit(smem_u32(&sh->empty[k_at.slot]));            // K tile consumed
                     }
                     __syncwarp();
+                    k_at.next(n_slots);
                 };
-                issue_qk(0, 0);
-                if (NL == 2) { if (lanes == 2) issue_qk(1, 0); }
-                else if (seg_tiles > 1) issue_qk(0, 1);
-                for (int ti = 0; ti < seg_tiles && ok; ++ti) {
-#pragma unroll
-                    for (int l = 0; l < NL; ++l) {
-                        if (l >= lanes || !ok) break;
-                        const uint32_t g = NL == 2 ? cnt[l] : u + ti;
-                        const int buf = NL == 2 ? l : (int)(g & 1);
-                        const uint32_t phase = NL == 2 ? g & 1 : (g >> 1) & 1;
-                        ok = seg_wait(smem_u32(&sh->p_full[buf]), phase, abort_flag, status);
-                        const uint32_t item = 2 * (u + ti) + 1, slot = item % (uint32_t)n_slots;
-                        if (ok) ok = seg_wait(smem_u32(&sh->full[slot]), (item / (uint32_t)n_slots) & 1, abort_flag, status);
+                if (active) {
+                    issue_qk(0);
+                    if (NB > 1 && seg_tiles > 1) issue_qk(1);
+                    for (int ti = 0; ti < seg_tiles && ok; ++ti) {
+                        const uint32_t g = cnt + ti;
+                        const int buf = l * NB + (int)(g % NB);
+                        ok = seg_wait(smem_u32(&sh->p_full[buf]), (g / NB) & 1, abort_flag, status);
+                        if (ok) ok = seg_wait(smem_u32(&sh->full[v_at.slot]), v_at.use & 1, abort_flag, status);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint64_t vd = smem_desc(smem_u32(ring + slot * SLOT_BYTES), HALF, 1024);
+                        const uint64_t vd = smem_desc(smem_u32(ring + v_at.slot * SLOT_BYTES), HALF, 1024);
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < TILE / 16; ++ks)
-                                tc_mma_ts(tmem + O_COL0 + l * 128, tmem + buf * TILE + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)),
+                                tc_mma_ts(tm + O_COL0 + l * 128, tm + buf * TILE + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)),
                                           idesc_pv, (ti > 0 || ks > 0) ? 1u : 0u);
                             tc_commit(smem_u32(&sh->o_done[buf]));
-                            if (l == lanes - 1) tc_commit(smem_u32(&sh->empty[slot]));     // V tile consumed
+                            tc_commit(smem_u32(&sh->empty[v_at.slot]));        // V tile consumed
                         }
                         __syncwarp();
-                        if (NL == 2) {
-                            ++cnt[l];
-                            if (ti + 1 < seg_tiles) issue_qk(l, ti + 1);
-                        } else if (ti + 2 < seg_tiles) {
-                            issue_qk(0, ti + 2);
-                        }
+                        v_at.next(n_slots);
+                        if (ti + NB < seg_tiles) issue_qk(ti + NB);
+                    }
+                    cnt += seg_tiles;
+                } else {                                       // no rows in this row tile: pass the tiles on
+                    for (int ti = 0; ti < seg_tiles && ok; ++ti) {
+                        ok = seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
+                        if (ok && lane == 0) mbar_arrive(smem_u32(&sh->empty[k_at.slot]));
+                        if (ok) ok = seg_wait(smem_u32(&sh->full[v_at.slot]), v_at.use & 1, abort_flag, status);
+                        if (ok && lane == 0) mbar_arrive(smem_u32(&sh->empty[v_at.slot]));
+                        k_at.next(n_slots);
+                        v_at.next(n_slots);
                     }
                 }
-                u += seg_tiles;
-                tg += seg_tiles;
+                left -= seg_tiles;
                 cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
             }
             if (!ok) {                                         // given up: let the issued instructions finish
-                if (elect_one()) tc_commit(smem_u32(&sh->drained));
+                if (elect_one()) tc_commit(smem_u32(&sh->drained[l]));
                 __syncwarp();
-                for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained), 0); ++it) { }
+                for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained[l]), 0); ++it) { }
             }
         }
     } else {
@@ -606,7 +559,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             const float c_scale = p.sm_scale * 1.4426950408889634f;          // scores in log2 units
             const int ri = r / G, hh = r - ri * G;             // position and head of the row within its tile
             SegCursor cur;
-            seg_start<KIND, NL, TILE>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, cur);
             uint32_t cnt = 0, seg_no = 0;                      // tiles of this row tile so far
             bool ok = true;
             for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
@@ -636,8 +589,8 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 }
                 mbar_arrive(smem_u32(&sh->q_full));
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
-                PrefixParts parts = {0, 0, -1, 0};
-                if (KIND == SEG_SEQ && whole && row_ok && cur.page0 > 0) parts = prefix_parts(a, cur.b, cur.h, i, hh);
+                PrefixPart part = {nullptr, 0};
+                if (KIND == SEG_SEQ && whole && row_ok && cur.page0 > 0) part = prefix_part(a, cur.b, cur.h, i, hh);
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
                 const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
@@ -645,8 +598,8 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 float m_ref = -CUDART_INF_F, l_sum = 0.f;
                 if (tile_active) {
                     for (int ti = 0; ti < seg_tiles && ok; ++ti, ++cnt) {
-                        const int buf = NL == 2 ? l : (int)(cnt & 1);
-                        const uint32_t phase = NL == 2 ? cnt & 1 : (cnt >> 1) & 1;
+                        const int buf = l * NB + (int)(cnt % NB);
+                        const uint32_t phase = (cnt / NB) & 1;
                         int lim[PPT];
                         if (KIND == SEG_LIST) {
 #pragma unroll
@@ -673,8 +626,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         tc_fence_after();
                         ok = seg_softmax<TILE, OCH>(tmem + lane_addr + buf * TILE, o_addr, lim, c_scale, ti == 0, m_ref, l_sum, [&]() {
                             const uint32_t g = cnt - 1;
-                            return seg_wait(smem_u32(&sh->o_done[NL == 2 ? l : (int)(g & 1)]), NL == 2 ? g & 1 : (g >> 1) & 1,
-                                            abort_flag, status);
+                            return seg_wait(smem_u32(&sh->o_done[l * NB + (int)(g % NB)]), (g / NB) & 1, abort_flag, status);
                         });
                         if (!ok) break;
                         tc_wait_st();
@@ -684,7 +636,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     if (!ok) break;
                     if (warp_active) {
                         const uint32_t g = cnt - 1;            // the last P V
-                        ok = seg_wait(smem_u32(&sh->o_done[NL == 2 ? l : (int)(g & 1)]), NL == 2 ? g & 1 : (g >> 1) & 1, abort_flag, status);
+                        ok = seg_wait(smem_u32(&sh->o_done[l * NB + (int)(g % NB)]), (g / NB) & 1, abort_flag, status);
                     }
                     if (!ok) break;
                     tc_fence_after();
@@ -692,18 +644,13 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (!warp_active) {
                     // nothing to write
                 } else if (KIND != SEG_GROUP && whole) {
-                    float m_all = m_ref, w0 = 1.f;
-                    if (KIND == SEG_SEQ && parts.last >= 0) {
-                        for (int c = parts.first; c <= parts.last; ++c)
-                            if (!prefix_part_empty(a, c))
-                                m_all = fmaxf(m_all, prefix_part_slot(a, parts, c)[256 * SEG_PITCH + parts.row]);
-                        w0 = m_ref == -CUDART_INF_F ? 0.f : exp2f(m_ref - m_all);
-                        l_sum *= w0;
-                        for (int c = parts.first; c <= parts.last; ++c)
-                            if (!prefix_part_empty(a, c)) {
-                                const float *slot = prefix_part_slot(a, parts, c) + 256 * SEG_PITCH + parts.row;
-                                l_sum += exp2f(slot[0] - m_all) * slot[256];
-                            }
+                    float m_all = m_ref, w0 = 1.f, w1 = 0.f;
+                    if (KIND == SEG_SEQ && part.slot != nullptr) {
+                        const float m1 = part.slot[256 * SEG_PITCH + part.row], l1 = part.slot[256 * SEG_PITCH + 256 + part.row];
+                        m_all = fmaxf(m_ref, m1);                              // both have keys: finite
+                        w0 = exp2f(m_ref - m_all);
+                        w1 = exp2f(m1 - m_all);
+                        l_sum = l_sum * w0 + l1 * w1;
                     }
                     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
@@ -712,22 +659,15 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         uint32_t o[32];
                         tc_ld32(o_addr + ch * 32, o);
                         if (row_ok) {
-                            if (KIND == SEG_SEQ && parts.last >= 0) {
+                            if (KIND == SEG_SEQ && part.slot != nullptr) {
+                                const float4 *x = reinterpret_cast<const float4 *>(part.slot + (size_t)part.row * SEG_PITCH + ch * 32);
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * w0);
-                                for (int bl = parts.first; bl <= parts.last; ++bl) {
-                                    if (prefix_part_empty(a, bl)) continue;
-                                    const float *slot = prefix_part_slot(a, parts, bl);
-                                    const float w = exp2f(slot[256 * SEG_PITCH + parts.row] - m_all);
-                                    const float4 *x = reinterpret_cast<const float4 *>(slot + (size_t)parts.row * SEG_PITCH + ch * 32);
-#pragma unroll
-                                    for (int c = 0; c < 8; ++c) {
-                                        const float4 v = x[c];
-                                        o[4 * c] = __float_as_uint(fmaf(w, v.x, __uint_as_float(o[4 * c])));
-                                        o[4 * c + 1] = __float_as_uint(fmaf(w, v.y, __uint_as_float(o[4 * c + 1])));
-                                        o[4 * c + 2] = __float_as_uint(fmaf(w, v.z, __uint_as_float(o[4 * c + 2])));
-                                        o[4 * c + 3] = __float_as_uint(fmaf(w, v.w, __uint_as_float(o[4 * c + 3])));
-                                    }
+                                for (int c = 0; c < 8; ++c) {
+                                    const float4 v = x[c];
+                                    o[4 * c] = __float_as_uint(fmaf(w1, v.x, w0 * __uint_as_float(o[4 * c])));
+                                    o[4 * c + 1] = __float_as_uint(fmaf(w1, v.y, w0 * __uint_as_float(o[4 * c + 1])));
+                                    o[4 * c + 2] = __float_as_uint(fmaf(w1, v.z, w0 * __uint_as_float(o[4 * c + 2])));
+                                    o[4 * c + 3] = __float_as_uint(fmaf(w1, v.w, w0 * __uint_as_float(o[4 * c + 3])));
                                 }
                             }
 #pragma unroll
@@ -765,22 +705,20 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                 }
                 tc_fence_before();
-                if (l == 0 && r == 0) {
-                    if (KIND == SEG_GROUP) {
-                        if (cur.t == 0) a.plan.pair_first[cur.pair] = blockIdx.x;
-                        if (cur.t + seg_tiles == cur.n_tiles) a.plan.pair_last[cur.pair] = blockIdx.x;
-                    } else if (cur.t == 0 && seg_tiles < cur.n_tiles) {
-                        // the pair goes on in the next blocks: this one's merges its parts
+                if (l == 0 && r == 0 && cur.t == 0) {
+                    if (KIND == SEG_GROUP) a.plan.pair_first[cur.pair] = blockIdx.x;
+                    if (seg_tiles < cur.n_tiles) {
+                        // the pair goes on in the next blocks: the combine kernel's block of this number merges its parts
                         int32_t *d = a.desc + blockIdx.x * 4;
-                        d[1] = cur.s;
-                        d[2] = blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
-                        d[3] = cur.n_tiles - seg_tiles;
                         d[0] = cur.o;
+                        d[1] = cur.s;
+                        d[2] = KIND == SEG_GROUP ? cur.pair : blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
+                        d[3] = (int)(tg + cur.n_tiles);
                     }
                 }
                 tg += seg_tiles;
                 cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL, TILE>(a, cur);
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
             }
         }
     }
@@ -795,55 +733,101 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
 
 // ---------------------------------------------------------------------------- pairs that were split over blocks
 constexpr int SEG_COMBINE_WARPS = 8;
+constexpr int SEG_COMBINE_Y = 4;               // blocks that share a pair's rows
 
-// Block c merges the pair that begins in block c of the main kernel and goes on behind it (gridDim.y shares the rows).
+// Blocks (c, *) merge the pair that begins in block c of the main kernel and goes on behind it, a warp per row, four parts
+// in flight.  A group's parts are merged into the first of them, in place.
 template <int KIND, int NL, int D>
 __global__ void __launch_bounds__(SEG_COMBINE_WARPS * 32)
 attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid)
 {
-    constexpr int TILE = SegConfig<NL>::TILE, SLOT_ROWS = NL * 128;
+    constexpr int SLOT_ROWS = NL * 128;
     pdl_enter();
-    const int32_t *d = a.desc + blockIdx.x * 4;
-    if (d[0] < 0) return;
+    __shared__ int s_slot[SEG_MAX_GRID];
+    __shared__ int s_n;
+    const int4 d = *reinterpret_cast<const int4 *>(a.desc + blockIdx.x * 4);
+    if (d.x < 0) return;
     const sv_attn_params &p = a.p;
-    SegCursor cur;
-    cur.o = d[0]; cur.s = d[1]; cur.t = cur.pair = 0;
-    const int first_slot = d[2], tiles_left = d[3];
-    seg_owner<KIND, NL, TILE>(a, cur, false);
-    seg_pair<KIND, NL>(a, cur);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.group;
+    if (warp == 0) {
+        // the blocks behind this one whose tiles begin before the pair ends (empty ones hold nothing)
+        if (lane == 0) s_slot[0] = KIND == SEG_GROUP ? d.z + (int)blockIdx.x : d.z;
+        int n = 1;
+        for (int c0 = blockIdx.x + 1; c0 < main_grid; c0 += 32) {
+            const int c = c0 + lane;
+            const int lo = c < main_grid ? a.bounds[c] : 0x7fffffff, hi = c < main_grid ? a.bounds[c + 1] : 0;
+            const bool have = lo < d.w && hi > lo;
+            const unsigned m = __ballot_sync(0xffffffffu, have);
+            if (have) s_slot[n + __popc(m & ((1u << lane) - 1))] = KIND == SEG_GROUP ? d.z + c : c * 2;
+            n += __popc(m);
+            if (__any_sync(0xffffffffu, lo >= d.w)) break;
+        }
+        if (lane == 0) s_n = n;
+    }
+    SegCursor cur;
+    cur.o = d.x; cur.s = d.y; cur.t = cur.pair = 0;
+    seg_owner<KIND, NL>(a, cur, false);
+    seg_pair<KIND, NL>(a, cur);
+    __syncthreads();
+    const int n_parts = s_n;
     const int pos0 = cur.chunk * NL * a.ppl, n_pos = min(cur.R - pos0, NL * a.ppl);
     const bool lane_on = 4 * lane < D;
-    const size_t slot_floats = seg_slot_floats(SLOT_ROWS);
-    for (int k = blockIdx.y * SEG_COMBINE_WARPS + warp; k < n_pos * G; k += gridDim.y * SEG_COMBINE_WARPS) {
+    constexpr size_t slot_floats = (size_t)SLOT_ROWS * (SEG_PITCH + 2);
+    float *parts = KIND == SEG_GROUP ? a.plan.part : a.part;
+    for (int k = blockIdx.y * SEG_COMBINE_WARPS + warp; k < n_pos * G; k += SEG_COMBINE_Y * SEG_COMBINE_WARPS) {
         const int in = k / G, hh = k - in * G, i = pos0 + in;
         const int tile = in / a.ppl, row = tile * 128 + (in - tile * a.ppl) * G + hh;
         float m_run = -CUDART_INF_F, l_run = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](const float *slot, int rows, int r) {
-            const float m = slot[(size_t)rows * SEG_PITCH + r], l = slot[(size_t)rows * SEG_PITCH + rows + r];
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (lane_on) v = reinterpret_cast<const float4 *>(slot + (size_t)r * SEG_PITCH)[lane];
-            if (m == -CUDART_INF_F) return;
-            const float m_new = fmaxf(m_run, m), w_old = exp2f(m_run - m_new), w = exp2f(m - m_new);
-            l_run = l_run * w_old + l * w;
-            acc.x = acc.x * w_old + v.x * w;
-            acc.y = acc.y * w_old + v.y * w;
-            acc.z = acc.z * w_old + v.z * w;
-            acc.w = acc.w * w_old + v.w * w;
+        // four partials (those that are there: have[u]) into the running one
+        auto merge = [&](const float (&m)[4], const float (&l)[4], const float4 (&v)[4]) {
+            float m_new = m_run;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, m[u]);
+            if (m_new == -CUDART_INF_F) return;
+            const float w_old = exp2f(m_run - m_new);
+            acc.x *= w_old; acc.y *= w_old; acc.z *= w_old; acc.w *= w_old;
+            l_run *= w_old;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (m[u] == -CUDART_INF_F) continue;
+                const float w = exp2f(m[u] - m_new);
+                l_run += w * l[u];
+                acc.x += w * v[u].x; acc.y += w * v[u].y; acc.z += w * v[u].z; acc.w += w * v[u].w;
+            }
             m_run = m_new;
         };
-        add(a.part + (size_t)first_slot * slot_floats, SLOT_ROWS, row);
-        for (int c = blockIdx.x + 1, left = tiles_left; left > 0 && c < main_grid; ++c) {
-            const int n = a.bounds[c + 1] - a.bounds[c];
-            if (n <= 0) continue;
-            add(a.part + (size_t)c * 2 * slot_floats, SLOT_ROWS, row);
-            left -= n;
+        for (int j0 = 0; j0 < n_parts; j0 += 4) {
+            float m[4], l[4];
+            float4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool have = j0 + u < n_parts;
+                const float *slot = parts + (size_t)s_slot[have ? j0 + u : 0] * slot_floats;
+                m[u] = have ? slot[(size_t)SLOT_ROWS * SEG_PITCH + row] : -CUDART_INF_F;
+                l[u] = have ? slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row] : 0.f;
+                v[u] = have && lane_on ? reinterpret_cast<const float4 *>(slot + (size_t)row * SEG_PITCH)[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            merge(m, l, v);
+        }
+        if (KIND == SEG_GROUP) {
+            float *slot = parts + (size_t)s_slot[0] * slot_floats;
+            __syncwarp();
+            if (lane_on) reinterpret_cast<float4 *>(slot + (size_t)row * SEG_PITCH)[lane] = acc;
+            if (lane == 0) {
+                slot[(size_t)SLOT_ROWS * SEG_PITCH + row] = m_run;
+                slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row] = l_run;
+            }
+            continue;
         }
         if (KIND == SEG_SEQ && cur.page0 > 0) {
-            const PrefixParts x = prefix_parts(a, cur.b, cur.h, i, hh);
-            for (int c = x.first; c <= x.last; ++c)
-                if (!prefix_part_empty(a, c)) add(prefix_part_slot(a, x, c), 256, x.row);
+            const PrefixPart x = prefix_part(a, cur.b, cur.h, i, hh);
+            float m[4] = {x.slot[256 * SEG_PITCH + x.row], -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+            float l[4] = {x.slot[256 * SEG_PITCH + 256 + x.row], 0.f, 0.f, 0.f};
+            float4 v[4];
+            v[0] = v[1] = v[2] = v[3] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (lane_on) v[0] = reinterpret_cast<const float4 *>(x.slot + (size_t)x.row * SEG_PITCH)[lane];
+            merge(m, l, v);
         }
         const long long q_row = ((long long)p.cu_q[cur.b] + i) * p.hq + (long long)cur.h * G + hh;
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
@@ -869,7 +853,7 @@ inline size_t seg_part_bytes(int nl) { return (size_t)seg_grid(nl) * 2 * seg_slo
 template <int KIND, int NL, int D>
 sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
 {
-    constexpr int slot_bytes = SegConfig<NL>::TILE * D * 2;
+    constexpr int slot_bytes = SEG_TILE * D * 2;
     // shared memory of a multiprocessor less 1 KB that each block takes by itself
     const size_t budget = 228 * 1024 / SegConfig<NL>::BLOCKS - 1024;
     const size_t fixed = (size_t)NL * 128 * D * 2 + ((sizeof(SegShared) + 15) & ~(size_t)15);
@@ -886,7 +870,7 @@ sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
 template <int KIND, int NL, int D>
 sv_status launch_seg_combine(const SegLaunch &a, int grid, cudaStream_t stream)
 {
-    return launch_kernel(true, attn_seg_combine_kernel<KIND, NL, D>, dim3((unsigned)grid, NL), SEG_COMBINE_WARPS * 32, 0, stream, a, grid);
+    return launch_kernel(true, attn_seg_combine_kernel<KIND, NL, D>, dim3((unsigned)grid, SEG_COMBINE_Y), SEG_COMBINE_WARPS * 32, 0, stream, a, grid);
 }
 
 }  // namespace sv

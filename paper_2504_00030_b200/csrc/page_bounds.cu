@@ -7,6 +7,7 @@
 // and two dependent loads (table entry, keys) on draft blocks.
 #include "attn_common.cuh"
 #include "common.cuh"
+#include "whole8.cuh"
 
 namespace sv {
 
@@ -107,15 +108,9 @@ page_bounds_kernel(const __grid_constant__ PageBoundsLaunch a)
     for (int d = 1; d < 2 * LANES; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
     // every step rounds once to the nearest float32, so that the stored whole numbers are reproducible
     const float scale = __fmul_rn(big, 1.f / 127.f);
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        int n = scale > 0.f ? __float2int_rn(__fdiv_rn(x[c], scale)) : 0;
-        n = min(max(n, -127), 127);
-        w[c >> 2] |= (uint32_t)(n & 255) << (8 * (c & 3));
-    }
+    const uint2 w = whole8x8(x, scale, whole8_inverse(scale));
     const long long at = (long long)page * a.hkv + h;
-    if (slot0 < 2) *reinterpret_cast<uint2 *>(p.bounds + at * 2 * D + (low ? D : 0) + dim8 * 8) = make_uint2(w[0], w[1]);
+    if (slot0 < 2) *reinterpret_cast<uint2 *>(p.bounds + at * 2 * D + (low ? D : 0) + dim8 * 8) = w;
     if (lane == 0) p.scales[at] = scale;
 }
 

@@ -13,6 +13,8 @@
 // of the scores, held in registers; then the union over a block's rows as a list with a row mask per page.
 #include "attn_common.cuh"
 #include "tc_ptx.cuh"
+#include "whole8.cuh"
+#include "work_share.cuh"
 
 #include <climits>
 
@@ -25,9 +27,8 @@ struct PageSelectLaunch {
     sv_page_select_params p;
     int group;                                 // query heads per kv head
     int pos_per_chunk;                         // positions whose rows * heads fit the columns
-    int n_chunks;
-    int tiles_per_block;
-    int max_pages;                             // of a sequence
+    int max_cols;                              // columns of a product: the rows of a chunk, in multiples of 16
+    int n_tile_bufs;
     int score_stride;                          // floats between rows of scores
     int bit_words;                             // 32-page words of a row of chosen bits
     float *scores;                             // [batch * hkv][gamma_max + 1][score_stride]
@@ -72,15 +73,106 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d, uint64_t adesc, uint64_t b
         : "memory");
 }
 
+// Roles of the score kernel's 16 warps (128 registers a thread: with more warps and fewer registers the spills, which find
+// hardly any L1 beside 227 KB of shared memory, doubled its time): 0 and 1 bring tiles of bounds into shared memory, 2 issues
+// the products, 3..7 bring the rows' queries in 8 bits, 8..11 and 12..15 turn every other tile's products into scores.
+// Everything is double buffered (the tiles up to four times): bounds stream while the next pair's queries are made.
+constexpr int SC_THREADS = 512;
+constexpr int SC_MMA_WARP = 2, SC_Q_WARP0 = 3, SC_Q_WARPS = 5, SC_OUT_WARP0 = 8;
+constexpr int SC_MAX_TILES = 4;
+constexpr int SC_PAIR_COST = 1;                // a pair's queries, in tiles
+
 struct ScoreShared {
-    uint64_t done;
+    uint64_t tile_full[SC_MAX_TILES], tile_empty[SC_MAX_TILES];
+    uint64_t q_full[2], q_empty[2];
+    uint64_t acc_full[2], acc_empty[2];
+    uint64_t drained;
     uint32_t tmem_base;
     int abort_flag;
+    WorkShare share;
 };
 
-// D: head_dim.  128 threads; thread t owns page t of a tile.
+// The walk over (sequence, kv head and chunk of rows, tile of pages).
+struct ScoreCursor {
+    SeqRows sr;
+    int o, s, t, n_sub, n_tiles;
+    int h, i0, n_pos;            // kv head, first position of the chunk, its positions
+};
+
+__device__ __forceinline__ OwnerWork score_owner(const PageSelectLaunch &a, int b, SeqRows &sr)
+{
+    sr = seq_rows(a.p, b, false);
+    if (sr.R == 0 || sr.n_pages <= a.p.n_select) return {0, 0};        // every row takes all it sees: no scores
+    return {a.p.hkv * ((sr.R + a.pos_per_chunk - 1) / a.pos_per_chunk), (sr.n_pages + PS_PAGES - 1) / PS_PAGES};
+}
+__device__ __forceinline__ void score_pair(const PageSelectLaunch &a, ScoreCursor &c)
+{
+    const int chunks = (c.sr.R + a.pos_per_chunk - 1) / a.pos_per_chunk;
+    c.h = c.s / chunks;
+    c.i0 = (c.s - c.h * chunks) * a.pos_per_chunk;
+    c.n_pos = min(c.sr.R - c.i0, a.pos_per_chunk);
+}
+__device__ __forceinline__ void score_next(const PageSelectLaunch &a, ScoreCursor &c)
+{
+    c.t = 0;
+    if (++c.s >= c.n_sub) {
+        c.s = 0;
+        c.n_tiles = 0;
+        while (c.n_tiles == 0 && ++c.o < a.p.batch) {
+            const OwnerWork w = score_owner(a, c.o, c.sr);
+            c.n_sub = w.n_sub;
+            c.n_tiles = w.n_tiles;
+        }
+        if (c.o >= a.p.batch) { c.n_tiles = c.n_sub = 1; c.sr.R = 1; c.sr.n_pages = 0; }        // past the end: never used
+    }
+    score_pair(a, c);
+}
+__device__ __forceinline__ void score_start(const PageSelectLaunch &a, const WorkShare &sh, ScoreCursor &c)
+{
+    c.o = sh.o; c.s = sh.s; c.t = sh.t;
+    const OwnerWork w = score_owner(a, c.o, c.sr);             // only called by blocks with tiles
+    c.n_sub = w.n_sub;
+    c.n_tiles = w.n_tiles;
+    score_pair(a, c);
+    if (c.t >= c.n_tiles) score_next(a, c);
+}
+
+// max over G columns at a time of one page's products, times the page's scale, to the rows' scores.  GT: G where it is known
+// (a power of two up to 32), else 0.
+template <int GT>
+__device__ __forceinline__ void store_scores(uint32_t acc, int cols, int G, float scale, bool used, float *dst, int stride)
+{
+    int best = INT_MIN, k = 0;
+    for (int c0 = 0; c0 < cols; c0 += 32) {
+        uint32_t r[32];
+        tc_ld32(acc + c0, r);
+        if (GT > 0) {
+#pragma unroll
+            for (int c = 0; c < 32; c += (GT > 0 ? GT : 1)) {
+                int m = (int)r[c];
+#pragma unroll
+                for (int j = 1; j < GT; ++j) m = max(m, (int)r[c + j]);
+                if (used && c0 + c < cols) *dst = __fmul_rn((float)m, scale) + 0.f;               // -0 becomes 0
+                dst += stride;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                best = max(best, (int)r[c]);
+                if (++k == G) {
+                    if (used && c0 + c < cols) *dst = __fmul_rn((float)best, scale) + 0.f;
+                    dst += stride;
+                    best = INT_MIN;
+                    k = 0;
+                }
+            }
+        }
+    }
+}
+
+// D: head_dim.  The lanes of the products are a tile's 128 pages, the columns the pair's rows.
 template <int D>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(SC_THREADS, 1)
 page_score_kernel(const __grid_constant__ PageSelectLaunch a)
 {
     constexpr int ROW = 2 * D;                 // bytes of a page's bounds, and of a column's queries
@@ -89,168 +181,277 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
     pdl_enter();
     const sv_page_select_params &p = a.p;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int h = blockIdx.y, b = blockIdx.z / a.n_chunks, chunk = blockIdx.z - b * a.n_chunks;
-    const SeqRows sr = seq_rows(p, b, false);
-    const int i0 = chunk * a.pos_per_chunk, n_pos = min(sr.R - i0, a.pos_per_chunk);
-    const int tile0 = blockIdx.x * a.tiles_per_block;
-    if (n_pos <= 0 || tile0 * PS_PAGES >= sr.n_pages) return;
-    if (sr.n_pages <= p.n_select) return;      // every row takes all it sees
-    const int tiles = min(a.tiles_per_block, (sr.n_pages - tile0 * PS_PAGES + PS_PAGES - 1) / PS_PAGES);
-    const int G = a.group, cols = n_pos * G, n_mma = (cols + 15) & ~15;
-
+    const int G = a.group, n_bufs = a.n_tile_bufs;
     extern __shared__ __align__(1024) uint8_t ps_smem[];
-    uint8_t *tile_buf = ps_smem;                                   // two tiles
-    uint8_t *q_buf = ps_smem + 2 * TILE_BYTES;                     // n_mma rows
-    ScoreShared *sh = reinterpret_cast<ScoreShared *>(q_buf + (size_t)((a.pos_per_chunk * G + 15) & ~15) * ROW);
     if ((smem_u32(ps_smem) & 1023u) != 0) {                        // never seen; refuse rather than compute garbage
         if (tid == 0) set_status(p.device_status, SV_DEV_TIMEOUT);
         return;
     }
-    uint32_t tmem_cols = 32;
-    while ((int)tmem_cols < n_mma) tmem_cols <<= 1;
+    uint8_t *tile_buf = ps_smem;
+    const int q_bytes = a.max_cols * ROW;
+    uint8_t *q_buf = tile_buf + n_bufs * TILE_BYTES;               // two buffers of max_cols rows
+    ScoreShared *sh = reinterpret_cast<ScoreShared *>(q_buf + 2 * q_bytes);
+    uint32_t acc_cols = 32;                                        // tensor-memory columns of one accumulator
+    while ((int)acc_cols < a.max_cols) acc_cols <<= 1;
     if (tid == 0) {
-        mbar_init(smem_u32(&sh->done), 1);
+        for (int i = 0; i < n_bufs; ++i) {
+            mbar_init(smem_u32(&sh->tile_full[i]), 64);
+            mbar_init(smem_u32(&sh->tile_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh->q_full[i]), SC_Q_WARPS * 32);
+            mbar_init(smem_u32(&sh->q_empty[i]), 1);
+            mbar_init(smem_u32(&sh->acc_full[i]), 1);
+            mbar_init(smem_u32(&sh->acc_empty[i]), 128);
+        }
+        mbar_init(smem_u32(&sh->drained), 1);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 0) {
+    if (warp == SC_MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
-                     "r"(tmem_cols)
+                     "r"(2 * acc_cols)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    const int32_t *table = p.block_table + (long long)b * p.block_table_stride;
-    // a tile's bounds: chunk tid % CH of rows tid / CH + k * (128 / CH)
-    auto fetch = [&](int t) {
-        const int c = tid % CH;
-        const uint32_t base = smem_u32(tile_buf + (t & 1) * TILE_BYTES) + (c >> 3) * (PS_PAGES * 128);
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int row = tid / CH + k * (128 / CH);
-            const int lp = (tile0 + t) * PS_PAGES + row;
-            const int phys = lp < sr.n_pages ? table[lp] : -1;
-            const bool have = phys >= 0 && phys < p.n_pages;
-            if (lp < sr.n_pages && !have && c == 0) set_status(p.device_status, SV_DEV_BAD_PAGE);
-            const int8_t *src = p.bounds + ((long long)(have ? phys : 0) * p.hkv + h) * ROW + c * 16;
-            cp_async16(base + row * 128 + (((c & 7) ^ (row & 7)) << 4), src, have);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-    fetch(0);
-    // the rows' queries in 8 bits: a warp per position, its G heads together (one scale)
-    for (int i = warp; i < (n_mma + G - 1) / G; i += 4) {
-        const bool used = i < n_pos;
-        const __nv_bfloat162 *src = reinterpret_cast<const __nv_bfloat162 *>(
-            static_cast<const __nv_bfloat16 *>(p.q) + (((long long)p.cu_q[b] + i0 + (used ? i : 0)) * p.hq + (long long)h * G) * D);
-        float big = 0.f;
-        if (used)
-            for (int e = lane; e < G * D / 2; e += 32) {
-                const float2 f = __bfloat1622float2(src[e]);
-                big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
-        const float scale = __fmul_rn(big, 1.f / 127.f);
-        for (int e = lane; e < G * D / 4; e += 32) {               // four dims of a head
-            const int hh = e / (D / 4), d4 = e - hh * (D / 4), col = i * G + hh;
-            if (col >= n_mma) break;
-            uint32_t pos = 0, neg = 0;
-            if (used && scale > 0.f) {
-                const float2 f0 = __bfloat1622float2(src[e * 2]), f1 = __bfloat1622float2(src[e * 2 + 1]);
-                const float f[4] = {f0.x, f0.y, f1.x, f1.y};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int n = min(max(__float2int_rn(__fdiv_rn(f[c], scale)), -127), 127);
-                    pos |= (uint32_t)max(n, 0) << (8 * c);
-                    neg |= (uint32_t)(min(n, 0) & 255) << (8 * c);
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {                          // positive parts meet the maxima, negative ones the minima
-                const int byte = s * D + d4 * 4, ch = byte >> 4;
-                const uint32_t off = (ch >> 3) * (n_mma * 128) + col * 128 + (((ch & 7) ^ (col & 7)) << 4) + (byte & 15);
-                *reinterpret_cast<uint32_t *>(q_buf + off) = s == 0 ? pos : neg;
-            }
-        }
-    }
+    // the sums of the plan use the tiles' memory, which nothing else touches before the barrier below
+    plan_work_share<SC_THREADS>(
+        p.batch, SC_PAIR_COST,
+        [&](int b, bool) {
+            SeqRows sr;
+            return score_owner(a, b, sr);
+        },
+        [](int, int) {}, &sh->share, reinterpret_cast<long long(*)[SC_THREADS / 32]>(tile_buf));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    const long long t_begin = sh->share.t_begin, t_end = sh->share.t_end;
     const uint32_t tmem = sh->tmem_base;
-    uint32_t idesc = 0;
-    idesc |= 2u << 4;                          // int32 accumulator
-    idesc |= 1u << 7;                          // A signed 8-bit
-    idesc |= 1u << 10;                         // B signed 8-bit
-    idesc |= (uint32_t)(n_mma >> 3) << 17;
-    idesc |= (uint32_t)(128 >> 4) << 24;
+    int *abort_flag = &sh->abort_flag;
+    uint32_t *status = p.device_status;
+    int left = (int)(t_end - t_begin);
     bool ok = true;
-    for (int t = 0; t < tiles; ++t) {
-        if (t + 1 < tiles) {
-            fetch(t + 1);
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-        } else {
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        tc_fence_before();                     // the accumulator was read by the tile before
-        if (__syncthreads_or(!ok)) break;      // a wait ran out: every thread leaves at the same barrier
-        tc_fence_after();
-        if (warp == 0) {
-            if (elect_one()) {
-                const uint64_t ad = smem_desc(smem_u32(tile_buf + (t & 1) * TILE_BYTES), 16, 1024);
-                const uint64_t bd = smem_desc(smem_u32(q_buf), 16, 1024);
+    auto wait = [&](uint64_t &bar, uint32_t parity) {
+        return __all_sync(0xffffffffu, bounded_wait(smem_u32(&bar), parity, abort_flag, status));
+    };
+    if (left > 0) {
+        ScoreCursor c;
+        score_start(a, sh->share, c);
+        if (warp < 2) {
+            // ================================================================ tiles: a warp for 64 of the 128 pages
+            constexpr int RPI = 32 / CH;                           // rows that one copy of the warp covers
+            const int ch = lane % CH, r0 = lane / CH;
+            int n = 0, buf = 0, arrive_at = 0, arrived = 0;
+            uint32_t use = 0;
+            auto release = [&]() {                                 // the oldest tile under way is complete
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sh->tile_full[arrive_at]));
+                if (++arrive_at == n_bufs) arrive_at = 0;
+                ++arrived;
+            };
+            // lane l: ids of pages l and 32 + l of the warp's 64 (-1: behind the last, or not a page)
+            auto ids_of = [&](int (&id)[2]) {
+                const int32_t *table = p.block_table + (long long)c.o * p.block_table_stride;
 #pragma unroll
-                for (int ks = 0; ks < ROW / 32; ++ks)
-                    tc_mma_i8(tmem, ad + (((ks >> 2) * (PS_PAGES * 128) + (ks & 3) * 32) >> 4),
-                              bd + (((ks >> 2) * (n_mma * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
-                tc_commit(smem_u32(&sh->done));
-            }
-            __syncwarp();
-        }
-        const int lp = (tile0 + t) * PS_PAGES + tid;
-        const int phys = lp < sr.n_pages ? table[lp] : -1;
-        const float scale = phys >= 0 && phys < p.n_pages ? p.scales[(long long)phys * p.hkv + h] : 0.f;
-        ok = bounded_wait(smem_u32(&sh->done), t & 1, &sh->abort_flag, p.device_status);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) continue;
-        tc_fence_after();
-        float *dst = a.scores + (((long long)b * p.hkv + h) * (p.gamma_max + 1) + i0) * a.score_stride + lp;
-        int best = INT_MIN, k = 0;
-        for (int c0 = 0; c0 < cols; c0 += 32) {
-            uint32_t r[32];
-            tc_ld32(tmem + ((uint32_t)(warp * 32) << 16) + c0, r);
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                best = max(best, (int)r[c]);
-                if (++k == G) {
-                    // past the last column: nothing more to store (columns beyond it are padding)
-                    if (c0 + c < cols && lp < sr.n_pages) *dst = __fmul_rn((float)best, scale) + 0.f;     // -0 becomes 0
-                    dst += a.score_stride;
-                    best = INT_MIN;
-                    k = 0;
+                for (int k = 0; k < 2; ++k) {
+                    const int lp = c.t * PS_PAGES + warp * 64 + k * 32 + lane;
+                    id[k] = lp < c.sr.n_pages ? __ldg(table + lp) : INT_MIN;
                 }
+            };
+            int id[2];
+            ids_of(id);
+            for (; left > 0 && ok; --left, ++n) {
+                const int h = c.h;
+                int now[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (id[k] != INT_MIN && (id[k] < 0 || id[k] >= p.n_pages)) set_status(status, SV_DEV_BAD_PAGE);
+                    now[k] = id[k] >= 0 && id[k] < p.n_pages ? id[k] : -1;
+                }
+                if (++c.t == c.n_tiles) score_next(a, c);
+                if (left > 1) ids_of(id);                          // the next tile's, under way meanwhile
+                if (use > 0) ok = wait(sh->tile_empty[buf], (use - 1) & 1);
+                if (!ok) break;
+                const uint32_t base = smem_u32(tile_buf + buf * TILE_BYTES) + (ch >> 3) * (PS_PAGES * 128);
+                const int8_t *src0 = p.bounds + (long long)h * ROW + ch * 16;
+                const long long page_bytes = (long long)p.hkv * ROW;
+#pragma unroll
+                for (int k = 0; k < 64 / RPI; ++k) {
+                    const int in = k * RPI + r0, row = warp * 64 + in;
+                    const int phys = __shfl_sync(0xffffffffu, now[k * RPI / 32], in & 31);
+                    cp_async16(base + row * 128 + (((ch & 7) ^ (row & 7)) << 4), src0 + max(phys, 0) * page_bytes, phys >= 0);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (n >= 1) {                                      // one tile stays under way behind the newest
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    release();
+                }
+                if (++buf == n_bufs) { buf = 0; ++use; }
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            if (ok && arrived < n) release();
+        } else if (warp >= SC_Q_WARP0 && warp < SC_OUT_WARP0) {
+            // ================================================================ queries: a warp per position, its G heads together
+            for (uint32_t pair = 0; left > 0 && ok; ++pair) {
+                const int qb = pair & 1;
+                if (pair >= 2) ok = wait(sh->q_empty[qb], ((pair >> 1) - 1) & 1);
+                if (!ok) break;
+                uint8_t *dst = q_buf + qb * q_bytes;
+                const int n_mma = (c.n_pos * G + 15) & ~15;
+                constexpr int HELD = 4;                            // 16-byte chunks of a position that a lane holds
+                const int chunks = G * D / 8;
+                auto src_of = [&](int i) {
+                    return reinterpret_cast<const uint4 *>(
+                        static_cast<const __nv_bfloat16 *>(p.q) + (((long long)p.cu_q[c.o] + c.i0 + i) * p.hq + (long long)c.h * G) * D);
+                };
+                auto load = [&](uint4 (&v)[HELD], int i) {
+                    const uint4 *src = src_of(i);
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e)
+                        v[e] = i < c.n_pos && lane + e * 32 < chunks ? __ldg(src + lane + e * 32) : make_uint4(0, 0, 0, 0);
+                };
+                uint4 v[HELD], ahead[HELD];
+                load(v, warp - SC_Q_WARP0);
+                for (int i = warp - SC_Q_WARP0; i < c.n_pos; i += SC_Q_WARPS) {
+                    load(ahead, i + SC_Q_WARPS);                            // under way while this position is worked on
+                    const uint4 *src = src_of(i);
+                    uint32_t big2 = 0;                             // largest magnitudes, even and odd dims; magnitudes order as bits
+                    auto fold = [&](const uint4 &x) {
+                        big2 = __vmaxu2(big2, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+                    };
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e) fold(v[e]);
+                    for (int e = lane + HELD * 32; e < chunks; e += 32) fold(__ldg(src + e));
+                    const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, max(big2 & 0xffffu, big2 >> 16)) << 16);
+                    const float scale = __fmul_rn(big, 1.f / 127.f), inv = whole8_inverse(scale);
+                    auto put = [&](uint2 n, int e) {
+                        const int hh = e / (D / 8), d8 = e - hh * (D / 8), col = i * G + hh;
+                        const uint32_t sx = negative_bytes(n.x), sy = negative_bytes(n.y);
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {              // positive parts meet the maxima, negative ones the minima
+                            const int byte = z * D + d8 * 8, ch = byte >> 4;
+                            const uint32_t off = (ch >> 3) * (n_mma * 128) + col * 128 + (((ch & 7) ^ (col & 7)) << 4) + (byte & 15);
+                            *reinterpret_cast<uint2 *>(dst + off) = z == 0 ? make_uint2(n.x & ~sx, n.y & ~sy) : make_uint2(n.x & sx, n.y & sy);
+                        }
+                    };
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e) {
+                        float f[8];
+                        unpack8(v[e], f);
+                        const uint2 n = whole8x8(f, scale, inv);
+                        if (lane + e * 32 < chunks) put(n, lane + e * 32);
+                    }
+                    for (int e = lane + HELD * 32; e < chunks; e += 32) {
+                        float f[8];
+                        unpack8(__ldg(src + e), f);
+                        put(whole8x8(f, scale, inv), e);
+                    }
+#pragma unroll
+                    for (int e = 0; e < HELD; ++e) v[e] = ahead[e];
+                }
+                // columns up to the next multiple of 16: zeros
+                const int pad = (n_mma - c.n_pos * G) * CH;
+                for (int e = tid - SC_Q_WARP0 * 32; e < pad; e += SC_Q_WARPS * 32) {
+                    const int col = c.n_pos * G + e / CH, ch = e % CH;
+                    *reinterpret_cast<uint4 *>(dst + (ch >> 3) * (n_mma * 128) + col * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(smem_u32(&sh->q_full[qb]));
+                left -= min(left, c.n_tiles - c.t);
+                score_next(a, c);
+            }
+        } else if (warp >= SC_OUT_WARP0) {
+            // ================================================================ scores: a thread per page, every other tile
+            const int g = (warp - SC_OUT_WARP0) >> 2;
+            const uint32_t acc = tmem + g * acc_cols + ((uint32_t)((warp & 3) * 32) << 16);
+            const int row = (warp & 3) * 32 + lane;
+            for (uint32_t n = 0; left > 0 && ok; ++n, --left) {
+                if ((int)(n & 1) == g) {
+                    const int lp = c.t * PS_PAGES + row;
+                    const int phys = lp < c.sr.n_pages ? __ldg(p.block_table + (long long)c.o * p.block_table_stride + lp) : -1;
+                    const float scale = phys >= 0 && phys < p.n_pages ? __ldg(p.scales + (long long)phys * p.hkv + c.h) : 0.f;
+                    ok = wait(sh->acc_full[g], (n >> 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    float *dst = a.scores + (((long long)c.o * p.hkv + c.h) * (p.gamma_max + 1) + c.i0) * a.score_stride + lp;
+                    const int cols = c.n_pos * G;
+                    const bool used = lp < c.sr.n_pages;
+                    switch (G) {
+                        case 1: store_scores<1>(acc, cols, G, scale, used, dst, a.score_stride); break;
+                        case 2: store_scores<2>(acc, cols, G, scale, used, dst, a.score_stride); break;
+                        case 4: store_scores<4>(acc, cols, G, scale, used, dst, a.score_stride); break;
+                        case 8: store_scores<8>(acc, cols, G, scale, used, dst, a.score_stride); break;
+                        default: store_scores<0>(acc, cols, G, scale, used, dst, a.score_stride); break;
+                    }
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(&sh->acc_empty[g]));
+                }
+                if (++c.t == c.n_tiles) score_next(a, c);
+            }
+        } else {
+            // ================================================================ products
+            uint32_t pair = 0, use = 0;
+            int buf = 0;
+            bool fresh = true;                                     // the first tile of a pair
+            for (uint32_t n = 0; left > 0 && ok; ++n, --left) {
+                const int qb = pair & 1, g = n & 1;
+                if (fresh) ok = wait(sh->q_full[qb], (pair >> 1) & 1);
+                if (ok && n >= 2) ok = wait(sh->acc_empty[g], ((n >> 1) - 1) & 1);
+                if (ok) ok = wait(sh->tile_full[buf], use & 1);
+                if (!ok) break;
+                tc_fence_after();
+                const int n_mma = (c.n_pos * G + 15) & ~15;
+                uint32_t idesc = 0;
+                idesc |= 2u << 4;                                  // int32 accumulator
+                idesc |= 1u << 7;                                  // A signed 8-bit
+                idesc |= 1u << 10;                                 // B signed 8-bit
+                idesc |= (uint32_t)(n_mma >> 3) << 17;
+                idesc |= (uint32_t)(128 >> 4) << 24;
+                const bool last = c.t + 1 == c.n_tiles || left == 1;
+                const uint64_t ad = smem_desc(smem_u32(tile_buf + buf * TILE_BYTES), 16, 1024);
+                const uint64_t bd = smem_desc(smem_u32(q_buf + qb * q_bytes), 16, 1024);
+                if (elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < ROW / 32; ++ks)
+                        tc_mma_i8(tmem + g * acc_cols, ad + (((ks >> 2) * (PS_PAGES * 128) + (ks & 3) * 32) >> 4),
+                                  bd + (((ks >> 2) * (n_mma * 128) + (ks & 3) * 32) >> 4), idesc, ks > 0);
+                    tc_commit(smem_u32(&sh->acc_full[g]));
+                    tc_commit(smem_u32(&sh->tile_empty[buf]));
+                    if (last) tc_commit(smem_u32(&sh->q_empty[qb]));
+                }
+                __syncwarp();
+                if (++buf == n_bufs) { buf = 0; ++use; }
+                fresh = last;
+                pair += last;
+                if (++c.t == c.n_tiles) score_next(a, c);
+            }
+            if (!ok) {                                             // given up: let the issued instructions finish
+                if (elect_one()) tc_commit(smem_u32(&sh->drained));
+                __syncwarp();
+                for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained), 0); ++it) { }
             }
         }
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) {
+    if (warp == SC_MMA_WARP) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * acc_cols) : "memory");
     }
 }
 
 // ---------------------------------------------------------------------------- choice and union
 constexpr int PK_WARPS = 16;
+constexpr int PK_WORDS = 512;                  // words of 32 pages that the union takes at a time
 
-// WPR: warps per row (PK_WARPS / WPR rows at a time); KPT: scores a thread holds.  More pages than WPR * 32 * KPT are
-// read again in every round.
+// WPR: warps per row; KPT: scores a thread holds.  More pages than WPR * 32 * KPT are read again in every round.
 template <int WPR, int KPT>
 __global__ void __launch_bounds__(PK_WARPS * 32)
 page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 {
-    constexpr int TEAM = WPR * 32, TEAMS = PK_WARPS / WPR;
+    constexpr int TEAM = WPR * 32;
+    const int n_warps = blockDim.x >> 5, TEAMS = n_warps / WPR;
     pdl_enter();
     const sv_page_select_params &p = a.p;
     extern __shared__ uint32_t pk_bits[];
@@ -272,6 +473,17 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 #pragma unroll
         for (int w = 0; w < WPR; ++w) x += s_count[parity][team * WPR + w];
         parity ^= 1;                           // the next sum writes elsewhere, so one barrier a sum is enough
+        return x;
+    };
+    auto team_max = [&](uint32_t x) {
+        x = __reduce_max_sync(0xffffffffu, x);
+        if (WPR == 1) return x;
+        if (lane == 0) s_count[parity][warp] = (int)x;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM) : "memory");
+        x = 0;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) x = max(x, (uint32_t)s_count[parity][team * WPR + w]);
+        parity ^= 1;
         return x;
     };
     for (int i = team; i < sr.R; i += TEAMS) {
@@ -301,9 +513,10 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
         auto count = [&](auto &&f) {
             int n = 0;
 #pragma unroll
-            for (int j = 0; j < KPT; ++j) {
-                if (j >= rounds) break;
-                n += f(key[j], j * TEAM + t) ? 1 : 0;
+            for (int j0 = 0; j0 < KPT; j0 += 8) {          // keys behind the row's last are 0
+                if (j0 >= rounds) break;
+#pragma unroll
+                for (int j = j0; j < j0 + 8; ++j) n += f(key[j], j * TEAM + t) ? 1 : 0;
             }
             for (int j = KPT; j < rounds; ++j) n += f(key_at(j * TEAM + t), j * TEAM + t) ? 1 : 0;
             return team_sum(n);
@@ -313,7 +526,25 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
         int above = 0;                         // keys >= cut, once that is known to be at least want
         bool exact = false;
         if (want > 0) {
-            for (int bit = 31; bit >= 0; --bit) {
+            uint32_t top = 0, low = 0xffffffffu;
+            const uint32_t none = 0xffffffffu;
+#pragma unroll
+            for (int j = 0; j < KPT; ++j) {
+                top = max(top, key[j]);
+                low = min(low, key[j] == 0 ? none : key[j]);
+            }
+            for (int j = KPT; j < rounds; ++j) {
+                const uint32_t k = key_at(j * TEAM + t);
+                top = max(top, k);
+                low = min(low, k == 0 ? none : k);
+            }
+            top = team_max(top);
+            low = ~team_max(~low);
+            // the bits that all candidates share, then the others one by one
+            const int bits = 32 - __clz(top ^ low);
+            cut = bits == 32 ? 0 : top >> bits << bits;
+            above = c_hi - c_lo;
+            for (int bit = bits - 1; bit >= 0; --bit) {
                 const uint32_t cand = cut | (1u << bit);
                 const int n = count([&](uint32_t k, int) { return k >= cand; });
                 if (n >= want) {
@@ -355,38 +586,53 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
         for (int j = KPT; j < all_rounds; ++j) store_word(j, j < rounds ? key_at(j * TEAM + t) : 0u);
     }
     __syncthreads();
-    // the union of the rows, in page order: a warp per word, lane = page
-    __shared__ int s_word[PK_WARPS];
+    // the union of the rows, in page order: first how many pages each word of 32 has and where they go, a thread per word,
+    // then the pages and their masks, a warp per word
+    __shared__ int s_at[PK_WORDS], s_total;
     int base = 0;
     const int n_words = sr.R > 0 ? (sr.n_pages + 31) / 32 : 0;
     int32_t *list = p.page_list + pair * p.list_stride;
     uint64_t *masks = p.row_mask + pair * p.list_stride;
     bool short_list = false;
-    for (int w0 = 0; w0 < n_words; w0 += PK_WARPS) {
-        const int w = w0 + warp;
-        uint64_t mask = 0;
-        if (w < n_words)
-            for (int i = 0; i < sr.R; ++i) mask |= (uint64_t)((bits[(long long)i * a.bit_words + w] >> lane) & 1u) << i;
-        const uint32_t any = __ballot_sync(0xffffffffu, mask != 0);
-        if (lane == 0) s_word[warp] = __popc(any);
-        __syncthreads();
-        int before = base, total = 0;
-#pragma unroll
-        for (int k = 0; k < PK_WARPS; ++k) {
-            const int n = s_word[k];
-            if (k < warp) before += n;
-            total += n;
+    for (int w0 = 0; w0 < n_words; w0 += PK_WORDS) {
+        const int words = min(PK_WORDS, n_words - w0);
+        for (int w = threadIdx.x; w < words; w += blockDim.x) {
+            uint32_t any = 0;
+            for (int i = 0; i < sr.R; ++i) any |= bits[(long long)i * a.bit_words + w0 + w];
+            s_at[w] = __popc(any);
         }
-        const int at = before + __popc(any & ((1u << lane) - 1));
-        if (mask != 0) {
-            if (at < p.list_stride) {
-                list[at] = w * 32 + lane;
-                masks[at] = mask;
-            } else {
-                short_list = true;
+        __syncthreads();
+        if (warp == 0) {
+            int run = base;
+            for (int w = 0; w < words; w += 32) {
+                const int n = w + lane < words ? s_at[w + lane] : 0;
+                int v = n;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int x = __shfl_up_sync(0xffffffffu, v, d);
+                    if (lane >= d) v += x;
+                }
+                if (w + lane < words) s_at[w + lane] = run + v - n;
+                run += __shfl_sync(0xffffffffu, v, 31);
+            }
+            if (lane == 0) s_total = run;
+        }
+        __syncthreads();
+        for (int w = warp; w < words; w += n_warps) {
+            uint64_t mask = 0;
+            for (int i = 0; i < sr.R; ++i) mask |= (uint64_t)((bits[(long long)i * a.bit_words + w0 + w] >> lane) & 1u) << i;
+            const uint32_t any = __ballot_sync(0xffffffffu, mask != 0);
+            const int at = s_at[w] + __popc(any & ((1u << lane) - 1));
+            if (mask != 0) {
+                if (at < p.list_stride) {
+                    list[at] = (w0 + w) * 32 + lane;
+                    masks[at] = mask;
+                } else {
+                    short_list = true;
+                }
             }
         }
-        base += total;
+        base = s_total;
         __syncthreads();
     }
     if (short_list) set_status(p.device_status, SV_DEV_BAD_LEN);
@@ -408,22 +654,23 @@ static size_t select_row_bits(int gamma_max, int max_seq_len)
 }
 
 template <int WPR, int KPT>
-static sv_status launch_pick(const PageSelectLaunch &a, size_t smem, cudaStream_t s)
+static sv_status launch_pick(const PageSelectLaunch &a, int teams, size_t smem, cudaStream_t s)
 {
     if (smem > 48 * 1024 &&
         cudaFuncSetAttribute(page_pick_kernel<WPR, KPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PK_SMEM_BITS) != cudaSuccess)
         return SV_ECUDA;
-    return launch_kernel(true, page_pick_kernel<WPR, KPT>, (unsigned)(a.p.batch * a.p.hkv), PK_WARPS * 32, smem, s, a);
+    return launch_kernel(true, page_pick_kernel<WPR, KPT>, (unsigned)(a.p.batch * a.p.hkv), teams * WPR * 32, smem, s, a);
 }
 
 template <int D>
-static sv_status launch_score(const PageSelectLaunch &a, dim3 grid, cudaStream_t s)
+static sv_status launch_score(PageSelectLaunch &a, int grid, cudaStream_t s)
 {
-    const size_t smem = 2 * (size_t)PS_PAGES * 2 * D + (size_t)((a.pos_per_chunk * a.group + 15) & ~15) * 2 * D + sizeof(ScoreShared);
-    if (cudaFuncSetAttribute(page_score_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)(2 * PS_PAGES * 2 * D + PS_MAX_COLS * 2 * D + sizeof(ScoreShared))) != cudaSuccess)
-        return SV_ECUDA;
-    return launch_kernel(true, page_score_kernel<D>, grid, 128, smem, s, a);
+    const int tile = PS_PAGES * 2 * D, queries = 2 * a.max_cols * 2 * D;
+    a.n_tile_bufs = (227 * 1024 - queries - (int)sizeof(ScoreShared)) / tile;          // at least two: 256 columns are 128 KB
+    if (a.n_tile_bufs > SC_MAX_TILES) a.n_tile_bufs = SC_MAX_TILES;
+    const int smem = a.n_tile_bufs * tile + queries + (int)sizeof(ScoreShared);
+    if (cudaFuncSetAttribute(page_score_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return SV_ECUDA;
+    return launch_kernel(true, page_score_kernel<D>, grid, SC_THREADS, smem, s, a);
 }
 
 }  // namespace sv
@@ -460,8 +707,7 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
     a.group = p->hq / p->hkv;
     const int R = p->gamma_max + 1;
     a.pos_per_chunk = PS_MAX_COLS / a.group < R ? PS_MAX_COLS / a.group : R;
-    a.n_chunks = (R + a.pos_per_chunk - 1) / a.pos_per_chunk;
-    a.max_pages = (int)max_pages;
+    a.max_cols = (a.pos_per_chunk * a.group + 15) & ~15;
     a.score_stride = select_score_stride(p->max_seq_len);
     a.bit_words = (int)((max_pages + 31) / 32);
     a.scores = static_cast<float *>(workspace);
@@ -471,28 +717,27 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
                      : reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) +
                                                     select_score_bytes(p->batch, p->gamma_max, p->hkv, p->max_seq_len));
     const long long pairs = (long long)p->batch * p->hkv;
-    if (pairs > 0x7fffffffLL || (long long)p->batch * a.n_chunks > 65535 || p->hkv > 65535) return SV_EUNSUPPORTED;
+    if (pairs > (1 << 24)) return SV_EUNSUPPORTED;
     cudaStream_t s = (cudaStream_t)stream;
-    // Tiles per block: a block spends about as long on its queries as on a tile, so up to four tiles share them where there
-    // are enough blocks to fill the GPU a few times over.
-    const long long tiles = (max_pages + PS_PAGES - 1) / PS_PAGES;
-    a.tiles_per_block = 1;
-    while (a.tiles_per_block < 4 && pairs * a.n_chunks * tiles / (2 * a.tiles_per_block) >= 4LL * sm_count()) a.tiles_per_block *= 2;
-    const dim3 grid((unsigned)((tiles + a.tiles_per_block - 1) / a.tiles_per_block), (unsigned)p->hkv, (unsigned)(p->batch * a.n_chunks));
     if (max_pages > p->n_select) {             // otherwise no sequence has more pages than a row takes
+        // a block per multiprocessor, fewer where there are not as many tiles
+        const long long tiles = pairs * ((R + a.pos_per_chunk - 1) / a.pos_per_chunk) * ((max_pages + PS_PAGES - 1) / PS_PAGES);
+        const int grid = (int)(tiles < sm_count() ? tiles : sm_count());
         const sv_status st = p->head_dim == 128 ? launch_score<128>(a, grid, s) : launch_score<64>(a, grid, s);
         if (st != SV_OK) return st;
     }
-    // Warps per row: enough to hold a row's scores in registers, and all of a block's where it has few rows.
+    // Warps per row: enough to hold a row's scores in registers, and four where a block has few rows.
     int need = 1;
     while (need < PK_WARPS && (long long)need * 32 * 32 < max_pages) need *= 2;
-    while (need < PK_WARPS && need * 2 * R <= PK_WARPS) need *= 2;
+    while (need < 4 && need * 2 * R <= 4) need *= 2;
+    // Rows at a time: as few rounds as 16 warps allow, and no more warps than these rounds need (17 rows: two rounds of nine)
+    const int rounds = (R * need + PK_WARPS - 1) / PK_WARPS, teams = (R + rounds - 1) / rounds;
     const size_t smem = in_smem ? row_bits : 0;
     switch (need) {
-        case 1: return launch_pick<1, 32>(a, smem, s);
-        case 2: return launch_pick<2, 32>(a, smem, s);
-        case 4: return launch_pick<4, 32>(a, smem, s);
-        case 8: return launch_pick<8, 32>(a, smem, s);
-        default: return launch_pick<16, 32>(a, smem, s);
+        case 1: return launch_pick<1, 32>(a, teams, smem, s);
+        case 2: return launch_pick<2, 32>(a, teams, smem, s);
+        case 4: return launch_pick<4, 32>(a, teams, smem, s);
+        case 8: return launch_pick<8, 32>(a, teams, smem, s);
+        default: return launch_pick<16, 32>(a, teams, smem, s);
     }
 }
