@@ -9,8 +9,9 @@
 // score is the same for a row of a draft block and for the same position decoded alone.  One thread per page takes the
 // maximum over the heads in its own registers.  Bytes: 2 head_dim + 4 per page and kv head (1/31 of its keys and values).
 //
-// page_pick_kernel.  Per row the n_select best (the first n_first and last n_last among them) by bisection over the bits
-// of the scores, held in registers; then the union over a block's rows as a list with a row mask per page.
+// page_pick_kernel.  Per row the n_select best (the first n_first and last n_last among them): the scores, held in registers,
+// are counted in 256 parts of their range, and the part that holds the last place again, until it is taken whole; then the
+// union over a block's rows as a list with a row mask per page.
 #include "attn_common.cuh"
 #include "tc_ptx.cuh"
 #include "whole8.cuh"
@@ -29,9 +30,9 @@ struct PageSelectLaunch {
     int pos_per_chunk;                         // positions whose rows * heads fit the columns
     int max_cols;                              // columns of a product: the rows of a chunk, in multiples of 16
     int n_tile_bufs;
-    int score_stride;                          // floats between rows of scores
+    int key_stride;                            // words between rows of keys
     int bit_words;                             // 32-page words of a row of chosen bits
-    float *scores;                             // [batch * hkv][gamma_max + 1][score_stride]
+    uint32_t *keys;                            // scores that order as whole numbers: [batch * hkv][gamma_max + 1][key_stride]
     uint32_t *bits;                            // [batch * hkv][gamma_max + 1][bit_words], or NULL: in shared memory
 };
 
@@ -75,10 +76,11 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d, uint64_t adesc, uint64_t b
 
 // Roles of the score kernel's 16 warps (128 registers a thread: with more warps and fewer registers the spills, which find
 // hardly any L1 beside 227 KB of shared memory, doubled its time): 0 and 1 bring tiles of bounds into shared memory, 2 issues
-// the products, 3..7 bring the rows' queries in 8 bits, 8..11 and 12..15 turn every other tile's products into scores.
-// Everything is double buffered (the tiles up to four times): bounds stream while the next pair's queries are made.
+// the products, 4..7 turn them into scores, 3 and 8..15 bring the rows' queries in 8 bits (17 positions take two rounds; with
+// five of these warps everything else waited for them).  Everything is double buffered (the tiles up to four times): bounds
+// stream while the next pair's queries are made.
 constexpr int SC_THREADS = 512;
-constexpr int SC_MMA_WARP = 2, SC_Q_WARP0 = 3, SC_Q_WARPS = 5, SC_OUT_WARP0 = 8;
+constexpr int SC_MMA_WARP = 2, SC_OUT_WARP0 = 4, SC_Q_WARPS = 9;
 constexpr int SC_MAX_TILES = 4;
 constexpr int SC_PAIR_COST = 1;                // a pair's queries, in tiles
 
@@ -137,10 +139,17 @@ __device__ __forceinline__ void score_start(const PageSelectLaunch &a, const Wor
     if (c.t >= c.n_tiles) score_next(a, c);
 }
 
-// max over G columns at a time of one page's products, times the page's scale, to the rows' scores.  GT: G where it is known
+// A score as a number that orders as it does and is never 0; -0 counts as 0
+__device__ __forceinline__ uint32_t score_key(int best, float scale)
+{
+    const uint32_t x = __float_as_uint(__fmul_rn((float)best, scale) + 0.f);
+    return (x & 0x80000000u) ? ~x : x | 0x80000000u;
+}
+
+// max over G columns at a time of one page's products, times the page's scale, as keys to the rows.  GT: G where it is known
 // (a power of two up to 32), else 0.
 template <int GT>
-__device__ __forceinline__ void store_scores(uint32_t acc, int cols, int G, float scale, bool used, float *dst, int stride)
+__device__ __forceinline__ void store_keys(uint32_t acc, int cols, int G, float scale, bool used, uint32_t *dst, int stride)
 {
     int best = INT_MIN, k = 0;
     for (int c0 = 0; c0 < cols; c0 += 32) {
@@ -152,7 +161,7 @@ __device__ __forceinline__ void store_scores(uint32_t acc, int cols, int G, floa
                 int m = (int)r[c];
 #pragma unroll
                 for (int j = 1; j < GT; ++j) m = max(m, (int)r[c + j]);
-                if (used && c0 + c < cols) *dst = __fmul_rn((float)m, scale) + 0.f;               // -0 becomes 0
+                if (used && c0 + c < cols) *dst = score_key(m, scale);
                 dst += stride;
             }
         } else {
@@ -160,7 +169,7 @@ __device__ __forceinline__ void store_scores(uint32_t acc, int cols, int G, floa
             for (int c = 0; c < 32; ++c) {
                 best = max(best, (int)r[c]);
                 if (++k == G) {
-                    if (used && c0 + c < cols) *dst = __fmul_rn((float)best, scale) + 0.f;
+                    if (used && c0 + c < cols) *dst = score_key(best, scale);
                     dst += stride;
                     best = INT_MIN;
                     k = 0;
@@ -290,41 +299,48 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
             if (ok && arrived < n) release();
-        } else if (warp >= SC_Q_WARP0 && warp < SC_OUT_WARP0) {
+        } else if (warp != SC_MMA_WARP && (warp < SC_OUT_WARP0 || warp >= SC_OUT_WARP0 + 4)) {
             // ================================================================ queries: a warp per position, its G heads together
+            const int qw = warp < SC_OUT_WARP0 ? 0 : warp - 7;     // warps 3, 8..15: 0..8
+            constexpr int HELD = 4;                                // 16-byte chunks of a position that a lane holds
+            const int chunks = G * D / 8;
+            auto src_of = [&](int i) {
+                return reinterpret_cast<const uint4 *>(
+                    static_cast<const __nv_bfloat16 *>(p.q) + (((long long)__ldg(p.cu_q + c.o) + c.i0 + i) * p.hq + (long long)c.h * G) * D);
+            };
+            auto load = [&](uint4 (&v)[HELD], int i) {
+                if (i >= c.n_pos) return;
+                const uint4 *src = src_of(i);
+#pragma unroll
+                for (int e = 0; e < HELD; ++e) v[e] = lane + e * 32 < chunks ? __ldg(src + lane + e * 32) : make_uint4(0, 0, 0, 0);
+            };
+            uint4 v[HELD];
+            load(v, qw);
             for (uint32_t pair = 0; left > 0 && ok; ++pair) {
                 const int qb = pair & 1;
                 if (pair >= 2) ok = wait(sh->q_empty[qb], ((pair >> 1) - 1) & 1);
                 if (!ok) break;
                 uint8_t *dst = q_buf + qb * q_bytes;
                 const int n_mma = (c.n_pos * G + 15) & ~15;
-                constexpr int HELD = 4;                            // 16-byte chunks of a position that a lane holds
-                const int chunks = G * D / 8;
-                auto src_of = [&](int i) {
-                    return reinterpret_cast<const uint4 *>(
-                        static_cast<const __nv_bfloat16 *>(p.q) + (((long long)p.cu_q[c.o] + c.i0 + i) * p.hq + (long long)c.h * G) * D);
-                };
-                auto load = [&](uint4 (&v)[HELD], int i) {
-                    const uint4 *src = src_of(i);
+                for (int i = qw; i < c.n_pos; i += SC_Q_WARPS) {
+                    uint4 x[HELD];
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e)
-                        v[e] = i < c.n_pos && lane + e * 32 < chunks ? __ldg(src + lane + e * 32) : make_uint4(0, 0, 0, 0);
-                };
-                uint4 v[HELD], ahead[HELD];
-                load(v, warp - SC_Q_WARP0);
-                for (int i = warp - SC_Q_WARP0; i < c.n_pos; i += SC_Q_WARPS) {
-                    load(ahead, i + SC_Q_WARPS);                            // under way while this position is worked on
+                    for (int e = 0; e < HELD; ++e) x[e] = v[e];
+                    load(v, i + SC_Q_WARPS);                       // under way while this position is worked on
                     const uint4 *src = src_of(i);
                     uint32_t big2 = 0;                             // largest magnitudes, even and odd dims; magnitudes order as bits
-                    auto fold = [&](const uint4 &x) {
-                        big2 = __vmaxu2(big2, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+                    auto fold = [&](const uint4 &y) {
+                        big2 = __vmaxu2(big2, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu), __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
                     };
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e) fold(v[e]);
+                    for (int e = 0; e < HELD; ++e) fold(x[e]);
                     for (int e = lane + HELD * 32; e < chunks; e += 32) fold(__ldg(src + e));
                     const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, max(big2 & 0xffffu, big2 >> 16)) << 16);
                     const float scale = __fmul_rn(big, 1.f / 127.f), inv = whole8_inverse(scale);
-                    auto put = [&](uint2 n, int e) {
+                    auto put = [&](const uint4 &y, int e) {
+                        float f[8];
+                        unpack8(y, f);
+                        const uint2 n = whole8x8(f, scale, inv);
                         const int hh = e / (D / 8), d8 = e - hh * (D / 8), col = i * G + hh;
                         const uint32_t sx = negative_bytes(n.x), sy = negative_bytes(n.y);
 #pragma unroll
@@ -335,23 +351,13 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
                         }
                     };
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e) {
-                        float f[8];
-                        unpack8(v[e], f);
-                        const uint2 n = whole8x8(f, scale, inv);
-                        if (lane + e * 32 < chunks) put(n, lane + e * 32);
-                    }
-                    for (int e = lane + HELD * 32; e < chunks; e += 32) {
-                        float f[8];
-                        unpack8(__ldg(src + e), f);
-                        put(whole8x8(f, scale, inv), e);
-                    }
-#pragma unroll
-                    for (int e = 0; e < HELD; ++e) v[e] = ahead[e];
+                    for (int e = 0; e < HELD; ++e)
+                        if (lane + e * 32 < chunks) put(x[e], lane + e * 32);
+                    for (int e = lane + HELD * 32; e < chunks; e += 32) put(__ldg(src + e), e);
                 }
                 // columns up to the next multiple of 16: zeros
                 const int pad = (n_mma - c.n_pos * G) * CH;
-                for (int e = tid - SC_Q_WARP0 * 32; e < pad; e += SC_Q_WARPS * 32) {
+                for (int e = qw * 32 + lane; e < pad; e += SC_Q_WARPS * 32) {
                     const int col = c.n_pos * G + e / CH, ch = e % CH;
                     *reinterpret_cast<uint4 *>(dst + (ch >> 3) * (n_mma * 128) + col * 128 + (ch & 7) * 16) = make_uint4(0, 0, 0, 0);
                 }
@@ -359,34 +365,38 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
                 mbar_arrive(smem_u32(&sh->q_full[qb]));
                 left -= min(left, c.n_tiles - c.t);
                 score_next(a, c);
+                if (left > 0) load(v, qw);                         // the next pair's first position
             }
-        } else if (warp >= SC_OUT_WARP0) {
-            // ================================================================ scores: a thread per page, every other tile
-            const int g = (warp - SC_OUT_WARP0) >> 2;
-            const uint32_t acc = tmem + g * acc_cols + ((uint32_t)((warp & 3) * 32) << 16);
+        } else if (warp >= SC_OUT_WARP0 && warp < SC_OUT_WARP0 + 4) {
+            // ================================================================ scores: a thread per page
             const int row = (warp & 3) * 32 + lane;
+            // scale of the thread's page of the cursor's tile, under way while the tile before is worked on
+            auto scale_of = [&]() {
+                const int lp = c.t * PS_PAGES + row;
+                const int phys = lp < c.sr.n_pages ? __ldg(p.block_table + (long long)c.o * p.block_table_stride + lp) : -1;
+                return phys >= 0 && phys < p.n_pages ? __ldg(p.scales + (long long)phys * p.hkv + c.h) : 0.f;
+            };
+            float scale = scale_of();
             for (uint32_t n = 0; left > 0 && ok; ++n, --left) {
-                if ((int)(n & 1) == g) {
-                    const int lp = c.t * PS_PAGES + row;
-                    const int phys = lp < c.sr.n_pages ? __ldg(p.block_table + (long long)c.o * p.block_table_stride + lp) : -1;
-                    const float scale = phys >= 0 && phys < p.n_pages ? __ldg(p.scales + (long long)phys * p.hkv + c.h) : 0.f;
-                    ok = wait(sh->acc_full[g], (n >> 1) & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    float *dst = a.scores + (((long long)c.o * p.hkv + c.h) * (p.gamma_max + 1) + c.i0) * a.score_stride + lp;
-                    const int cols = c.n_pos * G;
-                    const bool used = lp < c.sr.n_pages;
-                    switch (G) {
-                        case 1: store_scores<1>(acc, cols, G, scale, used, dst, a.score_stride); break;
-                        case 2: store_scores<2>(acc, cols, G, scale, used, dst, a.score_stride); break;
-                        case 4: store_scores<4>(acc, cols, G, scale, used, dst, a.score_stride); break;
-                        case 8: store_scores<8>(acc, cols, G, scale, used, dst, a.score_stride); break;
-                        default: store_scores<0>(acc, cols, G, scale, used, dst, a.score_stride); break;
-                    }
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&sh->acc_empty[g]));
-                }
+                const int g = n & 1, lp = c.t * PS_PAGES + row, cols = c.n_pos * G;
+                const uint32_t acc = tmem + g * acc_cols + ((uint32_t)((warp & 3) * 32) << 16);
+                uint32_t *dst = a.keys + (((long long)c.o * p.hkv + c.h) * (p.gamma_max + 1) + c.i0) * a.key_stride + lp;
+                const bool used = lp < c.sr.n_pages;
+                const float mine = scale;
                 if (++c.t == c.n_tiles) score_next(a, c);
+                if (left > 1) scale = scale_of();
+                ok = wait(sh->acc_full[g], (n >> 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                switch (G) {
+                    case 1: store_keys<1>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                    case 2: store_keys<2>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                    case 4: store_keys<4>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                    case 8: store_keys<8>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                    default: store_keys<0>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                }
+                tc_fence_before();
+                mbar_arrive(smem_u32(&sh->acc_empty[g]));
             }
         } else {
             // ================================================================ products
@@ -443,50 +453,50 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
 
 // ---------------------------------------------------------------------------- choice and union
 constexpr int PK_WARPS = 16;
+constexpr int PK_BINS = 256;                   // parts that a range of keys is divided into
 constexpr int PK_WORDS = 512;                  // words of 32 pages that the union takes at a time
 
-// WPR: warps per row; KPT: scores a thread holds.  More pages than WPR * 32 * KPT are read again in every round.
+// WPR: warps per row; KPT: keys a thread holds.  More pages than WPR * 32 * KPT are read again in every pass.
 template <int WPR, int KPT>
-__global__ void __launch_bounds__(PK_WARPS * 32)
+__global__ void __launch_bounds__(PK_WARPS * 32, 2)
 page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 {
     constexpr int TEAM = WPR * 32;
-    const int n_warps = blockDim.x >> 5, TEAMS = n_warps / WPR;
+    const int n_warps = blockDim.x >> 5, teams = n_warps / WPR;
     pdl_enter();
     const sv_page_select_params &p = a.p;
-    extern __shared__ uint32_t pk_bits[];
+    extern __shared__ __align__(16) uint32_t pk_smem[];
     __shared__ int s_count[2][PK_WARPS];
     const int h = blockIdx.x % p.hkv, b = blockIdx.x / p.hkv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int team = warp / WPR, tw = warp % WPR, t = tw * 32 + lane;
     const SeqRows sr = seq_rows(p, b, h == 0 && threadIdx.x == 0);
     const long long pair = blockIdx.x;
-    uint32_t *bits = a.bits != nullptr ? a.bits + pair * (p.gamma_max + 1) * a.bit_words : pk_bits;
+    int *hist = reinterpret_cast<int *>(pk_smem) + team * PK_BINS;       // the team's counts
+    uint32_t *bits = a.bits != nullptr ? a.bits + pair * (p.gamma_max + 1) * a.bit_words : pk_smem + teams * PK_BINS;
     int parity = 0;
-    // sum over the threads of a team
-    auto team_sum = [&](int x) {
-        x = __reduce_add_sync(0xffffffffu, x);
-        if (WPR == 1) return x;
-        if (lane == 0) s_count[parity][warp] = x;
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM) : "memory");
-        x = 0;
-#pragma unroll
-        for (int w = 0; w < WPR; ++w) x += s_count[parity][team * WPR + w];
-        parity ^= 1;                           // the next sum writes elsewhere, so one barrier a sum is enough
-        return x;
+    auto team_bar = [&]() {
+        if (WPR == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM) : "memory");
     };
-    auto team_max = [&](uint32_t x) {
-        x = __reduce_max_sync(0xffffffffu, x);
+    // f over the threads of a team (sums write alternate places, so one barrier each is enough)
+    auto team_reduce = [&](uint32_t x, auto &&f) {
         if (WPR == 1) return x;
         if (lane == 0) s_count[parity][warp] = (int)x;
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM) : "memory");
-        x = 0;
+        team_bar();
+        x = (uint32_t)s_count[parity][team * WPR];
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) x = max(x, (uint32_t)s_count[parity][team * WPR + w]);
+        for (int w = 1; w < WPR; ++w) x = f(x, (uint32_t)s_count[parity][team * WPR + w]);
         parity ^= 1;
         return x;
     };
-    for (int i = team; i < sr.R; i += TEAMS) {
+    auto team_sum = [&](int x) {
+        return (int)team_reduce((uint32_t)__reduce_add_sync(0xffffffffu, x), [](uint32_t u, uint32_t v) { return u + v; });
+    };
+    auto team_max = [&](uint32_t x) {
+        return team_reduce(__reduce_max_sync(0xffffffffu, x), [](uint32_t u, uint32_t v) { return max(u, v); });
+    };
+    for (int i = team; i < sr.R; i += teams) {
         const int last = (sr.L - sr.R + i) / 16, n_seen = last + 1;
         uint32_t *row = bits + (long long)i * a.bit_words;
         const int n_words = (sr.n_pages + 31) / 32;
@@ -497,93 +507,119 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
             }
             continue;
         }
-        // candidates: all but the fixed pages; their keys order as the scores do, and 0 stands for no candidate
-        const int c_lo = p.n_first, c_hi = n_seen - p.n_last, want = p.n_select - p.n_first - p.n_last;
-        const float *src = a.scores + (pair * (p.gamma_max + 1) + i) * a.score_stride;
-        auto key_at = [&](int page) -> uint32_t {
-            if (page < c_lo || page >= c_hi) return 0u;
-            const uint32_t x = __float_as_uint(src[page]);
-            return (x & 0x80000000u) ? ~x : x | 0x80000000u;
-        };
+        // candidates: all but the fixed pages; 0 stands for no candidate
+        const int c_lo = p.n_first, c_hi = n_seen - p.n_last;
+        int want = p.n_select - p.n_first - p.n_last;
+        const uint32_t *src = a.keys + (pair * (p.gamma_max + 1) + i) * a.key_stride;
+        auto key_at = [&](int page) -> uint32_t { return page >= c_lo && page < c_hi ? __ldg(src + page) : 0u; };
         uint32_t key[KPT];
         const int rounds = (n_seen + TEAM - 1) / TEAM;
+        // f(key, page) for the thread's pages (with keys of 0 up to the next eight)
+        auto each = [&](auto &&f) {
 #pragma unroll
-        for (int j = 0; j < KPT; ++j) key[j] = j < rounds ? key_at(j * TEAM + t) : 0u;
-        // f(key, page) summed over the team's pages
-        auto count = [&](auto &&f) {
-            int n = 0;
-#pragma unroll
-            for (int j0 = 0; j0 < KPT; j0 += 8) {          // keys behind the row's last are 0
+            for (int j0 = 0; j0 < KPT; j0 += 4) {
                 if (j0 >= rounds) break;
 #pragma unroll
-                for (int j = j0; j < j0 + 8; ++j) n += f(key[j], j * TEAM + t) ? 1 : 0;
+                for (int j = j0; j < j0 + 4; ++j) f(key[j], j * TEAM + t);
             }
-            for (int j = KPT; j < rounds; ++j) n += f(key_at(j * TEAM + t), j * TEAM + t) ? 1 : 0;
-            return team_sum(n);
+            for (int j = KPT; j < rounds; ++j) f(key_at(j * TEAM + t), j * TEAM + t);
         };
-        // the want-th largest key: its bits from the top (all candidates have keys above 0)
-        uint32_t cut = 0;
-        int above = 0;                         // keys >= cut, once that is known to be at least want
-        bool exact = false;
-        if (want > 0) {
-            uint32_t top = 0, low = 0xffffffffu;
-            const uint32_t none = 0xffffffffu;
+        uint32_t top = 0, low = 0xffffffffu;
 #pragma unroll
-            for (int j = 0; j < KPT; ++j) {
-                top = max(top, key[j]);
-                low = min(low, key[j] == 0 ? none : key[j]);
-            }
-            for (int j = KPT; j < rounds; ++j) {
-                const uint32_t k = key_at(j * TEAM + t);
-                top = max(top, k);
-                low = min(low, k == 0 ? none : k);
-            }
-            top = team_max(top);
-            low = ~team_max(~low);
-            // the bits that all candidates share, then the others one by one
-            const int bits = 32 - __clz(top ^ low);
-            cut = bits == 32 ? 0 : top >> bits << bits;
-            above = c_hi - c_lo;
-            for (int bit = bits - 1; bit >= 0; --bit) {
-                const uint32_t cand = cut | (1u << bit);
-                const int n = count([&](uint32_t k, int) { return k >= cand; });
-                if (n >= want) {
-                    cut = cand;
-                    above = n;
-                    if (n == want) { exact = true; break; }
-                }
-            }
-        } else {
-            cut = 0xffffffffu;
-            exact = true;
+        for (int j0 = 0; j0 < KPT; j0 += 4) {
+            if (j0 >= rounds) break;
+#pragma unroll
+            for (int j = j0; j < j0 + 4; ++j) key[j] = key_at(j * TEAM + t);
         }
-        // more candidates at the cut than places: the lowest pages among them
-        int until = 0x7fffffff;
-        if (!exact && above != want) {
-            const int greater = count([&](uint32_t k, int) { return k > cut; });
+        each([&](uint32_t k, int) {
+            top = max(top, k);
+            low = min(low, k - 1);             // 0 - 1 is the largest
+        });
+        top = team_max(top);
+        low = ~team_max(~low) + 1;
+        // The want-th largest key lies in [low, top]: counts of its 256 parts from the top down name one of them, which is
+        // divided again until it is taken whole or is a single key.  After a pass: all keys >= cut are among the best, and
+        // `want` more of [low, cut) are.
+        uint32_t cut = top + 1;
+        bool whole = want == 0, ties = false;
+        while (!whole && !ties) {
+            const uint32_t range = top - low;
+            const int shift = max(0, 24 - __clz(range));               // parts of 2^shift keys: at most 256 of them
+            team_bar();
+            for (int k = t; k < PK_BINS; k += TEAM) hist[k] = 0;
+            team_bar();
+            each([&](uint32_t k, int) {
+                const uint32_t off = top - k;                          // part 0 holds the largest
+                if (off <= range) atomicAdd(&hist[off >> shift], 1);
+            });
+            team_bar();
+            // lane l: parts 8 l .. 8 l + 7
+            int n[8], sum = 0;
+#pragma unroll
+            for (int k = 0; k < 8; k += 4) {
+                const int4 x = *reinterpret_cast<const int4 *>(hist + lane * 8 + k);
+                n[k] = x.x; n[k + 1] = x.y; n[k + 2] = x.z; n[k + 3] = x.w;
+                sum += x.x + x.y + x.z + x.w;
+            }
+            int before = sum;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, before, d);
+                if (lane >= d) before += x;
+            }
+            before -= sum;
+            const uint32_t hit = __ballot_sync(0xffffffffu, before < want && before + sum >= want);
+            const int at = __ffs(hit) - 1;
+            int part = 0, above = before, in = 0;                      // the part that holds the want-th, keys above it, in it
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (in == 0 && above + n[k] >= want) { part = lane * 8 + k; in = n[k]; }
+                else if (in == 0) above += n[k];
+            }
+            part = __shfl_sync(0xffffffffu, part, at);
+            above = __shfl_sync(0xffffffffu, above, at);
+            in = __shfl_sync(0xffffffffu, in, at);
+            want -= above;
+            const uint32_t part_top = top - ((uint32_t)part << shift);
+            const uint32_t span = (1u << shift) - 1, part_low = part_top - low > span ? part_top - span : low;
+            if (in == want) {
+                cut = part_low;
+                whole = true;
+            } else {
+                cut = part_top + 1;
+                top = part_top;
+                low = part_low;
+                ties = shift == 0;
+            }
+        }
+        // more candidates of one key than places: the lowest pages among them
+        int until = -1;
+        if (ties) {
             int lo = 0, hi = c_hi;             // smallest page with enough candidates up to it
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
-                const int n = count([&](uint32_t k, int page) { return k == cut && page <= mid; });
-                if (greater + n >= want) hi = mid; else lo = mid + 1;
+                int n = 0;
+                each([&](uint32_t k, int page) { n += k == low && page <= mid ? 1 : 0; });
+                if (team_sum(n) >= want) hi = mid; else lo = mid + 1;
             }
             until = lo;
         }
         auto store_word = [&](int j, uint32_t k) {
             const int page = j * TEAM + t;
-            const bool fixed = page < c_lo || (page >= c_hi && page < n_seen);
-            const bool take = fixed || (want > 0 && (k > cut || (k == cut && page <= until)));
+            const bool candidate = page >= c_lo && page < c_hi;
+            const bool take = candidate ? k >= cut || (k == low && page <= until) : page < n_seen;
             const uint32_t word = __ballot_sync(0xffffffffu, take);
             const int w = j * WPR + tw;
             if (lane == 0 && w < n_words) row[w] = word;
         };
-        const int all_rounds = (n_words + WPR - 1) / WPR;          // the pages behind the row's last one too
 #pragma unroll
-        for (int j = 0; j < KPT; ++j) {
-            if (j >= all_rounds) break;
-            store_word(j, key[j]);
+        for (int j0 = 0; j0 < KPT; j0 += 4) {
+            if (j0 >= rounds) break;
+#pragma unroll
+            for (int j = j0; j < j0 + 4; ++j) store_word(j, key[j]);
         }
-        for (int j = KPT; j < all_rounds; ++j) store_word(j, j < rounds ? key_at(j * TEAM + t) : 0u);
+        const int stored = min((rounds + 3) / 4 * 4, KPT);
+        for (int j = stored; j * WPR + tw < n_words; ++j) store_word(j, j < rounds ? key_at(j * TEAM + t) : 0u);
     }
     __syncthreads();
     // the union of the rows, in page order: first how many pages each word of 32 has and where they go, a thread per word,
@@ -643,10 +679,10 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 constexpr size_t PK_SMEM_BITS = 96 * 1024;
 
 static int select_max_pages(int max_seq_len) { return (int)(((long long)max_seq_len + 15) / 16); }
-static int select_score_stride(int max_seq_len) { return (select_max_pages(max_seq_len) + 31) / 32 * 32; }
-static size_t select_score_bytes(int batch, int gamma_max, int hkv, int max_seq_len)
+static int select_key_stride(int max_seq_len) { return (select_max_pages(max_seq_len) + 31) / 32 * 32; }
+static size_t select_key_bytes(int batch, int gamma_max, int hkv, int max_seq_len)
 {
-    return (size_t)batch * hkv * (gamma_max + 1) * select_score_stride(max_seq_len) * sizeof(float);
+    return (size_t)batch * hkv * (gamma_max + 1) * select_key_stride(max_seq_len) * sizeof(uint32_t);
 }
 static size_t select_row_bits(int gamma_max, int max_seq_len)
 {
@@ -657,7 +693,8 @@ template <int WPR, int KPT>
 static sv_status launch_pick(const PageSelectLaunch &a, int teams, size_t smem, cudaStream_t s)
 {
     if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(page_pick_kernel<WPR, KPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PK_SMEM_BITS) != cudaSuccess)
+        cudaFuncSetAttribute(page_pick_kernel<WPR, KPT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)(PK_SMEM_BITS + PK_WARPS * PK_BINS * sizeof(int))) != cudaSuccess)
         return SV_ECUDA;
     return launch_kernel(true, page_pick_kernel<WPR, KPT>, (unsigned)(a.p.batch * a.p.hkv), teams * WPR * 32, smem, s, a);
 }
@@ -680,7 +717,7 @@ extern "C" size_t spec_page_select_workspace_bytes(int32_t batch, int32_t gamma_
     using namespace sv;
     if (batch <= 0 || gamma_max < 0 || gamma_max > 63 || hkv <= 0 || max_seq_len <= 0) return 0;
     const size_t row_bits = select_row_bits(gamma_max, max_seq_len);
-    return select_score_bytes(batch, gamma_max, hkv, max_seq_len) + (row_bits > PK_SMEM_BITS ? row_bits * batch * hkv : 0) + 256;
+    return select_key_bytes(batch, gamma_max, hkv, max_seq_len) + (row_bits > PK_SMEM_BITS ? row_bits * batch * hkv : 0) + 256;
 }
 
 extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *workspace, size_t workspace_bytes, void *stream)
@@ -708,14 +745,14 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
     const int R = p->gamma_max + 1;
     a.pos_per_chunk = PS_MAX_COLS / a.group < R ? PS_MAX_COLS / a.group : R;
     a.max_cols = (a.pos_per_chunk * a.group + 15) & ~15;
-    a.score_stride = select_score_stride(p->max_seq_len);
+    a.key_stride = select_key_stride(p->max_seq_len);
     a.bit_words = (int)((max_pages + 31) / 32);
-    a.scores = static_cast<float *>(workspace);
+    a.keys = static_cast<uint32_t *>(workspace);
     const size_t row_bits = select_row_bits(p->gamma_max, p->max_seq_len);
     const bool in_smem = row_bits <= PK_SMEM_BITS;
     a.bits = in_smem ? nullptr
                      : reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(workspace) +
-                                                    select_score_bytes(p->batch, p->gamma_max, p->hkv, p->max_seq_len));
+                                                    select_key_bytes(p->batch, p->gamma_max, p->hkv, p->max_seq_len));
     const long long pairs = (long long)p->batch * p->hkv;
     if (pairs > (1 << 24)) return SV_EUNSUPPORTED;
     cudaStream_t s = (cudaStream_t)stream;
@@ -732,7 +769,7 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
     while (need < 4 && need * 2 * R <= 4) need *= 2;
     // Rows at a time: as few rounds as 16 warps allow, and no more warps than these rounds need (17 rows: two rounds of nine)
     const int rounds = (R * need + PK_WARPS - 1) / PK_WARPS, teams = (R + rounds - 1) / rounds;
-    const size_t smem = in_smem ? row_bits : 0;
+    const size_t smem = (size_t)teams * PK_BINS * sizeof(int) + (in_smem ? row_bits : 0);
     switch (need) {
         case 1: return launch_pick<1, 32>(a, teams, smem, s);
         case 2: return launch_pick<2, 32>(a, teams, smem, s);
