@@ -38,6 +38,7 @@ constexpr int SEG_PITCH = 128;                 // floats between rows of a parti
 constexpr int SEG_RING = 12;                   // most ring slots
 constexpr int SEG_TILE = 64;                   // tokens of a key tile
 constexpr int SEG_S_BUFS = 2;                  // S buffers of a row tile
+constexpr int SEG_Q_AHEAD = 32;                // most rows of a pair whose queries are brought ahead
 
 __host__ __device__ inline size_t seg_slot_floats(int rows) { return (size_t)rows * (SEG_PITCH + 2); }
 
@@ -61,6 +62,7 @@ struct SegLaunch {
     int group;               // query heads per kv head
     int ppl;                 // positions of a row tile: 128 / group
     int n_slots;             // K/V ring slots
+    int q_ahead;             // the query rows of the next pair are brought by a warp of their own (two buffers of 32 rows)
     int n_owners;
     const int32_t *page_list;      // SEG_LIST
     const uint64_t *row_mask;
@@ -202,7 +204,8 @@ struct SegShared {
     uint64_t s_full[4];          // S ready (row tile * 2 + parity of the key tile)
     uint64_t p_full[4];          // P written
     uint64_t o_done[4];          // P V finished
-    uint64_t q_full;             // a segment's query rows are in shared memory
+    uint64_t q_full[2];          // a segment's query rows are in shared memory
+    uint64_t q_empty[2];         // (q_ahead) and were read for the last time
     uint64_t drained[2];         // a row tile's instructions are through (after an expired wait)
     uint32_t tmem_base;
     int abort_flag;
@@ -352,15 +355,19 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
     constexpr int OCH = D / 32;
     pdl_enter();
     extern __shared__ __align__(1024) uint8_t seg_smem[];
-    uint8_t *ring = seg_smem;
     const sv_attn_params &p = a.p;
-    if ((smem_u32(ring) & 1023u) != 0) {                       // never seen; refuse rather than compute garbage
+    if ((smem_u32(seg_smem) & 1023u) != 0) {                       // never seen; refuse rather than compute garbage
         if (threadIdx.x == 0) set_status(p.device_status, SV_DEV_TIMEOUT);
         return;
     }
     const int n_slots = a.n_slots;
-    uint8_t *q_smem = ring + (size_t)n_slots * SLOT_BYTES;
-    SegShared *sh = reinterpret_cast<SegShared *>(q_smem + (size_t)NL * Q_BYTES);
+    // Query rows: a tile of 128 per row tile, or, with q_ahead, two buffers of 32 rows.  The instructions read 128 rows all
+    // the same: what lies behind the buffers (ring, barriers) gives rows of S that nobody looks at.
+    const bool q_ahead = NL == 1 && a.q_ahead != 0;
+    const int q_half = q_ahead ? SEG_Q_AHEAD * 128 : 16384;        // bytes between the 64-dim halves of the rows
+    uint8_t *q_smem = seg_smem;
+    uint8_t *ring = seg_smem + (q_ahead ? 2 * SEG_Q_AHEAD * D * 2 : NL * Q_BYTES);
+    SegShared *sh = reinterpret_cast<SegShared *>(ring + (size_t)n_slots * SLOT_BYTES);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.group, ppl = a.ppl;
 
@@ -374,7 +381,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             mbar_init(smem_u32(&sh->p_full[i]), 128);
             mbar_init(smem_u32(&sh->o_done[i]), 1);
         }
-        mbar_init(smem_u32(&sh->q_full), 128 * NL);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh->q_full[i]), a.q_ahead ? 1 : 128 * NL);
+            mbar_init(smem_u32(&sh->q_empty[i]), 1);
+        }
         for (int i = 0; i < NL; ++i) mbar_init(smem_u32(&sh->drained[i]), 1);
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -385,8 +395,8 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    // the plan's sums share the ring's memory, which no copy touches before the barrier below
-    seg_plan<KIND, NL, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(ring));
+    // the plan's sums share the queries' memory, which nothing touches before the barrier below
+    seg_plan<KIND, NL, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(seg_smem));
     tc_fence_before();
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
@@ -413,6 +423,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             int ids = 0;                                       // lane l: page of entry ids_base + l
             for (long long tg = t_begin; tg < t_end && ok;) {
                 const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+                SegCursor nxt = cur;                           // the next pair, looked up while this one's tiles are under way
                 const int32_t *table;
                 {
                     const int tb = KIND == SEG_GROUP ? a.plan.grp_rep[cur.o] : cur.b;
@@ -447,10 +458,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         const uint32_t dst = smem_u32(ring + at.slot * SLOT_BYTES + half * HALF + page_in_tile * 2048);
                         tma_load_4d(dst, is_v ? &v_map : &k_map, half * 64, 0, cur.h, phys, full);
                     }
+                    if (ti == 0) seg_next<KIND, NL>(a, nxt);
                 }
                 tg += seg_tiles;
-                cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
+                cur = nxt;                                     // a segment that ends inside its pair is the block's last
             }
             if (!ok && lane == 0) {
                 // given up: the copies under way end before the block does (each slot's last use by this warp)
@@ -476,15 +487,17 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             // compiler knows to be the same in all lanes: the operands of the instructions then stay in uniform registers,
             // where otherwise each instruction waits for its operands to be moved there.
             const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
-            const uint64_t qd = smem_desc(smem_u32(q_smem + l * Q_BYTES), 16, 1024);
             int left = __reduce_max_sync(0xffffffffu, (int)(t_end - t_begin));
             bool ok = true;
             for (; left > 0 && ok; ++seg_no) {
                 const int seg_tiles = __reduce_max_sync(0xffffffffu, min(cur.n_tiles - cur.t, left));
                 const int n_pos = cur.R - cur.chunk * NL * ppl;
                 const bool active = NL == 1 || l == 0 || __reduce_max_sync(0xffffffffu, n_pos > ppl ? 1 : 0) != 0;
-                ok = seg_wait(smem_u32(&sh->q_full), seg_no & 1, abort_flag, status);
+                SegCursor nxt = cur;
+                const int qb = q_ahead ? (int)(seg_no & 1) : 0;
+                ok = seg_wait(smem_u32(&sh->q_full[qb]), q_ahead ? (seg_no >> 1) & 1 : seg_no & 1, abort_flag, status);
                 tc_fence_after();
+                const uint64_t qd = smem_desc(smem_u32(q_smem + (q_ahead ? qb * SEG_Q_AHEAD * D * 2 : l * Q_BYTES)), 16, 1024);
                 auto issue_qk = [&](int ti) {
                     ok = ok && seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
                     if (!ok) return;
@@ -494,10 +507,11 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     if (elect_one()) {
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks)
-                            tc_mma_ss(tm + buf * TILE, qd + (((ks >> 2) * 16384 + (ks & 3) * 32) >> 4),
+                            tc_mma_ss(tm + buf * TILE, qd + (((ks >> 2) * q_half + (ks & 3) * 32) >> 4),
                                       kd + (((ks >> 2) * HALF + (ks & 3) * 32) >> 4), idesc_qk, ks > 0);
                         tc_commit(smem_u32(&sh->s_full[buf]));
                         tc_commit(smem_u32(&sh->empty[k_at.slot]));            // K tile consumed
+                        if (q_ahead && ti == seg_tiles - 1) tc_commit(smem_u32(&sh->q_empty[qb]));
                     }
                     __syncwarp();
                     k_at.next(n_slots);
@@ -505,6 +519,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (active) {
                     issue_qk(0);
                     if (NB > 1 && seg_tiles > 1) issue_qk(1);
+                    seg_next<KIND, NL>(a, nxt);
                     for (int ti = 0; ti < seg_tiles && ok; ++ti) {
                         const uint32_t g = cnt + ti;
                         const int buf = l * NB + (int)(g % NB);
@@ -527,6 +542,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                     cnt += seg_tiles;
                 } else {                                       // no rows in this row tile: pass the tiles on
+                    seg_next<KIND, NL>(a, nxt);
                     for (int ti = 0; ti < seg_tiles && ok; ++ti) {
                         ok = seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
                         if (ok && lane == 0) mbar_arrive(smem_u32(&sh->empty[k_at.slot]));
@@ -537,13 +553,54 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                 }
                 left -= seg_tiles;
-                cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
+                cur = nxt;
             }
             if (!ok) {                                         // given up: let the issued instructions finish
                 if (elect_one()) tc_commit(smem_u32(&sh->drained[l]));
                 __syncwarp();
                 for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained[l]), 0); ++it) { }
+            }
+        }
+        else if (NL == 1 && t_end > t_begin && warp == 3 && q_ahead) {
+            // ================================================================ query rows of the next pair
+            SegCursor cur;
+            seg_start<KIND, NL>(a, sh->share, cur);
+            constexpr int CH = D / 8, RPI = 32 / CH;           // 16-byte chunks of a row; rows that one load of the warp covers
+            const int ch = lane % CH, r0 = lane / CH;
+            bool ok = true;
+            uint32_t seg_no = 0;
+            for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
+                const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
+                const int qb = seg_no & 1;
+                const int pos0 = cur.chunk * ppl, n_rows = min(cur.R - pos0, ppl) * G;
+                if (seg_no >= 2) ok = seg_wait(smem_u32(&sh->q_empty[qb]), ((seg_no >> 1) - 1) & 1, abort_flag, status);
+                if (!ok) break;
+                uint8_t *dst = q_smem + qb * SEG_Q_AHEAD * D * 2 + (ch >> 3) * q_half;
+#pragma unroll 1
+                for (int b0 = 0; b0 < n_rows; b0 += 4 * RPI) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = b0 + k * RPI + r0, i = r / G;
+                        v[k] = make_uint4(0, 0, 0, 0);
+                        if (r < n_rows) {
+                            const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + pos0 + i] : p.cu_q[cur.b] + pos0 + i;
+                            const long long q_row = (long long)at * p.hq + (long long)cur.h * G + (r - i * G);
+                            v[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D) + ch);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = b0 + k * RPI + r0;               // up to the next multiple of 4 * RPI, at most SEG_Q_AHEAD
+                        *reinterpret_cast<uint4 *>(dst + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = v[k];
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->q_full[qb]));
+                tg += seg_tiles;
+                cur.t += seg_tiles;
+                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
             }
         }
     } else {
@@ -577,7 +634,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 }
                 // ---- this thread's query row into shared memory.  Every instruction that read the rows before has
                 // completed: this thread has seen the last S that they gave.
-                if (warp_active) {
+                if (!q_ahead && warp_active) {
                     const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D);
                     uint8_t *dst = q_smem + l * Q_BYTES + r * 128;
 #pragma unroll
@@ -587,7 +644,9 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                mbar_arrive(smem_u32(&sh->q_full));
+                if (!q_ahead) mbar_arrive(smem_u32(&sh->q_full[0]));
+                SegCursor nxt = cur;
+                seg_next<KIND, NL>(a, nxt);
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
                 PrefixPart part = {nullptr, 0};
                 if (KIND == SEG_SEQ && whole && row_ok && cur.page0 > 0) part = prefix_part(a, cur.b, cur.h, i, hh);
@@ -595,6 +654,9 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
                 const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
                 const int seq_pages = (cur.L + 15) / 16;
+                const bool far = p.gamma_max >= 32;            // masks have bits above the 32nd
+                int e_base = -32, e_lp = -1;                   // lane l: entry e_base + l of the list and its mask
+                uint32_t e_lo = 0, e_hi = 0;
                 float m_ref = -CUDART_INF_F, l_sum = 0.f;
                 if (tile_active) {
                     for (int ti = 0; ti < seg_tiles && ok; ++ti, ++cnt) {
@@ -602,15 +664,28 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         const uint32_t phase = (cnt / NB) & 1;
                         int lim[PPT];
                         if (KIND == SEG_LIST) {
+                            const int e0 = (cur.t + ti) * PPT;
+                            if (warp_active && (e0 < e_base || e0 >= e_base + 32)) {
+                                e_base = e0;
+                                const int e = e0 + lane;
+                                e_lp = -1;
+                                e_lo = e_hi = 0;
+                                if (e < cur.n_pages) {
+                                    e_lp = __ldg(list + e);
+                                    const uint64_t mk = __ldg(reinterpret_cast<const unsigned long long *>(masks) + e);
+                                    if (e_lp >= 0 && e_lp < seq_pages) { e_lo = (uint32_t)mk; e_hi = (uint32_t)(mk >> 32); }
+                                }
+                            }
 #pragma unroll
                             for (int j = 0; j < PPT; ++j) {
-                                const int e = (cur.t + ti) * PPT + j;
-                                lim[j] = -1;
-                                if (row_ok && e < cur.n_pages) {
-                                    const int lp = __ldg(list + e);
-                                    const uint64_t mk = __ldg(reinterpret_cast<const unsigned long long *>(masks) + e);
-                                    if (((mk >> i) & 1) && lp >= 0 && lp < seq_pages) lim[j] = max(last - lp * 16, -1);
+                                const int src = (e0 - e_base + j) & 31;
+                                const int lp = __shfl_sync(0xffffffffu, e_lp, src);
+                                uint32_t mk = __shfl_sync(0xffffffffu, e_lo, src);
+                                if (far) {
+                                    const uint32_t hi = __shfl_sync(0xffffffffu, e_hi, src);
+                                    if (i >= 32) mk = hi;
                                 }
+                                lim[j] = row_ok && ((mk >> (i & 31)) & 1) ? max(last - lp * 16, -1) : -1;
                             }
                         } else {
                             const int tok0 = (cur.page0 + (cur.t + ti) * PPT) * 16;
@@ -717,8 +792,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                 }
                 tg += seg_tiles;
-                cur.t += seg_tiles;
-                if (cur.t == cur.n_tiles) seg_next<KIND, NL>(a, cur);
+                cur = nxt;
             }
         }
     }
@@ -733,7 +807,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
 
 // ---------------------------------------------------------------------------- pairs that were split over blocks
 constexpr int SEG_COMBINE_WARPS = 8;
-constexpr int SEG_COMBINE_Y = 4;               // blocks that share a pair's rows
+constexpr int SEG_COMBINE_Y = 8;               // blocks that share a pair's rows
 
 // Blocks (c, *) merge the pair that begins in block c of the main kernel and goes on behind it, a warp per row, four parts
 // in flight.  A group's parts are merged into the first of them, in place.
@@ -856,7 +930,8 @@ sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
     constexpr int slot_bytes = SEG_TILE * D * 2;
     // shared memory of a multiprocessor less 1 KB that each block takes by itself
     const size_t budget = 228 * 1024 / SegConfig<NL>::BLOCKS - 1024;
-    const size_t fixed = (size_t)NL * 128 * D * 2 + ((sizeof(SegShared) + 15) & ~(size_t)15);
+    a.q_ahead = NL == 1 && a.group * (a.p.gamma_max + 1) <= SEG_Q_AHEAD;
+    const size_t fixed = (a.q_ahead ? (size_t)2 * SEG_Q_AHEAD : (size_t)NL * 128) * D * 2 + ((sizeof(SegShared) + 15) & ~(size_t)15);
     a.n_slots = (int)((budget - fixed) / slot_bytes);
     if (a.n_slots > SEG_RING) a.n_slots = SEG_RING;
     if (a.n_slots < 4) return SV_EUNSUPPORTED;

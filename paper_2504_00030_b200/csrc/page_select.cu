@@ -528,8 +528,13 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 #pragma unroll
         for (int j0 = 0; j0 < KPT; j0 += 4) {
             if (j0 >= rounds) break;
+            if (j0 * TEAM >= c_lo && (j0 + 4) * TEAM <= c_hi) {
 #pragma unroll
-            for (int j = j0; j < j0 + 4; ++j) key[j] = key_at(j * TEAM + t);
+                for (int j = j0; j < j0 + 4; ++j) key[j] = __ldg(src + j * TEAM + t);
+            } else {
+#pragma unroll
+                for (int j = j0; j < j0 + 4; ++j) key[j] = key_at(j * TEAM + t);
+            }
         }
         each([&](uint32_t k, int) {
             top = max(top, k);
@@ -606,8 +611,9 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
         }
         auto store_word = [&](int j, uint32_t k) {
             const int page = j * TEAM + t;
-            const bool candidate = page >= c_lo && page < c_hi;
-            const bool take = candidate ? k >= cut || (k == low && page <= until) : page < n_seen;
+            bool take = k >= cut;                                      // not for a key of 0
+            if (ties) take = take || (k == low && page <= until);
+            if (j * TEAM < c_lo || j * TEAM + TEAM > c_hi) take = take || page < c_lo || (page >= c_hi && page < n_seen);
             const uint32_t word = __ballot_sync(0xffffffffu, take);
             const int w = j * WPR + tw;
             if (lane == 0 && w < n_words) row[w] = word;
