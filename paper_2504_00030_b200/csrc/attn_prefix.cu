@@ -94,46 +94,34 @@ prefix_plan_kernel(const __grid_constant__ SegLaunch a, const int32_t *prefix_le
             if (w < warp) at += s_sum[0][w];
             at0 += s_sum[0][w];
         }
-        if (mine) {
-            pl.seq_pages[b] = member ? pages : 0;
-            pl.seq_at[b] = at;
-        }
+        if (mine) pl.seq_pages[b] = member ? pages : 0;
         if (member)
-            for (int i = 0; i < R; ++i) pl.row_list[before + at + i] = p.cu_q[b] + i;
+            for (int i = 0; i < R; ++i) pl.row_list[before + at + i] = make_int2(p.cu_q[b] + i, b * (p.gamma_max + 1) + i);
     }
 }
 
 // ---------------------------------------------------------------------------- host side
-// Pairs of the group launch: every group's rows in chunks of 2 * ppl positions, per kv head.
-static long long prefix_max_pairs(int batch, int gamma_max, int group, int hkv, int n_groups)
-{
-    const long long ppp = 2 * (128 / group), rows = (long long)batch * (gamma_max + 1);
-    return (rows / ppp + n_groups) * hkv;
-}
-
-constexpr int PREFIX_PARTS = 13;
+enum { PX_GRP_PAGES, PX_GRP_REP, PX_GRP_N, PX_GRP_BASE, PX_ROW_LIST, PX_SEQ_PAGES, PX_PART_O, PX_PART_ML, PX_TABLES, PX_PART, PX_N };
 
 struct PrefixLayout {
-    size_t at[PREFIX_PARTS], bytes;
+    size_t at[PX_N], bytes;
 };
 
 static PrefixLayout prefix_layout(int batch, int gamma_max, int hq, int hkv, int n_groups)
 {
-    const int group = hq / hkv;
-    const long long pairs = prefix_max_pairs(batch, gamma_max, group, hkv, n_groups);
-    const size_t w = sizeof(int32_t);
-    const size_t sizes[] = {
-        n_groups * w, n_groups * w, n_groups * w, n_groups * w,               // grp_pages, grp_rep, grp_n, grp_base
-        (size_t)batch * (gamma_max + 1) * w, batch * w, batch * w,            // row_list, seq_pages, seq_at
-        n_groups * w, (size_t)pairs * w,                                      // grp_pair0, pair_first
-        seg_table_bytes(),                                                    // bounds and desc of the group launch
-        seg_table_bytes(),                                                    // bounds and desc of the sequences' launch
-        seg_part_bytes(seg_nl(group * (gamma_max + 1))),                      // partials of the sequences' launch
-        (size_t)(pairs + seg_grid(2)) * seg_slot_floats(256) * sizeof(float), // partials of the group launch
-    };
+    const size_t w = sizeof(int32_t), positions = (size_t)batch * (gamma_max + 1);
+    size_t sizes[PX_N];
+    sizes[PX_GRP_PAGES] = sizes[PX_GRP_REP] = sizes[PX_GRP_N] = sizes[PX_GRP_BASE] = n_groups * w;
+    sizes[PX_ROW_LIST] = positions * sizeof(int2);
+    sizes[PX_SEQ_PAGES] = batch * w;
+    sizes[PX_PART_O] = positions * hq * SEG_PITCH * sizeof(float);
+    sizes[PX_PART_ML] = positions * hq * sizeof(float2);
+    sizes[PX_TABLES] = seg_table_bytes();                                     // bounds, desc and parts of split pairs: those of the
+    const size_t parts = seg_part_bytes(seg_nl(hq / hkv * (gamma_max + 1)));  // groups are done with before the sequences begin
+    sizes[PX_PART] = parts > seg_part_bytes(2) ? parts : seg_part_bytes(2);
     PrefixLayout l;
     size_t at = 0;
-    for (int i = 0; i < PREFIX_PARTS; ++i) {
+    for (int i = 0; i < PX_N; ++i) {
         l.at[i] = at;
         at += seg_round(sizes[i]);
     }
@@ -193,23 +181,23 @@ extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, voi
     a.ppl = 128 / a.group;
     a.seq_group = p->group;
     PrefixPlan &pl = a.plan;
-    pl.grp_pages = ints(0); pl.grp_rep = ints(1); pl.grp_n = ints(2); pl.grp_base = ints(3);
-    pl.row_list = ints(4); pl.seq_pages = ints(5); pl.seq_at = ints(6);
-    pl.grp_pair0 = ints(7); pl.pair_first = ints(8);
-    pl.part = reinterpret_cast<float *>(w + l.at[12]);
+    pl.grp_pages = ints(PX_GRP_PAGES);
+    pl.grp_rep = ints(PX_GRP_REP);
+    pl.grp_n = ints(PX_GRP_N);
+    pl.grp_base = ints(PX_GRP_BASE);
+    pl.row_list = reinterpret_cast<int2 *>(w + l.at[PX_ROW_LIST]);
+    pl.seq_pages = ints(PX_SEQ_PAGES);
+    pl.part_o = reinterpret_cast<float *>(w + l.at[PX_PART_O]);
+    pl.part_ml = reinterpret_cast<float2 *>(w + l.at[PX_PART_ML]);
+    a.bounds = ints(PX_TABLES);
+    a.desc = reinterpret_cast<int32_t *>(w + l.at[PX_TABLES] + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
+    a.part = reinterpret_cast<float *>(w + l.at[PX_PART]);
     cudaStream_t s = (cudaStream_t)stream;
     st = launch_kernel(true, prefix_plan_kernel, p->n_groups, PLAN_THREADS, 0, s, a, p->prefix_len, p->n_groups);
     if (st != SV_OK) return st;
-    auto tables = [&](int i) {
-        a.bounds = ints(i);
-        a.desc = reinterpret_cast<int32_t *>(w + l.at[i] + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
-    };
     a.n_owners = p->n_groups;
-    tables(9);
     st = at.head_dim == 128 ? launch_groups<128>(a, s) : launch_groups<64>(a, s);
     if (st != SV_OK) return st;
     a.n_owners = at.batch;
-    tables(10);
-    a.part = reinterpret_cast<float *>(w + l.at[11]);
     return seg_nl(a.group * (at.gamma_max + 1)) == 1 ? launch_sequences<1>(a, s) : launch_sequences<2>(a, s);
 }

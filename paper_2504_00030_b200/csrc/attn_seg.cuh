@@ -48,12 +48,10 @@ struct PrefixPlan {
     int32_t *grp_rep;        // [n_groups] a member: its block table row has the pages
     int32_t *grp_n;          // [n_groups] positions of all members
     int32_t *grp_base;       // [n_groups] first of them in row_list
-    int32_t *row_list;       // query row of each position, group by group
+    int2 *row_list;          // query row of each position, group by group, and b * (gamma_max+1) + i
     int32_t *seq_pages;      // [batch] shared pages in front of the sequence (0: none)
-    int32_t *seq_at;         // [batch] first of the sequence's positions among its group's
-    int32_t *grp_pair0;      // [n_groups] first pair of a group in the group launch
-    int32_t *pair_first;     // [pairs of the group launch] block that holds a pair's first tile
-    float *part;             // partials of the group launch: slot = pair + block
+    float *part_o;           // what the groups leave for the sequences: unnormalised fp32 O of position b * (gamma_max+1) + i and
+    float2 *part_ml;         // head, [positions * hq][128], and its running maximum and sum
 };
 
 struct SegLaunch {
@@ -68,7 +66,7 @@ struct SegLaunch {
     const uint64_t *row_mask;
     const int32_t *n_list;
     int64_t list_stride;
-    const int32_t *seq_group;      // SEG_SEQ, SEG_GROUP
+    const int32_t *seq_group;      // of the plan kernel
     PrefixPlan plan;
     int32_t *bounds;         // [grid + 1]: first tile of every block
     int32_t *desc;           // [grid * 4]: a block's last segment, if its pair begins there and goes on: owner (else -1), pair
@@ -80,7 +78,6 @@ struct SegLaunch {
 struct SegCursor {
     int o, s, t;             // owner, pair of the owner, tile of the pair
     int n_sub, n_tiles;      // pairs of the owner, tiles of each
-    int pair;                // pairs before this one (SEG_GROUP)
     int b, h, chunk;         // sequence (SEG_GROUP: group), kv head, row chunk
     int R, L;                // positions of the owner, length (SEG_GROUP: of the prefix)
     int n_pages, page0;      // pages to read: entries of the list, or of the table from page0 on
@@ -153,7 +150,6 @@ template <int KIND, int NL>
 __device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
 {
     c.t = 0;
-    ++c.pair;
     if (++c.s >= c.n_sub) {
         c.s = 0;
         c.n_tiles = 0;
@@ -163,8 +159,7 @@ __device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
     seg_pair<KIND, NL>(a, c);
 }
 
-// The calling block's share, by the whole block (NT threads); block 0 publishes where each group begins, every block its first
-// tile.
+// The calling block's share, by the whole block (NT threads); every block publishes its first tile.
 template <int KIND, int NL, int NT>
 __device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, WorkShare *sh, long long (*red)[NT / 32])
 {
@@ -175,9 +170,6 @@ __device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, Work
             c.o = o;
             seg_owner<KIND, NL>(a, c, first && blockIdx.x == 0);
             return OwnerWork{c.n_sub, c.n_tiles};
-        },
-        [&](int o, int pair) {
-            if (KIND == SEG_GROUP && blockIdx.x == 0) a.plan.grp_pair0[o] = pair;
         },
         sh, red);
     if (threadIdx.x == 0) {
@@ -190,7 +182,7 @@ __device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, Work
 template <int KIND, int NL>
 __device__ __forceinline__ void seg_start(const SegLaunch &a, const WorkShare &sh, SegCursor &c)
 {
-    c.o = sh.o; c.s = sh.s; c.t = sh.t; c.pair = sh.pair;
+    c.o = sh.o; c.s = sh.s; c.t = sh.t;
     c.b = c.h = c.chunk = 0;
     if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; return; }
     seg_owner<KIND, NL>(a, c, false);
@@ -231,6 +223,33 @@ __device__ __forceinline__ bool seg_wait(uint32_t bar, uint32_t parity, int *abo
     return __all_sync(0xffffffffu, bounded_wait(bar, parity, abort_flag, status));
 }
 
+// the larger of three, and float32 pairs in one instruction
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t pair2(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ void split2(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // The online softmax of one row's TILE scores, as softmax_tile, with the keys that the row may see given per page:
 // lim[j] is the last visible slot of the tile's page j (below 0: none; 15 or more: all).
 template <int TILE, int O_CHUNKS, typename WaitPV>
@@ -258,13 +277,13 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
     }
     float m0 = -CUDART_INF_F, m1 = -CUDART_INF_F, m2 = -CUDART_INF_F, m3 = -CUDART_INF_F;
 #pragma unroll
-    for (int c = 0; c < TILE; c += 4) {
-        m0 = fmaxf(m0, __uint_as_float(s[c]));
-        m1 = fmaxf(m1, __uint_as_float(s[c + 1]));
-        m2 = fmaxf(m2, __uint_as_float(s[c + 2]));
-        m3 = fmaxf(m3, __uint_as_float(s[c + 3]));
+    for (int c = 0; c < TILE; c += 8) {
+        m0 = max3(m0, __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+        m1 = max3(m1, __uint_as_float(s[c + 2]), __uint_as_float(s[c + 3]));
+        m2 = max3(m2, __uint_as_float(s[c + 4]), __uint_as_float(s[c + 5]));
+        m3 = max3(m3, __uint_as_float(s[c + 6]), __uint_as_float(s[c + 7]));
     }
-    const float m_tile = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)) * c_scale;
+    const float m_tile = fmaxf(max3(m0, m1, m2), m3) * c_scale;
     float factor = 1.f;
     bool rescale = false;
     if ((m_tile > m_ref + RESCALE_THRESHOLD || m_ref == -CUDART_INF_F) && m_tile > -CUDART_INF_F) {
@@ -290,20 +309,19 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
     }
     // P = 2^(s*c - m_ref) as bf16 pairs over S: the tensor core multiplies bf16; the sums stay fp32 and unrounded, so P's
     // rounding (2^-9 relative, independent from key to key) averages out below the output's own
-    float tile_sum = 0.f;
+    const uint64_t c2 = pair2(c_scale, c_scale), m2n = pair2(-m_use, -m_use);
+    uint64_t sum = 0;                                  // two float32 zeros
 #pragma unroll
     for (int ch = 0; ch < TILE / 32; ++ch) {
-        float sum0 = 0.f, sum1 = 0.f;
         uint32_t pk[16];
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
-            const float e0 = ex2_approx(fmaf(__uint_as_float(s[ch * 32 + c]), c_scale, -m_use));
-            const float e1 = ex2_approx(fmaf(__uint_as_float(s[ch * 32 + c + 1]), c_scale, -m_use));
-            sum0 += e0;
-            sum1 += e1;
+            float x0, x1;
+            split2(fma2(pair2(__uint_as_float(s[ch * 32 + c]), __uint_as_float(s[ch * 32 + c + 1])), c2, m2n), x0, x1);
+            const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+            sum = add2(sum, pair2(e0, e1));
             pk[c >> 1] = pack_bf16(e0, e1);
         }
-        tile_sum += sum0 + sum1;
         asm volatile(
             "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
             "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(s_addr + ch * 16),
@@ -311,25 +329,10 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
             "r"(pk[9]), "r"(pk[10]), "r"(pk[11]), "r"(pk[12]), "r"(pk[13]), "r"(pk[14]), "r"(pk[15])
             : "memory");
     }
-    l_sum += tile_sum;
+    float sum0, sum1;
+    split2(sum, sum0, sum1);
+    l_sum += sum0 + sum1;
     return true;
-}
-
-// The partial of a sequence row's shared prefix: row `row` of a slot of the group launch (a pair's parts have been merged into
-// the first of them).
-struct PrefixPart {
-    const float *slot;       // NULL: nothing is shared
-    int row;
-};
-
-__device__ __forceinline__ PrefixPart prefix_part(const SegLaunch &a, int b, int h, int i, int hh)
-{
-    const PrefixPlan &pl = a.plan;
-    const int g = a.seq_group[b], k = pl.seq_at[b] + i;
-    const int ppp = 2 * a.ppl, chunks = (pl.grp_n[g] + ppp - 1) / ppp;       // the group launch has two row tiles a pair
-    const int chunk = k / ppp, in = k - chunk * ppp, tile = in / a.ppl;
-    const int pair = pl.grp_pair0[g] + h * chunks + chunk;
-    return {pl.part + (size_t)(pair + pl.pair_first[pair]) * seg_slot_floats(256), tile * 128 + (in - tile * a.ppl) * a.group + hh};
 }
 
 template <int NL> struct SegConfig {
@@ -584,7 +587,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         const int r = b0 + k * RPI + r0, i = r / G;
                         v[k] = make_uint4(0, 0, 0, 0);
                         if (r < n_rows) {
-                            const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + pos0 + i] : p.cu_q[cur.b] + pos0 + i;
+                            const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + pos0 + i].x : p.cu_q[cur.b] + pos0 + i;
                             const long long q_row = (long long)at * p.hq + (long long)cur.h * G + (r - i * G);
                             v[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D) + ch);
                         }
@@ -627,10 +630,13 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 const bool warp_active = tile_active && quarter * 32 < n_pos * G;
                 const bool row_ok = ri < n_pos;
                 const int i = pos0 + ri;
-                long long q_row = 0;
+                long long q_row = 0, part_row = 0;             // of the queries and outputs, and of the groups' partials
                 if (row_ok) {
-                    const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + i] : p.cu_q[cur.b] + i;
-                    q_row = (long long)at * p.hq + (long long)cur.h * G + hh;
+                    int2 at;
+                    if (KIND == SEG_GROUP) at = a.plan.row_list[a.plan.grp_base[cur.o] + i];
+                    else at = make_int2(p.cu_q[cur.b] + i, cur.b * (p.gamma_max + 1) + i);
+                    q_row = (long long)at.x * p.hq + (long long)cur.h * G + hh;
+                    part_row = (long long)at.y * p.hq + (long long)cur.h * G + hh;
                 }
                 // ---- this thread's query row into shared memory.  Every instruction that read the rows before has
                 // completed: this thread has seen the last S that they gave.
@@ -648,8 +654,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 SegCursor nxt = cur;
                 seg_next<KIND, NL>(a, nxt);
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
-                PrefixPart part = {nullptr, 0};
-                if (KIND == SEG_SEQ && whole && row_ok && cur.page0 > 0) part = prefix_part(a, cur.b, cur.h, i, hh);
+                const bool shared = KIND == SEG_SEQ && row_ok && cur.page0 > 0;        // a prefix's partial joins this row
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
                 const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
@@ -720,29 +725,33 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     // nothing to write
                 } else if (KIND != SEG_GROUP && whole) {
                     float m_all = m_ref, w0 = 1.f, w1 = 0.f;
-                    if (KIND == SEG_SEQ && part.slot != nullptr) {
-                        const float m1 = part.slot[256 * SEG_PITCH + part.row], l1 = part.slot[256 * SEG_PITCH + 256 + part.row];
-                        m_all = fmaxf(m_ref, m1);                              // both have keys: finite
+                    if (shared) {
+                        const float2 ml = a.plan.part_ml[part_row];
+                        m_all = fmaxf(m_ref, ml.x);                            // both have keys: finite
                         w0 = exp2f(m_ref - m_all);
-                        w1 = exp2f(m1 - m_all);
-                        l_sum = l_sum * w0 + l1 * w1;
+                        w1 = exp2f(ml.x - m_all);
+                        l_sum = l_sum * w0 + ml.y * w1;
                     }
                     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
 #pragma unroll
                     for (int ch = 0; ch < OCH; ++ch) {
+                        float4 x[KIND == SEG_SEQ ? 8 : 1];
+                        if (KIND == SEG_SEQ && shared) {
+                            const float4 *src = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH + ch * 32);
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) x[c] = src[c];
+                        }
                         uint32_t o[32];
                         tc_ld32(o_addr + ch * 32, o);
                         if (row_ok) {
-                            if (KIND == SEG_SEQ && part.slot != nullptr) {
-                                const float4 *x = reinterpret_cast<const float4 *>(part.slot + (size_t)part.row * SEG_PITCH + ch * 32);
+                            if (KIND == SEG_SEQ && shared) {
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) {
-                                    const float4 v = x[c];
-                                    o[4 * c] = __float_as_uint(fmaf(w1, v.x, w0 * __uint_as_float(o[4 * c])));
-                                    o[4 * c + 1] = __float_as_uint(fmaf(w1, v.y, w0 * __uint_as_float(o[4 * c + 1])));
-                                    o[4 * c + 2] = __float_as_uint(fmaf(w1, v.z, w0 * __uint_as_float(o[4 * c + 2])));
-                                    o[4 * c + 3] = __float_as_uint(fmaf(w1, v.w, w0 * __uint_as_float(o[4 * c + 3])));
+                                    o[4 * c] = __float_as_uint(fmaf(w1, x[c].x, w0 * __uint_as_float(o[4 * c])));
+                                    o[4 * c + 1] = __float_as_uint(fmaf(w1, x[c].y, w0 * __uint_as_float(o[4 * c + 1])));
+                                    o[4 * c + 2] = __float_as_uint(fmaf(w1, x[c].z, w0 * __uint_as_float(o[4 * c + 2])));
+                                    o[4 * c + 3] = __float_as_uint(fmaf(w1, x[c].w, w0 * __uint_as_float(o[4 * c + 3])));
                                 }
                             }
 #pragma unroll
@@ -759,10 +768,11 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     if (row_ok && p.lse != nullptr)
                         p.lse[q_row] = l_sum > 0.f ? (m_all + log2f(l_sum)) * 0.6931471805599453f : -CUDART_INF_F;
                 } else {
-                    const int slot_rows = NL * 128;
-                    const size_t slot_no = KIND == SEG_GROUP ? (size_t)cur.pair + blockIdx.x : (size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
-                    float *slot = (KIND == SEG_GROUP ? a.plan.part : a.part) + slot_no * seg_slot_floats(slot_rows);
+                    // unnormalised: a whole pair of a group to the positions' rows, a piece of a pair to a slot of this block
+                    const bool to_rows = KIND == SEG_GROUP && whole;
+                    float *slot = a.part + ((size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1)) * seg_slot_floats(NL * 128);
                     const int row = l * 128 + r;
+                    float *dst = to_rows ? a.plan.part_o + part_row * SEG_PITCH : slot + (size_t)row * SEG_PITCH;
 #pragma unroll
                     for (int ch = 0; ch < OCH; ++ch) {
                         uint32_t o[32];
@@ -770,26 +780,23 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         if (row_ok) {
 #pragma unroll
                             for (int c = 0; c < 32; c += 4)
-                                *reinterpret_cast<uint4 *>(slot + (size_t)row * SEG_PITCH + ch * 32 + c) =
-                                    make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                                *reinterpret_cast<uint4 *>(dst + ch * 32 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
                         }
                     }
                     if (row_ok) {
-                        slot[(size_t)slot_rows * SEG_PITCH + row] = m_ref;
-                        slot[(size_t)slot_rows * SEG_PITCH + slot_rows + row] = l_sum;
+                        if (to_rows) {
+                            a.plan.part_ml[part_row] = make_float2(m_ref, l_sum);
+                        } else {
+                            slot[(size_t)NL * 128 * SEG_PITCH + row] = m_ref;
+                            slot[(size_t)NL * 128 * SEG_PITCH + NL * 128 + row] = l_sum;
+                        }
                     }
                 }
                 tc_fence_before();
-                if (l == 0 && r == 0 && cur.t == 0) {
-                    if (KIND == SEG_GROUP) a.plan.pair_first[cur.pair] = blockIdx.x;
-                    if (seg_tiles < cur.n_tiles) {
-                        // the pair goes on in the next blocks: the combine kernel's block of this number merges its parts
-                        int32_t *d = a.desc + blockIdx.x * 4;
-                        d[0] = cur.o;
-                        d[1] = cur.s;
-                        d[2] = KIND == SEG_GROUP ? cur.pair : blockIdx.x * 2 + (seg_no == 0 ? 0 : 1);
-                        d[3] = (int)(tg + cur.n_tiles);
-                    }
+                if (l == 0 && r == 0 && cur.t == 0 && seg_tiles < cur.n_tiles) {
+                    // the pair goes on in the next blocks: the combine kernel merges its parts
+                    *reinterpret_cast<int4 *>(a.desc + blockIdx.x * 4) =
+                        make_int4(cur.o, cur.s, blockIdx.x * 2 + (seg_no == 0 ? 0 : 1), (int)(tg + cur.n_tiles));
                 }
                 tg += seg_tiles;
                 cur = nxt;
@@ -807,103 +814,128 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
 
 // ---------------------------------------------------------------------------- pairs that were split over blocks
 constexpr int SEG_COMBINE_WARPS = 8;
-constexpr int SEG_COMBINE_Y = 8;               // blocks that share a pair's rows
 
-// Blocks (c, *) merge the pair that begins in block c of the main kernel and goes on behind it, a warp per row, four parts
-// in flight.  A group's parts are merged into the first of them, in place.
+// Merges the pairs that begin in a block of the main kernel and go on behind it.  The work -- eight rows of a pair, a warp
+// each, `chunks` times for a pair -- is dealt out over all blocks, since few pairs may have many parts; P parts of a row are in flight at a time.  A
+// group's rows go where its whole pairs' rows are.
 template <int KIND, int NL, int D>
 __global__ void __launch_bounds__(SEG_COMBINE_WARPS * 32)
-attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid)
+attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int chunks)
 {
-    constexpr int SLOT_ROWS = NL * 128;
+    constexpr int SLOT_ROWS = NL * 128, NT = SEG_COMBINE_WARPS * 32;
+    static_assert(SEG_MAX_GRID / 32 == 32 && SEG_MAX_GRID % NT == 0, "a warp holds the counts of all words");
     pdl_enter();
-    __shared__ int s_slot[SEG_MAX_GRID];
+    __shared__ int s_split[SEG_MAX_GRID];      // blocks in which a split pair begins
     __shared__ int s_n;
-    const int4 d = *reinterpret_cast<const int4 *>(a.desc + blockIdx.x * 4);
-    if (d.x < 0) return;
     const sv_attn_params &p = a.p;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = a.group;
-    if (warp == 0) {
-        // the blocks behind this one whose tiles begin before the pair ends (empty ones hold nothing)
-        if (lane == 0) s_slot[0] = KIND == SEG_GROUP ? d.z + (int)blockIdx.x : d.z;
-        int n = 1;
-        for (int c0 = blockIdx.x + 1; c0 < main_grid; c0 += 32) {
-            const int c = c0 + lane;
-            const int lo = c < main_grid ? a.bounds[c] : 0x7fffffff, hi = c < main_grid ? a.bounds[c + 1] : 0;
-            const bool have = lo < d.w && hi > lo;
-            const unsigned m = __ballot_sync(0xffffffffu, have);
-            if (have) s_slot[n + __popc(m & ((1u << lane) - 1))] = KIND == SEG_GROUP ? d.z + c : c * 2;
-            n += __popc(m);
-            if (__any_sync(0xffffffffu, lo >= d.w)) break;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.group;
+    {                                          // in order, so that all blocks deal out the same list
+        __shared__ int s_count[SEG_MAX_GRID / 32];
+        bool have[SEG_MAX_GRID / NT];
+        unsigned mine[SEG_MAX_GRID / NT];
+#pragma unroll
+        for (int j = 0; j < SEG_MAX_GRID / NT; ++j) have[j] = j * NT + tid < main_grid && a.desc[(j * NT + tid) * 4] >= 0;
+#pragma unroll
+        for (int j = 0; j < SEG_MAX_GRID / NT; ++j) {
+            mine[j] = __ballot_sync(0xffffffffu, have[j]);
+            if (lane == 0) s_count[j * SEG_COMBINE_WARPS + warp] = __popc(mine[j]);
         }
-        if (lane == 0) s_n = n;
+        __syncthreads();
+        const int n = s_count[lane];           // SEG_MAX_GRID / 32 = 32 words
+        int upto = n;
+#pragma unroll
+        for (int dd = 1; dd < 32; dd <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, dd);
+            if (lane >= dd) upto += x;
+        }
+#pragma unroll
+        for (int j = 0; j < SEG_MAX_GRID / NT; ++j) {
+            const int at = __shfl_sync(0xffffffffu, upto - n, j * SEG_COMBINE_WARPS + warp);
+            if (have[j]) s_split[at + __popc(mine[j] & ((1u << lane) - 1))] = j * NT + tid;
+        }
+        if (warp == 0 && lane == 31) s_n = upto;
     }
-    SegCursor cur;
-    cur.o = d.x; cur.s = d.y; cur.t = cur.pair = 0;
-    seg_owner<KIND, NL>(a, cur, false);
-    seg_pair<KIND, NL>(a, cur);
     __syncthreads();
-    const int n_parts = s_n;
-    const int pos0 = cur.chunk * NL * a.ppl, n_pos = min(cur.R - pos0, NL * a.ppl);
     const bool lane_on = 4 * lane < D;
     constexpr size_t slot_floats = (size_t)SLOT_ROWS * (SEG_PITCH + 2);
-    float *parts = KIND == SEG_GROUP ? a.plan.part : a.part;
-    for (int k = blockIdx.y * SEG_COMBINE_WARPS + warp; k < n_pos * G; k += SEG_COMBINE_Y * SEG_COMBINE_WARPS) {
+    for (int u = blockIdx.x; u < s_n * chunks; u += gridDim.x) {
+        const int begin = s_split[u / chunks], k = u % chunks * SEG_COMBINE_WARPS + warp;
+        const int4 d = *reinterpret_cast<const int4 *>(a.desc + begin * 4);
+        SegCursor cur;
+        cur.o = d.x; cur.s = d.y; cur.t = 0;
+        seg_owner<KIND, NL>(a, cur, false);
+        seg_pair<KIND, NL>(a, cur);
+        const int pos0 = cur.chunk * NL * a.ppl, n_pos = min(cur.R - pos0, NL * a.ppl);
+        if (k >= n_pos * G) continue;
         const int in = k / G, hh = k - in * G, i = pos0 + in;
         const int tile = in / a.ppl, row = tile * 128 + (in - tile * a.ppl) * G + hh;
+        int2 at;
+        if (KIND == SEG_GROUP) at = a.plan.row_list[a.plan.grp_base[cur.o] + i];
+        else at = make_int2(p.cu_q[cur.b] + i, cur.b * (p.gamma_max + 1) + i);
+        const long long q_row = (long long)at.x * p.hq + (long long)cur.h * G + hh, part_row = (long long)at.y * p.hq + (long long)cur.h * G + hh;
         float m_run = -CUDART_INF_F, l_run = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        // four partials (those that are there: have[u]) into the running one
-        auto merge = [&](const float (&m)[4], const float (&l)[4], const float4 (&v)[4]) {
+        constexpr int P = NL == 1 ? 8 : 4;
+        // P partials into the running one; -inf: not there
+        auto merge = [&](const float (&m)[P], const float (&l)[P], const float4 (&v)[P]) {
             float m_new = m_run;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, m[u]);
+            for (int j = 0; j < P; ++j) m_new = fmaxf(m_new, m[j]);
             if (m_new == -CUDART_INF_F) return;
             const float w_old = exp2f(m_run - m_new);
             acc.x *= w_old; acc.y *= w_old; acc.z *= w_old; acc.w *= w_old;
             l_run *= w_old;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (m[u] == -CUDART_INF_F) continue;
-                const float w = exp2f(m[u] - m_new);
-                l_run += w * l[u];
-                acc.x += w * v[u].x; acc.y += w * v[u].y; acc.z += w * v[u].z; acc.w += w * v[u].w;
+            for (int j = 0; j < P; ++j) {
+                if (m[j] == -CUDART_INF_F) continue;
+                const float w = exp2f(m[j] - m_new);
+                l_run += w * l[j];
+                acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
             }
             m_run = m_new;
         };
-        for (int j0 = 0; j0 < n_parts; j0 += 4) {
-            float m[4], l[4];
-            float4 v[4];
+        auto take = [&](const float *slot, float &m, float &l, float4 &v) {
+            m = slot[(size_t)SLOT_ROWS * SEG_PITCH + row];
+            l = slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row];
+            v = lane_on ? reinterpret_cast<const float4 *>(slot + (size_t)row * SEG_PITCH)[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+        };
+        // the first part (and the shared prefix's), then the first slots of the blocks behind it whose tiles begin before the
+        // pair ends
+        bool first = true;
+        for (int c0 = begin + 1; first || c0 < main_grid; c0 += 32) {
+            const int c = c0 + lane;
+            const int lo = c < main_grid ? a.bounds[c] : 0x7fffffff, hi = c < main_grid ? a.bounds[c + 1] : 0;
+            unsigned have = __ballot_sync(0xffffffffu, lo < d.w && hi > lo);       // empty blocks hold nothing
+            while (first || have != 0) {
+                float m[P], l[P];
+                float4 v[P];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const bool have = j0 + u < n_parts;
-                const float *slot = parts + (size_t)s_slot[have ? j0 + u : 0] * slot_floats;
-                m[u] = have ? slot[(size_t)SLOT_ROWS * SEG_PITCH + row] : -CUDART_INF_F;
-                l[u] = have ? slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row] : 0.f;
-                v[u] = have && lane_on ? reinterpret_cast<const float4 *>(slot + (size_t)row * SEG_PITCH)[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int j = 0; j < P; ++j) {
+                    m[j] = -CUDART_INF_F;
+                    l[j] = 0.f;
+                    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (j == 0 && first) {
+                        take(a.part + (size_t)d.z * slot_floats, m[j], l[j], v[j]);
+                    } else if (j == 1 && first && KIND == SEG_SEQ && cur.page0 > 0) {
+                        const float2 ml = a.plan.part_ml[part_row];
+                        m[j] = ml.x;
+                        l[j] = ml.y;
+                        if (lane_on) v[j] = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH)[lane];
+                    } else if (have != 0) {
+                        take(a.part + (size_t)(c0 + __ffs(have) - 1) * 2 * slot_floats, m[j], l[j], v[j]);
+                        have &= have - 1;
+                    }
+                }
+                merge(m, l, v);
+                first = false;
             }
-            merge(m, l, v);
+            if (__any_sync(0xffffffffu, lo >= d.w)) break;
         }
         if (KIND == SEG_GROUP) {
-            float *slot = parts + (size_t)s_slot[0] * slot_floats;
-            __syncwarp();
-            if (lane_on) reinterpret_cast<float4 *>(slot + (size_t)row * SEG_PITCH)[lane] = acc;
-            if (lane == 0) {
-                slot[(size_t)SLOT_ROWS * SEG_PITCH + row] = m_run;
-                slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row] = l_run;
-            }
+            if (lane_on) reinterpret_cast<float4 *>(a.plan.part_o + part_row * SEG_PITCH)[lane] = acc;
+            if (lane == 0) a.plan.part_ml[part_row] = make_float2(m_run, l_run);
             continue;
         }
-        if (KIND == SEG_SEQ && cur.page0 > 0) {
-            const PrefixPart x = prefix_part(a, cur.b, cur.h, i, hh);
-            float m[4] = {x.slot[256 * SEG_PITCH + x.row], -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-            float l[4] = {x.slot[256 * SEG_PITCH + 256 + x.row], 0.f, 0.f, 0.f};
-            float4 v[4];
-            v[0] = v[1] = v[2] = v[3] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (lane_on) v[0] = reinterpret_cast<const float4 *>(x.slot + (size_t)x.row * SEG_PITCH)[lane];
-            merge(m, l, v);
-        }
-        const long long q_row = ((long long)p.cu_q[cur.b] + i) * p.hq + (long long)cur.h * G + hh;
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
         if (lane_on) {
             uint2 w;
@@ -945,7 +977,11 @@ sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
 template <int KIND, int NL, int D>
 sv_status launch_seg_combine(const SegLaunch &a, int grid, cudaStream_t stream)
 {
-    return launch_kernel(true, attn_seg_combine_kernel<KIND, NL, D>, dim3((unsigned)grid, SEG_COMBINE_Y), SEG_COMBINE_WARPS * 32, 0, stream, a, grid);
+    // a pair's rows: a group's fill their tiles, a sequence has at most G (gamma_max+1)
+    int rows = NL * 128;
+    if (KIND != SEG_GROUP && a.group * (a.p.gamma_max + 1) < rows) rows = a.group * (a.p.gamma_max + 1);
+    return launch_kernel(true, attn_seg_combine_kernel<KIND, NL, D>, sm_count() * (NL == 1 ? 4 : 6), SEG_COMBINE_WARPS * 32, 0, stream, a, grid,
+                         (rows + SEG_COMBINE_WARPS - 1) / SEG_COMBINE_WARPS);
 }
 
 }  // namespace sv

@@ -160,7 +160,8 @@ __device__ __forceinline__ void store_keys(uint32_t acc, int cols, int G, float 
             for (int c = 0; c < 32; c += (GT > 0 ? GT : 1)) {
                 int m = (int)r[c];
 #pragma unroll
-                for (int j = 1; j < GT; ++j) m = max(m, (int)r[c + j]);
+                for (int j = 1; j + 1 < GT; j += 2) m = __vimax3_s32(m, (int)r[c + j], (int)r[c + j + 1]);
+                if (GT > 1) m = max(m, (int)r[c + GT - 1]);            // GT is even
                 if (used && c0 + c < cols) *dst = score_key(m, scale);
                 dst += stride;
             }
@@ -230,7 +231,7 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
             SeqRows sr;
             return score_owner(a, b, sr);
         },
-        [](int, int) {}, &sh->share, reinterpret_cast<long long(*)[SC_THREADS / 32]>(tile_buf));
+        &sh->share, reinterpret_cast<long long(*)[SC_THREADS / 32]>(tile_buf));
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -769,10 +770,10 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
         const sv_status st = p->head_dim == 128 ? launch_score<128>(a, grid, s) : launch_score<64>(a, grid, s);
         if (st != SV_OK) return st;
     }
-    // Warps per row: enough to hold a row's scores in registers, and four where a block has few rows.
+    // Warps per row: enough to hold a row's keys in registers, and more where a block has few rows, down to four keys a thread
     int need = 1;
     while (need < PK_WARPS && (long long)need * 32 * 32 < max_pages) need *= 2;
-    while (need < 4 && need * 2 * R <= 4) need *= 2;
+    while (need < PK_WARPS && need * 2 * R <= PK_WARPS && need * 32 * 4 < max_pages) need *= 2;
     // Rows at a time: as few rounds as 16 warps allow, and no more warps than these rounds need (17 rows: two rounds of nine)
     const int rounds = (R * need + PK_WARPS - 1) / PK_WARPS, teams = (R + rounds - 1) / rounds;
     const size_t smem = (size_t)teams * PK_BINS * sizeof(int) + (in_smem ? row_bits : 0);

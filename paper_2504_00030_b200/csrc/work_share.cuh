@@ -16,14 +16,13 @@ struct OwnerWork {
 struct WorkShare {
     long long t_begin, t_end;    // the block's tiles
     long long total;             // tiles of the list
-    int o, s, t, pair;           // owner, pair of the owner and tile of t_begin (t may be n_tiles: the next pair); pairs before it
+    int o, s, t;                 // owner, pair of the owner and tile of t_begin (t may be n_tiles: the next pair)
 };
 
-// By the whole block of NT threads, with a barrier at the end.  owner(o, report): the work of owner o (report: first look);
-// seen(o, pair): called once per owner that has work, with the pairs in front of it.  red: shared scratch.
-template <int NT, typename Owner, typename Seen>
-__device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Owner &&owner, Seen &&seen, WorkShare *sh,
-                                                long long (*red)[NT / 32])
+// By the whole block of NT threads, with a barrier at the end.  owner(o, report): the work of owner o (report: first look).
+// red: two rows of shared scratch.
+template <int NT, typename Owner>
+__device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Owner &&owner, WorkShare *sh, long long (*red)[NT / 32])
 {
     constexpr int NW = NT / 32;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -48,10 +47,10 @@ __device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Own
     const long long xb = blockIdx.x * cost_all / gridDim.x, xe = (blockIdx.x + 1LL) * cost_all / gridDim.x;
     if (tid == 0) {
         sh->t_begin = sh->t_end = sh->total = tiles_all;
-        sh->o = n_owners; sh->s = sh->t = sh->pair = 0;
+        sh->o = n_owners; sh->s = sh->t = 0;
     }
     __syncthreads();
-    long long cost0 = 0, tiles0 = 0, pairs0 = 0;
+    long long cost0 = 0, tiles0 = 0;
     for (int base = 0; base < n_owners; base += NT) {
         const int o = base + tid;
         if (!one) {
@@ -59,31 +58,29 @@ __device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Own
             if (o < n_owners) w = owner(o, false);
         }
         const long long w_cost = w.n_tiles > 0 ? (long long)w.n_sub * (w.n_tiles + pair_cost) : 0;
-        const long long w_tiles = (long long)w.n_sub * w.n_tiles, w_pairs = w.n_tiles > 0 ? w.n_sub : 0;
-        long long vc = w_cost, vt = w_tiles, vp = w_pairs;
+        const long long w_tiles = (long long)w.n_sub * w.n_tiles;
+        long long vc = w_cost, vt = w_tiles;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, vc, d), y = __shfl_up_sync(0xffffffffu, vt, d),
-                            z = __shfl_up_sync(0xffffffffu, vp, d);
-            if (lane >= d) { vc += x; vt += y; vp += z; }
+            const long long x = __shfl_up_sync(0xffffffffu, vc, d), y = __shfl_up_sync(0xffffffffu, vt, d);
+            if (lane >= d) { vc += x; vt += y; }
         }
-        if (lane == 31) { red[0][warp] = vc; red[1][warp] = vt; red[2][warp] = vp; }
+        if (lane == 31) { red[0][warp] = vc; red[1][warp] = vt; }
         __syncthreads();
-        long long bc = cost0, bt = tiles0, bp = pairs0;
+        long long bc = cost0, bt = tiles0;
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            if (i < warp) { bc += red[0][i]; bt += red[1][i]; bp += red[2][i]; }
-            cost0 += red[0][i]; tiles0 += red[1][i]; pairs0 += red[2][i];
+            if (i < warp) { bc += red[0][i]; bt += red[1][i]; }
+            cost0 += red[0][i]; tiles0 += red[1][i];
         }
         const long long lo = bc + vc - w_cost, hi = bc + vc;
-        const long long tile_lo = bt + vt - w_tiles, pair_lo = bp + vp - w_pairs;
+        const long long tile_lo = bt + vt - w_tiles;
         if (w_cost > 0) {
-            seen(o, (int)pair_lo);
             const int per = w.n_tiles + pair_cost;
             if (lo <= xb && xb < hi) {
                 const long long j = (xb - lo) / per, off = min(xb - lo - j * per, (long long)w.n_tiles);
                 sh->t_begin = tile_lo + j * w.n_tiles + off;
-                sh->o = o; sh->s = (int)j; sh->t = (int)off; sh->pair = (int)(pair_lo + j);
+                sh->o = o; sh->s = (int)j; sh->t = (int)off;
             }
             if (lo <= xe && xe < hi) {
                 const long long j = (xe - lo) / per, off = min(xe - lo - j * per, (long long)w.n_tiles);
