@@ -5,7 +5,7 @@
 //   plan      the members of each group and where their rows are;
 //   groups    the prefixes: 256 rows of any members meet each key tile (tensor-core bound; a rows * heads * head_dim fp32
 //             partial per group is written and read once, 520 bytes a row and head);
-//   sequences the rest of every sequence, finished with the group's partials;
+//   sequences the rest of every sequence: its rows begin with the group's partial O, maximum and sum in place of zeros;
 //   combine   behind either of the two: pairs that were split over blocks.
 #include "attn_seg.cuh"
 

@@ -495,6 +495,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             for (; left > 0 && ok; ++seg_no) {
                 const int seg_tiles = __reduce_max_sync(0xffffffffu, min(cur.n_tiles - cur.t, left));
                 const int n_pos = cur.R - cur.chunk * NL * ppl;
+                const uint32_t o_there = KIND == SEG_SEQ && __reduce_max_sync(0xffffffffu, cur.page0 > 0 && cur.t == 0) ? 1u : 0u;
                 const bool active = NL == 1 || l == 0 || __reduce_max_sync(0xffffffffu, n_pos > ppl ? 1 : 0) != 0;
                 SegCursor nxt = cur;
                 const int qb = q_ahead ? (int)(seg_no & 1) : 0;
@@ -535,7 +536,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
 #pragma unroll
                             for (int ks = 0; ks < TILE / 16; ++ks)
                                 tc_mma_ts(tm + O_COL0 + l * 128, tm + buf * TILE + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)),
-                                          idesc_pv, (ti > 0 || ks > 0) ? 1u : 0u);
+                                          idesc_pv, (ti > 0 || ks > 0) ? 1u : o_there);
                             tc_commit(smem_u32(&sh->o_done[buf]));
                             tc_commit(smem_u32(&sh->empty[v_at.slot]));        // V tile consumed
                         }
@@ -654,7 +655,6 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 SegCursor nxt = cur;
                 seg_next<KIND, NL>(a, nxt);
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
-                const bool shared = KIND == SEG_SEQ && row_ok && cur.page0 > 0;        // a prefix's partial joins this row
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
                 const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
@@ -663,6 +663,34 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 int e_base = -32, e_lp = -1;                   // lane l: entry e_base + l of the list and its mask
                 uint32_t e_lo = 0, e_hi = 0;
                 float m_ref = -CUDART_INF_F, l_sum = 0.f;
+                // behind a shared prefix the row begins with what its group left
+                const bool joins = KIND == SEG_SEQ && cur.page0 > 0 && cur.t == 0;
+                if (joins && warp_active) {
+                    if (row_ok) {
+                        const float2 ml = a.plan.part_ml[part_row];
+                        m_ref = ml.x;
+                        l_sum = ml.y;
+                    }
+                    const float4 *src = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH);
+#pragma unroll
+                    for (int ch = 0; ch < OCH; ch += 2) {
+                        float4 x[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) x[c] = row_ok ? src[ch * 8 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            uint32_t o[32];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                o[4 * c] = __float_as_uint(x[z * 8 + c].x);
+                                o[4 * c + 1] = __float_as_uint(x[z * 8 + c].y);
+                                o[4 * c + 2] = __float_as_uint(x[z * 8 + c].z);
+                                o[4 * c + 3] = __float_as_uint(x[z * 8 + c].w);
+                            }
+                            tc_st32(o_addr + (ch + z) * 32, o);
+                        }
+                    }
+                }
                 if (tile_active) {
                     for (int ti = 0; ti < seg_tiles && ok; ++ti, ++cnt) {
                         const int buf = l * NB + (int)(cnt % NB);
@@ -704,7 +732,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                             continue;
                         }
                         tc_fence_after();
-                        ok = seg_softmax<TILE, OCH>(tmem + lane_addr + buf * TILE, o_addr, lim, c_scale, ti == 0, m_ref, l_sum, [&]() {
+                        ok = seg_softmax<TILE, OCH>(tmem + lane_addr + buf * TILE, o_addr, lim, c_scale, ti == 0 && !joins, m_ref, l_sum, [&]() {
                             const uint32_t g = cnt - 1;
                             return seg_wait(smem_u32(&sh->o_done[l * NB + (int)(g % NB)]), (g / NB) & 1, abort_flag, status);
                         });
@@ -724,36 +752,13 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (!warp_active) {
                     // nothing to write
                 } else if (KIND != SEG_GROUP && whole) {
-                    float m_all = m_ref, w0 = 1.f, w1 = 0.f;
-                    if (shared) {
-                        const float2 ml = a.plan.part_ml[part_row];
-                        m_all = fmaxf(m_ref, ml.x);                            // both have keys: finite
-                        w0 = exp2f(m_ref - m_all);
-                        w1 = exp2f(ml.x - m_all);
-                        l_sum = l_sum * w0 + ml.y * w1;
-                    }
                     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
 #pragma unroll
                     for (int ch = 0; ch < OCH; ++ch) {
-                        float4 x[KIND == SEG_SEQ ? 8 : 1];
-                        if (KIND == SEG_SEQ && shared) {
-                            const float4 *src = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH + ch * 32);
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) x[c] = src[c];
-                        }
                         uint32_t o[32];
                         tc_ld32(o_addr + ch * 32, o);
                         if (row_ok) {
-                            if (KIND == SEG_SEQ && shared) {
-#pragma unroll
-                                for (int c = 0; c < 8; ++c) {
-                                    o[4 * c] = __float_as_uint(fmaf(w1, x[c].x, w0 * __uint_as_float(o[4 * c])));
-                                    o[4 * c + 1] = __float_as_uint(fmaf(w1, x[c].y, w0 * __uint_as_float(o[4 * c + 1])));
-                                    o[4 * c + 2] = __float_as_uint(fmaf(w1, x[c].z, w0 * __uint_as_float(o[4 * c + 2])));
-                                    o[4 * c + 3] = __float_as_uint(fmaf(w1, x[c].w, w0 * __uint_as_float(o[4 * c + 3])));
-                                }
-                            }
 #pragma unroll
                             for (int c = 0; c < 32; c += 8) {
                                 uint4 w;
@@ -766,7 +771,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         }
                     }
                     if (row_ok && p.lse != nullptr)
-                        p.lse[q_row] = l_sum > 0.f ? (m_all + log2f(l_sum)) * 0.6931471805599453f : -CUDART_INF_F;
+                        p.lse[q_row] = l_sum > 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -CUDART_INF_F;
                 } else {
                     // unnormalised: a whole pair of a group to the positions' rows, a piece of a pair to a slot of this block
                     const bool to_rows = KIND == SEG_GROUP && whole;
@@ -869,10 +874,9 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
         if (k >= n_pos * G) continue;
         const int in = k / G, hh = k - in * G, i = pos0 + in;
         const int tile = in / a.ppl, row = tile * 128 + (in - tile * a.ppl) * G + hh;
-        int2 at;
-        if (KIND == SEG_GROUP) at = a.plan.row_list[a.plan.grp_base[cur.o] + i];
-        else at = make_int2(p.cu_q[cur.b] + i, cur.b * (p.gamma_max + 1) + i);
-        const long long q_row = (long long)at.x * p.hq + (long long)cur.h * G + hh, part_row = (long long)at.y * p.hq + (long long)cur.h * G + hh;
+        // where the row goes: to the positions' partials of a group, or to the outputs
+        const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + i].y : p.cu_q[cur.b] + i;
+        const long long dst_row = (long long)at * p.hq + (long long)cur.h * G + hh;
         float m_run = -CUDART_INF_F, l_run = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int P = NL == 1 ? 8 : 4;
@@ -899,7 +903,7 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
             l = slot[(size_t)SLOT_ROWS * SEG_PITCH + SLOT_ROWS + row];
             v = lane_on ? reinterpret_cast<const float4 *>(slot + (size_t)row * SEG_PITCH)[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
         };
-        // the first part (and the shared prefix's), then the first slots of the blocks behind it whose tiles begin before the
+        // the first part, then the first slots of the blocks behind it whose tiles begin before the
         // pair ends
         bool first = true;
         for (int c0 = begin + 1; first || c0 < main_grid; c0 += 32) {
@@ -916,11 +920,6 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
                     v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (j == 0 && first) {
                         take(a.part + (size_t)d.z * slot_floats, m[j], l[j], v[j]);
-                    } else if (j == 1 && first && KIND == SEG_SEQ && cur.page0 > 0) {
-                        const float2 ml = a.plan.part_ml[part_row];
-                        m[j] = ml.x;
-                        l[j] = ml.y;
-                        if (lane_on) v[j] = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH)[lane];
                     } else if (have != 0) {
                         take(a.part + (size_t)(c0 + __ffs(have) - 1) * 2 * slot_floats, m[j], l[j], v[j]);
                         have &= have - 1;
@@ -932,8 +931,8 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
             if (__any_sync(0xffffffffu, lo >= d.w)) break;
         }
         if (KIND == SEG_GROUP) {
-            if (lane_on) reinterpret_cast<float4 *>(a.plan.part_o + part_row * SEG_PITCH)[lane] = acc;
-            if (lane == 0) a.plan.part_ml[part_row] = make_float2(m_run, l_run);
+            if (lane_on) reinterpret_cast<float4 *>(a.plan.part_o + dst_row * SEG_PITCH)[lane] = acc;
+            if (lane == 0) a.plan.part_ml[dst_row] = make_float2(m_run, l_run);
             continue;
         }
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
@@ -941,10 +940,10 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
             uint2 w;
             w.x = pack_bf16(acc.x * inv, acc.y * inv);
             w.y = pack_bf16(acc.z * inv, acc.w * inv);
-            reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + q_row * D)[lane] = w;
+            reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + dst_row * D)[lane] = w;
         }
         if (lane == 0 && p.lse != nullptr)
-            p.lse[q_row] = l_run > 0.f ? (m_run + log2f(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
+            p.lse[dst_row] = l_run > 0.f ? (m_run + log2f(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
     }
 }
 
