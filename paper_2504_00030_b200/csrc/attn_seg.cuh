@@ -335,11 +335,13 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
     return true;
 }
 
+// a pair's start and end, in key tiles
+__host__ __device__ constexpr int seg_pair_cost(int kind) { return kind == SEG_LIST ? 3 : kind == SEG_SEQ ? 8 : 12; }
+
 template <int NL> struct SegConfig {
     static constexpr int THREADS = 128 + 128 * NL;
     static constexpr int BLOCKS = NL == 1 ? 2 : 1;             // blocks per multiprocessor
     static constexpr uint32_t TMEM_COLS = NL == 1 ? 256 : 512;
-    static constexpr int COST = 4;                             // a pair's start and end, in key tiles
 };
 
 template <int KIND, int NL, int D>
@@ -399,7 +401,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // the plan's sums share the queries' memory, which nothing touches before the barrier below
-    seg_plan<KIND, NL, NT>(a, SegConfig<NL>::COST, &sh->share, reinterpret_cast<long long(*)[NT / 32]>(seg_smem));
+    seg_plan<KIND, NL, NT>(a, seg_pair_cost(KIND), &sh->share, reinterpret_cast<long long(*)[NT / 32]>(seg_smem));
     tc_fence_before();
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
