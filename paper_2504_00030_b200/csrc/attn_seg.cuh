@@ -223,6 +223,21 @@ __device__ __forceinline__ bool seg_wait(uint32_t bar, uint32_t parity, int *abo
     return __all_sync(0xffffffffu, bounded_wait(bar, parity, abort_flag, status));
 }
 
+// eight float32 of a partial row (32-byte aligned) at a time: a whole sector of the memory, where 16 bytes a thread would
+// touch each sector twice
+__device__ __forceinline__ void store8(float *dst, const uint32_t *o)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]),
+                 "r"(o[5]), "r"(o[6]), "r"(o[7])
+                 : "memory");
+}
+__device__ __forceinline__ void load8(const float *src, uint32_t *x)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
+                 : "l"(src));
+}
+
 // the larger of three, and float32 pairs in one instruction
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -644,12 +659,22 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 // ---- this thread's query row into shared memory.  Every instruction that read the rows before has
                 // completed: this thread has seen the last S that they gave.
                 if (!q_ahead && warp_active) {
-                    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D);
-                    uint8_t *dst = q_smem + l * Q_BYTES + r * 128;
+                    // D / 8 lanes for a row: whole lines, where a thread for each row would touch 32 lines a load
+                    constexpr int LPR = D / 8, RPI = 32 / LPR;
+                    const int ch = lane % LPR, sub = lane / LPR;
+                    uint4 v[32 / RPI];
 #pragma unroll
-                    for (int c = 0; c < D / 8; ++c) {
-                        const uint4 v = row_ok ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-                        *reinterpret_cast<uint4 *>(dst + (c >> 3) * 16384 + (((c & 7) ^ (r & 7)) << 4)) = v;
+                    for (int k = 0; k < 32 / RPI; ++k) {
+                        const int from = k * RPI + sub;                        // the warp's row: the lane that knows its place
+                        const long long qr = __shfl_sync(0xffffffffu, q_row, from);
+                        const int have = __shfl_sync(0xffffffffu, (int)row_ok, from);
+                        v[k] = have ? __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + qr * D) + ch) : make_uint4(0, 0, 0, 0);
+                    }
+                    uint8_t *dst = q_smem + l * Q_BYTES + (ch >> 3) * 16384;
+#pragma unroll
+                    for (int k = 0; k < 32 / RPI; ++k) {
+                        const int rr = quarter * 32 + k * RPI + sub;
+                        *reinterpret_cast<uint4 *>(dst + rr * 128 + (((ch & 7) ^ (rr & 7)) << 4)) = v[k];
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
@@ -673,24 +698,18 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         m_ref = ml.x;
                         l_sum = ml.y;
                     }
-                    const float4 *src = reinterpret_cast<const float4 *>(a.plan.part_o + part_row * SEG_PITCH);
+                    const float *src = a.plan.part_o + part_row * SEG_PITCH;
 #pragma unroll
                     for (int ch = 0; ch < OCH; ch += 2) {
-                        float4 x[16];
+                        uint32_t x[2][32];
 #pragma unroll
-                        for (int c = 0; c < 16; ++c) x[c] = row_ok ? src[ch * 8 + c] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int c = 0; c < 64; c += 8) {
 #pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            uint32_t o[32];
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) {
-                                o[4 * c] = __float_as_uint(x[z * 8 + c].x);
-                                o[4 * c + 1] = __float_as_uint(x[z * 8 + c].y);
-                                o[4 * c + 2] = __float_as_uint(x[z * 8 + c].z);
-                                o[4 * c + 3] = __float_as_uint(x[z * 8 + c].w);
-                            }
-                            tc_st32(o_addr + (ch + z) * 32, o);
+                            for (int z = 0; z < 8; ++z) x[c >> 5][(c & 31) + z] = 0;
+                            if (row_ok) load8(src + ch * 32 + c, &x[c >> 5][c & 31]);
                         }
+                        tc_st32(o_addr + ch * 32, x[0]);
+                        tc_st32(o_addr + ch * 32 + 32, x[1]);
                     }
                 }
                 if (tile_active) {
@@ -786,8 +805,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         tc_ld32(o_addr + ch * 32, o);
                         if (row_ok) {
 #pragma unroll
-                            for (int c = 0; c < 32; c += 4)
-                                *reinterpret_cast<uint4 *>(dst + ch * 32 + c) = make_uint4(o[c], o[c + 1], o[c + 2], o[c + 3]);
+                            for (int c = 0; c < 32; c += 8) store8(dst + ch * 32 + c, o + c);
                         }
                     }
                     if (row_ok) {
