@@ -196,7 +196,7 @@ struct SegShared {
     uint64_t s_full[4];          // S ready (row tile * 2 + parity of the key tile)
     uint64_t p_full[4];          // P written
     uint64_t o_done[4];          // P V finished
-    uint64_t q_full[2];          // a segment's query rows are in shared memory
+    uint64_t q_full[2];          // query rows are in shared memory: (q_ahead) of the buffer, else of the row tile
     uint64_t q_empty[2];         // (q_ahead) and were read for the last time
     uint64_t drained[2];         // a row tile's instructions are through (after an expired wait)
     uint32_t tmem_base;
@@ -402,7 +402,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             mbar_init(smem_u32(&sh->o_done[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh->q_full[i]), a.q_ahead ? 1 : 128 * NL);
+            mbar_init(smem_u32(&sh->q_full[i]), q_ahead ? 1 : 128);
             mbar_init(smem_u32(&sh->q_empty[i]), 1);
         }
         for (int i = 0; i < NL; ++i) mbar_init(smem_u32(&sh->drained[i]), 1);
@@ -501,7 +501,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             const uint32_t idesc_qk = instr_desc(false, TILE), idesc_pv = instr_desc(true, D);
             SegCursor cur;
             seg_start<KIND, NL>(a, sh->share, cur);
-            uint32_t seg_no = 0, cnt = 0;                      // cnt: tiles of this row tile so far
+            uint32_t seg_no = 0, cnt = 0;                      // segments and tiles in which this row tile has rows, so far
             RingPos k_at(0), v_at(1);                          // of the next Q K^T and the next P V
             // What steers the loops and makes up the descriptors goes through a warp-wide reduction, whose result the
             // compiler knows to be the same in all lanes: the operands of the instructions then stay in uniform registers,
@@ -509,15 +509,20 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
             int left = __reduce_max_sync(0xffffffffu, (int)(t_end - t_begin));
             bool ok = true;
-            for (; left > 0 && ok; ++seg_no) {
+            while (left > 0 && ok) {
                 const int seg_tiles = __reduce_max_sync(0xffffffffu, min(cur.n_tiles - cur.t, left));
                 const int n_pos = cur.R - cur.chunk * NL * ppl;
                 const uint32_t o_there = KIND == SEG_SEQ && __reduce_max_sync(0xffffffffu, cur.page0 > 0 && cur.t == 0) ? 1u : 0u;
                 const bool active = NL == 1 || l == 0 || __reduce_max_sync(0xffffffffu, n_pos > ppl ? 1 : 0) != 0;
                 SegCursor nxt = cur;
                 const int qb = q_ahead ? (int)(seg_no & 1) : 0;
-                ok = seg_wait(smem_u32(&sh->q_full[qb]), q_ahead ? (seg_no >> 1) & 1 : seg_no & 1, abort_flag, status);
-                tc_fence_after();
+                if (active) {                                  // a row tile without rows brings no queries and counts no segment
+                    ok = q_ahead ? seg_wait(smem_u32(&sh->q_full[qb]), (seg_no >> 1) & 1, abort_flag, status)
+                                 : seg_wait(smem_u32(&sh->q_full[l]), seg_no & 1, abort_flag, status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    ++seg_no;
+                }
                 const uint64_t qd = smem_desc(smem_u32(q_smem + (q_ahead ? qb * SEG_Q_AHEAD * D * 2 : l * Q_BYTES)), 16, 1024);
                 auto issue_qk = [&](int ti) {
                     ok = ok && seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
@@ -678,7 +683,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                if (!q_ahead) mbar_arrive(smem_u32(&sh->q_full[0]));
+                if (!q_ahead && tile_active) mbar_arrive(smem_u32(&sh->q_full[l]));
                 SegCursor nxt = cur;
                 seg_next<KIND, NL>(a, nxt);
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
