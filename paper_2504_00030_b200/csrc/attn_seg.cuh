@@ -716,6 +716,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         tc_st32(o_addr + ch * 32, x[0]);
                         tc_st32(o_addr + ch * 32 + 32, x[1]);
                     }
+                    tc_wait_st();                              // the first tile's maximum may have them read again at once
                 }
                 if (tile_active) {
                     for (int ti = 0; ti < seg_tiles && ok; ++ti, ++cnt) {

@@ -70,3 +70,13 @@ def test_row_tiles_without_rows(head_dim):
     check(cfg, sl, gamma, 40, [-1] * 60, [16])
     lists = lists_to_arrays(random_lists(rng, sl, gamma, 4, 0.5), 22)
     check(cfg, sl, gamma, 40, lists=lists)
+
+
+@pytest.mark.parametrize("gmax", [0, 3, 15, 20])
+def test_own_keys_that_outweigh_the_prefix(gmax):
+    """The first tile behind the prefix raises the maximum, so that the partial is scaled as soon as it is there."""
+    rng = np.random.default_rng(72)
+    cfg = config("ar", 40, 16, 2, 128, 72, q_scale=1.5)
+    gamma = rng.integers(0, gmax + 1, 40)
+    gamma[0] = gmax
+    check(cfg, 128 + gamma + 1 + rng.integers(20, 200, 40), gamma, gmax, [0] * 40, [128], louder=(8, 4.0))
