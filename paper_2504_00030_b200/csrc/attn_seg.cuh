@@ -769,8 +769,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         mbar_arrive(smem_u32(&sh->p_full[buf]));
                     }
                     if (!ok) break;
-                    if (warp_active) {
-                        const uint32_t g = cnt - 1;            // the last P V
+                    // the last P V.  It writes all rows: where the next pair's rows may begin with a partial, a warp without
+                    // rows in this pair has to see it end too
+                    if (warp_active || KIND == SEG_SEQ) {
+                        const uint32_t g = cnt - 1;
                         ok = seg_wait(smem_u32(&sh->o_done[l * NB + (int)(g % NB)]), (g / NB) & 1, abort_flag, status);
                     }
                     if (!ok) break;

@@ -80,3 +80,14 @@ def test_own_keys_that_outweigh_the_prefix(gmax):
     gamma = rng.integers(0, gmax + 1, 40)
     gamma[0] = gmax
     check(cfg, 128 + gamma + 1 + rng.integers(20, 200, 40), gamma, gmax, [0] * 40, [128], louder=(8, 4.0))
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("gmax", [7, 15, 33])
+def test_warps_without_rows_before_warps_with(gmax, head_dim):
+    """Pairs of one and of many rows take turns in a block, all behind prefixes."""
+    rng = np.random.default_rng(73)
+    cfg = config("ar", 100, 64, 8, head_dim, 73)
+    group = np.arange(100) % 3
+    gamma = np.where(rng.random(100) < 0.5, 0, gmax)
+    check(cfg, 160 + gamma + 1 + rng.integers(0, 90, 100), gamma, gmax, group, [160, 96, 128])
