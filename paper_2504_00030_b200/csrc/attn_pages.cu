@@ -20,7 +20,7 @@ extern "C" size_t spec_verify_attn_pages_workspace_bytes(int32_t batch, int32_t 
     if (batch <= 0 || gamma_max < 0 || gamma_max > 63 || hq <= 0 || hkv <= 0 || hq % hkv != 0 || hq / hkv > 128 ||
         (head_dim != 64 && head_dim != 128))
         return 0;
-    return seg_table_bytes() + seg_part_bytes(seg_nl(hq / hkv * (gamma_max + 1)));
+    return SEG_WS_SLACK + seg_table_bytes() + seg_part_bytes(seg_nl(hq / hkv * (gamma_max + 1)));
 }
 
 extern "C" sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void *workspace, size_t workspace_bytes, void *stream)
@@ -48,7 +48,7 @@ extern "C" sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void 
     a.row_mask = p->row_mask;
     a.n_list = p->n_list;
     a.list_stride = p->list_stride;
-    uint8_t *w = static_cast<uint8_t *>(workspace);
+    uint8_t *w = seg_workspace(workspace);
     a.bounds = reinterpret_cast<int32_t *>(w);
     a.desc = reinterpret_cast<int32_t *>(w + seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)));
     a.part = reinterpret_cast<float *>(w + seg_table_bytes());

@@ -154,7 +154,7 @@ extern "C" size_t spec_verify_attn_prefix_workspace_bytes(int32_t batch, int32_t
     if (batch <= 0 || batch > MAX_PREFIX_BATCH || gamma_max < 0 || gamma_max > 4095 || hq <= 0 || hkv <= 0 || hq % hkv != 0 ||
         hq / hkv > 128 || (head_dim != 64 && head_dim != 128) || n_groups <= 0 || n_groups > batch)
         return 0;
-    return prefix_layout(batch, gamma_max, hq, hkv, n_groups).bytes;
+    return SEG_WS_SLACK + prefix_layout(batch, gamma_max, hq, hkv, n_groups).bytes;
 }
 
 extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, void *workspace, size_t workspace_bytes, void *stream)
@@ -172,7 +172,7 @@ extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, voi
     if (!aligned16(workspace)) return SV_EALIGN;
     if (seg_grid(1) > SEG_MAX_GRID) return SV_EUNSUPPORTED;
     const PrefixLayout l = prefix_layout(at.batch, at.gamma_max, at.hq, at.hkv, p->n_groups);
-    uint8_t *w = static_cast<uint8_t *>(workspace);
+    uint8_t *w = seg_workspace(workspace);
     auto ints = [&](int i) { return reinterpret_cast<int32_t *>(w + l.at[i]); };
     SegLaunch a = {};
     a.p = at;

@@ -979,6 +979,9 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
 inline int seg_nl(int rows) { return rows <= 128 ? 1 : 2; }
 inline int seg_grid(int nl) { return sm_count() * (nl == 1 ? 2 : 1); }
 inline size_t seg_round(size_t n) { return (n + 255) & ~(size_t)255; }
+// Partial rows move 32 bytes at a time, a caller's workspace begins on any 16: the tables and partials begin on the next 32.
+constexpr size_t SEG_WS_SLACK = 16;
+inline uint8_t *seg_workspace(void *w) { return reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(w) + 31) & ~(uintptr_t)31); }
 // bounds, descriptors and partials of one launch
 inline size_t seg_table_bytes() { return seg_round((SEG_MAX_GRID + 1) * sizeof(int32_t)) + seg_round(SEG_MAX_GRID * 4 * sizeof(int32_t)); }
 inline size_t seg_part_bytes(int nl) { return (size_t)seg_grid(nl) * 2 * seg_slot_floats(nl * 128) * sizeof(float); }

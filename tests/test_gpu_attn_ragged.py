@@ -91,3 +91,12 @@ def test_warps_without_rows_before_warps_with(gmax, head_dim):
     group = np.arange(100) % 3
     gamma = np.where(rng.random(100) < 0.5, 0, gmax)
     check(cfg, 160 + gamma + 1 + rng.integers(0, 90, 100), gamma, gmax, group, [160, 96, 128])
+
+
+@pytest.mark.parametrize("offset", [16, 32, 48])
+def test_workspace_on_any_16_bytes(offset):
+    rng = np.random.default_rng(74)
+    cfg = config("ar", 4, 16, 2, 128, 74)
+    sl, gamma = np.array([900, 850, 1200, 870], np.int32), np.array([2, 0, 3, 1])
+    check(cfg, sl, gamma, 3, [0] * 4, [800], ws_offset=offset)
+    check(cfg, sl, gamma, 3, lists=lists_to_arrays(random_lists(rng, sl, gamma, 2, 0.5, every=True), 80), ws_offset=offset)
