@@ -307,7 +307,7 @@ sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
  *     s = max_{h,d} |q_hd| * (1/127),  qi_hd = round(q_hd / s)                (as above; at most 127 in magnitude)
  *     score(page) = scales[page] * max_h sum_d max(qi_hd bounds[page][g][0][d], qi_hd bounds[page][g][1][d])
  * The row reads the first n_first pages, the last n_last up to and including its own, and of the others those with the
- * highest scores, the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole
+ * highest scores (what is no number counts as the highest), the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole
  * numbers and the product with the scale is rounded once, so a row of a block reads the pages that the same position would
  * have read decoded alone: n_last >= 1 keeps pages with keys behind the row out of the comparison.
  * Output per sequence and kv head: the pages that any row of the block reads, in ascending order (indices into the block

@@ -773,6 +773,7 @@ void oracle_page_choice(const uint16_t *q, int G, int D, const int8_t *bounds, c
             if (g == 0 || sum > best) best = sum;
         }
         score[p] = (float)best * scales[(int64_t)table[p] * hkv + head];
+        if (isnan(score[p])) score[p] = INFINITY;            /* no number counts as the highest */
         chosen[p] = (uint8_t)(p < n_first || p >= n_seen - n_last || n_seen <= n_select);
     }
     for (int left = n_select - n_first - n_last; n_seen > n_select && left > 0; --left) {

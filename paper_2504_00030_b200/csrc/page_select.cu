@@ -18,6 +18,7 @@
 #include "work_share.cuh"
 
 #include <climits>
+#include <math_constants.h>
 
 namespace sv {
 
@@ -139,10 +140,11 @@ __device__ __forceinline__ void score_start(const PageSelectLaunch &a, const Wor
     if (c.t >= c.n_tiles) score_next(a, c);
 }
 
-// A score as a number that orders as it does and is never 0; -0 counts as 0
+// A score as a number that orders as it does and is neither 0 nor the largest; -0 counts as 0, what is no number as the highest
+// (fminf takes the other operand for it)
 __device__ __forceinline__ uint32_t score_key(int best, float scale)
 {
-    const uint32_t x = __float_as_uint(__fmul_rn((float)best, scale) + 0.f);
+    const uint32_t x = __float_as_uint(fminf(__fmul_rn((float)best, scale) + 0.f, CUDART_INF_F));
     return (x & 0x80000000u) ? ~x : x | 0x80000000u;
 }
 

@@ -168,3 +168,20 @@ def test_graph_replay_and_side_stream():
     np.testing.assert_array_equal(np.where(used, out[0].cpu().numpy(), -1), ref[0])
     ref = lists_to_arrays(oracle.page_select(q, bounds, scales, table, sl, g, cu, 15, 1, 1), 60)
     np.testing.assert_array_equal(first[2].cpu().numpy(), ref[2])
+
+
+@pytest.mark.parametrize("gamma", [0, 5])
+def test_scales_that_are_no_numbers(gamma):
+    """Such pages come first, and a row still takes n_select pages."""
+    cfg = config("ps", 2, 8, 2, 128, 22)
+    sl, g = [1500, 2900], [gamma, gamma]
+    table, cu, q, bounds, scales = setup(cfg, sl, g, gamma, 1)
+    scales[table[0, [3, 40, 41]]], scales[table[1, 5:60]] = np.nan, -np.nan
+    scales[table[0, 50]], scales[table[1, 70]] = np.inf, -np.inf
+    bounds[table[1, 5:20]] = 0
+    pl, rm, n, status = select_gpu(cfg, q, bounds, scales, table, sl, g, cu, gamma, 20, 1, 1)
+    ref = lists_to_arrays(oracle.page_select(q, bounds, scales, table, sl, g, cu, 20, 1, 1), pl.shape[2])
+    used = np.arange(pl.shape[2]) < n[..., None]
+    assert status == 0 and (n == ref[2]).all()
+    np.testing.assert_array_equal(np.where(used, pl, -1), ref[0])
+    np.testing.assert_array_equal(np.where(used, rm, 0), ref[1])
