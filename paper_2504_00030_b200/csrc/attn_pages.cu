@@ -33,6 +33,7 @@ extern "C" sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void 
     if (p->page_list == nullptr || p->row_mask == nullptr || p->n_list == nullptr || p->list_stride <= 0) return SV_EINVAL;
     if (at.gamma_max > 63 || at.hq / at.hkv > 128 || !at.pool->has_maps) return SV_EUNSUPPORTED;
     if ((long long)at.batch * at.hkv > (1 << 24) || p->list_stride > (1 << 26)) return SV_EUNSUPPORTED;
+    if (!seg_tiles_fit((long long)at.batch * at.hkv * seg_chunks(at.hq / at.hkv, at.gamma_max), p->list_stride)) return SV_EUNSUPPORTED;
     if ((reinterpret_cast<uintptr_t>(p->row_mask) & 7u) != 0) return SV_EALIGN;
     if (workspace == nullptr ||
         workspace_bytes < spec_verify_attn_pages_workspace_bytes(at.batch, at.gamma_max, at.hq, at.hkv, at.head_dim))

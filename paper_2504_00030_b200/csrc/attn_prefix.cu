@@ -166,6 +166,8 @@ extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, voi
     if (st != SV_OK) return st;
     if (p->group == nullptr || p->prefix_len == nullptr || p->n_groups <= 0 || p->n_groups > at.batch) return SV_EINVAL;
     if (at.batch > MAX_PREFIX_BATCH || at.gamma_max > 4095 || at.hq / at.hkv > 128 || !at.pool->has_maps) return SV_EUNSUPPORTED;
+    // pairs of the sequences; the groups, whose pairs have two row tiles, have no more
+    if (!seg_tiles_fit((long long)at.batch * at.hkv * seg_chunks(at.hq / at.hkv, at.gamma_max), at.max_seq_len / 16 + 1)) return SV_EUNSUPPORTED;
     if (workspace == nullptr ||
         workspace_bytes < spec_verify_attn_prefix_workspace_bytes(at.batch, at.gamma_max, at.hq, at.hkv, at.head_dim, p->n_groups))
         return SV_EWORKSPACE;

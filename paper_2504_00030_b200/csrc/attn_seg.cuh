@@ -978,6 +978,18 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
 // ---------------------------------------------------------------------------- host side
 inline int seg_nl(int rows) { return rows <= 128 ? 1 : 2; }
 inline int seg_grid(int nl) { return sm_count() * (nl == 1 ? 2 : 1); }
+// Whether the key tiles of `pairs` pairs with at most `pages` pages each can be numbered with 31 bits, as the launches number them.
+inline bool seg_tiles_fit(long long pairs, long long pages)
+{
+    const long long tiles = pages / (SEG_TILE / 16) + 1;
+    return pairs <= 0x7fffffffLL / tiles;
+}
+// pairs of a sequence and kv head
+inline long long seg_chunks(int group, int gamma_max)
+{
+    const int ppp = 128 / group * seg_nl(group * (gamma_max + 1));
+    return (gamma_max + ppp) / ppp;
+}
 inline size_t seg_round(size_t n) { return (n + 255) & ~(size_t)255; }
 // Partial rows move 32 bytes at a time, a caller's workspace begins on any 16: the tables and partials begin on the next 32.
 constexpr size_t SEG_WS_SLACK = 16;

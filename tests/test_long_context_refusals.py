@@ -115,6 +115,19 @@ def test_shared_prefixes(lib):
     assert call(ws=None) == sv.SV_EWORKSPACE and call(n=size - 1) == sv.SV_EWORKSPACE
 
 
+def test_more_tiles_than_31_bits_number(lib):
+    """64 tokens a tile: 2^31 - 1 of them over all pairs (of up to 256 rows of a sequence and kv head)."""
+    pl = pool(hkv=1)
+    last = 2 ** 31 - 1
+    big = dict(batch=64, hq=128, hkv=1, max_seq_len=last, block_table_stride=(last + 15) // 16)
+    size = lib.spec_verify_attn_prefix_workspace_bytes(64, 4, 128, 1, 128, 2)
+    args = dict(group=P, prefix_len=P, n_groups=2)
+    assert lib.spec_verify_attn_prefix(C.byref(made(sv.AttnPrefixParams, dict(attn=attn(pl, **big), **args))), P, size, None) == sv.SV_EUNSUPPORTED
+    lists = dict(page_list=P, row_mask=P, n_list=P, list_stride=1 << 26)
+    size = lib.spec_verify_attn_pages_workspace_bytes(128, 4, 128, 1, 128)
+    assert lib.spec_verify_attn_pages(C.byref(made(sv.AttnPagesParams, dict(attn=attn(pl, **{**big, "batch": 128}), **lists))), P, size, None) == sv.SV_EUNSUPPORTED
+
+
 def test_parameter_structs_are_laid_out_as_the_header_has_them(tmp_path):
     classes = {"sv_page_bounds_params": sv.PageBoundsParams, "sv_page_select_params": sv.PageSelectParams, "sv_attn_pages_params": sv.AttnPagesParams,
                "sv_attn_prefix_params": sv.AttnPrefixParams}
