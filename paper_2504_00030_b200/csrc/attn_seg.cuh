@@ -19,7 +19,13 @@
 // quarter cheaper on the tensor core: 600 us for the groups of 128 sequences behind three prefixes where this takes 520.)
 //
 // Warps: 0 = TMA of K, 2 = TMA of V, 1 and 3 = MMA issuers of the row tiles (1 owns the tensor memory; with one row tile 3
-// idles); then four softmax warps per row tile (thread = row = TMEM lane).  All hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
+// brings the queries of pairs of up to 32 rows ahead); then four softmax warps per row tile (thread = row = TMEM lane).  All
+// hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
+//
+// Measured (B200, device time of the call, 128-dim heads): lists of 128 pages for one row of each of 128 sequences 183 us (6.2
+// TB/s, 94 % of a copy); of 64 pages a row for 17 rows of 64 heads 260 us (163 us of bytes: rows of different sequences
+// fill 136 of 256, the chain S -> softmax -> P V of a row tile sets the pace); one token over 64 pages 15 us (latency of
+// two launches).
 #pragma once
 
 #include "attn_common.cuh"

@@ -4,7 +4,8 @@
 // One warp per (page, kv head): its 16 keys are 4 KB (head_dim 128), eight 16-byte loads a lane, all in flight at once;
 // a lane keeps the maxima and minima of its eight dims over its slots as packed bf16 (exact), the lanes that share
 // dims combine by shuffle.  Bound by HBM on prompts (2 bytes read per key element, 1/8 of a byte written), by launch
-// and two dependent loads (table entry, keys) on draft blocks.
+// and two dependent loads (table entry, keys) on draft blocks.  Measured: 16 prompts of up to 8192 tokens 45 us (40.5 at a
+// copy's rate), a block of one sequence 3.0 us.
 #include "attn_common.cuh"
 #include "common.cuh"
 #include "whole8.cuh"

