@@ -30,6 +30,7 @@
 
 #include "attn_common.cuh"
 #include "attn_softmax.cuh"
+#include "f32x2.cuh"
 #include "tc_ptx.cuh"
 #include "work_share.cuh"
 
@@ -244,33 +245,13 @@ __device__ __forceinline__ void load8(const float *src, uint32_t *x)
                  : "l"(src));
 }
 
-// the larger of three, and float32 pairs in one instruction
+// the larger of three
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-__device__ __forceinline__ uint64_t pair2(float a, float b)
-{
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ void split2(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 // The online softmax of one row's TILE scores, as softmax_tile, with the keys that the row may see given per page:
 // lim[j] is the last visible slot of the tile's page j (below 0: none; 15 or more: all).
 template <int TILE, int O_CHUNKS, typename WaitPV>

@@ -109,7 +109,7 @@ page_bounds_kernel(const __grid_constant__ PageBoundsLaunch a)
     for (int d = 1; d < 2 * LANES; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
     // every step rounds once to the nearest float32, so that the stored whole numbers are reproducible
     const float scale = __fmul_rn(big, 1.f / 127.f);
-    const uint2 w = whole8x8(x, scale, whole8_inverse(scale));
+    const uint2 w = whole8x8(x, Whole8(scale));
     const long long at = (long long)page * a.hkv + h;
     if (slot0 < 2) *reinterpret_cast<uint2 *>(p.bounds + at * 2 * D + (low ? D : 0) + dim8 * 8) = w;
     if (lane == 0) p.scales[at] = scale;

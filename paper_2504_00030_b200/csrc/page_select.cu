@@ -291,10 +291,10 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
                 const uint32_t base = smem_u32(tile_buf + buf * TILE_BYTES) + (ch >> 3) * (PS_PAGES * 128);
                 const int8_t *src0 = p.bounds + (long long)h * ROW + ch * 16;
                 const long long page_bytes = (long long)p.hkv * ROW;
-#pragma unroll
+#pragma unroll 4
                 for (int k = 0; k < 64 / RPI; ++k) {
                     const int in = k * RPI + r0, row = warp * 64 + in;
-                    const int phys = __shfl_sync(0xffffffffu, now[k * RPI / 32], in & 31);
+                    const int phys = __shfl_sync(0xffffffffu, k * RPI < 32 ? now[0] : now[1], in & 31);
                     cp_async16(base + row * 128 + (((ch & 7) ^ (row & 7)) << 4), src0 + max(phys, 0) * page_bytes, phys >= 0);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
@@ -343,11 +343,11 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
                     for (int e = 0; e < HELD; ++e) fold(x[e]);
                     for (int e = lane + HELD * 32; e < chunks; e += 32) fold(__ldg(src + e));
                     const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, max(big2 & 0xffffu, big2 >> 16)) << 16);
-                    const float scale = __fmul_rn(big, 1.f / 127.f), inv = whole8_inverse(scale);
+                    const Whole8 by(__fmul_rn(big, 1.f / 127.f));
                     auto put = [&](const uint4 &y, int e) {
                         float f[8];
                         unpack8(y, f);
-                        const uint2 n = whole8x8(f, scale, inv);
+                        const uint2 n = whole8x8(f, by);
                         const int hh = e / (D / 8), d8 = e - hh * (D / 8), col = i * G + hh;
                         const uint32_t sx = negative_bytes(n.x), sy = negative_bytes(n.y);
 #pragma unroll
@@ -357,10 +357,15 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
                             *reinterpret_cast<uint2 *>(dst + off) = z == 0 ? make_uint2(n.x & ~sx, n.y & ~sy) : make_uint2(n.x & sx, n.y & sy);
                         }
                     };
+                    // one copy of the code for all chunks (the held ones move up): with a copy for each the four roles' code did
+                    // not fit the instruction cache
+#pragma unroll 1
+                    for (int e = lane, k = 0; e < chunks; e += 32, ++k) {
+                        const uint4 y = k < HELD ? x[0] : __ldg(src + e);
 #pragma unroll
-                    for (int e = 0; e < HELD; ++e)
-                        if (lane + e * 32 < chunks) put(x[e], lane + e * 32);
-                    for (int e = lane + HELD * 32; e < chunks; e += 32) put(__ldg(src + e), e);
+                        for (int z = 0; z + 1 < HELD; ++z) x[z] = x[z + 1];
+                        put(y, e);
+                    }
                 }
                 // columns up to the next multiple of 16: zeros
                 const int pad = (n_mma - c.n_pos * G) * CH;
@@ -377,33 +382,49 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
         } else if (warp >= SC_OUT_WARP0 && warp < SC_OUT_WARP0 + 4) {
             // ================================================================ scores: a thread per page
             const int row = (warp & 3) * 32 + lane;
-            // scale of the thread's page of the cursor's tile, under way while the tile before is worked on
-            auto scale_of = [&]() {
-                const int lp = c.t * PS_PAGES + row;
-                const int phys = lp < c.sr.n_pages ? __ldg(p.block_table + (long long)c.o * p.block_table_stride + lp) : -1;
-                return phys >= 0 && phys < p.n_pages ? __ldg(p.scales + (long long)phys * p.hkv + c.h) : 0.f;
+            // Where the thread's page of a tile goes, and which page it is.  Ids are looked up two tiles ahead and scales one: with
+            // the id of the next tile fetched in front of its scale, every tile began with a wait of 800 cycles.
+            struct Place {
+                uint32_t *dst;
+                int cols, h, id;
+                bool used;
             };
-            float scale = scale_of();
-            for (uint32_t n = 0; left > 0 && ok; ++n, --left) {
-                const int g = n & 1, lp = c.t * PS_PAGES + row, cols = c.n_pos * G;
-                const uint32_t acc = tmem + g * acc_cols + ((uint32_t)((warp & 3) * 32) << 16);
-                uint32_t *dst = a.keys + (((long long)c.o * p.hkv + c.h) * (p.gamma_max + 1) + c.i0) * a.key_stride + lp;
-                const bool used = lp < c.sr.n_pages;
-                const float mine = scale;
+            auto look_up = [&]() {
+                Place w;
+                const int lp = c.t * PS_PAGES + row;
+                w.dst = a.keys + (((long long)c.o * p.hkv + c.h) * (p.gamma_max + 1) + c.i0) * a.key_stride + lp;
+                w.cols = c.n_pos * G;
+                w.h = c.h;
+                w.used = lp < c.sr.n_pages;
+                w.id = w.used ? __ldg(p.block_table + (long long)c.o * p.block_table_stride + lp) : -1;
                 if (++c.t == c.n_tiles) score_next(a, c);
-                if (left > 1) scale = scale_of();
+                return w;
+            };
+            auto scale_of = [&](const Place &w) { return w.id >= 0 && w.id < p.n_pages ? __ldg(p.scales + (long long)w.id * p.hkv + w.h) : 0.f; };
+            Place now = look_up(), next = now;
+            if (left > 1) next = look_up();
+            float scale = scale_of(now);
+            for (uint32_t n = 0; left > 0 && ok; ++n, --left) {
+                const int g = n & 1;
+                const uint32_t acc = tmem + g * acc_cols + ((uint32_t)((warp & 3) * 32) << 16);
+                const float scale_next = scale_of(next);
+                Place after = next;
+                if (left > 2) after = look_up();
                 ok = wait(sh->acc_full[g], (n >> 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
                 switch (G) {
-                    case 1: store_keys<1>(acc, cols, G, mine, used, dst, a.key_stride); break;
-                    case 2: store_keys<2>(acc, cols, G, mine, used, dst, a.key_stride); break;
-                    case 4: store_keys<4>(acc, cols, G, mine, used, dst, a.key_stride); break;
-                    case 8: store_keys<8>(acc, cols, G, mine, used, dst, a.key_stride); break;
-                    default: store_keys<0>(acc, cols, G, mine, used, dst, a.key_stride); break;
+                    case 1: store_keys<1>(acc, now.cols, G, scale, now.used, now.dst, a.key_stride); break;
+                    case 2: store_keys<2>(acc, now.cols, G, scale, now.used, now.dst, a.key_stride); break;
+                    case 4: store_keys<4>(acc, now.cols, G, scale, now.used, now.dst, a.key_stride); break;
+                    case 8: store_keys<8>(acc, now.cols, G, scale, now.used, now.dst, a.key_stride); break;
+                    default: store_keys<0>(acc, now.cols, G, scale, now.used, now.dst, a.key_stride); break;
                 }
                 tc_fence_before();
                 mbar_arrive(smem_u32(&sh->acc_empty[g]));
+                now = next;
+                next = after;
+                scale = scale_next;
             }
         } else {
             // ================================================================ products

@@ -2,41 +2,53 @@
 #pragma once
 
 #include "common.cuh"
+#include "f32x2.cuh"
 
 namespace sv {
 
-// The whole number nearest to x / scale (the quotient rounded to float32 first, halves to even), in [-127, 127]; 0 where
-// scale is 0.
-__device__ __forceinline__ int whole8(float x, float scale)
-{
-    return scale > 0.f ? min(max(__float2int_rn(__fdiv_rn(x, scale)), -127), 127) : 0;
-}
-
+// Of x / scale: the quotient rounded to float32, then to the nearest whole number (halves to even), in [-127, 127]; 0 where scale
+// is 0 or no finite number.
+//
 // Eight of them as bytes, without dividing.  With inv = 1 / scale rounded to nearest, q = x inv rounded is within one unit in
 // the last place of x / scale, and q + (x - q scale) inv, with the remainder exact in one fused operation, is x / scale
 // rounded to nearest (Markstein's theorem on division by a correctly rounded reciprocal; nothing underflows where |q| > 1/4
-// and scale > 1e-25).  Quotients of bf16 numbers are near or on halves too often (0.3 % of them) for an approximate
-// quotient with a check: the divisions it fell back to were four fifths of the time of the kernel that scores pages.
-// inv = 0 (whole8_inverse of a scale that is too small): real divisions.
-__device__ __forceinline__ float whole8_inverse(float scale) { return scale > 1e-25f ? __frcp_rn(scale) : 0.f; }
+// and scale > 1e-25; below, x and scale are taken 2^96 times as large, which is exact).  Quotients of bf16 numbers are near or
+// on halves too often (0.3 % of them) for an approximate quotient with a check: the divisions it fell back to were four fifths
+// of the time of the kernel that scores pages.
+struct Whole8 {
+    float scale, inv, up;
+    __device__ __forceinline__ explicit Whole8(float s)
+    {
+        up = s <= 1e-25f ? 7.9228162514264338e28f : 1.f;       // 2^96
+        scale = s * up;
+        inv = scale > 0.f && scale <= 3.402823466e38f ? __frcp_rn(scale) : 0.f;
+    }
+};
 
-__device__ __forceinline__ uint2 whole8x8(const float (&x)[8], float scale, float inv)
+__device__ __forceinline__ uint2 whole8x8(const float (&x)[8], const Whole8 &by)
 {
     constexpr float MAGIC = 12582912.f;                // 1.5 * 2^23: the sum rounds to whole numbers, its low bits hold them
+    const uint64_t inv = pair2(by.inv, by.inv), neg = pair2(-by.scale, -by.scale), magic = pair2(MAGIC, MAGIC);
     uint32_t t[8];
+    uint64_t v[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float q = __fmul_rn(x[e], inv);
-        t[e] = __float_as_uint(__fadd_rn(fmaf(fmaf(-q, scale, x[e]), inv, q), MAGIC));
+    for (int e = 0; e < 4; ++e) v[e] = pair2(x[2 * e], x[2 * e + 1]);
+    if (by.up != 1.f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = mul2(v[e], pair2(by.up, by.up));
     }
-    if (inv == 0.f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = (uint32_t)whole8(x[e], scale);
+    for (int e = 0; e < 4; ++e) {
+        const uint64_t q = mul2(v[e], inv);
+        float a, b;
+        split2(add2(fma2(fma2(q, neg, v[e]), inv, q), magic), a, b);
+        t[2 * e] = __float_as_uint(a);
+        t[2 * e + 1] = __float_as_uint(b);
     }
     uint2 w;
     w.x = __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
     w.y = __byte_perm(__byte_perm(t[4], t[5], 0x0040), __byte_perm(t[6], t[7], 0x0040), 0x5410);
-    return w;
+    return by.inv != 0.f ? w : make_uint2(0, 0);
 }
 
 // the eight bf16 of 16 bytes
