@@ -632,6 +632,24 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             seg_start<KIND, NL>(a, sh->share, cur);
             uint32_t cnt = 0, seg_no = 0;                      // tiles of this row tile so far
             bool ok = true;
+            int q0 = KIND == SEG_GROUP ? 0 : p.cu_q[cur.b];
+            // List entries: lane l holds entry f_e + l of owner f_o and its mask.  With two row tiles they are brought ahead (17 rows
+            // of 64 heads for 128 sequences: 261 -> 253 us); with one, where a second block works meanwhile, the more code cost
+            // more than the waits (13 rows of one head, 40 kv heads: 180 -> 191 us).
+            constexpr bool AHEAD = NL == 2;
+            int f_o = -1, f_e = 0, f_lp = -1;
+            unsigned long long f_mk = 0;
+            auto fetch = [&](const SegCursor &w, int e0) {
+                f_o = w.o;
+                f_e = e0;
+                f_lp = -1;
+                f_mk = 0;
+                if (e0 + lane < w.n_pages) {
+                    const long long at = (long long)w.o * a.list_stride + e0 + lane;
+                    f_lp = __ldg(a.page_list + at);
+                    f_mk = __ldg(reinterpret_cast<const unsigned long long *>(a.row_mask) + at);
+                }
+            };
             for (long long tg = t_begin; tg < t_end && ok; ++seg_no) {
                 const int seg_tiles = (int)min((long long)(cur.n_tiles - cur.t), t_end - tg);
                 const int pos0 = cur.chunk * NL * ppl + l * ppl;               // first position of the row tile
@@ -644,7 +662,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (row_ok) {
                     int2 at;
                     if (KIND == SEG_GROUP) at = a.plan.row_list[a.plan.grp_base[cur.o] + i];
-                    else at = make_int2(p.cu_q[cur.b] + i, cur.b * (p.gamma_max + 1) + i);
+                    else at = make_int2(q0 + i, cur.b * (p.gamma_max + 1) + i);
                     q_row = (long long)at.x * p.hq + (long long)cur.h * G + hh;
                     part_row = (long long)at.y * p.hq + (long long)cur.h * G + hh;
                 }
@@ -673,10 +691,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (!q_ahead && tile_active) mbar_arrive(smem_u32(&sh->q_full[l]));
                 SegCursor nxt = cur;
                 seg_next<KIND, NL>(a, nxt);
+                int nxt_q0 = 0;                                // under way while this pair is worked on
+                if (KIND != SEG_GROUP && nxt.o < a.n_owners) nxt_q0 = p.cu_q[nxt.b];
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
-                const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
-                const uint64_t *masks = KIND == SEG_LIST ? a.row_mask + (long long)cur.o * a.list_stride : nullptr;
                 const int seq_pages = (cur.L + 15) / 16;
                 const bool far = p.gamma_max >= 32;            // masks have bits above the 32nd
                 int e_base = -32, e_lp = -1;                   // lane l: entry e_base + l of the list and its mask
@@ -713,14 +731,15 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         if (KIND == SEG_LIST) {
                             const int e0 = (cur.t + ti) * PPT;
                             if (warp_active && (e0 < e_base || e0 >= e_base + 32)) {
+                                if (!AHEAD || f_o != cur.o || f_e != e0) fetch(cur, e0);
                                 e_base = e0;
-                                const int e = e0 + lane;
-                                e_lp = -1;
-                                e_lo = e_hi = 0;
-                                if (e < cur.n_pages) {
-                                    e_lp = __ldg(list + e);
-                                    const uint64_t mk = __ldg(reinterpret_cast<const unsigned long long *>(masks) + e);
-                                    if (e_lp >= 0 && e_lp < seq_pages) { e_lo = (uint32_t)mk; e_hi = (uint32_t)(mk >> 32); }
+                                e_lp = f_lp;
+                                const bool have = f_lp >= 0 && f_lp < seq_pages;
+                                e_lo = have ? (uint32_t)f_mk : 0;
+                                e_hi = have ? (uint32_t)(f_mk >> 32) : 0;
+                                if (AHEAD) {                   // under way while these are worked on: the segment's next, or the next pair's first
+                                    if (ti + 32 / PPT < seg_tiles) fetch(cur, e0 + 32);
+                                    else if (nxt.o < a.n_owners) fetch(nxt, 0);
                                 }
                             }
 #pragma unroll
@@ -820,6 +839,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 }
                 tg += seg_tiles;
                 cur = nxt;
+                q0 = nxt_q0;
             }
         }
     }
