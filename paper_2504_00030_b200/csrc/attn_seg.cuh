@@ -532,7 +532,9 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (active) {
                     issue_qk(0);
                     if (NB > 1 && seg_tiles > 1) issue_qk(1);
-                    seg_next<KIND, NL>(a, nxt);
+                }
+                seg_next<KIND, NL>(a, nxt);
+                if (active) {
                     for (int ti = 0; ti < seg_tiles && ok; ++ti) {
                         const uint32_t g = cnt + ti;
                         const int buf = l * NB + (int)(g % NB);
@@ -555,7 +557,6 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     }
                     cnt += seg_tiles;
                 } else {                                       // no rows in this row tile: pass the tiles on
-                    seg_next<KIND, NL>(a, nxt);
                     for (int ti = 0; ti < seg_tiles && ok; ++ti) {
                         ok = seg_wait(smem_u32(&sh->full[k_at.slot]), k_at.use & 1, abort_flag, status);
                         if (ok && lane == 0) mbar_arrive(smem_u32(&sh->empty[k_at.slot]));
@@ -787,9 +788,11 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (!warp_active) {
                     // nothing to write
                 } else if (KIND != SEG_GROUP && whole) {
+                    // rolled loops here and below: the roles' code competes for the instruction cache (13 rows of one head, 40 kv
+                    // heads, 9 pairs a block: 182 us unrolled, 172 rolled)
                     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
-#pragma unroll
+#pragma unroll 1
                     for (int ch = 0; ch < OCH; ++ch) {
                         uint32_t o[32];
                         tc_ld32(o_addr + ch * 32, o);
@@ -813,7 +816,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     float *slot = a.part + ((size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1)) * seg_slot_floats(NL * 128);
                     const int row = l * 128 + r;
                     float *dst = to_rows ? a.plan.part_o + part_row * SEG_PITCH : slot + (size_t)row * SEG_PITCH;
-#pragma unroll
+#pragma unroll 1
                     for (int ch = 0; ch < OCH; ++ch) {
                         uint32_t o[32];
                         tc_ld32(o_addr + ch * 32, o);
