@@ -168,17 +168,17 @@ __device__ __forceinline__ void seg_next(const SegLaunch &a, SegCursor &c)
 
 // The calling block's share, by the whole block (NT threads); every block publishes its first tile.
 template <int KIND, int NL, int NT>
-__device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, WorkShare *sh, long long (*red)[NT / 32])
+__device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, WorkShare *sh, SegCursor *start, long long (*red)[NT / 32])
 {
+    SegCursor c;
     plan_work_share<NT>(
         a.n_owners, pair_cost,
         [&](int o, bool first) {
-            SegCursor c;
             c.o = o;
             seg_owner<KIND, NL>(a, c, first && blockIdx.x == 0);
             return OwnerWork{c.n_sub, c.n_tiles};
         },
-        sh, red);
+        [&]() { *start = c; }, sh, red);
     if (threadIdx.x == 0) {
         a.bounds[blockIdx.x] = (int)sh->t_begin;
         if (blockIdx.x + 1 == gridDim.x) a.bounds[gridDim.x] = (int)sh->total;
@@ -187,12 +187,10 @@ __device__ __forceinline__ void seg_plan(const SegLaunch &a, int pair_cost, Work
 }
 
 template <int KIND, int NL>
-__device__ __forceinline__ void seg_start(const SegLaunch &a, const WorkShare &sh, SegCursor &c)
+__device__ __forceinline__ void seg_start(const SegLaunch &a, const WorkShare &sh, const SegCursor &start, SegCursor &c)
 {
-    c.o = sh.o; c.s = sh.s; c.t = sh.t;
-    c.b = c.h = c.chunk = 0;
-    if (c.o >= a.n_owners) { c.n_tiles = c.n_sub = 1; c.R = 1; return; }
-    seg_owner<KIND, NL>(a, c, false);
+    c = start;                                                 // only called by blocks with tiles
+    c.s = sh.s; c.t = sh.t;
     seg_pair<KIND, NL>(a, c);
     if (c.t >= c.n_tiles) seg_next<KIND, NL>(a, c);
 }
@@ -209,6 +207,7 @@ struct SegShared {
     uint32_t tmem_base;
     int abort_flag;
     WorkShare share;
+    SegCursor start;             // of the owner that the block begins in
 };
 
 // Place in the ring of the tiles' K (first = 0) or V (first = 1): the items K, V of tile 0, K, V of tile 1 ... take the slots in
@@ -403,7 +402,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // the plan's sums share the queries' memory, which nothing touches before the barrier below
-    seg_plan<KIND, NL, NT>(a, seg_pair_cost(KIND), &sh->share, reinterpret_cast<long long(*)[NT / 32]>(seg_smem));
+    seg_plan<KIND, NL, NT>(a, seg_pair_cost(KIND), &sh->share, &sh->start, reinterpret_cast<long long(*)[NT / 32]>(seg_smem));
     tc_fence_before();
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();
@@ -420,7 +419,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         if (t_end > t_begin && (warp == 0 || warp == 2)) {
             // ================================================================ TMA producers: warp 0 K, warp 2 V
             SegCursor cur;
-            seg_start<KIND, NL>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, sh->start, cur);
             const bool is_v = warp == 2;
             constexpr int HV = D / 64;                         // 64-dim halves of a page
             const int page_in_tile = lane / HV, half = lane % HV;
@@ -487,7 +486,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             const int l = NL == 2 && warp == 3 ? 1 : 0;
             const uint32_t idesc_qk = instr_desc(false, TILE), idesc_pv = instr_desc(true, D);
             SegCursor cur;
-            seg_start<KIND, NL>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, sh->start, cur);
             uint32_t seg_no = 0, cnt = 0;                      // segments and tiles in which this row tile has rows, so far
             RingPos k_at(0), v_at(1);                          // of the next Q K^T and the next P V
             // What steers the loops and makes up the descriptors goes through a warp-wide reduction, whose result the
@@ -578,7 +577,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         else if (NL == 1 && t_end > t_begin && warp == 3 && q_ahead) {
             // ================================================================ query rows of the next pair
             SegCursor cur;
-            seg_start<KIND, NL>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, sh->start, cur);
             constexpr int CH = D / 8, RPI = 32 / CH;           // 16-byte chunks of a row; rows that one load of the warp covers
             const int ch = lane % CH, r0 = lane / CH;
             bool ok = true;
@@ -630,7 +629,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
             const float c_scale = p.sm_scale * 1.4426950408889634f;          // scores in log2 units
             const int ri = r / G, hh = r - ri * G;             // position and head of the row within its tile
             SegCursor cur;
-            seg_start<KIND, NL>(a, sh->share, cur);
+            seg_start<KIND, NL>(a, sh->share, sh->start, cur);
             uint32_t cnt = 0, seg_no = 0;                      // tiles of this row tile so far
             bool ok = true;
             int q0 = KIND == SEG_GROUP ? 0 : p.cu_q[cur.b];

@@ -97,6 +97,8 @@ struct ScoreShared {
     uint32_t tmem_base;
     int abort_flag;
     WorkShare share;
+    SeqRows start;               // of the sequence that the block begins in
+    OwnerWork start_work;
 };
 
 // The walk over (sequence, kv head and chunk of rows, tile of pages).
@@ -134,12 +136,12 @@ __device__ __forceinline__ void score_next(const PageSelectLaunch &a, ScoreCurso
     }
     score_pair(a, c);
 }
-__device__ __forceinline__ void score_start(const PageSelectLaunch &a, const WorkShare &sh, ScoreCursor &c)
+__device__ __forceinline__ void score_start(const PageSelectLaunch &a, const ScoreShared &sh, ScoreCursor &c)
 {
-    c.o = sh.o; c.s = sh.s; c.t = sh.t;
-    const OwnerWork w = score_owner(a, c.o, c.sr);             // only called by blocks with tiles
-    c.n_sub = w.n_sub;
-    c.n_tiles = w.n_tiles;
+    c.o = sh.share.o; c.s = sh.share.s; c.t = sh.share.t;      // only called by blocks with tiles
+    c.sr = sh.start;
+    c.n_sub = sh.start_work.n_sub;
+    c.n_tiles = sh.start_work.n_tiles;
     score_pair(a, c);
     if (c.t >= c.n_tiles) score_next(a, c);
 }
@@ -231,11 +233,14 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // the sums of the plan use the tiles' memory, which nothing else touches before the barrier below
+    SeqRows rows;
+    OwnerWork work;
     plan_work_share<SC_THREADS>(
         p.batch, SC_PAIR_COST,
-        [&](int b, bool) {
-            SeqRows sr;
-            return score_owner(a, b, sr);
+        [&](int b, bool) { return work = score_owner(a, b, rows); },
+        [&]() {
+            sh->start = rows;
+            sh->start_work = work;
         },
         &sh->share, reinterpret_cast<long long(*)[SC_THREADS / 32]>(tile_buf));
     tc_fence_before();
@@ -252,7 +257,7 @@ page_score_kernel(const __grid_constant__ PageSelectLaunch a)
     };
     if (left > 0) {
         ScoreCursor c;
-        score_start(a, sh->share, c);
+        score_start(a, *sh, c);
         if (warp < 2) {
             // ================================================================ tiles: a warp for 64 of the 128 pages
             constexpr int RPI = 32 / CH;                           // rows that one copy of the warp covers
