@@ -100,3 +100,15 @@ def test_workspace_on_any_16_bytes(offset):
     sl, gamma = np.array([900, 850, 1200, 870], np.int32), np.array([2, 0, 3, 1])
     check(cfg, sl, gamma, 3, [0] * 4, [800], ws_offset=offset)
     check(cfg, sl, gamma, 3, lists=lists_to_arrays(random_lists(rng, sl, gamma, 2, 0.5, every=True), 80), ws_offset=offset)
+
+
+@pytest.mark.parametrize("hq", [2, 16])
+def test_more_sequences_than_threads(hq):
+    """The shares of work are found in several rounds: one and two row tiles (1 and 8 heads of 17 rows)."""
+    rng = np.random.default_rng(75)
+    B, gmax = 420, 16
+    cfg = config("ar", B, hq, 2, 64, 75)
+    gamma = rng.integers(0, gmax + 1, B)
+    sl = gamma + 1 + rng.integers(0, 120, B)
+    check(cfg, sl, gamma, gmax, lists=lists_to_arrays(random_lists(rng, sl, gamma, 2, 0.5), 9), runs=2)
+    check(cfg, sl + 48, gamma, gmax, rng.integers(-1, 5, B), [48, 16, 32, 48, 48], runs=2)

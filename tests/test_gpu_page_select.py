@@ -185,3 +185,8 @@ def test_scales_that_are_no_numbers(gamma):
     assert status == 0 and (n == ref[2]).all()
     np.testing.assert_array_equal(np.where(used, pl, -1), ref[0])
     np.testing.assert_array_equal(np.where(used, rm, 0), ref[1])
+
+
+def test_more_sequences_than_threads():
+    rng = np.random.default_rng(23)
+    check(config("ps", 700, 4, 1, 64, 23), rng.integers(5, 400, 700), rng.integers(0, 4, 700), 3, 6, 1, 1)
