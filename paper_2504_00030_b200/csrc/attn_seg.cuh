@@ -359,10 +359,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
     constexpr uint32_t TMEM_COLS = SegConfig<NL>::TMEM_COLS;
     constexpr int O_COL0 = NL * NB * TILE;                     // the row tiles' S buffers, then their O
     constexpr int OCH = D / 32;
-    pdl_enter();
     extern __shared__ __align__(1024) uint8_t seg_smem[];
     const sv_attn_params &p = a.p;
     if ((smem_u32(seg_smem) & 1023u) != 0) {                       // never seen; refuse rather than compute garbage
+        pdl_enter();
         if (threadIdx.x == 0) set_status(p.device_status, SV_DEV_TIMEOUT);
         return;
     }
@@ -377,6 +377,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.group, ppl = a.ppl;
 
+    // in front of the wait for the launch before: what needs nothing of it (not the tensor memory, which that one may hold)
     if (tid == 0) {
         for (int i = 0; i < n_slots; ++i) {
             mbar_init(smem_u32(&sh->full[i]), 1);
@@ -393,8 +394,11 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
         }
         for (int i = 0; i < NL; ++i) mbar_init(smem_u32(&sh->drained[i]), 1);
         sh->abort_flag = 0;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    pdl_enter();
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
                      "r"(TMEM_COLS)
