@@ -22,9 +22,9 @@
 // brings the queries of pairs of up to 32 rows ahead); then four softmax warps per row tile (thread = row = TMEM lane).  All
 // hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
 //
-// Measured (B200, device time of the call, 128-dim heads): lists of 128 pages for one row of each of 128 sequences 183 us (6.2
-// TB/s, 94 % of a copy); of 64 pages a row for 17 rows of 64 heads 260 us (163 us of bytes: rows of different sequences
-// fill 136 of 256, the chain S -> softmax -> P V of a row tile sets the pace); one token over 64 pages 15 us (latency of
+// Measured (B200, device time of the call, 128-dim heads): lists of 128 pages for one row of each of 128 sequences 185 us (6.1
+// TB/s, 94 % of a copy); of 64 pages a row for 17 rows of 64 heads 253 us (163 us of bytes: rows of different sequences
+// fill 136 of 256, the chain S -> softmax -> P V of a row tile sets the pace); one token over 64 pages 14.6 us (latency of
 // two launches).
 #pragma once
 
@@ -792,7 +792,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     // nothing to write
                 } else if (KIND != SEG_GROUP && whole) {
                     // rolled loops here and below: the roles' code competes for the instruction cache (13 rows of one head, 40 kv
-                    // heads, 9 pairs a block: 182 us unrolled, 172 rolled)
+                    // heads, 9 pairs a block: 182 us unrolled, 172 rolled when it was tried)
                     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
 #pragma unroll 1

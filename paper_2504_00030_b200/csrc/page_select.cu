@@ -13,9 +13,9 @@
 // are counted in 256 parts of their range, and the part that holds the last place again, until it is taken whole; then the
 // union over a block's rows as a list with a row mask per page.
 //
-// Measured (B200): 128 sequences of up to 16384 tokens, 17 rows of 64 heads: 131 us, about 75 for the scores (bound by the instructions
+// Measured (B200): 128 sequences of up to 16384 tokens, 17 rows of 64 heads: 121 us, about 70 for the scores (bound by the instructions
 // that make the queries' 8-bit halves and the maxima; 27 us of bytes) and 50 for the choice (bound by
-// shared-memory atomics and barriers); one token at 32768 tokens 16 us, 16 ragged blocks 21 us (latency).
+// shared-memory atomics and barriers); one token at 32768 tokens 14.2 us, 16 ragged blocks 20.7 us (latency).
 #include "attn_common.cuh"
 #include "tc_ptx.cuh"
 #include "whole8.cuh"
@@ -79,11 +79,11 @@ __device__ __forceinline__ void tc_mma_i8(uint32_t d, uint64_t adesc, uint64_t b
         : "memory");
 }
 
-// Roles of the score kernel's 16 warps (128 registers a thread: with more warps and fewer registers the spills, which find
-// hardly any L1 beside 227 KB of shared memory, doubled its time): 0 and 1 bring tiles of bounds into shared memory, 2 issues
-// the products, 4..7 turn them into scores, 3 and 8..15 bring the rows' queries in 8 bits (17 positions take two rounds; with
-// five of these warps everything else waited for them).  Everything is double buffered (the tiles up to four times): bounds
-// stream while the next pair's queries are made.
+// Roles of the score kernel's 16 warps: 0 and 1 bring tiles of bounds into shared memory, 2 issues the products, 4..7 turn them
+// into scores, 3 and 8..15 bring the rows' queries in 8 bits (17 positions take two rounds; with five of these warps everything
+// else waited for them; 20 warps, eight of them for the scores, took 123 us for the largest calls where these took 125, and 4 %
+// more for a single token).  Everything is double buffered (the tiles up to four times): bounds stream while the next pair's
+// queries are made.
 constexpr int SC_THREADS = 512;
 constexpr int SC_MMA_WARP = 2, SC_OUT_WARP0 = 4, SC_Q_WARPS = 9;
 constexpr int SC_MAX_TILES = 4;
