@@ -112,3 +112,17 @@ def test_more_sequences_than_threads(hq):
     sl = gamma + 1 + rng.integers(0, 120, B)
     check(cfg, sl, gamma, gmax, lists=lists_to_arrays(random_lists(rng, sl, gamma, 2, 0.5), 9), runs=2)
     check(cfg, sl + 48, gamma, gmax, rng.integers(-1, 5, B), [48, 16, 32, 48, 48], runs=2)
+
+
+def test_blocks_of_hundreds_of_rows():
+    """Rows of one sequence over several pairs: a prompt's part behind a shared prefix."""
+    check(config("ar", 3, 8, 2, 128, 76), [1500, 1300, 900], [700, 3, 0], 700, [0, 0, 0], [592], runs=2)
+    check(config("ar", 2, 4, 4, 64, 76), [2100, 300], [1999, 100], 2047, [-1, -1], [16], runs=2)
+
+
+def test_largest_batch():
+    """8192 sequences, as many as may share prefixes; lists for three times 8192 owners."""
+    rng = np.random.default_rng(77)
+    sl = rng.integers(17, 60, 8192)
+    check(config("ar", 8192, 3, 3, 64, 77), sl, np.zeros(8192, int), 0, rng.integers(-1, 8, 8192), [16] * 8, runs=2)
+    check(config("ar", 8192, 3, 3, 64, 77), sl, np.zeros(8192, int), 0, lists=lists_to_arrays(random_lists(rng, sl, np.zeros(8192, int), 3, 0.6), 4), runs=2)
