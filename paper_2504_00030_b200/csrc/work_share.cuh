@@ -54,7 +54,7 @@ __device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Own
         for (int i = 0; i < NW; ++i) { cost_all += red[0][i]; tiles_all += red[1][i]; }
         __syncthreads();
     }
-    long long cost0 = 0, tiles0 = 0;           // of the owners in front of this round's
+    long long cost0 = 0, tiles0 = 0;           // of the owners in front of these NT
     for (int base = 0; base == 0 || base < n_owners; base += NT) {
         const int o = base + tid;
         OwnerWork w = {0, 0};
