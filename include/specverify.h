@@ -350,8 +350,9 @@ sv_status spec_page_select(const sv_page_select_params *p, void *workspace_devic
 /*
  * spec_verify_attn where row i of sequence b reads, for kv head g, only the keys of those listed pages whose mask has bit
  * i set (and, as there, none behind its position): j runs over the positions of pages page_list[b][g][e], e <
- * n_list[b][g], with bit i of row_mask[b][g][e].  A row without any key gives o = 0 and lse = -inf.  The lists are those
- * of spec_page_select, or any others: pages in any order, each once.
+ * n_list[b][g], with bit i of row_mask[b][g][e].  A row without any key gives o = 0 and lse = -inf (so does one whose
+ * scores are all -inf); one with a score that is NaN or +inf gives NaN in both.  The lists are those of spec_page_select,
+ * or any others: pages in any order, each once.
  * Arguments of attn as in spec_verify_attn; gamma_max at most 63, hq / hkv at most 128.
  * Device-detected: as spec_verify_attn; a listed page outside the sequence's pages -> SV_DEV_BAD_PAGE, not read; n_list
  * outside [0, list_stride] -> SV_DEV_BAD_LEN, clamped.  Two launches.

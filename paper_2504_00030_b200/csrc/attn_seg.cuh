@@ -793,7 +793,9 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 } else if (KIND != SEG_GROUP && whole) {
                     // rolled loops here and below: the roles' code competes for the instruction cache (13 rows of one head, 40 kv
                     // heads, 9 pairs a block: 182 us unrolled, 172 rolled when it was tried)
-                    const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;         // a row without keys: zeros
+                    // a row without keys, which lists alone can leave: zeros, -inf.  A sum that is no number (a NaN or an infinite
+                    // score) stays one in both outputs
+                    const float inv = KIND == SEG_LIST && l_sum == 0.f ? 0.f : 1.f / l_sum;
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
 #pragma unroll 1
                     for (int ch = 0; ch < OCH; ++ch) {
@@ -811,8 +813,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                             }
                         }
                     }
-                    if (row_ok && p.lse != nullptr)
-                        p.lse[q_row] = l_sum > 0.f ? (m_ref + log2f(l_sum)) * 0.6931471805599453f : -CUDART_INF_F;
+                    if (row_ok && p.lse != nullptr) p.lse[q_row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
                 } else {
                     // unnormalised: a whole pair of a group to the positions' rows, a piece of a pair to a slot of this block
                     const bool to_rows = KIND == SEG_GROUP && whole;
@@ -921,19 +922,20 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
         float m_run = -CUDART_INF_F, l_run = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int P = NL == 1 ? 8 : 4;
-        // P partials into the running one; -inf: not there
+        // P partials into the running one.  A maximum of -inf with a sum of 0 is a part that is not there or has no keys for the
+        // row; with a sum that is no number (all its scores are none) it goes into the row's
         auto merge = [&](const float (&m)[P], const float (&l)[P], const float4 (&v)[P]) {
             float m_new = m_run;
 #pragma unroll
             for (int j = 0; j < P; ++j) m_new = fmaxf(m_new, m[j]);
-            if (m_new == -CUDART_INF_F) return;
-            const float w_old = exp2f(m_run - m_new);
+            const float ref = m_new == -CUDART_INF_F ? 0.f : m_new;
+            const float w_old = exp2f(m_run - ref);
             acc.x *= w_old; acc.y *= w_old; acc.z *= w_old; acc.w *= w_old;
             l_run *= w_old;
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                if (m[j] == -CUDART_INF_F) continue;
-                const float w = exp2f(m[j] - m_new);
+                if (m[j] == -CUDART_INF_F && l[j] == 0.f) continue;
+                const float w = exp2f(m[j] - ref);
                 l_run += w * l[j];
                 acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
             }
@@ -976,15 +978,14 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
             if (lane == 0) a.plan.part_ml[dst_row] = make_float2(m_run, l_run);
             continue;
         }
-        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+        const float inv = KIND == SEG_LIST && l_run == 0.f ? 0.f : 1.f / l_run;        // as in the main kernel
         if (lane_on) {
             uint2 w;
             w.x = pack_bf16(acc.x * inv, acc.y * inv);
             w.y = pack_bf16(acc.z * inv, acc.w * inv);
             reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + dst_row * D)[lane] = w;
         }
-        if (lane == 0 && p.lse != nullptr)
-            p.lse[dst_row] = l_run > 0.f ? (m_run + log2f(l_run)) * 0.6931471805599453f : -CUDART_INF_F;
+        if (lane == 0 && p.lse != nullptr) p.lse[dst_row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
     }
 }
 
