@@ -304,7 +304,8 @@ sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
 /*
  * For row i of sequence b's block at position pos = seq_len[b] - (gamma[b]+1) + i (the pages 0 .. pos / 16 are before it)
  * and kv head g, with the group's query heads h:
- *     s = max_{h,d} |q_hd| * (1/127),  qi_hd = round(q_hd / s)                (as above; at most 127 in magnitude)
+ *     s = max_{h,d} |q_hd| * (1/127),  qi_hd = round(q_hd / s)                (as above; at most 127 in magnitude; all 0
+ *                                                                              where one of the queries is not finite)
  *     score(page) = scales[page] * max_h sum_d max(qi_hd bounds[page][g][0][d], qi_hd bounds[page][g][1][d])
  * The row reads the first n_first pages, the last n_last up to and including its own, and of the others those with the
  * highest scores (what is no number counts as the highest), the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole

@@ -715,7 +715,7 @@ static float bf16_bits_to_f32(uint16_t h)
 
 static int whole(float x, float scale)
 {
-    if (!(scale > 0.f)) return 0;
+    if (!(scale > 0.f) || isinf(scale)) return 0;        /* NaN too */
     float n = rintf(x / scale);                          /* half to even: the default rounding mode */
     return n > 127.f ? 127 : n < -127.f ? -127 : (int)n;
 }
@@ -758,8 +758,8 @@ void oracle_page_choice(const uint16_t *q, int G, int D, const int8_t *bounds, c
                         const int32_t *table, int n_seen, int n_select, int n_first, int n_last, float *score, uint8_t *chosen)
 {
     float big = 0.f;
-    for (int e = 0; e < G * D; ++e)
-        if (fabsf(bf16_bits_to_f32(q[e])) > big) big = fabsf(bf16_bits_to_f32(q[e]));
+    for (int e = 0; e < G * D; ++e)                      /* a query that is no number leaves none */
+        if (fabsf(bf16_bits_to_f32(q[e])) > big || isnan(bf16_bits_to_f32(q[e]))) big = fabsf(bf16_bits_to_f32(q[e]));
     float scale = big * (1.f / 127.f);
     for (int p = 0; p < n_seen; ++p) {
         const int8_t *bd = bounds + ((int64_t)table[p] * hkv + head) * 2 * D;
