@@ -277,9 +277,10 @@ sv_status spec_kv_append(const sv_kv_append_params *p, void *stream);
  * page of sequence b that holds a position of [start, seq_len[b]), with start = seq_len[b] - (gamma[b]+1), or first[b]
  * where first is given (gamma NULL), and for every kv head, over the page's positions below seq_len[b]:
  *     M_d = max k_d,  m_d = min k_d,  scale = max_d max(|M_d|, |m_d|) * (1/127)
- *     bounds[page][head][0][d] = round(M_d / scale),  bounds[page][head][1][d] = round(m_d / scale)      (0 if scale is 0)
- * float32, each operation and the constant 1/127 rounded once, round half to even.  Other pages' entries stay.  seq_len[b] = 0 is an absent
- * sequence.  A page that two sequences bring up to date is written by both; they have to fill it alike.
+ *     bounds[page][head][0][d] = round(M_d / scale),  bounds[page][head][1][d] = round(m_d / scale)
+ * float32, each operation and the constant 1/127 rounded once, round half to even.  The bounds are 0 where scale is 0 or
+ * not finite; a key that is NaN makes it NaN.  Other pages' entries stay.  seq_len[b] = 0 is an absent sequence.  A page
+ * that two sequences bring up to date is written by both; they have to fill it alike.
  * Device-detected: gamma[b] outside [0, max_new) -> SV_DEV_BAD_GAMMA, clamped; a start below 0, more than max_new
  * positions or a length beyond the table row -> SV_DEV_BAD_LEN, sequence skipped; a page id outside the pool ->
  * SV_DEV_BAD_PAGE, page skipped.  One launch.
@@ -308,9 +309,10 @@ sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
  *                                                                              where one of the queries is not finite)
  *     score(page) = scales[page] * max_h sum_d max(qi_hd bounds[page][g][0][d], qi_hd bounds[page][g][1][d])
  * The row reads the first n_first pages, the last n_last up to and including its own, and of the others those with the
- * highest scores (what is no number counts as the highest), the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole
- * numbers and the product with the scale is rounded once, so a row of a block reads the pages that the same position would
- * have read decoded alone: n_last >= 1 keeps pages with keys behind the row out of the comparison.
+ * highest scores (one that is NaN, as the scale of a page whose keys are not all finite gives it, counts as the highest),
+ * the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole numbers and the
+ * product with the scale is rounded once, so a row of a block reads the pages that the same position would have read
+ * decoded alone: n_last >= 1 keeps pages with keys behind the row out of the comparison.
  * Output per sequence and kv head: the pages that any row of the block reads, in ascending order (indices into the block
  * table row), and for each the rows that do (bit i: row i).  Entries at and beyond n_list are left as they are.  A skipped
  * sequence has n_list 0.

@@ -736,10 +736,10 @@ void oracle_page_bounds_update(const uint16_t *k_pool, const int64_t *kv_strides
                     lo[d] = INFINITY;
                     for (int s = 0; s < n; ++s) {
                         float k = bf16_bits_to_f32(k_pool[page * kv_strides[0] + h * kv_strides[1] + s * kv_strides[2] + d * kv_strides[3]]);
-                        if (k > hi[d]) hi[d] = k;
-                        if (k < lo[d]) lo[d] = k;
+                        if (k > hi[d] || isnan(k)) hi[d] = k;        /* a NaN stays */
+                        if (k < lo[d] || isnan(k)) lo[d] = k;
                     }
-                    if (fabsf(hi[d]) > big) big = fabsf(hi[d]);
+                    if (fabsf(hi[d]) > big || isnan(hi[d])) big = fabsf(hi[d]);
                     if (fabsf(lo[d]) > big) big = fabsf(lo[d]);
                 }
                 float scale = big * (1.f / 127.f);

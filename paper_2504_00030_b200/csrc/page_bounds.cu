@@ -77,7 +77,8 @@ page_bounds_kernel(const __grid_constant__ PageBoundsLaunch a)
     }
     uint32_t hi[4] = {v[0].x, v[0].y, v[0].z, v[0].w}, lo[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
     auto fold = [&](int c, uint32_t x, uint32_t y) {
-        const __nv_bfloat162 m = __hmax2(as_bf2(hi[c]), as_bf2(x)), n = __hmin2(as_bf2(lo[c]), as_bf2(y));
+        // a NaN stays: the page's scale becomes one, so that the choice takes the page for the highest
+        const __nv_bfloat162 m = __hmax2_nan(as_bf2(hi[c]), as_bf2(x)), n = __hmin2_nan(as_bf2(lo[c]), as_bf2(y));
         hi[c] = *reinterpret_cast<const uint32_t *>(&m);
         lo[c] = *reinterpret_cast<const uint32_t *>(&n);
     };
@@ -97,18 +98,19 @@ page_bounds_kernel(const __grid_constant__ PageBoundsLaunch a)
         }
     // the first LANES lanes store the maxima, the next the minima
     const bool low = slot0 == 1;
-    float x[8], big = 0.f;
+    float x[8];
+    uint32_t big = 0;                                  // largest magnitude: these order as bits, NaN above all
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         const float2 f = __bfloat1622float2(as_bf2(low ? lo[c] : hi[c]));
         x[2 * c] = f.x;
         x[2 * c + 1] = f.y;
-        big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+        big = max(big, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
     }
 #pragma unroll
-    for (int d = 1; d < 2 * LANES; d <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+    for (int d = 1; d < 2 * LANES; d <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
     // every step rounds once to the nearest float32, so that the stored whole numbers are reproducible
-    const float scale = __fmul_rn(big, 1.f / 127.f);
+    const float scale = __fmul_rn(__uint_as_float(big), 1.f / 127.f);
     const uint2 w = whole8x8(x, Whole8(scale));
     const long long at = (long long)page * a.hkv + h;
     if (slot0 < 2) *reinterpret_cast<uint2 *>(p.bounds + at * 2 * D + (low ? D : 0) + dim8 * 8) = w;
