@@ -716,6 +716,8 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
 
 // ---------------------------------------------------------------------------- host side
 constexpr size_t PK_SMEM_BITS = 96 * 1024;
+// What a launch may bring without asking: 48 KB less the kernel's own arrays and what the system keeps, 3 KB together
+constexpr size_t PK_SMEM_DEFAULT = 44 * 1024;
 
 static int select_max_pages(int max_seq_len) { return (int)(((long long)max_seq_len + 15) / 16); }
 static int select_key_stride(int max_seq_len) { return (select_max_pages(max_seq_len) + 31) / 32 * 32; }
@@ -728,23 +730,15 @@ static size_t select_row_bits(int gamma_max, int max_seq_len)
     return (size_t)(gamma_max + 1) * ((select_max_pages(max_seq_len) + 31) / 32) * sizeof(uint32_t);
 }
 
-template <int WPR, int KPT>
-static sv_status launch_pick(const PageSelectLaunch &a, int teams, size_t smem, cudaStream_t s)
-{
-    if (smem > 48 * 1024 &&
-        cudaFuncSetAttribute(page_pick_kernel<WPR, KPT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)(PK_SMEM_BITS + PK_WARPS * PK_BINS * sizeof(int))) != cudaSuccess)
-        return SV_ECUDA;
-    return launch_kernel(true, page_pick_kernel<WPR, KPT>, (unsigned)(a.p.batch * a.p.hkv), teams * WPR * 32, smem, s, a);
-}
+using PickKernel = void (*)(PageSelectLaunch);
 
 // As many keys a thread as the longest row needs: with 32 for all a single token over 2048 pages took 15.1 us where it takes 14.5
 // (less code to fetch); 16 for all, with more warps for the longer rows, 134 us for the largest batch where 32 take 124.
 template <int WPR>
-static sv_status launch_pick_keys(const PageSelectLaunch &a, int teams, size_t smem, cudaStream_t s)
+static PickKernel pick_kernel_of(int pages)
 {
-    const int keys = (a.key_stride + WPR * 32 - 1) / (WPR * 32);
-    return keys <= 8 ? launch_pick<WPR, 8>(a, teams, smem, s) : keys <= 16 ? launch_pick<WPR, 16>(a, teams, smem, s) : launch_pick<WPR, 32>(a, teams, smem, s);
+    const int keys = (pages + WPR * 32 - 1) / (WPR * 32);
+    return keys <= 8 ? page_pick_kernel<WPR, 8> : keys <= 16 ? page_pick_kernel<WPR, 16> : page_pick_kernel<WPR, 32>;
 }
 
 template <int D>
@@ -804,6 +798,26 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
     const long long pairs = (long long)p->batch * p->hkv;
     if (pairs > (1 << 24)) return SV_EUNSUPPORTED;
     cudaStream_t s = (cudaStream_t)stream;
+    // Warps per row: enough to hold a row's keys in registers, and more where a block has few rows, down to four keys a thread
+    int need = 1;
+    while (need < PK_WARPS && (long long)need * 32 * 32 < max_pages) need *= 2;
+    while (need < PK_WARPS && need * 2 * R <= PK_WARPS && need * 32 * 4 < max_pages) need *= 2;
+    // Rows at a time: as few rounds as 16 warps allow, and no more warps than these rounds need (17 rows: two rounds of nine)
+    const int rounds = (R * need + PK_WARPS - 1) / PK_WARPS, teams = (R + rounds - 1) / rounds;
+    const size_t pick_smem = (size_t)teams * PK_BINS * sizeof(int) + (in_smem ? row_bits : 0);
+    PickKernel pick;
+    switch (need) {
+        case 1: pick = pick_kernel_of<1>(a.key_stride); break;
+        case 2: pick = pick_kernel_of<2>(a.key_stride); break;
+        case 4: pick = pick_kernel_of<4>(a.key_stride); break;
+        case 8: pick = pick_kernel_of<8>(a.key_stride); break;
+        default: pick = pick_kernel_of<16>(a.key_stride); break;
+    }
+    // in front of the first launch, so that a refusal leaves nothing under way; the limit is the largest block's, so that calls of
+    // several threads do not lower it for one another
+    if (pick_smem > PK_SMEM_DEFAULT &&
+        cudaFuncSetAttribute(pick, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(PK_SMEM_BITS + PK_WARPS * PK_BINS * sizeof(int))) != cudaSuccess)
+        return SV_ECUDA;
     if (max_pages > p->n_select) {             // otherwise no sequence has more pages than a row takes
         // a block per multiprocessor, fewer where there are not as many tiles
         const long long tiles = pairs * ((R + a.pos_per_chunk - 1) / a.pos_per_chunk) * ((max_pages + PS_PAGES - 1) / PS_PAGES);
@@ -811,18 +825,5 @@ extern "C" sv_status spec_page_select(const sv_page_select_params *p, void *work
         const sv_status st = p->head_dim == 128 ? launch_score<128>(a, grid, s) : launch_score<64>(a, grid, s);
         if (st != SV_OK) return st;
     }
-    // Warps per row: enough to hold a row's keys in registers, and more where a block has few rows, down to four keys a thread
-    int need = 1;
-    while (need < PK_WARPS && (long long)need * 32 * 32 < max_pages) need *= 2;
-    while (need < PK_WARPS && need * 2 * R <= PK_WARPS && need * 32 * 4 < max_pages) need *= 2;
-    // Rows at a time: as few rounds as 16 warps allow, and no more warps than these rounds need (17 rows: two rounds of nine)
-    const int rounds = (R * need + PK_WARPS - 1) / PK_WARPS, teams = (R + rounds - 1) / rounds;
-    const size_t smem = (size_t)teams * PK_BINS * sizeof(int) + (in_smem ? row_bits : 0);
-    switch (need) {
-        case 1: return launch_pick_keys<1>(a, teams, smem, s);
-        case 2: return launch_pick_keys<2>(a, teams, smem, s);
-        case 4: return launch_pick_keys<4>(a, teams, smem, s);
-        case 8: return launch_pick_keys<8>(a, teams, smem, s);
-        default: return launch_pick_keys<16>(a, teams, smem, s);
-    }
+    return launch_kernel(true, pick, (unsigned)pairs, teams * need * 32, pick_smem, s, a);
 }
