@@ -318,7 +318,7 @@ sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
  * sequence has n_list 0.
  * Device-detected: gamma[b] out of range -> SV_DEV_BAD_GAMMA, clamped; seq_len[b] < gamma[b]+1 or > max_seq_len ->
  * SV_DEV_BAD_LEN, sequence skipped; a page id outside [0, n_pages) -> SV_DEV_BAD_PAGE, that page's score is 0.
- * Two launches.
+ * Two launches; one where max_seq_len tokens have no more than n_select pages.
  */
 typedef struct sv_page_select_params {
     const void *q;              /* device bf16 [n_rows, hq, head_dim], 16-byte aligned: what the attention reads */
