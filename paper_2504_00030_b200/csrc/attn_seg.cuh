@@ -1024,7 +1024,9 @@ sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
     if (a.n_slots > SEG_RING) a.n_slots = SEG_RING;
     if (a.n_slots < 4) return SV_EUNSUPPORTED;
     const size_t smem = fixed + (size_t)a.n_slots * slot_bytes;
-    if (cudaFuncSetAttribute(attn_seg_kernel<KIND, NL, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    // the limit is all that a block may have, not this call's part of it: calls of several threads would lower it for one another
+    // between here and the launch
+    if (cudaFuncSetAttribute(attn_seg_kernel<KIND, NL, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)budget) != cudaSuccess)
         return SV_ECUDA;
     return launch_kernel(early, attn_seg_kernel<KIND, NL, D>, grid, SegConfig<NL>::THREADS, smem, stream, a, a.p.pool->k_map,
                          a.p.pool->v_map);
