@@ -132,7 +132,7 @@ static sv_status check_attn(const sv_attn_params *p)
     if (p->hq % p->hkv != 0) return SV_EUNSUPPORTED;
     if (p->hkv != p->pool->hkv || p->head_dim != p->pool->head_dim) return SV_EINVAL;
     if (p->head_dim != 64 && p->head_dim != 128) return SV_EUNSUPPORTED;
-    if (p->block_table_stride < (p->max_seq_len + 15) / 16) return SV_EINVAL;
+    if (p->block_table_stride < ((long long)p->max_seq_len + 15) / 16) return SV_EINVAL;
     if (!sv::aligned16(p->q) || !sv::aligned16(p->o)) return SV_EALIGN;
     if (!(p->sm_scale > 0.f)) return SV_EINVAL;
     return SV_OK;
