@@ -18,6 +18,9 @@ struct sv_kv_pool {
 
 namespace sv {
 
+// Pages of a sequence of L > 0 tokens, for the largest L too.
+__device__ __forceinline__ int pages_of(int L) { return (int)(((unsigned)L + 15u) >> 4); }
+
 // Argument checks of the verify attention (api.cu).
 sv_status check_attn_params(const sv_attn_params *p);
 

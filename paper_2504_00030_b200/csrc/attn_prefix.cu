@@ -40,7 +40,7 @@ prefix_plan_kernel(const __grid_constant__ SegLaunch a, const int32_t *prefix_le
             gid = -1;
         }
         const int gam = min(max(p.gamma[b], 0), p.gamma_max), L = p.seq_len[b];
-        if (L < gam + 1 || (long long)(L + 15) / 16 > p.block_table_stride || L > p.max_seq_len) return 0;
+        if (L < gam + 1 || pages_of(L) > p.block_table_stride || L > p.max_seq_len) return 0;
         return gam + 1;
     };
     int before = 0, rows = 0, members = 0, rep = 0x7fffffff;

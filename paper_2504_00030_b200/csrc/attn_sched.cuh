@@ -45,8 +45,8 @@ __device__ __forceinline__ int seq_tiles(const sv_attn_params &p, int b, int *ga
         g = min(max(g, 0), p.gamma_max);
     }
     const int L = p.seq_len[b];
-    int nt = (L + tile - 1) / tile;
-    if (L < g + 1 || (long long)(L + 15) / 16 > p.block_table_stride || L > p.max_seq_len) {
+    int nt = (int)(((unsigned)L + tile - 1) / tile);
+    if (L < g + 1 || pages_of(L) > p.block_table_stride || L > p.max_seq_len) {
         if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
         nt = 0;
     }

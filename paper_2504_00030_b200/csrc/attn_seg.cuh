@@ -118,7 +118,7 @@ __device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool
         g = min(max(g, 0), p.gamma_max);
     }
     c.R = g + 1;
-    if (c.L < c.R || (long long)(c.L + 15) / 16 > p.block_table_stride || c.L > p.max_seq_len) {
+    if (c.L < c.R || pages_of(c.L) > p.block_table_stride || c.L > p.max_seq_len) {
         if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
         return;
     }
@@ -133,7 +133,7 @@ __device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool
         c.n_tiles = max(1, (n + PPT - 1) / PPT);       // an empty list still has outputs
     } else {
         c.page0 = n;
-        c.n_pages = (c.L + 15) / 16 - n;
+        c.n_pages = pages_of(c.L) - n;
         c.n_sub = p.hkv * chunks;
         c.n_tiles = (c.n_pages + PPT - 1) / PPT;
     }
@@ -440,7 +440,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     table = p.block_table + (long long)tb * p.block_table_stride;
                 }
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
-                const int seq_pages = (cur.L + 15) / 16;
+                const int seq_pages = pages_of(cur.L);
                 int ids_base = -1;
                 for (int ti = 0; ti < seg_tiles; ++ti, ++u, at.next(n_slots)) {
                     const int e0 = (cur.t + ti) * PPT;
@@ -699,7 +699,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (KIND != SEG_GROUP && nxt.o < a.n_owners) nxt_q0 = p.cu_q[nxt.b];
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
-                const int seq_pages = (cur.L + 15) / 16;
+                const int seq_pages = pages_of(cur.L);
                 const bool far = p.gamma_max >= 32;            // masks have bits above the 32nd
                 int e_base = -32, e_lp = -1;                   // lane l: entry e_base + l of the list and its mask
                 uint32_t e_lo = 0, e_hi = 0;
@@ -758,9 +758,10 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                                 lim[j] = row_ok && ((mk >> (i & 31)) & 1) ? max(last - lp * 16, -1) : -1;
                             }
                         } else {
-                            const int tok0 = (cur.page0 + (cur.t + ti) * PPT) * 16;
+                            // without a sign: the last tile of the longest sequence ends behind the largest int
+                            const unsigned tok0 = (unsigned)(cur.page0 + (cur.t + ti) * PPT) * 16u;
 #pragma unroll
-                            for (int j = 0; j < PPT; ++j) lim[j] = last - tok0 - j * 16;
+                            for (int j = 0; j < PPT; ++j) lim[j] = (int)((unsigned)last - tok0 - j * 16u);
                         }
                         ok = seg_wait(smem_u32(&sh->s_full[buf]), phase, abort_flag, status);
                         if (!ok) break;

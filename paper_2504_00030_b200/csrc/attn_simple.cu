@@ -57,7 +57,7 @@ attn_simple_kernel(sv_attn_params p, sv_kv_pool pool)
     if (i > g) return;
     const int L = p.seq_len[b];
     const int R = g + 1;
-    if (L < R || (long long)(L + 15) / 16 > p.block_table_stride) {
+    if (L < R || pages_of(L) > p.block_table_stride) {
         set_status(p.device_status, SV_DEV_BAD_LEN);
         return;
     }

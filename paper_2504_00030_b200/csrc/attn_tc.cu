@@ -137,7 +137,7 @@ attn_tc_kernel(const AttnTcLaunch a, const __grid_constant__ CUtensorMap k_map,
             for (long long tg = t_begin; tg < t_end; ++tg) {
                 const int b = cur.b;
                 const int L = p.seq_len[b];
-                const int n_pages = (L + 15) >> 4;
+                const int n_pages = pages_of(L);
                 const int32_t *bt = p.block_table + (long long)b * p.block_table_stride;
                 // lane l fetches (page l/2, dims half l%2) of K, then of V
                 const int page_in_tile = (lane >> 1) % PAGES_PER_TILE, half = lane & 1;

@@ -193,7 +193,7 @@ attn_tq_kernel(const AttnTcLaunch a, const __grid_constant__ CUtensorMap k_map,
                 }
                 const int b = cur.b;
                 const int L = p.seq_len[b];
-                const int n_pages = (L + 15) >> 4;
+                const int n_pages = pages_of(L);
                 const int32_t *bt = p.block_table + (long long)b * p.block_table_stride;
                 const int lp = cur.t * (TILE / 16) + page_in_tile;
                 int phys = (int)a.n_pool_pages;       // out of range: TMA fills zeros, no traffic

@@ -59,7 +59,7 @@ __device__ __forceinline__ SeqRows seq_rows(const sv_page_select_params &p, int 
         if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
         s.R = 0;
     }
-    s.n_pages = (s.L + 15) / 16;
+    s.n_pages = pages_of(s.L);                  // of use where there are rows
     return s;
 }
 
