@@ -7,7 +7,7 @@ namespace sv {
 template <int NL>
 static sv_status launch_pages(SegLaunch &a, int grid, cudaStream_t s)
 {
-    sv_status st = a.p.head_dim == 128 ? launch_seg<SEG_LIST, NL, 128>(a, grid, true, s) : launch_seg<SEG_LIST, NL, 64>(a, grid, true, s);
+    sv_status st = a.p.head_dim == 128 ? launch_seg<SEG_LIST, NL, 128>(a, grid, s) : launch_seg<SEG_LIST, NL, 64>(a, grid, s);
     if (st != SV_OK) return st;
     return a.p.head_dim == 128 ? launch_seg_combine<SEG_LIST, NL, 128>(a, grid, s) : launch_seg_combine<SEG_LIST, NL, 64>(a, grid, s);
 }

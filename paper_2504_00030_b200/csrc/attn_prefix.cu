@@ -134,7 +134,7 @@ static PrefixLayout prefix_layout(int batch, int gamma_max, int hq, int hkv, int
 template <int D>
 static sv_status launch_groups(SegLaunch &a, cudaStream_t s)
 {
-    const sv_status st = launch_seg<SEG_GROUP, 2, D>(a, seg_grid(2), true, s);
+    const sv_status st = launch_seg<SEG_GROUP, 2, D>(a, seg_grid(2), s);
     return st != SV_OK ? st : launch_seg_combine<SEG_GROUP, 2, D>(a, seg_grid(2), s);
 }
 
@@ -142,7 +142,7 @@ template <int NL>
 static sv_status launch_sequences(SegLaunch &a, cudaStream_t s)
 {
     const int grid = seg_grid(NL);
-    sv_status st = a.p.head_dim == 128 ? launch_seg<SEG_SEQ, NL, 128>(a, grid, true, s) : launch_seg<SEG_SEQ, NL, 64>(a, grid, true, s);
+    sv_status st = a.p.head_dim == 128 ? launch_seg<SEG_SEQ, NL, 128>(a, grid, s) : launch_seg<SEG_SEQ, NL, 64>(a, grid, s);
     if (st != SV_OK) return st;
     return a.p.head_dim == 128 ? launch_seg_combine<SEG_SEQ, NL, 128>(a, grid, s) : launch_seg_combine<SEG_SEQ, NL, 64>(a, grid, s);
 }

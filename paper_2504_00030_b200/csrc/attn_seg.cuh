@@ -308,8 +308,9 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
             tc_st32(o_addr + ch * 32, o);
         }
     }
-    // P = 2^(s*c - m_ref) as bf16 pairs over S: the tensor core multiplies bf16; the sums stay fp32 and unrounded, so P's
-    // rounding (2^-9 relative, independent from key to key) averages out below the output's own
+    // P = 2^(s*c - m_ref) as bf16 pairs over S: the tensor core multiplies bf16, so each weight is rounded, by at most 2^-8 of it
+    // and independently from key to key; an output is off by at most 2^-8 of the weighted sum of |v|, next to its own rounding
+    // (2^-8 of it).  The sums stay fp32 and unrounded, so the log-sum-exp has none of it
     const uint64_t c2 = pair2(c_scale, c_scale), m2n = pair2(-m_use, -m_use);
     uint64_t sum = 0;                                  // two float32 zeros
 #pragma unroll
@@ -578,7 +579,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 for (int it = 0; it < (1 << 20) && !mbar_try_wait(smem_u32(&sh->drained[l]), 0); ++it) { }
             }
         }
-        else if (NL == 1 && t_end > t_begin && warp == 3 && q_ahead) {
+        else if (NL == 1 && t_end > t_begin && warp == 3 && q_ahead) {         // groups have two row tiles
             // ================================================================ query rows of the next pair
             SegCursor cur;
             seg_start<KIND, NL>(a, sh->share, sh->start, cur);
@@ -601,8 +602,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         const int r = b0 + k * RPI + r0, i = r / G;
                         v[k] = make_uint4(0, 0, 0, 0);
                         if (r < n_rows) {
-                            const int at = KIND == SEG_GROUP ? a.plan.row_list[a.plan.grp_base[cur.o] + pos0 + i].x : p.cu_q[cur.b] + pos0 + i;
-                            const long long q_row = (long long)at * p.hq + (long long)cur.h * G + (r - i * G);
+                            const long long q_row = ((long long)p.cu_q[cur.b] + pos0 + i) * p.hq + (long long)cur.h * G + (r - i * G);
                             v[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D) + ch);
                         }
                     }
@@ -1014,7 +1014,7 @@ inline size_t seg_table_bytes() { return seg_round((SEG_MAX_GRID + 1) * sizeof(i
 inline size_t seg_part_bytes(int nl) { return (size_t)seg_grid(nl) * 2 * seg_slot_floats(nl * 128) * sizeof(float); }
 
 template <int KIND, int NL, int D>
-sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
+sv_status launch_seg(SegLaunch &a, int grid, cudaStream_t stream)
 {
     constexpr int slot_bytes = SEG_TILE * D * 2;
     // shared memory of a multiprocessor less 1 KB that each block takes by itself
@@ -1029,7 +1029,7 @@ sv_status launch_seg(SegLaunch &a, int grid, bool early, cudaStream_t stream)
     // between here and the launch
     if (cudaFuncSetAttribute(attn_seg_kernel<KIND, NL, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)budget) != cudaSuccess)
         return SV_ECUDA;
-    return launch_kernel(early, attn_seg_kernel<KIND, NL, D>, grid, SegConfig<NL>::THREADS, smem, stream, a, a.p.pool->k_map,
+    return launch_kernel(true, attn_seg_kernel<KIND, NL, D>, grid, SegConfig<NL>::THREADS, smem, stream, a, a.p.pool->k_map,
                          a.p.pool->v_map);
 }
 

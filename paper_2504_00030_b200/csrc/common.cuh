@@ -17,12 +17,15 @@ inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 // The small kernels of a step (decisions, combine, controller update, cache append) are enqueued as programmatic
 // dependent launches: they may be set up on the SMs while their predecessor in the stream drains, which hides the
-// launch latency between the several kernels of a step (a third of the step time of the small workloads).  The
-// first statement of every kernel, pdl_enter(), waits until the predecessor has completed and its memory is
-// visible -- so the order of effects is that of a plain stream -- and then lets its own successor be set up in turn.
-// The persistent kernels with a static split of their work (the logit streams, the attention main kernels) are
-// launched plainly (early = false): set up early, their blocks start at different times on SMs that the
+// launch latency between the several kernels of a step (a third of the step time of the small workloads).
+// pdl_enter(), at the head of every kernel, waits until the predecessor has completed and its memory is visible -- so
+// the order of effects is that of a plain stream -- and then lets its own successor be set up in turn.  In front of it
+// stands at most what touches no global memory but the kernel's own parameters: barriers of the block's shared memory,
+// a prefetch of a tensor map (attn_seg.cuh).
+// The persistent kernels with a static split of their work in the verify step itself (the logit streams, the verify
+// attention) are launched plainly (early = false): set up early, their blocks start at different times on SMs that the
 // predecessor's last blocks still share, and the blocks that start late finish late (+4 % on the largest workload).
+// The page scores and the attention over parts of the cache, whose calls are two to five launches in a row, are set up early.
 template <typename... KArgs, typename... Args>
 inline sv_status launch_kernel(bool early, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                                cudaStream_t stream, Args &&...args)
@@ -46,7 +49,7 @@ inline sv_status launch_kernel(bool early, void (*kernel)(KArgs...), dim3 grid, 
 // multiprocessors of the current device (cached per device)
 int sm_count();
 
-// first statement of every kernel (see launch_kernel)
+// at the head of every kernel (see launch_kernel)
 __device__ __forceinline__ void pdl_enter()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

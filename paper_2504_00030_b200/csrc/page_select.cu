@@ -1,6 +1,7 @@
 // Selection of the pages that each row of a draft block reads (spec_page_select), two kernels.
 //
-// page_score_kernel.  The score of a page is an upper estimate of what any of its keys can give with the row's queries,
+// page_score_kernel.  The score of a page estimates the most that any of its keys can give with the row's queries (a bound but for
+// the roundings to 8 bits, half a step of each),
 //     max over the group's heads h of  sum_d max(q_hd M_d, q_hd m_d),
 // with the queries in 8 bits (one scale per row and kv head, which no comparison needs) and the page's bounds M, m in 8
 // bits times the page's scale.  max(q M, q m) = max(q, 0) M + min(q, 0) m, so it is an integer matrix product of depth
@@ -554,7 +555,7 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
         auto key_at = [&](int page) -> uint32_t { return page >= c_lo && page < c_hi ? __ldg(src + page) : 0u; };
         uint32_t key[KPT];
         const int rounds = (n_seen + TEAM - 1) / TEAM;
-        // f(key, page) for the thread's pages (with keys of 0 up to the next eight)
+        // f(key, page) for the thread's pages (with keys of 0 up to the next four)
         auto each = [&](auto &&f) {
 #pragma unroll
             for (int j0 = 0; j0 < KPT; j0 += 4) {
