@@ -508,13 +508,6 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
     const long long pair = blockIdx.x;
     int *hist = reinterpret_cast<int *>(pk_smem) + team * PK_BINS;       // the team's counts
     uint32_t *bits = a.bits != nullptr ? a.bits + pair * (p.gamma_max + 1) * a.bit_words : pk_smem + teams * PK_BINS;
-    if (h == 0 && sr.R > 0 && sr.n_pages <= p.n_select) {      // no scores, so nobody has looked at these ids
-        const int32_t *table = p.block_table + (long long)b * p.block_table_stride;
-        for (int page = threadIdx.x; page < sr.n_pages; page += blockDim.x) {
-            const int id = __ldg(table + page);
-            if (id < 0 || id >= p.n_pages) set_status(p.device_status, SV_DEV_BAD_PAGE);
-        }
-    }
     int parity = 0;
     auto team_bar = [&]() {
         if (WPR == 1) __syncwarp();
@@ -720,6 +713,13 @@ page_pick_kernel(const __grid_constant__ PageSelectLaunch a)
     }
     if (short_list) set_status(p.device_status, SV_DEV_BAD_LEN);
     if (threadIdx.x == 0) p.n_list[pair] = (int)min((long long)base, (long long)p.list_stride);
+    if (h == 0 && sr.R > 0 && sr.n_pages <= p.n_select) {      // no scores, so nobody has looked at these ids
+        const int32_t *table = p.block_table + (long long)b * p.block_table_stride;
+        for (int page = threadIdx.x; page < sr.n_pages; page += blockDim.x) {
+            const int id = __ldg(table + page);
+            if (id < 0 || id >= p.n_pages) set_status(p.device_status, SV_DEV_BAD_PAGE);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------- host side
