@@ -356,7 +356,7 @@ sv_status spec_page_select(const sv_page_select_params *p, void *workspace_devic
  * n_list[b][g], with bit i of row_mask[b][g][e].  A row without any key gives o = 0 and lse = -inf (so does one whose
  * scores are all -inf); one with a score that is NaN or +inf gives NaN in both.  The lists are those of spec_page_select,
  * or any others: pages in any order, each once.
- * Arguments of attn as in spec_verify_attn; gamma_max at most 63, hq / hkv at most 128.
+ * Arguments of attn as in spec_verify_attn; gamma_max at most 63, hq / hkv at most 128, max_seq_len at most 2^31 - 65.
  * Device-detected: as spec_verify_attn; a listed page outside the sequence's pages -> SV_DEV_BAD_PAGE, not read; n_list
  * outside [0, list_stride] -> SV_DEV_BAD_LEN, clamped.  Two launches.
  */
@@ -383,7 +383,7 @@ sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void *workspace_
  * row -> SV_DEV_BAD_LEN, the sequence or group is computed without sharing.  Five launches.
  */
 typedef struct sv_attn_prefix_params {
-    sv_attn_params attn;        /* batch at most 8192, hq / hkv at most 128 */
+    sv_attn_params attn;        /* batch at most 8192, gamma_max at most 4095, hq / hkv at most 128, max_seq_len at most 2^31 - 65 */
     const int32_t *group;       /* device [batch] */
     const int32_t *prefix_len;  /* device [n_groups], tokens */
     int32_t n_groups;           /* 1 .. batch */

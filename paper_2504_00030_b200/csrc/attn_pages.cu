@@ -31,7 +31,7 @@ extern "C" sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void 
     const sv_status st = check_attn_params(&at);
     if (st != SV_OK) return st;
     if (p->page_list == nullptr || p->row_mask == nullptr || p->n_list == nullptr || p->list_stride <= 0) return SV_EINVAL;
-    if (at.gamma_max > 63 || at.hq / at.hkv > 128 || !at.pool->has_maps) return SV_EUNSUPPORTED;
+    if (at.gamma_max > 63 || at.hq / at.hkv > 128 || at.max_seq_len > SEG_MAX_LEN || !at.pool->has_maps) return SV_EUNSUPPORTED;
     if ((long long)at.batch * at.hkv > (1 << 24) || p->list_stride > (1 << 26)) return SV_EUNSUPPORTED;
     if (!seg_tiles_fit((long long)at.batch * at.hkv * seg_chunks(at.hq / at.hkv, at.gamma_max), p->list_stride)) return SV_EUNSUPPORTED;
     if ((reinterpret_cast<uintptr_t>(p->row_mask) & 7u) != 0) return SV_EALIGN;

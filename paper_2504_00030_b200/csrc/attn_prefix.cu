@@ -40,7 +40,7 @@ prefix_plan_kernel(const __grid_constant__ SegLaunch a, const int32_t *prefix_le
             gid = -1;
         }
         const int gam = min(max(p.gamma[b], 0), p.gamma_max), L = p.seq_len[b];
-        if (L < gam + 1 || pages_of(L) > p.block_table_stride || L > p.max_seq_len) return 0;
+        if (L < gam + 1 || L > p.max_seq_len || (L + 15) / 16 > p.block_table_stride) return 0;
         return gam + 1;
     };
     int before = 0, rows = 0, members = 0, rep = 0x7fffffff;
@@ -167,7 +167,8 @@ extern "C" sv_status spec_verify_attn_prefix(const sv_attn_prefix_params *p, voi
     sv_status st = check_attn_params(&at);
     if (st != SV_OK) return st;
     if (p->group == nullptr || p->prefix_len == nullptr || p->n_groups <= 0 || p->n_groups > at.batch) return SV_EINVAL;
-    if (at.batch > MAX_PREFIX_BATCH || at.gamma_max > 4095 || at.hq / at.hkv > 128 || !at.pool->has_maps) return SV_EUNSUPPORTED;
+    if (at.batch > MAX_PREFIX_BATCH || at.gamma_max > 4095 || at.hq / at.hkv > 128 || at.max_seq_len > SEG_MAX_LEN || !at.pool->has_maps)
+        return SV_EUNSUPPORTED;
     // pairs of the sequences; the groups, whose pairs have two row tiles, have no more
     if (!seg_tiles_fit((long long)at.batch * at.hkv * seg_chunks(at.hq / at.hkv, at.gamma_max), at.max_seq_len / 16 + 1)) return SV_EUNSUPPORTED;
     if (workspace == nullptr ||

@@ -118,7 +118,7 @@ __device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool
         g = min(max(g, 0), p.gamma_max);
     }
     c.R = g + 1;
-    if (c.L < c.R || pages_of(c.L) > p.block_table_stride || c.L > p.max_seq_len) {
+    if (c.L < c.R || c.L > p.max_seq_len || (c.L + 15) / 16 > p.block_table_stride) {        // in this order: the sum stays in range
         if (report) set_status(p.device_status, SV_DEV_BAD_LEN);
         return;
     }
@@ -133,7 +133,7 @@ __device__ __forceinline__ void seg_owner(const SegLaunch &a, SegCursor &c, bool
         c.n_tiles = max(1, (n + PPT - 1) / PPT);       // an empty list still has outputs
     } else {
         c.page0 = n;
-        c.n_pages = pages_of(c.L) - n;
+        c.n_pages = (c.L + 15) / 16 - n;
         c.n_sub = p.hkv * chunks;
         c.n_tiles = (c.n_pages + PPT - 1) / PPT;
     }
@@ -441,7 +441,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                     table = p.block_table + (long long)tb * p.block_table_stride;
                 }
                 const int32_t *list = KIND == SEG_LIST ? a.page_list + (long long)cur.o * a.list_stride : nullptr;
-                const int seq_pages = pages_of(cur.L);
+                const int seq_pages = (cur.L + 15) / 16;
                 int ids_base = -1;
                 for (int ti = 0; ti < seg_tiles; ++ti, ++u, at.next(n_slots)) {
                     const int e0 = (cur.t + ti) * PPT;
@@ -602,7 +602,8 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         const int r = b0 + k * RPI + r0, i = r / G;
                         v[k] = make_uint4(0, 0, 0, 0);
                         if (r < n_rows) {
-                            const long long q_row = ((long long)p.cu_q[cur.b] + pos0 + i) * p.hq + (long long)cur.h * G + (r - i * G);
+                            const int at = p.cu_q[cur.b] + pos0 + i;
+                            const long long q_row = (long long)at * p.hq + (long long)cur.h * G + (r - i * G);
                             v[k] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.q) + q_row * D) + ch);
                         }
                     }
@@ -699,7 +700,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 if (KIND != SEG_GROUP && nxt.o < a.n_owners) nxt_q0 = p.cu_q[nxt.b];
                 const bool whole = cur.t == 0 && seg_tiles == cur.n_tiles;
                 const int last = KIND == SEG_GROUP ? cur.L - 1 : cur.L - cur.R + i;       // last visible key of the row
-                const int seq_pages = pages_of(cur.L);
+                const int seq_pages = (cur.L + 15) / 16;
                 const bool far = p.gamma_max >= 32;            // masks have bits above the 32nd
                 int e_base = -32, e_lp = -1;                   // lane l: entry e_base + l of the list and its mask
                 uint32_t e_lo = 0, e_hi = 0;
@@ -758,10 +759,9 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                                 lim[j] = row_ok && ((mk >> (i & 31)) & 1) ? max(last - lp * 16, -1) : -1;
                             }
                         } else {
-                            // without a sign: the last tile of the longest sequence ends behind the largest int
-                            const unsigned tok0 = (unsigned)(cur.page0 + (cur.t + ti) * PPT) * 16u;
+                            const int tok0 = (cur.page0 + (cur.t + ti) * PPT) * 16;        // the longest sequence leaves room for a tile
 #pragma unroll
-                            for (int j = 0; j < PPT; ++j) lim[j] = (int)((unsigned)last - tok0 - j * 16u);
+                            for (int j = 0; j < PPT; ++j) lim[j] = last - tok0 - j * 16;
                         }
                         ok = seg_wait(smem_u32(&sh->s_full[buf]), phase, abort_flag, status);
                         if (!ok) break;
@@ -831,10 +831,13 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                         }
                     }
                     if (row_ok) {
+                        // A sum that is no number goes with the highest maximum: with -inf (all scores NaN) the merge would take
+                        // the part for one without keys
+                        const float m_part = l_sum != l_sum ? CUDART_INF_F : m_ref;
                         if (to_rows) {
-                            a.plan.part_ml[part_row] = make_float2(m_ref, l_sum);
+                            a.plan.part_ml[part_row] = make_float2(m_part, l_sum);
                         } else {
-                            slot[(size_t)NL * 128 * SEG_PITCH + row] = m_ref;
+                            slot[(size_t)NL * 128 * SEG_PITCH + row] = m_part;
                             slot[(size_t)NL * 128 * SEG_PITCH + NL * 128 + row] = l_sum;
                         }
                     }
@@ -923,20 +926,19 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
         float m_run = -CUDART_INF_F, l_run = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int P = NL == 1 ? 8 : 4;
-        // P partials into the running one.  A maximum of -inf with a sum of 0 is a part that is not there or has no keys for the
-        // row; with a sum that is no number (all its scores are none) it goes into the row's
+        // P partials into the running one; -inf: not there, or no keys for the row
         auto merge = [&](const float (&m)[P], const float (&l)[P], const float4 (&v)[P]) {
             float m_new = m_run;
 #pragma unroll
             for (int j = 0; j < P; ++j) m_new = fmaxf(m_new, m[j]);
-            const float ref = m_new == -CUDART_INF_F ? 0.f : m_new;
-            const float w_old = exp2f(m_run - ref);
+            if (m_new == -CUDART_INF_F) return;
+            const float w_old = exp2f(m_run - m_new);
             acc.x *= w_old; acc.y *= w_old; acc.z *= w_old; acc.w *= w_old;
             l_run *= w_old;
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                if (m[j] == -CUDART_INF_F && l[j] == 0.f) continue;
-                const float w = exp2f(m[j] - ref);
+                if (m[j] == -CUDART_INF_F) continue;
+                const float w = exp2f(m[j] - m_new);
                 l_run += w * l[j];
                 acc.x += w * v[j].x; acc.y += w * v[j].y; acc.z += w * v[j].z; acc.w += w * v[j].w;
             }
@@ -993,6 +995,8 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
 // ---------------------------------------------------------------------------- host side
 inline int seg_nl(int rows) { return rows <= 128 ? 1 : 2; }
 inline int seg_grid(int nl) { return sm_count() * (nl == 1 ? 2 : 1); }
+// Longest sequence: the positions of its last tile fit an int.
+constexpr int SEG_MAX_LEN = 0x7fffffff - SEG_TILE;
 // Whether the key tiles of `pairs` pairs with at most `pages` pages each can be numbered with 31 bits, as the launches number them.
 inline bool seg_tiles_fit(long long pairs, long long pages)
 {
