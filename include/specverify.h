@@ -206,7 +206,8 @@ sv_status spec_kv_pages_update(const sv_kv_pages_params *p, void *stream);
  *     pos = seq_len[b] - (gamma[b]+1) + i ;  kv head = h / (hq / hkv)
  *     s_j = sm_scale * <q, k_j>   for j = 0 .. pos
  *     o   = sum_j softmax(s)_j v_j ;   lse = ln sum_j exp(s_j)
- * bf16 inputs, fp32 accumulation and softmax, bf16 output.
+ * bf16 inputs, fp32 accumulation and softmax, bf16 output.  A row with a score that is NaN or +inf, or with nothing but
+ * scores of -inf, gives NaN.
  */
 typedef struct sv_attn_params {
     const void *q;              /* device bf16 [n_rows, hq, head_dim], 16-byte aligned */

@@ -539,7 +539,8 @@ attn_combine_kernel(const AttnTcLaunch a)
             packed.x = *reinterpret_cast<const uint32_t *>(&lo);
             packed.y = *reinterpret_cast<const uint32_t *>(&hi);
             if (lane_on) reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + q_row * D)[lane] = packed;
-            if (lane == 0 && p.lse != nullptr) p.lse[q_row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+            // every row has keys: nothing merged means that none of its scores is a number (the output is 0 / 0 then)
+            if (lane == 0 && p.lse != nullptr) p.lse[q_row] = l_run == 0.f ? CUDART_NAN_F : (m_run + log2f(l_run)) * 0.6931471805599453f;
         }
     }
 }

@@ -673,7 +673,8 @@ attn_tq_kernel(const AttnTcLaunch a, const __grid_constant__ CUtensorMap k_map,
                                 w4.w = pack_bf16(acc[c + 6] * inv, acc[c + 7] * inv);
                                 *reinterpret_cast<uint4 *>(dst + c) = w4;
                             }
-                            if ((j & 7) == 0 && p.lse != nullptr) p.lse[qr] = (M + log2f(lsum)) * 0.6931471805599453f;
+                            // nothing merged: none of the row's scores is a number (the output is 0 / 0 then)
+                            if ((j & 7) == 0 && p.lse != nullptr) p.lse[qr] = lsum == 0.f ? CUDART_NAN_F : (M + log2f(lsum)) * 0.6931471805599453f;
                         } else {
                             float *slot = a.ws_part + ((size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1)) * part_slot_floats(a.slot_rows);
                             float *orow = slot + (size_t)r * HD + d0;
