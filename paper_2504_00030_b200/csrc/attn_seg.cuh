@@ -337,6 +337,20 @@ __device__ __forceinline__ bool seg_softmax(uint32_t s_addr, uint32_t o_addr, co
     return true;
 }
 
+// What a row's sum makes of its output and log-sum-exp.  A sum of 0 is a row without keys, which lists alone can leave: zeros and
+// -inf; elsewhere all scores are -inf, 0 / 0.  A sum that is no number (a NaN or an infinite score) stays one in both.
+template <int KIND>
+__device__ __forceinline__ float seg_inv(float l)
+{
+    return KIND == SEG_LIST && l == 0.f ? 0.f : 1.f / l;
+}
+template <int KIND>
+__device__ __forceinline__ float seg_lse(float m, float l)
+{
+    if (KIND != SEG_LIST && l == 0.f) return CUDART_NAN_F;
+    return (m + log2f(l)) * 0.6931471805599453f;
+}
+
 // a pair's start and end, in key tiles
 __host__ __device__ constexpr int seg_pair_cost(int kind) { return kind == SEG_LIST ? 3 : kind == SEG_SEQ ? 8 : 12; }
 
@@ -794,9 +808,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                 } else if (KIND != SEG_GROUP && whole) {
                     // rolled loops here and below: the roles' code competes for the instruction cache (13 rows of one head, 40 kv
                     // heads, 9 pairs a block: 182 us unrolled, 172 rolled when it was tried)
-                    // a row without keys, which lists alone can leave: zeros, -inf.  A sum that is no number (a NaN or an infinite
-                    // score) stays one in both outputs
-                    const float inv = KIND == SEG_LIST && l_sum == 0.f ? 0.f : 1.f / l_sum;
+                    const float inv = seg_inv<KIND>(l_sum);
                     __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(p.o) + q_row * D;
 #pragma unroll 1
                     for (int ch = 0; ch < OCH; ++ch) {
@@ -814,7 +826,7 @@ attn_seg_kernel(const __grid_constant__ SegLaunch a, const __grid_constant__ CUt
                             }
                         }
                     }
-                    if (row_ok && p.lse != nullptr) p.lse[q_row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+                    if (row_ok && p.lse != nullptr) p.lse[q_row] = seg_lse<KIND>(m_ref, l_sum);
                 } else {
                     // unnormalised: a whole pair of a group to the positions' rows, a piece of a pair to a slot of this block
                     const bool to_rows = KIND == SEG_GROUP && whole;
@@ -981,14 +993,14 @@ attn_seg_combine_kernel(const __grid_constant__ SegLaunch a, int main_grid, int 
             if (lane == 0) a.plan.part_ml[dst_row] = make_float2(m_run, l_run);
             continue;
         }
-        const float inv = KIND == SEG_LIST && l_run == 0.f ? 0.f : 1.f / l_run;        // as in the main kernel
+        const float inv = seg_inv<KIND>(l_run);
         if (lane_on) {
             uint2 w;
             w.x = pack_bf16(acc.x * inv, acc.y * inv);
             w.y = pack_bf16(acc.z * inv, acc.w * inv);
             reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.o) + dst_row * D)[lane] = w;
         }
-        if (lane == 0 && p.lse != nullptr) p.lse[dst_row] = (m_run + log2f(l_run)) * 0.6931471805599453f;
+        if (lane == 0 && p.lse != nullptr) p.lse[dst_row] = seg_lse<KIND>(m_run, l_run);
     }
 }
 

@@ -369,7 +369,7 @@ attn_tc_kernel(const AttnTcLaunch a, const __grid_constant__ CUtensorMap k_map,
                         }
                     }
                     if (row_ok && p.lse != nullptr)
-                        p.lse[q_row] = (m_ref + log2f(l_sum)) * 0.6931471805599453f;
+                        p.lse[q_row] = l_sum == 0.f ? CUDART_NAN_F : (m_ref + log2f(l_sum)) * 0.6931471805599453f;       // as the output, 0 / 0
                 } else {
                     // partial: fp32 O row, then max and sum; slot 0 = the block's first segment
                     float *slot = a.ws_part + ((size_t)blockIdx.x * 2 + (seg_no == 0 ? 0 : 1)) * part_slot_floats(NQ * 128);
