@@ -314,6 +314,8 @@ sv_status spec_page_bounds_update(const sv_page_bounds_params *p, void *stream);
  * the lower page on ties, n_select in all (all of them where there are no more).  The sum is of whole numbers and the
  * product with the scale is rounded once, so a row of a block reads the pages that the same position would have read
  * decoded alone: n_last >= 1 keeps pages with keys behind the row out of the comparison.
+ * Choice and listed pages together are worth it (B200, 64 pages a row) for single tokens from some 20000 tokens of one
+ * sequence, 4000 of 16 or 2000 of 128; for blocks where the pages of all rows together are a small part of the cache.
  * Output per sequence and kv head: the pages that any row of the block reads, in ascending order (indices into the block
  * table row), and for each the rows that do (bit i: row i).  Entries at and beyond n_list are left as they are.  A skipped
  * sequence has n_list 0.
@@ -380,6 +382,9 @@ sv_status spec_verify_attn_pages(const sv_attn_pages_params *p, void *workspace_
  * Sequence b belongs to group[b] (0 .. n_groups-1; -1: to none).  The first prefix_len[g] / 16 entries (whole pages; a
  * rest counts to the sequences) of the members' block table rows must be the same pages.  A member whose block begins
  * inside these pages (seq_len[b] - (gamma[b]+1) < 16 * pages) is computed by itself; so is the only member of a group.
+ * Worth it (B200) where spec_verify_attn would read (members - 1) * prefix_len * hkv * head_dim * 4 bytes again that are
+ * 300 MB or more, with up to some 40 rows (positions * hq / hkv) to a member and kv head; 1 GB with 136 rows, and not for a
+ * hundred such members.
  * Device-detected: as spec_verify_attn; group[b] outside [-1, n_groups) or prefix_len[g] negative or beyond the table
  * row -> SV_DEV_BAD_LEN, the sequence or group is computed without sharing.  Five launches.
  */

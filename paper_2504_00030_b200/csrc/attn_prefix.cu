@@ -7,8 +7,10 @@
 //             partial per group is written and read once, 520 bytes a row and head);
 //   sequences the rest of every sequence: its rows begin with the group's partial O, maximum and sum in place of zeros;
 //   combine   behind either of the two: pairs that were split over blocks.
-// Measured (B200): 64 tokens behind one prompt of 8192 75 us (26 us of bytes; five launches), 128 blocks of up to 17 rows of 64
-// heads behind three prefixes of up to 12000 tokens 689 us, about 520 of them the groups (331 us for all products at the tensor core's full rate).
+// Measured (B200): 64 tokens behind one prompt of 8192 77 us (26 us of bytes; five launches; 268 by the verify attention), 128
+// blocks of up to 17 rows of 64 heads behind three prefixes of up to 12000 tokens 643 us at 1965 MHz, 446 of them the groups (331
+// us for all products at the tensor core's full rate), and 770 after a second of such calls (1690 MHz): there the verify
+// attention, which reads the prefixes for every sequence, takes 651 and 704.
 #include "attn_seg.cuh"
 
 namespace sv {

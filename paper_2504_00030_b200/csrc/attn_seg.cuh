@@ -16,16 +16,16 @@
 //   the exponentials are the limit.
 // A key tile has 64 tokens, so that every row tile has two S buffers in tensor memory (2 * 64 columns beside O's 128): the
 // scores of the next tile are there when the softmax of this one is done.  (128 tokens and one buffer, whose S = Q K^T is a
-// quarter cheaper on the tensor core: 600 us for the groups of 128 sequences behind three prefixes where this takes 520.)
+// quarter cheaper on the tensor core: 600 us for the groups of 128 sequences behind three prefixes where this took 520 beside it.)
 //
 // Warps: 0 = TMA of K, 2 = TMA of V, 1 and 3 = MMA issuers of the row tiles (1 owns the tensor memory; with one row tile 3
 // brings the queries of pairs of up to 32 rows ahead); then four softmax warps per row tile (thread = row = TMEM lane).  All
 // hand-offs are mbarriers; every wait is bounded, an expired wait sets SV_DEV_TIMEOUT and drains the block.
 //
-// Measured (B200, device time of the call, 128-dim heads): lists of 128 pages for one row of each of 128 sequences 185 us (6.1
-// TB/s, 94 % of a copy); of 64 pages a row for 17 rows of 64 heads 253 us (163 us of bytes: rows of different sequences
-// fill 136 of 256, the chain S -> softmax -> P V of a row tile sets the pace); one token over 64 pages 14.6 us (latency of
-// two launches).
+// Measured (B200, device time of the call, 128-dim heads; at 1965 MHz, and in brackets where calls in a row for a second have
+// brought the clock to 1400 to 1490): lists of 128 pages for one row of each of 128 sequences 189 us (221; 173 us of bytes at a
+// copy's rate); of 64 pages a row for 17 rows of 64 heads 254 us (369; 163 us of bytes: rows of different sequences fill 136 of
+// 256, the chain S -> softmax -> P V of a row tile sets the pace); one token over 64 pages 13.5 us (latency of two launches).
 #pragma once
 
 #include "attn_common.cuh"

@@ -14,9 +14,10 @@
 // are counted in 256 parts of their range, and the part that holds the last place again, until it is taken whole; then the
 // union over a block's rows as a list with a row mask per page.
 //
-// Measured (B200): 128 sequences of up to 16384 tokens, 17 rows of 64 heads: 121 us, about 70 for the scores (bound by the instructions
-// that make the queries' 8-bit halves and the maxima; 27 us of bytes) and 50 for the choice (bound by
-// shared-memory atomics and barriers); one token at 32768 tokens 14.2 us, 16 ragged blocks 20.7 us (latency).
+// Measured (B200): 128 sequences of up to 16384 tokens, 17 rows of 64 heads: 112 us, about 70 for the scores (bound by the
+// instructions that make the queries' 8-bit halves and the maxima; 27 us of bytes) and 45 for the choice (bound by shared-memory
+// atomics and barriers); one head a kv head, with scores on both sides of zero, 118 to 123; one token at 32768 tokens 13.0 us,
+// 16 ragged blocks 19.0 us (latency).
 #include "attn_common.cuh"
 #include "tc_ptx.cuh"
 #include "whole8.cuh"

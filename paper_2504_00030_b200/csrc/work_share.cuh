@@ -29,7 +29,7 @@ __device__ __forceinline__ long long share_div(long long a, int b)
 // begins(): called by the thread whose last look was at the owner that t_begin lies in.
 // red: two rows of shared scratch.  One scan over the owners where each thread has one of them; what it costs is paid by
 // every launch: as a sum, a scan and 64-bit divisions, and a second look at the owner by every warp role, a token over 64 pages
-// took 15.3 us (now 14.6), three launches of spec_verify_attn_prefix 29.7 (28.3).
+// took 15.3 us in place of 14.6, a small prefix with its three launches 29.7 in place of 28.3.
 template <int NT, typename Owner, typename Begins>
 __device__ __forceinline__ void plan_work_share(int n_owners, int pair_cost, Owner &&owner, Begins &&begins, WorkShare *sh, long long (*red)[NT / 32])
 {
